@@ -223,29 +223,6 @@ struct Shape {
 };
 constexpr int kMaxDepth = 4;
 
-using f2 = uint64_t;                                    // two fp32 values
-__device__ __forceinline__ f2 twice(float x) { return pack_f32x2(x, x); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ float halves(f2 a) {         // the sum of the two
-  float lo, hi;
-  unpack_f32x2(a, lo, hi);
-  return lo + hi;
-}
-
 template <typename T>
 __device__ __forceinline__ void copy_span(uint32_t dst, const T* src, int col0, int cols, int lane) {   // 256 columns of one tensor
   constexpr int n = 16 / sizeof(T);
@@ -267,72 +244,9 @@ __device__ __forceinline__ void read_span(const uint8_t* src, int lane, f2 (&x)[
     x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
   }
 }
-// Four E4M3 codes as two pairs of fp32, exact.
-__device__ __forceinline__ void decode4(uint32_t w, f2& lo, f2& hi) {
-  float v[4];
-  asm("{\n\t.reg .b16 a, b, h0, h1, h2, h3;\n\t.reg .b32 p, q;\n\t"
-      "mov.b32 {a, b}, %4;\n\t"
-      "cvt.rn.f16x2.e4m3x2 p, a;\n\t"
-      "cvt.rn.f16x2.e4m3x2 q, b;\n\t"
-      "mov.b32 {h0, h1}, p;\n\tmov.b32 {h2, h3}, q;\n\t"
-      "cvt.f32.f16 %0, h0;\n\tcvt.f32.f16 %1, h1;\n\tcvt.f32.f16 %2, h2;\n\tcvt.f32.f16 %3, h3;\n\t}"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
-      : "r"(w));
-  lo = pack_f32x2(v[0], v[1]);
-  hi = pack_f32x2(v[2], v[3]);
-}
 // f: the scale, or its product with a factor of the row (a power of two times a factor is exact).
 __device__ __forceinline__ void read_codes(const uint8_t* src, int lane, float f, f2 (&x)[4]) {
-  const uint2 q = *reinterpret_cast<const uint2*>(src + lane * 8);
-  decode4(q.x, x[0], x[1]);
-  decode4(q.y, x[2], x[3]);
-  const f2 ff = twice(f);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], ff);
-}
-// 2^(e - 127) for codes as checkpoints hold them: a block marked 255 has NaN codes, whatever they are multiplied by.
-__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-// The largest |value| a thread has stored (NaN if there was one).
-template <typename T>
-struct Largest;
-template <>
-struct Largest<float> {
-  float m = 0.0f;
-  __device__ __forceinline__ void see(const Vec8<float>& v) {
-    const float x[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
-  }
-  __device__ __forceinline__ uint32_t bits() const { return abs_bits(m); }
-};
-template <>
-struct Largest<bf16_t> {
-  uint32_t m = 0u;      // two values
-  __device__ __forceinline__ void see(const Vec8<bf16_t>& v) {
-    const uint32_t w[4] = {v.q.x, v.q.y, v.q.z, v.q.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      asm("{\n\t.reg .b32 t;\n\tabs.bf16x2 t, %1;\n\tmax.NaN.bf16x2 %0, %0, t;\n\t}" : "+r"(m) : "r"(w[k]));
-  }
-  __device__ __forceinline__ uint32_t bits() const { return max(m << 16, m & 0xFFFF0000u); }
-};
-
-// Eight results, rounded once.
-template <typename T>
-__device__ __forceinline__ Vec8<T> write8(T* p, const f2 (&x)[4]) {
-  float v[8];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
-  Vec8<T> o;
-  o.pack(v);
-  o.store(p);
-  return o;
+  mx8_decode8(*reinterpret_cast<const uint2*>(src + lane * 8), f, x);
 }
 // cp.async.wait_group takes a constant: at most depth - 1 younger groups may be open.
 __device__ __forceinline__ void wait_stage(int depth) {
@@ -464,10 +378,7 @@ __device__ __forceinline__ void put_codes8(const f2 (&x)[4], uint8_t* codes, uin
   for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(v[e]));
   const uint32_t e8 = mx8_exponent(quad_max(abs_bits(m)));
   if (!in) return;
-  const f2 f = twice(mx8_encode_factor(e8));
-#pragma unroll
-  for (int k = 0; k < 4; ++k) unpack_f32x2(mul2(x[k], f), v[2 * k], v[2 * k + 1]);
-  *reinterpret_cast<uint2*>(codes) = make_uint2(cvt_fp8x4<0>(v[0], v[1], v[2], v[3]), cvt_fp8x4<0>(v[4], v[5], v[6], v[7]));
+  *reinterpret_cast<uint2*>(codes) = mx8_encode8(x, mx8_encode_factor(e8));
   if ((lane & 3) == 0) *scale = static_cast<uint8_t>(e8);
 }
 

@@ -26,6 +26,11 @@ __device__ __forceinline__ float mx8_decode_factor(uint32_t e) {
   return __uint_as_float(e == 255u ? 0x7FC00000u : e == 0u ? 0x00400000u : e << 23);
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 template <typename T>
@@ -39,10 +44,21 @@ struct Vec8<bf16_t> {
   __device__ __forceinline__ void load(const bf16_t* p) { q = ld_stream(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void zero() { q = make_uint4(0u, 0u, 0u, 0u); }
   __device__ __forceinline__ void unpack(float (&x)[8]) const { unpack8(q, x); }
+  __device__ __forceinline__ void pairs(uint64_t (&x)[4]) const {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
+  }
   __device__ __forceinline__ void pack(const float (&x)[8]) { q = pack8(x); }
   __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<uint4*>(p) = q; }
-  // fp32 bit pattern of the largest |value|
-  __device__ __forceinline__ uint32_t max_abs() const { return max_abs_bf16(q, 0u) << 16; }
+  // fp32 bit pattern of the largest |value| (a NaN if there is one)
+  __device__ __forceinline__ uint32_t max_abs() const {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t m = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm("{\n\t.reg .b32 t;\n\tabs.bf16x2 t, %1;\n\tmax.NaN.bf16x2 %0, %0, t;\n\t}" : "+r"(m) : "r"(w[k]));
+    return max(m << 16, m & 0xFFFF0000u);
+  }
 };
 template <>
 struct Vec8<float> {
@@ -55,6 +71,9 @@ struct Vec8<float> {
   __device__ __forceinline__ void unpack(float (&x)[8]) const {
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
   }
+  __device__ __forceinline__ void pairs(uint64_t (&x)[4]) const {
+    x[0] = pack_f32x2(a.x, a.y), x[1] = pack_f32x2(a.z, a.w), x[2] = pack_f32x2(b.x, b.y), x[3] = pack_f32x2(b.z, b.w);
+  }
   __device__ __forceinline__ void pack(const float (&x)[8]) {
     a = make_float4(x[0], x[1], x[2], x[3]);
     b = make_float4(x[4], x[5], x[6], x[7]);
@@ -64,8 +83,8 @@ struct Vec8<float> {
     reinterpret_cast<float4*>(p)[1] = b;
   }
   __device__ __forceinline__ uint32_t max_abs() const {
-    return max(max(max(abs_bits(a.x), abs_bits(a.y)), max(abs_bits(a.z), abs_bits(a.w))),
-               max(max(abs_bits(b.x), abs_bits(b.y)), max(abs_bits(b.z), abs_bits(b.w))));
+    return abs_bits(max_nan(max_nan(max_nan(fabsf(a.x), fabsf(a.y)), max_nan(fabsf(a.z), fabsf(a.w))),
+                            max_nan(max_nan(fabsf(b.x), fabsf(b.y)), max_nan(fabsf(b.z), fabsf(b.w)))));
   }
 };
 
@@ -84,19 +103,7 @@ __device__ __forceinline__ uint32_t store1(float* p, float v) {
   return abs_bits(v);
 }
 
-// The codes of eight values under an encode factor; each product is exact.
-__device__ __forceinline__ uint2 mx8_encode8(const float (&x)[8], float f) {
-  return make_uint2(cvt_fp8x4<0>(x[0] * f, x[1] * f, x[2] * f, x[3] * f), cvt_fp8x4<0>(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
-}
 __device__ __forceinline__ uint8_t mx8_encode1(float x, float f) { return static_cast<uint8_t>(cvt_fp8x2<0>(x * f, 0.0f) & 0xFFu); }
-__device__ __forceinline__ void mx8_decode8(const uint2& q, float f, float (&x)[8]) {
-  const uint32_t w[2] = {q.x, q.y};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float2 lo = e4m3x2_to_float2(w[i] & 0xFFFFu), hi = e4m3x2_to_float2(w[i] >> 16);
-    x[4 * i] = lo.x * f, x[4 * i + 1] = lo.y * f, x[4 * i + 2] = hi.x * f, x[4 * i + 3] = hi.y * f;
-  }
-}
 __device__ __forceinline__ float mx8_decode1(uint8_t c, float f) { return e4m3x2_to_float2(c).x * f; }
 
 // Block maxima across lanes: four lanes of eight values, or a warp of one value each.
@@ -114,6 +121,99 @@ __device__ __forceinline__ void raise_amax(uint32_t m, float* amax) {
   if ((threadIdx.x & 31) == 0 && m != 0u) atomicMax(&s_amax, m);
   __syncthreads();
   if (threadIdx.x == 0 && s_amax != 0u) atomicMax(reinterpret_cast<unsigned int*>(amax), s_amax);
+}
+
+
+// ---- arithmetic on two fp32 values per instruction (each half an ordinary rounded operation)
+using f2 = uint64_t;                                    // two fp32 values
+__device__ __forceinline__ f2 twice(float x) { return pack_f32x2(x, x); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float halves(f2 a) {         // the sum of the two
+  float lo, hi;
+  unpack_f32x2(a, lo, hi);
+  return lo + hi;
+}
+
+// Four E4M3 codes as two pairs of fp32, exact.
+__device__ __forceinline__ void decode4(uint32_t w, f2& lo, f2& hi) {
+  float v[4];
+  asm("{\n\t.reg .b16 a, b, h0, h1, h2, h3;\n\t.reg .b32 p, q;\n\t"
+      "mov.b32 {a, b}, %4;\n\t"
+      "cvt.rn.f16x2.e4m3x2 p, a;\n\t"
+      "cvt.rn.f16x2.e4m3x2 q, b;\n\t"
+      "mov.b32 {h0, h1}, p;\n\tmov.b32 {h2, h3}, q;\n\t"
+      "cvt.f32.f16 %0, h0;\n\tcvt.f32.f16 %1, h1;\n\tcvt.f32.f16 %2, h2;\n\tcvt.f32.f16 %3, h3;\n\t}"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+      : "r"(w));
+  lo = pack_f32x2(v[0], v[1]);
+  hi = pack_f32x2(v[2], v[3]);
+}
+// 2^(e - 127) for codes as checkpoints hold them: a block marked 255 has NaN codes, whatever they are multiplied by.
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(max(e << 23, 0x00400000u)); }
+
+// The largest |value| a thread has stored (NaN if there was one).
+template <typename T>
+struct Largest;
+template <>
+struct Largest<float> {
+  float m = 0.0f;
+  __device__ __forceinline__ void see(const Vec8<float>& v) {
+    const float x[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
+  }
+  __device__ __forceinline__ uint32_t bits() const { return abs_bits(m); }
+};
+template <>
+struct Largest<bf16_t> {
+  uint32_t m = 0u;      // two values
+  __device__ __forceinline__ void see(const Vec8<bf16_t>& v) {
+    const uint32_t w[4] = {v.q.x, v.q.y, v.q.z, v.q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      asm("{\n\t.reg .b32 t;\n\tabs.bf16x2 t, %1;\n\tmax.NaN.bf16x2 %0, %0, t;\n\t}" : "+r"(m) : "r"(w[k]));
+  }
+  __device__ __forceinline__ uint32_t bits() const { return max(m << 16, m & 0xFFFF0000u); }
+};
+
+// Eight results, rounded once.
+template <typename T>
+__device__ __forceinline__ Vec8<T> write8(T* p, const f2 (&x)[4]) {
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+  Vec8<T> o;
+  o.pack(v);
+  o.store(p);
+  return o;
+}
+// The codes of eight values under an encode factor; each product is exact.
+__device__ __forceinline__ uint2 mx8_encode8(const f2 (&x)[4], float f) {
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(mul2(x[k], twice(f)), v[2 * k], v[2 * k + 1]);
+  return make_uint2(cvt_fp8x4<0>(v[0], v[1], v[2], v[3]), cvt_fp8x4<0>(v[4], v[5], v[6], v[7]));
+}
+// Eight codes times f.
+__device__ __forceinline__ void mx8_decode8(const uint2& q, float f, f2 (&x)[4]) {
+  decode4(q.x, x[0], x[1]);
+  decode4(q.y, x[2], x[3]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], twice(f));
 }
 
 }  // namespace falqon
