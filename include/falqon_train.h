@@ -30,7 +30,8 @@ int falqon_checkpoint_save(const void *x, int dtype, int64_t rows, int64_t cols,
 int falqon_checkpoint_load(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *x, int dtype,
                            falqon_stream stream);
 
-/* z = silu(g) * u, silu(x) = x / (1 + exp(-x)), and (all four or none) the checkpoints of g and u in the same pass. */
+/* z = silu(g) * u, silu(x) = x / (1 + exp(-x)), and (all four or none) the checkpoints of g and u in the same pass.
+ * z is neither g nor u. */
 int falqon_gate_forward(const void *g, const void *u, int dtype, int64_t rows, int64_t cols, void *z, uint8_t *g_codes,
                         uint8_t *g_scales, uint8_t *u_codes, uint8_t *u_scales, float *amax_out, falqon_stream stream);
 /* Its gradient from the checkpoints: with s = 1 / (1 + exp(-g)):  du = dz * g * s,  dg = dz * u * s * (1 + g * (1 - s)).

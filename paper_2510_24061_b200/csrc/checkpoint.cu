@@ -14,96 +14,57 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// How rows are cut into lanes' shares ("slots").
-//   kFlat   rows are whole blocks of 32: eight values per lane, slots and values run in step over the whole tensor
-//   kVector rows are multiples of eight: eight values per lane, four lanes to a block, a row's last block may be short
-//   kSingle any other width: one value per lane, a warp to a block
-enum Cut { kFlat, kVector, kSingle };
-template <Cut kCut>
-constexpr int kShare = kCut == kSingle ? 1 : 8;
+// How a tensor is cut into vectors of eight values:
+//   kFlat   rows are whole blocks of 32: vectors and blocks run in step over the whole tensor, four lanes to a block
+//   kVector rows are multiples of eight: four lanes to a block, a row's last block may be short
+//   kRagged any other width: vectors run over the whole tensor regardless of rows, so that all but its last are aligned, and
+//           blocks begin anywhere in them (kernels of their own below; single values per lane took five times as long)
+enum Cut { kFlat, kVector, kRagged };
 
-// Where a lane's values lie.
+// Where a lane's vector lies (kFlat, kVector).  `slot` counts vectors, four to a block, the blocks of all rows laid end to end.
 template <Cut kCut>
 struct Place {
-  static constexpr int kLanes = kMx8Block / kShare<kCut>;
   int64_t block, at;   // scale byte, first value
   bool valid;
   __device__ __forceinline__ Place(int64_t slot, int64_t slots, int64_t cols, int64_t blocks_per_row) {
     valid = slot < slots;
-    block = slot / kLanes;
+    block = slot >> 2;
     if (kCut == kFlat) {
       at = slot * 8;
     } else {
       const int64_t row = (slots >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(block) / static_cast<uint32_t>(blocks_per_row))
                                              : block / blocks_per_row;
-      const int64_t col = (block - row * blocks_per_row) * kMx8Block + (slot % kLanes) * kShare<kCut>;
+      const int64_t col = (block - row * blocks_per_row) * kMx8Block + (slot & 3) * 8;
       valid = valid && col < cols;
       at = row * cols + col;
     }
   }
 };
 
-// A lane's share of a tensor: eight values or one (then only the first pair's first half is used).
-template <typename T, Cut kCut>
-struct Share {
+template <typename T>
+__device__ __forceinline__ Vec8<T> load_if(const T* p, bool valid) {
   Vec8<T> v;
-  float x;
-  __device__ __forceinline__ void load(const T* p, bool valid) {
-    if constexpr (kCut == kSingle) {
-      x = valid ? load1(p) : 0.0f;
-    } else {
-      if (valid) v.load(p); else v.zero();
-    }
-  }
-  __device__ __forceinline__ uint32_t max_abs() const {
-    if constexpr (kCut == kSingle) return abs_bits(x); else return v.max_abs();
-  }
-  __device__ __forceinline__ void pairs(f2 (&p)[4]) const {
-    if constexpr (kCut == kSingle) p[0] = pack_f32x2(x, 0.0f); else v.pairs(p);
-  }
-};
-template <Cut kCut>
-constexpr int kPairs = kCut == kSingle ? 1 : 4;
-
-template <typename T, Cut kCut>
-__device__ __forceinline__ uint32_t write(T* p, const f2 (&x)[4], bool want_max) {   // the bit pattern of the largest |value| stored
-  if constexpr (kCut == kSingle) {
-    float lo, hi;
-    unpack_f32x2(x[0], lo, hi);
-    return store1(p, lo);
-  } else {
-    const Vec8<T> o = write8(p, x);
-    return want_max ? o.max_abs() : 0u;
-  }
+  if (valid) v.load(p); else v.zero();
+  return v;
 }
 
 // Encodes the lanes' values of one block; all lanes of the warp call it.  m: the bit pattern of the lane's largest |value|.
 template <Cut kCut>
 __device__ __forceinline__ void encode(const f2 (&x)[4], uint32_t m, const Place<kCut>& pl, uint8_t* codes, uint8_t* scales) {
-  const uint32_t e = mx8_exponent(kCut == kSingle ? __reduce_max_sync(0xFFFFFFFFu, m) : quad_max(m));
+  const uint32_t e = mx8_exponent(quad_max(m));
   if (!pl.valid) return;
-  const float f = mx8_encode_factor(e);
-  if constexpr (kCut == kSingle) {
-    float lo, hi;
-    unpack_f32x2(x[0], lo, hi);
-    codes[pl.at] = mx8_encode1(lo, f);
-  } else {
-    *reinterpret_cast<uint2*>(codes + pl.at) = mx8_encode8(x, f);
-  }
-  if (threadIdx.x % Place<kCut>::kLanes == 0) scales[pl.block] = static_cast<uint8_t>(e);
+  *reinterpret_cast<uint2*>(codes + pl.at) = mx8_encode8(x, mx8_encode_factor(e));
+  if ((threadIdx.x & 3) == 0) scales[pl.block] = static_cast<uint8_t>(e);
 }
 
-// A lane's share of a checkpoint, as it lies in memory.
+// A lane's vector of a checkpoint, as it lies in memory.
 template <Cut kCut>
 struct Coded {
   uint2 q;
   uint32_t e;
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, const Place<kCut>& pl) {
     e = ld_stream(scales + pl.block);
-    if constexpr (kCut == kSingle) q.x = ld_stream(codes + pl.at); else q = ld_stream(reinterpret_cast<const uint2*>(codes + pl.at));
-  }
-  __device__ __forceinline__ void pairs(f2 (&x)[4], float f) const {
-    if constexpr (kCut == kSingle) x[0] = pack_f32x2(mx8_decode1(static_cast<uint8_t>(q.x), f), 0.0f); else mx8_decode8(q, f, x);
+    q = ld_stream(reinterpret_cast<const uint2*>(codes + pl.at));
   }
 };
 
@@ -127,12 +88,30 @@ __device__ __forceinline__ f2 sigmoid2(f2 x) {
   return pack_f32x2(sigmoid_of<T>(lo), sigmoid_of<T>(hi));
 }
 
-// The lanes' loop: kUnroll slots at a time with all their loads in flight before the first is used; whole warps stay together.
+template <typename T>
+__device__ __forceinline__ void gate8(const f2 (&g)[4], const f2 (&u)[4], f2 (&z)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) z[k] = mul2(mul2(g[k], sigmoid2<T>(g[k])), u[k]);
+}
+template <typename T>
+__device__ __forceinline__ void gate_grad8(const f2 (&g)[4], const f2 (&u)[4], const f2 (&dz)[4], f2 (&dg)[4], f2 (&du)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f2 s = sigmoid2<T>(g[k]), gs = mul2(g[k], s);
+    du[k] = mul2(dz[k], gs);
+    // s * (1 + g * (1 - s)) = s + g * s * (1 - s)
+    dg[k] = mul2(mul2(dz[k], u[k]), fma2(gs, fma2(s, twice(-1.0f), twice(1.0f)), s));
+  }
+}
+
+// The lanes' loop: a CTA takes kUnroll neighbouring runs of kThreads slots at a time, with all their loads in flight before the
+// first is used; whole warps stay together.
 template <int kUnroll, class Body>
 __device__ __forceinline__ void for_slots(int64_t slots, Body body) {
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
   const int lane = threadIdx.x & 31;
-  for (int64_t s = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; s - lane < slots; s += kUnroll * step) body(s, step);
+  for (int64_t s = static_cast<int64_t>(blockIdx.x) * (kUnroll * kThreads) + threadIdx.x; s - lane < slots;
+       s += static_cast<int64_t>(gridDim.x) * (kUnroll * kThreads))
+    body(s);
 }
 
 template <typename T, Cut kCut>
@@ -140,10 +119,9 @@ __global__ void __launch_bounds__(kThreads) save_kernel(const T* x, int64_t slot
                                                         uint8_t* scales) {
   pdl_trigger();
   pdl_wait();
-  for_slots<1>(slots, [&](int64_t s, int64_t) {
+  for_slots<1>(slots, [&](int64_t s) {
     const Place<kCut> pl(s, slots, cols, blocks_per_row);
-    Share<T, kCut> v;
-    v.load(x + pl.at, pl.valid);
+    const Vec8<T> v = load_if(x + pl.at, pl.valid);
     f2 p[4];
     v.pairs(p);
     encode<kCut>(p, v.max_abs(), pl, codes, scales);
@@ -155,14 +133,14 @@ __global__ void __launch_bounds__(kThreads) load_kernel(T* x, int64_t slots, int
                                                         const uint8_t* scales) {
   pdl_trigger();
   pdl_wait();
-  for_slots<1>(slots, [&](int64_t s, int64_t) {
+  for_slots<1>(slots, [&](int64_t s) {
     const Place<kCut> pl(s, slots, cols, blocks_per_row);
     if (!pl.valid) return;
     Coded<kCut> c;
     c.load(codes, scales, pl);
     f2 p[4];
-    c.pairs(p, mx8_decode_factor(c.e));
-    write<T, kCut>(x + pl.at, p, false);
+    mx8_decode8(c.q, mx8_decode_factor(c.e), p);
+    write8(x + pl.at, p);
   });
 }
 
@@ -174,31 +152,33 @@ __global__ void __launch_bounds__(kThreads) gate_forward_kernel(const T* g, cons
                                                                 uint8_t* u_codes, uint8_t* u_scales, float* amax) {
   pdl_trigger();
   pdl_wait();
-  uint32_t mx = 0;
-  for_slots<kGateUnroll>(slots, [&](int64_t s, int64_t step) {
-    Share<T, kCut> a[kGateUnroll], b[kGateUnroll];
+  Largest<T> largest;
+  for_slots<kGateUnroll>(slots, [&](int64_t s) {
+    Vec8<T> a[kGateUnroll], b[kGateUnroll];
 #pragma unroll
     for (int j = 0; j < kGateUnroll; ++j) {
-      const Place<kCut> pl(s + j * step, slots, cols, blocks_per_row);
-      a[j].load(g + pl.at, pl.valid);
-      b[j].load(u + pl.at, pl.valid);
+      const Place<kCut> pl(s + j * kThreads, slots, cols, blocks_per_row);
+      a[j] = load_if(g + pl.at, pl.valid);
+      b[j] = load_if(u + pl.at, pl.valid);
     }
 #pragma unroll
     for (int j = 0; j < kGateUnroll; ++j) {
-      const Place<kCut> pl(s + j * step, slots, cols, blocks_per_row);
+      const Place<kCut> pl(s + j * kThreads, slots, cols, blocks_per_row);
       f2 x[4], y[4], o[4];
       a[j].pairs(x);
       b[j].pairs(y);
-#pragma unroll
-      for (int k = 0; k < kPairs<kCut>; ++k) o[k] = mul2(mul2(x[k], sigmoid2<T>(x[k])), y[k]);
-      if (pl.valid) mx = max(mx, write<T, kCut>(z + pl.at, o, amax != nullptr));
+      gate8<T>(x, y, o);
+      if (pl.valid) {
+        const Vec8<T> w = write8(z + pl.at, o);
+        if (amax != nullptr) largest.see(w);
+      }
       if (g_codes != nullptr) {
         encode<kCut>(x, a[j].max_abs(), pl, g_codes, g_scales);
         encode<kCut>(y, b[j].max_abs(), pl, u_codes, u_scales);
       }
     }
   });
-  if (amax != nullptr) raise_amax(mx, amax);
+  if (amax != nullptr) raise_amax(largest.bits(), amax);
 }
 
 template <typename T, Cut kCut>
@@ -207,42 +187,295 @@ __global__ void __launch_bounds__(kThreads) gate_backward_kernel(const uint8_t* 
                                                                  int64_t cols, int64_t blocks_per_row, float* amax_dg, float* amax_du) {
   pdl_trigger();
   pdl_wait();
-  uint32_t mg = 0, mu = 0;
-  for_slots<kGateUnroll>(slots, [&](int64_t s, int64_t step) {
+  Largest<T> lg, lu;
+  for_slots<kGateUnroll>(slots, [&](int64_t s) {
     Coded<kCut> a[kGateUnroll], b[kGateUnroll];
-    Share<T, kCut> t[kGateUnroll];
+    Vec8<T> t[kGateUnroll];
 #pragma unroll
     for (int j = 0; j < kGateUnroll; ++j) {
-      const Place<kCut> pl(s + j * step, slots, cols, blocks_per_row);
+      const Place<kCut> pl(s + j * kThreads, slots, cols, blocks_per_row);
       if (!pl.valid) continue;
       a[j].load(g_codes, g_scales, pl);
       b[j].load(u_codes, u_scales, pl);
-      t[j].load(dz + pl.at, true);
+      t[j].load(dz + pl.at);
     }
 #pragma unroll
     for (int j = 0; j < kGateUnroll; ++j) {
-      const Place<kCut> pl(s + j * step, slots, cols, blocks_per_row);
+      const Place<kCut> pl(s + j * kThreads, slots, cols, blocks_per_row);
       if (!pl.valid) continue;
       f2 x[4], y[4], d[4], og[4], ou[4];
-      a[j].pairs(x, scale_of(a[j].e));
-      b[j].pairs(y, scale_of(b[j].e));
+      mx8_decode8(a[j].q, scale_of(a[j].e), x);
+      mx8_decode8(b[j].q, scale_of(b[j].e), y);
       t[j].pairs(d);
-#pragma unroll
-      for (int k = 0; k < kPairs<kCut>; ++k) {
-        const f2 sg = sigmoid2<T>(x[k]), gs = mul2(x[k], sg);
-        ou[k] = mul2(d[k], gs);
-        // s * (1 + g * (1 - s)) = s + g * s * (1 - s)
-        const f2 slope = fma2(gs, fma2(sg, twice(-1.0f), twice(1.0f)), sg);
-        og[k] = mul2(mul2(d[k], y[k]), slope);
-      }
-      mg = max(mg, write<T, kCut>(dg + pl.at, og, amax_dg != nullptr));
-      mu = max(mu, write<T, kCut>(du + pl.at, ou, amax_du != nullptr));
+      gate_grad8<T>(x, y, d, og, ou);
+      const Vec8<T> wg = write8(dg + pl.at, og), wu = write8(du + pl.at, ou);
+      if (amax_dg != nullptr) lg.see(wg);
+      if (amax_du != nullptr) lu.see(wu);
     }
   });
-  if (amax_dg != nullptr) raise_amax(mg, amax_dg);
+  if (amax_dg != nullptr) raise_amax(lg.bits(), amax_dg);
   if (amax_du != nullptr) {
     __syncthreads();   // raise_amax's shared word
-    raise_amax(mu, amax_du);
+    raise_amax(lu.bits(), amax_du);
+  }
+}
+
+// ---- any width: aligned vectors over the tensor as one run of values
+// The block of a value and where the next begins: blocks are numbered through, so every boundary, within a row or at its end, is one on.
+struct Walk {
+  int64_t block;
+  int col, cols;
+  __device__ __forceinline__ Walk(int64_t at, int64_t total, int64_t width, int64_t blocks_per_row) {
+    const int64_t row = (total >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(at) / static_cast<uint32_t>(width)) : at / width;
+    col = static_cast<int>(at - row * width);
+    cols = static_cast<int>(width);
+    block = row * blocks_per_row + (col >> 5);
+  }
+  __device__ __forceinline__ bool step() {                     // to the next value; whether a new block begins there
+    ++col;
+    const bool end = col == cols;
+    if (end) col = 0;
+    return end || (col & (kMx8Block - 1)) == 0;
+  }
+};
+// The vector at value `at`, of which `total` may leave only a part (the tensor's last): then single values, zeros after them.
+template <typename T>
+__device__ __forceinline__ void load_part(const T* p, int64_t at, int64_t total, f2 (&x)[4]) {
+  if (at + 8 <= total) {
+    Vec8<T> v;
+    v.load(p + at);
+    v.pairs(x);
+    return;
+  }
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = at + e < total ? load1(p + at + e) : 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(v[2 * k], v[2 * k + 1]);
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* p, int64_t at, int64_t total, const f2 (&x)[4], Largest<T>& largest) {
+  if (at + 8 <= total) {
+    largest.see(write8(p + at, x));
+    return;
+  }
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (at + e >= total) v[e] = 0.0f; else store1(p + at + e, v[e]);
+  }
+  Vec8<T> w;
+  w.pack(v);
+  largest.see(w);
+}
+__device__ __forceinline__ uint2 load_codes_part(const uint8_t* p, int64_t at, int64_t total) {
+  if (at + 8 <= total) return ld_stream(reinterpret_cast<const uint2*>(p + at));
+  uint32_t w[2] = {0u, 0u};
+  for (int e = 0; e < 8 && at + e < total; ++e) w[e >> 2] |= static_cast<uint32_t>(ld_stream(p + at + e)) << (8 * (e & 3));
+  return make_uint2(w[0], w[1]);
+}
+
+// Saves one tensor (kGate false), or two and their gated product.  A CTA takes a tile of values; the largest |value| of every block
+// that touches it is collected in shared memory (a thread's eight values lie in one or two blocks: as many shared-memory
+// maxima), with up to 31 values to both sides read again so that the blocks at its ends are complete.
+constexpr int kTileVecs = 2 * kThreads, kTileBlocks = kTileVecs * 8 + 64;   // rows of one value: a block each
+
+template <typename T, bool kGate>
+__global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, const T* u, T* z, int64_t total, int64_t cols, int64_t blocks_per_row,
+                                                                 uint8_t* g_codes, uint8_t* g_scales, uint8_t* u_codes, uint8_t* u_scales, float* amax) {
+  __shared__ uint32_t top[kGate ? 2 : 1][kTileBlocks];
+  pdl_trigger();
+  pdl_wait();
+  Largest<T> largest;
+  const bool coded = g_codes != nullptr;
+  const int64_t vecs = (total + 7) / 8;
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kTileVecs; first < vecs; first += static_cast<int64_t>(gridDim.x) * kTileVecs) {
+    const int64_t end = min(first + kTileVecs, vecs), lo = max(first - 4, static_cast<int64_t>(0)), hi = min(end + 4, vecs);
+    const int64_t block0 = Walk(lo * 8, total, cols, blocks_per_row).block;
+    const int blocks = static_cast<int>(Walk(min(hi * 8, total) - 1, total, cols, blocks_per_row).block - block0) + 1;
+    if (coded) {
+      for (int i = threadIdx.x; i < blocks; i += kThreads) {
+        top[0][i] = 0u;
+        if (kGate) top[1][i] = 0u;
+      }
+      __syncthreads();
+    }
+    f2 x[2][4], y[2][4];
+    const auto collect = [&](int64_t at, const f2 (&p)[4], const f2 (&q)[4]) {
+      Walk w(at, total, cols, blocks_per_row);
+      int b = static_cast<int>(w.block - block0);
+      uint32_t m = 0u, n = 0u;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v[2];
+        unpack_f32x2(p[e >> 1], v[0], v[1]);
+        m = max(m, abs_bits(v[e & 1]));
+        if (kGate) {
+          unpack_f32x2(q[e >> 1], v[0], v[1]);
+          n = max(n, abs_bits(v[e & 1]));
+        }
+        const bool next = w.step();
+        if (next || e == 7) {
+          if (m != 0u) atomicMax(&top[0][b], m);
+          if (kGate && n != 0u) atomicMax(&top[1][b], n);
+          m = n = 0u;
+          b = min(b + 1, blocks - 1);                          // beyond the tensor's end there are only zeros
+        }
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t v = first + j * kThreads + threadIdx.x;
+      if (v >= end) continue;
+      load_part(g, v * 8, total, x[j]);
+      if (kGate) load_part(u, v * 8, total, y[j]);
+    }
+    if (coded) {
+      if (threadIdx.x < 8) {                                   // the neighbours' values
+        const int64_t v = threadIdx.x < 4 ? first - 4 + threadIdx.x : end + threadIdx.x - 4;
+        if (v >= lo && v < hi) {
+          f2 p[4], q[4];
+          load_part(g, v * 8, total, p);
+          if (kGate) load_part(u, v * 8, total, q);
+          collect(v * 8, p, q);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int64_t v = first + j * kThreads + threadIdx.x;
+        if (v < end) collect(v * 8, x[j], y[j]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t v = first + j * kThreads + threadIdx.x, at = v * 8;
+      if (v >= end) continue;
+      if (kGate) {
+        f2 o[4];
+        gate8<T>(x[j], y[j], o);
+        store_part(z, at, total, o, largest);
+      }
+      if (!coded) continue;
+      Walk w(at, total, cols, blocks_per_row);
+      int b = static_cast<int>(w.block - block0);
+      float f = mx8_encode_factor(mx8_exponent(top[0][b])), h = kGate ? mx8_encode_factor(mx8_exponent(top[1][b])) : 0.0f;
+      float cg[8], cu[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float p[2];
+        unpack_f32x2(x[j][e >> 1], p[0], p[1]);
+        cg[e] = p[e & 1] * f;
+        if (kGate) {
+          unpack_f32x2(y[j][e >> 1], p[0], p[1]);
+          cu[e] = p[e & 1] * h;
+        }
+        if (e < 7 && w.step()) {
+          b = min(b + 1, blocks - 1);
+          f = mx8_encode_factor(mx8_exponent(top[0][b]));
+          if (kGate) h = mx8_encode_factor(mx8_exponent(top[1][b]));
+        }
+      }
+      const auto put = [&](uint8_t* codes, const float (&c)[8]) {
+        const uint2 q = make_uint2(cvt_fp8x4<0>(c[0], c[1], c[2], c[3]), cvt_fp8x4<0>(c[4], c[5], c[6], c[7]));
+        if (at + 8 <= total) {
+          *reinterpret_cast<uint2*>(codes + at) = q;
+        } else {
+          for (int e = 0; at + e < total; ++e) codes[at + e] = static_cast<uint8_t>((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+        }
+      };
+      put(g_codes, cg);
+      if (kGate) put(u_codes, cu);
+    }
+    if (coded) {
+      for (int i = threadIdx.x; i < blocks; i += kThreads) {   // the scales of the blocks that begin in this tile
+        const int64_t b = block0 + i, row = b / blocks_per_row, at = row * cols + (b - row * blocks_per_row) * kMx8Block;
+        if (at < first * 8 || at >= end * 8) continue;
+        g_scales[b] = static_cast<uint8_t>(mx8_exponent(top[0][i]));
+        if (kGate) u_scales[b] = static_cast<uint8_t>(mx8_exponent(top[1][i]));
+      }
+      __syncthreads();                                         // before the next tile's maxima
+    }
+  }
+  if (amax != nullptr) raise_amax(largest.bits(), amax);
+}
+
+// Eight codes from value `at` on, each times its own block's scale: two blocks as a rule, more where rows end.
+struct RaggedCodes {
+  uint2 q;
+  uint32_t e0, e1;
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t at, int64_t total, int64_t block, int64_t blocks) {
+    q = load_codes_part(codes, at, total);
+    e0 = ld_stream(scales + block);
+    e1 = ld_stream(scales + min(block + 1, blocks - 1));
+  }
+  template <class Factor>
+  __device__ __forceinline__ void decode(const uint8_t* scales, int64_t blocks, Walk w, Factor factor, f2 (&x)[4]) const {
+    decode4(q.x, x[0], x[1]);
+    decode4(q.y, x[2], x[3]);
+    float f[8];
+    float now = factor(e0);
+    int passed = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      f[e] = now;
+      if (e < 7 && w.step()) {
+        ++passed;
+        now = factor(passed == 1 ? e1 : ld_stream(scales + min(w.block + passed, blocks - 1)));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], pack_f32x2(f[2 * k], f[2 * k + 1]));
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) ragged_load_kernel(T* x, int64_t total, int64_t cols, int64_t blocks_per_row, int64_t blocks,
+                                                               const uint8_t* codes, const uint8_t* scales) {
+  pdl_trigger();
+  pdl_wait();
+  Largest<T> unused;
+  const int64_t vecs = (total + 7) / 8;
+  for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < vecs; v += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const Walk w(v * 8, total, cols, blocks_per_row);
+    RaggedCodes c;
+    c.load(codes, scales, v * 8, total, w.block, blocks);
+    f2 p[4];
+    c.decode(scales, blocks, w, [](uint32_t e) { return mx8_decode_factor(e); }, p);
+    store_part(x, v * 8, total, p, unused);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) ragged_gate_backward_kernel(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes,
+                                                                        const uint8_t* u_scales, const T* dz, T* dg, T* du, int64_t total,
+                                                                        int64_t cols, int64_t blocks_per_row, int64_t blocks, float* amax_dg,
+                                                                        float* amax_du) {
+  pdl_trigger();
+  pdl_wait();
+  Largest<T> lg, lu;
+  const int64_t vecs = (total + 7) / 8;
+  for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < vecs; v += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int64_t at = v * 8;
+    const Walk w(at, total, cols, blocks_per_row);
+    RaggedCodes a, b;
+    a.load(g_codes, g_scales, at, total, w.block, blocks);
+    b.load(u_codes, u_scales, at, total, w.block, blocks);
+    f2 x[4], y[4], d[4], og[4], ou[4];
+    load_part(dz, at, total, d);
+    const auto factor = [](uint32_t e) { return scale_of(e); };
+    a.decode(g_scales, blocks, w, factor, x);
+    b.decode(u_scales, blocks, w, factor, y);
+    gate_grad8<T>(x, y, d, og, ou);
+    store_part(dg, at, total, og, lg);
+    store_part(du, at, total, ou, lu);
+  }
+  if (amax_dg != nullptr) raise_amax(lg.bits(), amax_dg);
+  if (amax_du != nullptr) {
+    __syncthreads();   // raise_amax's shared word
+    raise_amax(lu.bits(), amax_du);
   }
 }
 
@@ -250,28 +483,32 @@ inline bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) =
 
 // The extent of a call, checked.
 struct Extent {
-  int64_t slots, blocks_per_row;
+  int64_t total, blocks, blocks_per_row, slots;   // slots: kFlat, kVector
   Cut cut;
-  unsigned grid;
   bool set(int64_t rows, int64_t cols, int dtype) {
     if (rows < 1 || cols < 1 || rows > (1ll << 31) || cols > (1ll << 31) || rows > (1ll << 42) / cols) return false;
     if (dtype != FALQON_BF16 && dtype != FALQON_F32) return false;
-    cut = cols % kMx8Block == 0 ? kFlat : cols % 8 == 0 ? kVector : kSingle;
+    cut = cols % kMx8Block == 0 ? kFlat : cols % 8 == 0 ? kVector : kRagged;
     blocks_per_row = (cols + kMx8Block - 1) / kMx8Block;
-    slots = rows * blocks_per_row * (cut == kSingle ? 32 : 4);
-    const int64_t ctas = (slots + kThreads - 1) / kThreads, cap = static_cast<int64_t>(sm_count()) * 8;
-    grid = static_cast<unsigned>(ctas < cap ? ctas : cap);
+    blocks = rows * blocks_per_row;
+    slots = blocks * 4;
+    total = rows * cols;
     return true;
   }
+  // CTAs for runs of `per_cta` vectors, eight to an SM at the most.
+  dim3 grid(int64_t per_cta) const {
+    const int64_t vecs = cut == kRagged ? (total + 7) / 8 : slots, ctas = (vecs + per_cta - 1) / per_cta, cap = static_cast<int64_t>(sm_count()) * 8;
+    return dim3(static_cast<unsigned>(ctas < cap ? ctas : cap));
+  }
 };
-// Calls go(value type, cut) for the kernel of this extent and type.
+// Calls go(value type, cut) for the kernel of this extent and type, cut being kFlat or kVector; ragged(value type) for kRagged.
 template <Cut kCut>
 using CutIs = std::integral_constant<Cut, kCut>;
-template <typename F>
-int with_kernel(const Extent& e, int dtype, F go) {
-  if (dtype == FALQON_BF16)
-    return e.cut == kFlat ? go(bf16_t{}, CutIs<kFlat>{}) : e.cut == kVector ? go(bf16_t{}, CutIs<kVector>{}) : go(bf16_t{}, CutIs<kSingle>{});
-  return e.cut == kFlat ? go(0.0f, CutIs<kFlat>{}) : e.cut == kVector ? go(0.0f, CutIs<kVector>{}) : go(0.0f, CutIs<kSingle>{});
+template <typename F, typename G>
+int with_kernel(const Extent& e, int dtype, F go, G ragged) {
+  if (e.cut == kRagged) return dtype == FALQON_BF16 ? ragged(bf16_t{}) : ragged(0.0f);
+  if (dtype == FALQON_BF16) return e.cut == kFlat ? go(bf16_t{}, CutIs<kFlat>{}) : go(bf16_t{}, CutIs<kVector>{});
+  return e.cut == kFlat ? go(0.0f, CutIs<kFlat>{}) : go(0.0f, CutIs<kVector>{});
 }
 
 int finish(cudaError_t e) { return e == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA; }
@@ -288,11 +525,20 @@ int falqon_checkpoint_save(const void* x, int dtype, int64_t rows, int64_t cols,
   Extent e;
   if (x == nullptr || codes == nullptr || scales == nullptr || !ok16(x) || !ok16(codes) || !e.set(rows, cols, dtype))
     return FALQON_ERR_INVALID_ARG;
-  return with_kernel(e, dtype, [&](auto type, auto cut) {
-    using T = decltype(type);
-    return finish(launch_pdl(save_kernel<T, cut.value>, dim3(e.grid), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), 1,
-                             static_cast<const T*>(x), e.slots, cols, e.blocks_per_row, codes, scales));
-  });
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return with_kernel(
+      e, dtype,
+      [&](auto type, auto cut) {
+        using T = decltype(type);
+        return finish(launch_pdl(save_kernel<T, cut.value>, e.grid(kThreads), dim3(kThreads), 0, st, 1, static_cast<const T*>(x), e.slots, cols,
+                                 e.blocks_per_row, codes, scales));
+      },
+      [&](auto type) {
+        using T = decltype(type);
+        return finish(launch_pdl(ragged_encode_kernel<T, false>, e.grid(kTileVecs), dim3(kThreads), 0, st, 1, static_cast<const T*>(x),
+                                 static_cast<const T*>(nullptr), static_cast<T*>(nullptr), e.total, cols, e.blocks_per_row, codes, scales,
+                                 static_cast<uint8_t*>(nullptr), static_cast<uint8_t*>(nullptr), static_cast<float*>(nullptr)));
+      });
 }
 
 int falqon_checkpoint_load(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* x, int dtype,
@@ -300,11 +546,19 @@ int falqon_checkpoint_load(const uint8_t* codes, const uint8_t* scales, int64_t 
   Extent e;
   if (x == nullptr || codes == nullptr || scales == nullptr || !ok16(x) || !ok16(codes) || !e.set(rows, cols, dtype))
     return FALQON_ERR_INVALID_ARG;
-  return with_kernel(e, dtype, [&](auto type, auto cut) {
-    using T = decltype(type);
-    return finish(launch_pdl(load_kernel<T, cut.value>, dim3(e.grid), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), 1,
-                             static_cast<T*>(x), e.slots, cols, e.blocks_per_row, codes, scales));
-  });
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return with_kernel(
+      e, dtype,
+      [&](auto type, auto cut) {
+        using T = decltype(type);
+        return finish(launch_pdl(load_kernel<T, cut.value>, e.grid(kThreads), dim3(kThreads), 0, st, 1, static_cast<T*>(x), e.slots, cols,
+                                 e.blocks_per_row, codes, scales));
+      },
+      [&](auto type) {
+        using T = decltype(type);
+        return finish(launch_pdl(ragged_load_kernel<T>, e.grid(kThreads), dim3(kThreads), 0, st, 1, static_cast<T*>(x), e.total, cols,
+                                 e.blocks_per_row, e.blocks, codes, scales));
+      });
 }
 
 int falqon_gate_forward(const void* g, const void* u, int dtype, int64_t rows, int64_t cols, void* z, uint8_t* g_codes,
@@ -312,14 +566,23 @@ int falqon_gate_forward(const void* g, const void* u, int dtype, int64_t rows, i
   Extent e;
   const int kept = (g_codes != nullptr) + (g_scales != nullptr) + (u_codes != nullptr) + (u_scales != nullptr);
   if (g == nullptr || u == nullptr || z == nullptr || !ok16(g) || !ok16(u) || !ok16(z) || !ok16(g_codes) || !ok16(u_codes) ||
-      (kept != 0 && kept != 4) || !e.set(rows, cols, dtype))
+      z == g || z == u || (kept != 0 && kept != 4) || !e.set(rows, cols, dtype))
     return FALQON_ERR_INVALID_ARG;
-  return with_kernel(e, dtype, [&](auto type, auto cut) {
-    using T = decltype(type);
-    return finish(launch_pdl(gate_forward_kernel<T, cut.value>, dim3(e.grid), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), 1,
-                             static_cast<const T*>(g), static_cast<const T*>(u), static_cast<T*>(z), e.slots, cols, e.blocks_per_row,
-                             g_codes, g_scales, u_codes, u_scales, amax_out));
-  });
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return with_kernel(
+      e, dtype,
+      [&](auto type, auto cut) {
+        using T = decltype(type);
+        return finish(launch_pdl(gate_forward_kernel<T, cut.value>, e.grid(kGateUnroll * kThreads), dim3(kThreads), 0, st, 1,
+                                 static_cast<const T*>(g), static_cast<const T*>(u), static_cast<T*>(z), e.slots, cols, e.blocks_per_row, g_codes,
+                                 g_scales, u_codes, u_scales, amax_out));
+      },
+      [&](auto type) {
+        using T = decltype(type);
+        return finish(launch_pdl(ragged_encode_kernel<T, true>, e.grid(kTileVecs), dim3(kThreads), 0, st, 1, static_cast<const T*>(g),
+                                 static_cast<const T*>(u), static_cast<T*>(z), e.total, cols, e.blocks_per_row, g_codes, g_scales, u_codes,
+                                 u_scales, amax_out));
+      });
 }
 
 int falqon_gate_backward(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes, const uint8_t* u_scales,
@@ -329,12 +592,21 @@ int falqon_gate_backward(const uint8_t* g_codes, const uint8_t* g_scales, const 
   if (g_codes == nullptr || g_scales == nullptr || u_codes == nullptr || u_scales == nullptr || dz == nullptr || dg == nullptr ||
       du == nullptr || dg == du || !ok16(g_codes) || !ok16(u_codes) || !ok16(dz) || !ok16(dg) || !ok16(du) || !e.set(rows, cols, dtype))
     return FALQON_ERR_INVALID_ARG;
-  return with_kernel(e, dtype, [&](auto type, auto cut) {
-    using T = decltype(type);
-    return finish(launch_pdl(gate_backward_kernel<T, cut.value>, dim3(e.grid), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), 1,
-                             g_codes, g_scales, u_codes, u_scales, static_cast<const T*>(dz), static_cast<T*>(dg), static_cast<T*>(du),
-                             e.slots, cols, e.blocks_per_row, amax_dg, amax_du));
-  });
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return with_kernel(
+      e, dtype,
+      [&](auto type, auto cut) {
+        using T = decltype(type);
+        return finish(launch_pdl(gate_backward_kernel<T, cut.value>, e.grid(kGateUnroll * kThreads), dim3(kThreads), 0, st, 1, g_codes, g_scales,
+                                 u_codes, u_scales, static_cast<const T*>(dz), static_cast<T*>(dg), static_cast<T*>(du), e.slots, cols,
+                                 e.blocks_per_row, amax_dg, amax_du));
+      },
+      [&](auto type) {
+        using T = decltype(type);
+        return finish(launch_pdl(ragged_gate_backward_kernel<T>, e.grid(kThreads), dim3(kThreads), 0, st, 1, g_codes, g_scales, u_codes, u_scales,
+                                 static_cast<const T*>(dz), static_cast<T*>(dg), static_cast<T*>(du), e.total, cols, e.blocks_per_row, e.blocks,
+                                 amax_dg, amax_du));
+      });
 }
 
 }  // extern "C"

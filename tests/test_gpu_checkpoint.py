@@ -7,7 +7,8 @@ from tests import train_oracle as orc
 
 pytestmark = pytest.mark.gpu
 
-SHAPES = [(1, 1), (1, 7), (3, 8), (2, 31), (5, 32), (4, 33), (7, 40), (1, 11008), (33, 1000), (65, 1011), (129, 256), (3, 16384)]
+SHAPES = [(1, 1), (1, 7), (3, 8), (2, 31), (5, 32), (4, 33), (7, 40), (1, 11008), (33, 1000), (65, 1011), (129, 256), (3, 16384),
+          (4500, 1), (3000, 3), (700, 33), (150, 63), (1, 4097), (2, 9001), (1200, 9)]
 
 
 @pytest.fixture(scope="module")

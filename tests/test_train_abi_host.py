@@ -69,6 +69,7 @@ def test_checkpoint_refusals(fq, tr):
     assert lib.falqon_checkpoint_load(FAKE, FAKE, 4, -1, FAKE, 0, None) == inv
     assert lib.falqon_gate_forward(FAKE, None, 0, 4, 8, FAKE, None, None, None, None, None, None) == inv
     assert lib.falqon_gate_forward(FAKE, FAKE, 0, 4, 8, FAKE, FAKE, FAKE, FAKE, None, None, None) == inv    # some of the four
+    assert lib.falqon_gate_forward(FAKE, 2 * FAKE, 0, 4, 8, FAKE, None, None, None, None, None, None) == inv      # z is g
     assert lib.falqon_gate_backward(FAKE, FAKE, FAKE, FAKE, FAKE, 0, 4, 8, FAKE, FAKE, None, None, None) == inv   # dg is du
     assert lib.falqon_gate_backward(FAKE, FAKE, FAKE, FAKE, FAKE + 4, 0, 4, 8, FAKE, 2 * FAKE, None, None, None) == inv
 
