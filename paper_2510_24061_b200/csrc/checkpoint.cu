@@ -221,16 +221,37 @@ __global__ void __launch_bounds__(kThreads) gate_backward_kernel(const uint8_t* 
 }
 
 // ---- any width: aligned vectors over the tensor as one run of values
-// The block of a value and where the next begins: blocks are numbered through, so every boundary, within a row or at its end, is one on.
-struct Walk {
-  int64_t block;
-  int col, cols;
-  __device__ __forceinline__ Walk(int64_t at, int64_t total, int64_t width, int64_t blocks_per_row) {
-    const int64_t row = (total >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(at) / static_cast<uint32_t>(width)) : at / width;
-    col = static_cast<int>(at - row * width);
-    cols = static_cast<int>(width);
-    block = row * blocks_per_row + (col >> 5);
+// Rows of any width: their length, the blocks they have, and a multiplier for division by the length (exact below 2^32: the
+// 64-bit reciprocal's error times the number stays below one quotient's step).
+struct Rows {
+  int64_t cols, blocks_per_row, total, blocks;
+  uint64_t reciprocal;
+  __device__ __forceinline__ int64_t row_of(int64_t at) const {
+    if (cols == 1) return at;                                  // its reciprocal is 2^64
+    return (total >> 32) == 0 ? static_cast<int64_t>(__umul64hi(static_cast<uint64_t>(at), reciprocal)) : at / cols;
   }
+};
+// Where eight values from `at` on lie: the first `split` in block `block`, the rest in the next one; `more`: not all of them (blocks
+// are numbered through, so every boundary, within a row or at its end, is one on; only short rows and row ends have two within
+// eight values).
+struct Spread {
+  int64_t block;
+  int col, split;
+  bool more;
+  __device__ __forceinline__ Spread(int64_t at, const Rows& r) {
+    const int64_t row = r.row_of(at);
+    const int cols = static_cast<int>(r.cols);
+    col = static_cast<int>(at - row * r.cols);
+    block = row * r.blocks_per_row + (col >> 5);
+    split = min(kMx8Block - (col & (kMx8Block - 1)), cols - col);
+    const int rest = cols - col - split;                       // of the row
+    more = split + min(kMx8Block, rest == 0 ? cols : rest) < 8;
+  }
+};
+// The block of each single value, one after the other.
+struct Walk {
+  int col, cols;
+  __device__ __forceinline__ Walk(const Spread& p, const Rows& r) : col(p.col), cols(static_cast<int>(r.cols)) {}
   __device__ __forceinline__ bool step() {                     // to the next value; whether a new block begins there
     ++col;
     const bool end = col == cols;
@@ -282,49 +303,74 @@ __device__ __forceinline__ uint2 load_codes_part(const uint8_t* p, int64_t at, i
 // maxima), with up to 31 values to both sides read again so that the blocks at its ends are complete.
 constexpr int kTileVecs = 2 * kThreads, kTileBlocks = kTileVecs * 8 + 64;   // rows of one value: a block each
 
+// The largest |value| of each block, from eight values of one tensor.
+__device__ __forceinline__ void collect(const f2 (&x)[4], const Spread& p, const Rows& r, int64_t block0, int blocks, uint32_t* top) {
+  const int b = static_cast<int>(p.block - block0);
+  uint32_t v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float lo, hi;
+    unpack_f32x2(x[k], lo, hi);
+    v[2 * k] = abs_bits(lo);
+    v[2 * k + 1] = abs_bits(hi);
+  }
+  if (!p.more) {
+    uint32_t m = 0u, n = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      m = max(m, e < p.split ? v[e] : 0u);
+      n = max(n, e < p.split ? 0u : v[e]);
+    }
+    if (m != 0u) atomicMax(top + b, m);
+    if (n != 0u) atomicMax(top + b + 1, n);                    // a value beyond the tensor's end is 0
+    return;
+  }
+  Walk w(p, r);
+  int at = b;
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = i == e ? v[i] : m;
+    if (m != 0u) atomicMax(top + at, m);
+    if (w.step()) at = min(at + 1, blocks - 1);
+  }
+}
+// The factor of each of eight values: factor(b) is that of block b.
+template <class Factor>
+__device__ __forceinline__ void spread_factors(const Spread& p, const Rows& r, float f0, float f1, Factor factor, f2 (&f)[4]) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < p.split ? f0 : f1;
+  if (p.more) {
+    Walk w(p, r);
+    int64_t b = p.block;
+    float now = f0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = now;
+      if (e < 7 && w.step()) {
+        b = min(b + 1, r.blocks - 1);
+        now = factor(b);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) f[k] = pack_f32x2(v[2 * k], v[2 * k + 1]);
+}
+
 template <typename T, bool kGate>
-__global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, const T* u, T* z, int64_t total, int64_t cols, int64_t blocks_per_row,
-                                                                 uint8_t* g_codes, uint8_t* g_scales, uint8_t* u_codes, uint8_t* u_scales, float* amax) {
+__global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, const T* u, T* z, const Rows r, uint8_t* g_codes, uint8_t* g_scales,
+                                                                 uint8_t* u_codes, uint8_t* u_scales, float* amax) {
   __shared__ uint32_t top[kGate ? 2 : 1][kTileBlocks];
   pdl_trigger();
   pdl_wait();
   Largest<T> largest;
   const bool coded = g_codes != nullptr;
-  const int64_t vecs = (total + 7) / 8;
+  const int64_t total = r.total, vecs = (total + 7) / 8;
   for (int64_t first = static_cast<int64_t>(blockIdx.x) * kTileVecs; first < vecs; first += static_cast<int64_t>(gridDim.x) * kTileVecs) {
     const int64_t end = min(first + kTileVecs, vecs), lo = max(first - 4, static_cast<int64_t>(0)), hi = min(end + 4, vecs);
-    const int64_t block0 = Walk(lo * 8, total, cols, blocks_per_row).block;
-    const int blocks = static_cast<int>(Walk(min(hi * 8, total) - 1, total, cols, blocks_per_row).block - block0) + 1;
-    if (coded) {
-      for (int i = threadIdx.x; i < blocks; i += kThreads) {
-        top[0][i] = 0u;
-        if (kGate) top[1][i] = 0u;
-      }
-      __syncthreads();
-    }
     f2 x[2][4], y[2][4];
-    const auto collect = [&](int64_t at, const f2 (&p)[4], const f2 (&q)[4]) {
-      Walk w(at, total, cols, blocks_per_row);
-      int b = static_cast<int>(w.block - block0);
-      uint32_t m = 0u, n = 0u;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v[2];
-        unpack_f32x2(p[e >> 1], v[0], v[1]);
-        m = max(m, abs_bits(v[e & 1]));
-        if (kGate) {
-          unpack_f32x2(q[e >> 1], v[0], v[1]);
-          n = max(n, abs_bits(v[e & 1]));
-        }
-        const bool next = w.step();
-        if (next || e == 7) {
-          if (m != 0u) atomicMax(&top[0][b], m);
-          if (kGate && n != 0u) atomicMax(&top[1][b], n);
-          m = n = 0u;
-          b = min(b + 1, blocks - 1);                          // beyond the tensor's end there are only zeros
-        }
-      }
-    };
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int64_t v = first + j * kThreads + threadIdx.x;
@@ -332,20 +378,34 @@ __global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, con
       load_part(g, v * 8, total, x[j]);
       if (kGate) load_part(u, v * 8, total, y[j]);
     }
+    const int64_t block0 = Spread(lo * 8, r).block;
+    const int blocks = static_cast<int>(Spread(min(hi * 8, total) - 1, r).block - block0) + 1;
     if (coded) {
+      for (int i = threadIdx.x; i < blocks; i += kThreads) {
+        top[0][i] = 0u;
+        if (kGate) top[1][i] = 0u;
+      }
+      __syncthreads();
       if (threadIdx.x < 8) {                                   // the neighbours' values
         const int64_t v = threadIdx.x < 4 ? first - 4 + threadIdx.x : end + threadIdx.x - 4;
         if (v >= lo && v < hi) {
-          f2 p[4], q[4];
-          load_part(g, v * 8, total, p);
-          if (kGate) load_part(u, v * 8, total, q);
-          collect(v * 8, p, q);
+          const Spread p(v * 8, r);
+          f2 n[4];
+          load_part(g, v * 8, total, n);
+          collect(n, p, r, block0, blocks, top[0]);
+          if (kGate) {
+            load_part(u, v * 8, total, n);
+            collect(n, p, r, block0, blocks, top[1]);
+          }
         }
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int64_t v = first + j * kThreads + threadIdx.x;
-        if (v < end) collect(v * 8, x[j], y[j]);
+        if (v >= end) continue;
+        const Spread p(v * 8, r);
+        collect(x[j], p, r, block0, blocks, top[0]);
+        if (kGate) collect(y[j], p, r, block0, blocks, top[1]);
       }
       __syncthreads();
     }
@@ -359,26 +419,15 @@ __global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, con
         store_part(z, at, total, o, largest);
       }
       if (!coded) continue;
-      Walk w(at, total, cols, blocks_per_row);
-      int b = static_cast<int>(w.block - block0);
-      float f = mx8_encode_factor(mx8_exponent(top[0][b])), h = kGate ? mx8_encode_factor(mx8_exponent(top[1][b])) : 0.0f;
-      float cg[8], cu[8];
+      const Spread p(at, r);
+      const int b = static_cast<int>(p.block - block0), next = min(b + 1, blocks - 1);
+      const auto put = [&](const f2 (&v8)[4], const uint32_t* tops, uint8_t* codes) {
+        const auto of = [&](uint32_t m) { return mx8_encode_factor(mx8_exponent(m)); };
+        f2 f[4];
+        spread_factors(p, r, of(tops[b]), of(tops[next]), [&](int64_t i) { return of(tops[min(static_cast<int>(i - block0), blocks - 1)]); }, f);
+        float c[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float p[2];
-        unpack_f32x2(x[j][e >> 1], p[0], p[1]);
-        cg[e] = p[e & 1] * f;
-        if (kGate) {
-          unpack_f32x2(y[j][e >> 1], p[0], p[1]);
-          cu[e] = p[e & 1] * h;
-        }
-        if (e < 7 && w.step()) {
-          b = min(b + 1, blocks - 1);
-          f = mx8_encode_factor(mx8_exponent(top[0][b]));
-          if (kGate) h = mx8_encode_factor(mx8_exponent(top[1][b]));
-        }
-      }
-      const auto put = [&](uint8_t* codes, const float (&c)[8]) {
+        for (int k = 0; k < 4; ++k) unpack_f32x2(mul2(v8[k], f[k]), c[2 * k], c[2 * k + 1]);
         const uint2 q = make_uint2(cvt_fp8x4<0>(c[0], c[1], c[2], c[3]), cvt_fp8x4<0>(c[4], c[5], c[6], c[7]));
         if (at + 8 <= total) {
           *reinterpret_cast<uint2*>(codes + at) = q;
@@ -386,12 +435,12 @@ __global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, con
           for (int e = 0; at + e < total; ++e) codes[at + e] = static_cast<uint8_t>((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
         }
       };
-      put(g_codes, cg);
-      if (kGate) put(u_codes, cu);
+      put(x[j], top[0], g_codes);
+      if (kGate) put(y[j], top[1], u_codes);
     }
     if (coded) {
       for (int i = threadIdx.x; i < blocks; i += kThreads) {   // the scales of the blocks that begin in this tile
-        const int64_t b = block0 + i, row = b / blocks_per_row, at = row * cols + (b - row * blocks_per_row) * kMx8Block;
+        const int64_t b = block0 + i, row = b / r.blocks_per_row, at = row * r.cols + (b - row * r.blocks_per_row) * kMx8Block;
         if (at < first * 8 || at >= end * 8) continue;
         g_scales[b] = static_cast<uint8_t>(mx8_exponent(top[0][i]));
         if (kGate) u_scales[b] = static_cast<uint8_t>(mx8_exponent(top[1][i]));
@@ -402,75 +451,75 @@ __global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, con
   if (amax != nullptr) raise_amax(largest.bits(), amax);
 }
 
-// Eight codes from value `at` on, each times its own block's scale: two blocks as a rule, more where rows end.
+// Eight codes from value `at` on, as they lie in memory, with the scales of the two blocks they lie in as a rule.
 struct RaggedCodes {
   uint2 q;
   uint32_t e0, e1;
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t at, int64_t total, int64_t block, int64_t blocks) {
-    q = load_codes_part(codes, at, total);
-    e0 = ld_stream(scales + block);
-    e1 = ld_stream(scales + min(block + 1, blocks - 1));
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t at, const Spread& p, const Rows& r) {
+    q = load_codes_part(codes, at, r.total);
+    e0 = ld_stream(scales + p.block);
+    e1 = ld_stream(scales + min(p.block + 1, r.blocks - 1));
   }
   template <class Factor>
-  __device__ __forceinline__ void decode(const uint8_t* scales, int64_t blocks, Walk w, Factor factor, f2 (&x)[4]) const {
+  __device__ __forceinline__ void decode(const uint8_t* scales, const Spread& p, const Rows& r, Factor factor, f2 (&x)[4]) const {
+    f2 f[4];
+    spread_factors(p, r, factor(e0), factor(e1), [&](int64_t b) { return factor(ld_stream(scales + b)); }, f);
     decode4(q.x, x[0], x[1]);
     decode4(q.y, x[2], x[3]);
-    float f[8];
-    float now = factor(e0);
-    int passed = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      f[e] = now;
-      if (e < 7 && w.step()) {
-        ++passed;
-        now = factor(passed == 1 ? e1 : ld_stream(scales + min(w.block + passed, blocks - 1)));
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], pack_f32x2(f[2 * k], f[2 * k + 1]));
+    for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], f[k]);
   }
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) ragged_load_kernel(T* x, int64_t total, int64_t cols, int64_t blocks_per_row, int64_t blocks,
-                                                               const uint8_t* codes, const uint8_t* scales) {
+__global__ void __launch_bounds__(kThreads) ragged_load_kernel(T* x, const Rows r, const uint8_t* codes, const uint8_t* scales) {
   pdl_trigger();
   pdl_wait();
   Largest<T> unused;
-  const int64_t vecs = (total + 7) / 8;
+  const int64_t vecs = (r.total + 7) / 8;
   for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < vecs; v += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const Walk w(v * 8, total, cols, blocks_per_row);
+    const Spread p(v * 8, r);
     RaggedCodes c;
-    c.load(codes, scales, v * 8, total, w.block, blocks);
-    f2 p[4];
-    c.decode(scales, blocks, w, [](uint32_t e) { return mx8_decode_factor(e); }, p);
-    store_part(x, v * 8, total, p, unused);
+    c.load(codes, scales, v * 8, p, r);
+    f2 o[4];
+    c.decode(scales, p, r, [](uint32_t e) { return mx8_decode_factor(e); }, o);
+    store_part(x, v * 8, r.total, o, unused);
   }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) ragged_gate_backward_kernel(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes,
-                                                                        const uint8_t* u_scales, const T* dz, T* dg, T* du, int64_t total,
-                                                                        int64_t cols, int64_t blocks_per_row, int64_t blocks, float* amax_dg,
-                                                                        float* amax_du) {
+                                                                        const uint8_t* u_scales, const T* dz, T* dg, T* du, const Rows r,
+                                                                        float* amax_dg, float* amax_du) {
   pdl_trigger();
   pdl_wait();
   Largest<T> lg, lu;
-  const int64_t vecs = (total + 7) / 8;
-  for (int64_t v = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; v < vecs; v += static_cast<int64_t>(gridDim.x) * kThreads) {
-    const int64_t at = v * 8;
-    const Walk w(at, total, cols, blocks_per_row);
-    RaggedCodes a, b;
-    a.load(g_codes, g_scales, at, total, w.block, blocks);
-    b.load(u_codes, u_scales, at, total, w.block, blocks);
-    f2 x[4], y[4], d[4], og[4], ou[4];
-    load_part(dz, at, total, d);
-    const auto factor = [](uint32_t e) { return scale_of(e); };
-    a.decode(g_scales, blocks, w, factor, x);
-    b.decode(u_scales, blocks, w, factor, y);
-    gate_grad8<T>(x, y, d, og, ou);
-    store_part(dg, at, total, og, lg);
-    store_part(du, at, total, ou, lu);
+  const int64_t vecs = (r.total + 7) / 8, step = static_cast<int64_t>(gridDim.x) * (2 * kThreads);
+  for (int64_t v0 = static_cast<int64_t>(blockIdx.x) * (2 * kThreads) + threadIdx.x; v0 < vecs; v0 += step) {
+    RaggedCodes a[2], b[2];
+    f2 d[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t at = (v0 + j * kThreads) * 8;
+      if (at >= r.total) continue;
+      const Spread p(at, r);
+      a[j].load(g_codes, g_scales, at, p, r);
+      b[j].load(u_codes, u_scales, at, p, r);
+      load_part(dz, at, r.total, d[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t at = (v0 + j * kThreads) * 8;
+      if (at >= r.total) continue;
+      const Spread p(at, r);
+      f2 x[4], y[4], og[4], ou[4];
+      const auto factor = [](uint32_t e) { return scale_of(e); };
+      a[j].decode(g_scales, p, r, factor, x);
+      b[j].decode(u_scales, p, r, factor, y);
+      gate_grad8<T>(x, y, d[j], og, ou);
+      store_part(dg, at, r.total, og, lg);
+      store_part(du, at, r.total, ou, lu);
+    }
   }
   if (amax_dg != nullptr) raise_amax(lg.bits(), amax_dg);
   if (amax_du != nullptr) {
@@ -483,21 +532,21 @@ inline bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) =
 
 // The extent of a call, checked.
 struct Extent {
-  int64_t total, blocks, blocks_per_row, slots;   // slots: kFlat, kVector
+  int64_t blocks_per_row, slots;   // slots: kFlat, kVector
+  Rows rows_;                      // kRagged
   Cut cut;
   bool set(int64_t rows, int64_t cols, int dtype) {
     if (rows < 1 || cols < 1 || rows > (1ll << 31) || cols > (1ll << 31) || rows > (1ll << 42) / cols) return false;
     if (dtype != FALQON_BF16 && dtype != FALQON_F32) return false;
     cut = cols % kMx8Block == 0 ? kFlat : cols % 8 == 0 ? kVector : kRagged;
     blocks_per_row = (cols + kMx8Block - 1) / kMx8Block;
-    blocks = rows * blocks_per_row;
-    slots = blocks * 4;
-    total = rows * cols;
+    slots = rows * blocks_per_row * 4;
+    rows_ = Rows{cols, blocks_per_row, rows * cols, rows * blocks_per_row, ~0ull / static_cast<uint64_t>(cols) + 1};
     return true;
   }
   // CTAs for runs of `per_cta` vectors, eight to an SM at the most.
   dim3 grid(int64_t per_cta) const {
-    const int64_t vecs = cut == kRagged ? (total + 7) / 8 : slots, ctas = (vecs + per_cta - 1) / per_cta, cap = static_cast<int64_t>(sm_count()) * 8;
+    const int64_t vecs = cut == kRagged ? (rows_.total + 7) / 8 : slots, ctas = (vecs + per_cta - 1) / per_cta, cap = static_cast<int64_t>(sm_count()) * 8;
     return dim3(static_cast<unsigned>(ctas < cap ? ctas : cap));
   }
 };
@@ -536,7 +585,7 @@ int falqon_checkpoint_save(const void* x, int dtype, int64_t rows, int64_t cols,
       [&](auto type) {
         using T = decltype(type);
         return finish(launch_pdl(ragged_encode_kernel<T, false>, e.grid(kTileVecs), dim3(kThreads), 0, st, 1, static_cast<const T*>(x),
-                                 static_cast<const T*>(nullptr), static_cast<T*>(nullptr), e.total, cols, e.blocks_per_row, codes, scales,
+                                 static_cast<const T*>(nullptr), static_cast<T*>(nullptr), e.rows_, codes, scales,
                                  static_cast<uint8_t*>(nullptr), static_cast<uint8_t*>(nullptr), static_cast<float*>(nullptr)));
       });
 }
@@ -556,8 +605,8 @@ int falqon_checkpoint_load(const uint8_t* codes, const uint8_t* scales, int64_t 
       },
       [&](auto type) {
         using T = decltype(type);
-        return finish(launch_pdl(ragged_load_kernel<T>, e.grid(kThreads), dim3(kThreads), 0, st, 1, static_cast<T*>(x), e.total, cols,
-                                 e.blocks_per_row, e.blocks, codes, scales));
+        return finish(launch_pdl(ragged_load_kernel<T>, e.grid(kThreads), dim3(kThreads), 0, st, 1, static_cast<T*>(x), e.rows_,
+                                 codes, scales));
       });
 }
 
@@ -580,7 +629,7 @@ int falqon_gate_forward(const void* g, const void* u, int dtype, int64_t rows, i
       [&](auto type) {
         using T = decltype(type);
         return finish(launch_pdl(ragged_encode_kernel<T, true>, e.grid(kTileVecs), dim3(kThreads), 0, st, 1, static_cast<const T*>(g),
-                                 static_cast<const T*>(u), static_cast<T*>(z), e.total, cols, e.blocks_per_row, g_codes, g_scales, u_codes,
+                                 static_cast<const T*>(u), static_cast<T*>(z), e.rows_, g_codes, g_scales, u_codes,
                                  u_scales, amax_out));
       });
 }
@@ -603,9 +652,8 @@ int falqon_gate_backward(const uint8_t* g_codes, const uint8_t* g_scales, const 
       },
       [&](auto type) {
         using T = decltype(type);
-        return finish(launch_pdl(ragged_gate_backward_kernel<T>, e.grid(kThreads), dim3(kThreads), 0, st, 1, g_codes, g_scales, u_codes, u_scales,
-                                 static_cast<const T*>(dz), static_cast<T*>(dg), static_cast<T*>(du), e.total, cols, e.blocks_per_row, e.blocks,
-                                 amax_dg, amax_du));
+        return finish(launch_pdl(ragged_gate_backward_kernel<T>, e.grid(2 * kThreads), dim3(kThreads), 0, st, 1, g_codes, g_scales, u_codes, u_scales,
+                                 static_cast<const T*>(dz), static_cast<T*>(dg), static_cast<T*>(du), e.rows_, amax_dg, amax_du));
       });
 }
 
