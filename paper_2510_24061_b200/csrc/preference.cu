@@ -6,6 +6,7 @@
 // a row of the type's lowest values (a mask over the whole vocabulary) does not overflow on the way.
 // HBM-bound: the forward reads each counted row once, the backward reads it again and writes every row once.
 #include <cfloat>
+#include <type_traits>
 
 #include "../../include/falqon_train.h"
 #include "internal.h"
@@ -19,6 +20,7 @@ constexpr int kRowThreads = 256;
 constexpr int kSeqThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxParts = 64;              // parts of one row
+constexpr float kNotCounted = -1.0f;       // in the place of a row's (first part's) sum, which is never negative
 constexpr size_t kCounterBytes = 256;      // the last-CTA counter at the head of the scratch
 
 __device__ __forceinline__ float ex2(float x) {
@@ -29,15 +31,52 @@ __device__ __forceinline__ float ex2(float x) {
 
 template <typename T>
 struct Row {                               // vectors of 16 bytes
-  static constexpr int kN = 16 / sizeof(T);
+  static constexpr int kN = 16 / sizeof(T), kPairs = kN / 2;
 };
-__device__ __forceinline__ void expand(const uint4& q, float (&x)[8], bf16_t) { unpack8(q, x); }
-__device__ __forceinline__ void expand(const uint4& q, float (&x)[4], float) {
-  x[0] = __uint_as_float(q.x), x[1] = __uint_as_float(q.y), x[2] = __uint_as_float(q.z), x[3] = __uint_as_float(q.w);
+__device__ __forceinline__ void expand(const uint4& q, f2 (&x)[4], bf16_t) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
 }
-__device__ __forceinline__ uint4 shrink(const float (&x)[8], bf16_t) { return pack8(x); }
-__device__ __forceinline__ uint4 shrink(const float (&x)[4], float) {
-  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+__device__ __forceinline__ void expand(const uint4& q, f2 (&x)[2], float) {
+  x[0] = pack_f32x2(__uint_as_float(q.x), __uint_as_float(q.y));
+  x[1] = pack_f32x2(__uint_as_float(q.z), __uint_as_float(q.w));
+}
+__device__ __forceinline__ uint4 shrink(const f2 (&x)[4], bf16_t) {
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+  return pack8(v);
+}
+__device__ __forceinline__ uint4 shrink(const f2 (&x)[2], float) {
+  float v[4];
+  unpack_f32x2(x[0], v[0], v[1]);
+  unpack_f32x2(x[1], v[2], v[3]);
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+// The largest of a vector's values (a NaN may be passed over: its exponential is one all the same).
+__device__ __forceinline__ float largest_of(const uint4* q, int n, bf16_t) {
+  uint32_t m = 0xFF80FF80u;                // two times -inf
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    const uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[k]));
+  }
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+}
+__device__ __forceinline__ float largest_of(const uint4* q, int n, float) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < n; ++j)
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(q[j].x), __uint_as_float(q[j].y)), fmaxf(__uint_as_float(q[j].z), __uint_as_float(q[j].w))));
+  return m;
+}
+// exp(x - m) of two values.
+__device__ __forceinline__ f2 exp_of2(f2 x, f2 minus_m) {
+  float lo, hi;
+  unpack_f32x2(mul2(add2(x, minus_m), twice(kLog2e)), lo, hi);
+  return pack_f32x2(ex2(lo), ex2(hi));
 }
 
 // A row that may start anywhere: `head` single values up to a 16-byte boundary, `body` vectors, and the rest.
@@ -81,45 +120,56 @@ struct Running {
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
-                                                                int parts, float2* out, unsigned int* counter, int* status) {
+                                                                int parts, float2* out, float* target_logit, unsigned int* counter, int* status) {
   __shared__ float red_m[kRowThreads / 32], red_s[kRowThreads / 32];
   pdl_trigger();
   pdl_wait();
-  constexpr int n = Row<T>::kN;
   if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0u;   // for the kernel after this one
   const int64_t row = blockIdx.x / parts;
   const int part = static_cast<int>(blockIdx.x - row * parts);
   const int64_t target = ld_stream(targets + row);
-  if (target < 0) return;
-  if (target >= vocab) {
-    if (part == 0 && threadIdx.x == 0) atomicExch(status, FALQON_ERR_INVALID_ARG);
+  if (target < 0 || target >= vocab) {
+    if (part == 0 && threadIdx.x == 0) {
+      out[row * parts] = make_float2(0.0f, kNotCounted);
+      if (target >= vocab) atomicExch(status, FALQON_ERR_INVALID_ARG);
+    }
     return;
   }
   const T* p = logits + row * ld;
+  float at_target = 0.0f;                  // fetched here, beside the stream, and not in a gather of the next kernel
+  if (part == 0 && threadIdx.x == 0) at_target = load1(p + target);
   const Span sp = span_of(p, vocab);
   Running r;
   const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
   const int64_t begin = sp.body * part / parts, end = sp.body * (part + 1) / parts;
+  f2 sum = 0;                              // the running sum, two halves of it
   constexpr int kUnroll = 4;
-  for (int64_t v = begin + threadIdx.x; v < end; v += kRowThreads * kUnroll) {
+  constexpr uint32_t kNone = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;   // -inf: adds nothing
+  for (int64_t v = begin + threadIdx.x; v < end; v += kUnroll * kRowThreads) {
     uint4 q[kUnroll];
+    if (v + (kUnroll - 1) * kRowThreads < end) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j)
-      if (v + j * kRowThreads < end) q[j] = ld_stream(body + v + j * kRowThreads);
+      for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kRowThreads);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j)
+        q[j] = v + j * kRowThreads < end ? ld_stream(body + v + j * kRowThreads) : make_uint4(kNone, kNone, kNone, kNone);
+    }
+    const float top = largest_of(q, kUnroll, T{});
+    if (top > r.m) {                       // seldom after the first vectors
+      sum = mul2(sum, twice(exp_of(r.m - top)));
+      r.m = top;
+    }
+    const f2 minus = twice(-r.base());
 #pragma unroll
     for (int j = 0; j < kUnroll; ++j) {
-      if (v + j * kRowThreads >= end) break;
-      float x[n];
+      f2 x[Row<T>::kPairs];
       expand(q[j], x, T{});
-      float top = x[0];
 #pragma unroll
-      for (int i = 1; i < n; ++i) top = fmaxf(top, x[i]);
-      r.raise(top);
-      const float b = r.base();
-#pragma unroll
-      for (int i = 0; i < n; ++i) r.s += exp_of(x[i] - b);
+      for (int k = 0; k < Row<T>::kPairs; ++k) sum = add2(sum, exp_of2(x[k], minus));
     }
   }
+  r.s = halves(sum);
   if (part == 0) {
     if (static_cast<int>(threadIdx.x) < sp.head) r.add(load1(p + threadIdx.x));
     if (threadIdx.x < vocab - sp.tail) r.add(load1(p + sp.tail + threadIdx.x));
@@ -138,13 +188,15 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits,
 #pragma unroll
     for (int w = 1; w < kRowThreads / 32; ++w) r.join(red_m[w], red_s[w]);
     out[row * parts + part] = make_float2(r.m, r.s);
+    if (part == 0) target_logit[row] = at_target;
   }
 }
 
 struct SeqArgs {
-  const int64_t *targets, *cu;
-  int64_t rows, vocab, ld, seqs;
+  const int64_t* cu;
+  int64_t rows;
   const float2* part;                      // [rows][parts]
+  const float* target_logit;               // [rows]
   int parts;
   float2* stats;                           // [rows], nullable (may be `part` when parts == 1)
   float *logp, *seq_logp;                  // logp nullable
@@ -156,50 +208,53 @@ struct SeqArgs {
   float beta, margin, smoothing, nll_weight;
 };
 
-__device__ __forceinline__ double block_sum(double v, double* red) {   // fixed order; every thread gets it
+// Sums over the CTA in a fixed order, for its first warp.  64-bit additions are slow here (a warp's takes many cycles), so sums are
+// taken in 64 bits once per row and then by shuffles, counts as integers, and one warp does the rest for all.
+struct Sums {
+  double first, second;                    // of the chosen (or only) and the rejected sequence
+  unsigned n_first, n_second;
+};
+__device__ __forceinline__ Sums warp_sums(Sums v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  for (int o = 16; o > 0; o >>= 1) {
+    v.first += __shfl_xor_sync(0xFFFFFFFFu, v.first, o);
+    v.second += __shfl_xor_sync(0xFFFFFFFFu, v.second, o);
+  }
+  v.n_first = __reduce_add_sync(0xFFFFFFFFu, v.n_first);
+  v.n_second = __reduce_add_sync(0xFFFFFFFFu, v.n_second);
+  return v;
+}
+__device__ __forceinline__ Sums cta_sums(Sums v, Sums* red) {
+  v = warp_sums(v);
+  const int warps = static_cast<int>(blockDim.x >> 5);
+  if (warps == 1) return v;
   __syncthreads();
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  double t = 0.0;
-#pragma unroll
-  for (int w = 0; w < kSeqThreads / 32; ++w) t += red[w];
-  return t;
+  if (threadIdx.x >= 32) return v;
+  return warp_sums(static_cast<int>(threadIdx.x) < warps ? red[threadIdx.x] : Sums{0.0, 0.0, 0u, 0u});
 }
 
-// The log-probability of one row (0, not counted: false).
-template <typename T>
-__device__ __forceinline__ bool row_logp(const SeqArgs& a, const T* logits, int64_t row, float& lp) {
-  const int64_t target = ld_stream(a.targets + row);
-  lp = 0.0f;
-  if (target < 0 || target >= a.vocab) return false;
-  const float x = load1(logits + row * a.ld + target);
-  Running r;
-  for (int i = 0; i < a.parts; ++i) {
-    const float2 q = ld_stream(a.part + row * a.parts + i);
-    r.join(q.x, q.y);
+// The log-probability of one row (0 and false: not counted) from its parts.
+__device__ __forceinline__ bool row_logp(const SeqArgs& a, int64_t row, float& lp) {
+  const float x = ld_stream(a.target_logit + row);   // anything where the row is not counted
+  const float2* part = a.part + row * a.parts;
+  const float2 head = ld_stream(part);
+  Running r{head.x, head.y};
+  constexpr int kAhead = 8;
+  for (int i = 1; i < a.parts; i += kAhead) {
+    float2 q[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) q[j] = i + j < a.parts ? ld_stream(part + i + j) : make_float2(-INFINITY, 0.0f);
+    if (head.y == kNotCounted) break;                // the other parts were not written
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) r.join(q[j].x, q[j].y);
   }
+  lp = 0.0f;
+  if (head.y == kNotCounted) return false;
   if (a.stats != nullptr) a.stats[row] = make_float2(r.m, r.s);
   lp = (x - r.m) - logf(r.s);
   return true;
-}
-
-// Rows [begin, end) of one sequence: the sum of their log-probabilities and how many are counted; logp per row is stored.
-template <typename T>
-__device__ __forceinline__ void sequence_sum(const SeqArgs& a, const T* logits, int64_t begin, int64_t end, double* red, double& sum,
-                                             double& count) {
-  double s = 0.0, n = 0.0;
-  for (int64_t row = begin + threadIdx.x; row < end; row += kSeqThreads) {
-    float lp;
-    if (row_logp(a, logits, row, lp)) {
-      s += static_cast<double>(lp);
-      n += 1.0;
-    }
-    if (a.logp != nullptr) a.logp[row] = lp;
-  }
-  sum = block_sum(s, red);
-  count = block_sum(n, red);
 }
 
 __device__ __forceinline__ int64_t bound_at(const SeqArgs& a, int64_t i) {   // cu_rows[i], brought into [0, rows]
@@ -209,80 +264,109 @@ __device__ __forceinline__ int64_t bound_at(const SeqArgs& a, int64_t i) {   // 
 
 // Rows outside every sequence: not counted.
 __device__ __forceinline__ void clear_rows(const SeqArgs& a, int64_t begin, int64_t end) {
-  for (int64_t row = begin + threadIdx.x; row < end; row += kSeqThreads) {
+  for (int64_t row = begin + threadIdx.x; row < end; row += blockDim.x) {
     if (a.logp != nullptr) a.logp[row] = 0.0f;
     if (a.dlogp != nullptr) a.dlogp[row] = 0.0f;
   }
 }
 
-__device__ __forceinline__ double log_sigmoid(double d) { return (d < 0.0 ? d : 0.0) - log1p(exp(-fabs(d))); }
+__device__ __forceinline__ float log_sigmoid(float d) { return fminf(d, 0.0f) - log1pf(expf(-fabsf(d))); }
+__device__ __forceinline__ float logistic(float d) { return 1.0f / (1.0f + expf(-d)); }
 
-template <typename T, bool kPairs>
-__global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a, const T* logits) {
-  __shared__ double red[kSeqThreads / 32];
+template <bool kPairs>
+__global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) {
+  __shared__ Sums red[kSeqThreads / 32];
+  __shared__ float s_coef[2];
   __shared__ bool s_last;
   pdl_trigger();
   pdl_wait();
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kPairs ? 2 : 1);
-  const int64_t begin = bound_at(a, first), mid = max(begin, bound_at(a, first + 1));
-  double sum, count;
+  const int64_t begin = bound_at(a, first), mid = max(begin, bound_at(a, first + 1)), end = kPairs ? max(mid, bound_at(a, first + 2)) : mid;
+  float ref[2] = {0.0f, 0.0f};
+  if (kPairs && a.ref != nullptr) {
+    ref[0] = ld_stream(a.ref + first);
+    ref[1] = ld_stream(a.ref + first + 1);
+  }
   if (blockIdx.x == 0) clear_rows(a, 0, begin);
-  sequence_sum(a, logits, begin, mid, red, sum, count);
-  const double per = a.average ? 1.0 / max(count, 1.0) : 1.0;
-  if constexpr (!kPairs) {
-    if (blockIdx.x == gridDim.x - 1) clear_rows(a, mid, a.rows);
-    if (threadIdx.x == 0) a.seq_logp[first] = static_cast<float>(sum * per);
-  } else {
-    const int64_t end = max(mid, bound_at(a, first + 2));
-    double sum2, count2;
-    sequence_sum(a, logits, mid, end, red, sum2, count2);
-    if (blockIdx.x == gridDim.x - 1) clear_rows(a, end, a.rows);
-    const double per2 = a.average ? 1.0 / max(count2, 1.0) : 1.0;
-    const double chosen = sum * per, rejected = sum2 * per2;
-    const double u = a.ref != nullptr ? (chosen - static_cast<double>(ld_stream(a.ref + first))) -
-                                            (rejected - static_cast<double>(ld_stream(a.ref + first + 1)))
-                                      : chosen - rejected;
-    const double beta = a.beta, d = beta * u - a.margin;
-    double l, du;
-    if (a.kind == FALQON_PREFERENCE_SIGMOID) {
-      const double eps = a.smoothing;      // a term of weight 0 is left out: its logarithm may be infinite
-      l = (eps < 1.0 ? -(1.0 - eps) * log_sigmoid(d) : 0.0) - (eps > 0.0 ? eps * log_sigmoid(-d) : 0.0);
-      du = beta * (-(1.0 - eps) / (1.0 + exp(d)) + eps / (1.0 + exp(-d)));
-    } else if (a.kind == FALQON_PREFERENCE_HINGE) {
-      l = d < 1.0 ? 1.0 - d : d >= 1.0 ? 0.0 : d;     // a NaN stays one
-      du = d < 1.0 ? -beta : d >= 1.0 ? 0.0 : d;
+  if (blockIdx.x == gridDim.x - 1) clear_rows(a, end, a.rows);
+  uint64_t seen = 0;                       // which of the thread's first 64 rows are counted
+  int turn = 0;
+  Sums t{0.0, 0.0, 0u, 0u};
+  for (int64_t row = begin + threadIdx.x; row < end; row += blockDim.x, ++turn) {
+    float lp;
+    const bool counted = row_logp(a, row, lp);
+    if (a.logp != nullptr) a.logp[row] = lp;
+    if (!counted) continue;
+    if (turn < 64) seen |= 1ull << turn;
+    if (kPairs && row >= mid) {
+      t.second += static_cast<double>(lp);
+      ++t.n_second;
     } else {
-      const double t = u - a.margin - 1.0 / (2.0 * beta);
-      l = t * t;
-      du = 2.0 * t;
+      t.first += static_cast<double>(lp);
+      ++t.n_first;
     }
-    const double pairs = static_cast<double>(gridDim.x);
-    const double nll = static_cast<double>(a.nll_weight) / max(count, 1.0);
-    if (nll != 0.0) l -= nll * sum;
-    if (threadIdx.x == 0) {
-      a.seq_logp[first] = static_cast<float>(chosen);
-      a.seq_logp[first + 1] = static_cast<float>(rejected);
-      a.pair_loss[blockIdx.x] = static_cast<float>(l);
-    }
-    if (a.dlogp != nullptr) {
-      const float c = static_cast<float>((du * per - nll) / pairs), r = static_cast<float>(-du * per2 / pairs);
-      for (int64_t row = begin + threadIdx.x; row < end; row += kSeqThreads) {
-        const int64_t target = ld_stream(a.targets + row);
-        a.dlogp[row] = target < 0 || target >= a.vocab ? 0.0f : row < mid ? c : r;
+  }
+  t = cta_sums(t, red);
+  if (threadIdx.x < 32) {
+    const float n1 = static_cast<float>(max(t.n_first, 1u)), n2 = static_cast<float>(max(t.n_second, 1u));
+    const float chosen = static_cast<float>(t.first) / (a.average ? n1 : 1.0f);
+    if constexpr (!kPairs) {
+      if (threadIdx.x == 0) a.seq_logp[first] = chosen;
+    } else {
+      const float rejected = static_cast<float>(t.second) / (a.average ? n2 : 1.0f);
+      // u in 64 bits where it is a difference of sums of many rows
+      const float u = a.average ? (chosen - ref[0]) - (rejected - ref[1])
+                                : static_cast<float>((t.first - static_cast<double>(ref[0])) - (t.second - static_cast<double>(ref[1])));
+      const float beta = a.beta, d = __fmaf_rn(beta, u, -a.margin);
+      float l, du;
+      if (a.kind == FALQON_PREFERENCE_SIGMOID) {
+        const float eps = a.smoothing;     // a term of weight 0 is left out: its logarithm may be infinite
+        l = (eps < 1.0f ? -(1.0f - eps) * log_sigmoid(d) : 0.0f) - (eps > 0.0f ? eps * log_sigmoid(-d) : 0.0f);
+        du = beta * (eps * logistic(d) - (1.0f - eps) * logistic(-d));
+      } else if (a.kind == FALQON_PREFERENCE_HINGE) {
+        l = d < 1.0f ? 1.0f - d : d >= 1.0f ? 0.0f : d;     // a NaN stays one
+        du = d < 1.0f ? -beta : d >= 1.0f ? 0.0f : d;
+      } else {
+        const float v = u - a.margin - 0.5f / beta;
+        l = v * v;
+        du = 2.0f * v;
+      }
+      const float pairs = static_cast<float>(gridDim.x), nll = a.nll_weight / n1;
+      if (nll != 0.0f) l = __fmaf_rn(-nll, static_cast<float>(t.first), l);
+      if (threadIdx.x == 0) {
+        a.seq_logp[first] = chosen;
+        a.seq_logp[first + 1] = rejected;
+        a.pair_loss[blockIdx.x] = l;
+        if (gridDim.x == 1) *a.loss = l;
+        s_coef[0] = ((a.average ? du / n1 : du) - nll) / pairs;
+        s_coef[1] = -(a.average ? du / n2 : du) / pairs;
       }
     }
+  }
+  if constexpr (kPairs) {
     // the CTA that finishes last takes the mean of all pairs' losses, in an order of its own that never changes
     if (threadIdx.x == 0) {
-      __threadfence();
-      s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
+      s_last = false;
+      if (gridDim.x > 1) {
+        __threadfence();
+        s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
+      }
     }
     __syncthreads();
+    if (a.dlogp != nullptr) {
+      const float c = s_coef[0], r = s_coef[1];
+      turn = 0;
+      for (int64_t row = begin + threadIdx.x; row < end; row += blockDim.x, ++turn) {
+        const bool counted = turn < 64 ? (seen >> turn & 1) != 0 : ld_stream(&a.part[row * a.parts].y) != kNotCounted;
+        a.dlogp[row] = !counted ? 0.0f : row < mid ? c : r;
+      }
+    }
     if (s_last) {
       __threadfence();
-      double t = 0.0;
-      for (int64_t i = threadIdx.x; i < gridDim.x; i += kSeqThreads) t += static_cast<double>(ld_stream(a.pair_loss + i));
-      t = block_sum(t, red);
-      if (threadIdx.x == 0) *a.loss = static_cast<float>(t / pairs);
+      Sums all{0.0, 0.0, 0u, 0u};
+      for (int64_t i = threadIdx.x; i < gridDim.x; i += blockDim.x) all.first += static_cast<double>(ld_stream(a.pair_loss + i));
+      all = cta_sums(all, red);
+      if (threadIdx.x == 0) *a.loss = static_cast<float>(all.first / static_cast<double>(gridDim.x));
     }
   }
 }
@@ -295,8 +379,9 @@ __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(const T* logits
   pdl_trigger();
   pdl_wait();
   constexpr int n = Row<T>::kN;
-  const int64_t row = blockIdx.x / parts;
-  const int part = static_cast<int>(blockIdx.x - row * parts);
+  // the last rows first: of what the forward has read, they are still in L2
+  const int64_t task = static_cast<int64_t>(gridDim.x) - 1 - blockIdx.x, row = task / parts;
+  const int part = static_cast<int>(task - row * parts);
   const float c = ld_stream(dlogp + row) * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
   const T* p = logits + row * ld;
   T* o = out + row * ld_out;
@@ -312,45 +397,58 @@ __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(const T* logits
     const float g = zero ? 0.0f : __fmaf_rn(f, exp_of(load1(p + i) - st.x), i == target ? c : 0.0f);
     mx = max(mx, store1(o + i, g));
   };
-  constexpr int kUnroll = 4;
-  for (int64_t v = begin + threadIdx.x; v < end; v += kRowThreads * kUnroll) {
-    uint4 q[kUnroll];
+  // one vector: its values' gradients
+  const auto put = [&](int64_t v, const uint4& q) {
+    const int64_t at = sp.head + v * n;
+    f2 x[Row<T>::kPairs];
+    if (zero) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j)
-      if (!zero && v + j * kRowThreads < end) q[j] = ld_stream(body + v + j * kRowThreads);
+      for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = 0;
+    } else {
+      expand(q, x, T{});
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      if (v + j * kRowThreads >= end) break;
-      const int64_t at = sp.head + (v + j * kRowThreads) * n;
-      float x[n];
-      if (zero) {
+      for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = mul2(twice(f), exp_of2(x[k], twice(-st.x)));
+      if (target >= at && target < at + n) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = 0.0f;
-      } else {
-        expand(q[j], x, T{});
-#pragma unroll
-        for (int i = 0; i < n; ++i) x[i] = f * exp_of(x[i] - st.x);
-        if (target >= at && target < at + n) {
-#pragma unroll
-          for (int i = 0; i < n; ++i)
-            if (at + i == target) x[i] += c;
+        for (int k = 0; k < Row<T>::kPairs; ++k) {
+          if (at + 2 * k == target) x[k] = add2(x[k], pack_f32x2(c, 0.0f));
+          if (at + 2 * k + 1 == target) x[k] = add2(x[k], pack_f32x2(0.0f, c));
         }
-      }
-      if (kSame) {
-        const uint4 w = shrink(x, T{});
-        *reinterpret_cast<uint4*>(o + at) = w;
-        if (amax != nullptr) {
-          float s[n];
-          expand(w, s, T{});
-#pragma unroll
-          for (int i = 0; i < n; ++i) mx = max(mx, abs_bits(s[i]));
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < n; ++i) mx = max(mx, store1(o + at + i, x[i]));
       }
     }
+    const uint4 w = shrink(x, T{});
+    if (kSame) {
+      *reinterpret_cast<uint4*>(o + at) = w;
+      if (amax != nullptr) {
+        expand(w, x, T{});
+#pragma unroll
+        for (int k = 0; k < Row<T>::kPairs; ++k) {
+          float lo, hi;
+          unpack_f32x2(x[k], lo, hi);
+          mx = max(mx, max(abs_bits(lo), abs_bits(hi)));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < Row<T>::kPairs; ++k) {
+        float lo, hi;
+        unpack_f32x2(x[k], lo, hi);
+        mx = max(mx, max(store1(o + at + 2 * k, lo), store1(o + at + 2 * k + 1, hi)));
+      }
+    }
+  };
+  constexpr int kUnroll = 4;
+  int64_t v = begin + threadIdx.x;
+  for (; v + (kUnroll - 1) * kRowThreads < end; v += kUnroll * kRowThreads) {
+    uint4 q[kUnroll];
+    if (!zero) {
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kRowThreads);
+    }
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) put(v + j * kRowThreads, q[j]);
   }
+  for (; v < end; v += kRowThreads) put(v, zero ? make_uint4(0u, 0u, 0u, 0u) : ld_stream(body + v));
   if (part == 0) {
     if (static_cast<int>(threadIdx.x) < sp.head) one(threadIdx.x);
     if (threadIdx.x < vocab - sp.tail) one(sp.tail + threadIdx.x);
@@ -377,13 +475,19 @@ int parts_for(int64_t rows, int64_t vocab, int dtype) {
   return static_cast<int>(parts < 1 ? 1 : parts);
 }
 
+// A thread per row of the average sequence (or pair), a warp at least.
+unsigned sequence_threads(int64_t rows, int64_t ctas) {
+  const int64_t t = (rows / ctas + 31) / 32 * 32;
+  return static_cast<unsigned>(t < 32 ? 32 : t > kSeqThreads ? kSeqThreads : t);
+}
+
 cudaError_t launch_row_stats(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts,
-                             float2* out, unsigned int* counter, int* status, cudaStream_t stream) {
+                             float2* out, float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
   const dim3 grid(static_cast<unsigned>(rows * parts)), block(kRowThreads);
   return dtype == FALQON_BF16 ? launch_pdl(row_stats_kernel<bf16_t>, grid, block, 0, stream, 1, static_cast<const bf16_t*>(logits), vocab,
-                                           ld, targets, parts, out, counter, status)
+                                           ld, targets, parts, out, target_logit, counter, status)
                               : launch_pdl(row_stats_kernel<float>, grid, block, 0, stream, 1, static_cast<const float*>(logits), vocab,
-                                           ld, targets, parts, out, counter, status);
+                                           ld, targets, parts, out, target_logit, counter, status);
 }
 
 }  // namespace
@@ -395,7 +499,7 @@ extern "C" {
 
 size_t falqon_preference_scratch_bytes(int64_t rows, int64_t vocab, int dtype) {
   if (!sizes_ok(rows, vocab, dtype)) return 0;
-  return kCounterBytes + static_cast<size_t>(rows) * parts_for(rows, vocab, dtype) * sizeof(float2);
+  return kCounterBytes + static_cast<size_t>(rows) * (parts_for(rows, vocab, dtype) * sizeof(float2) + sizeof(float));
 }
 
 int falqon_sequence_logprob(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets,
@@ -411,23 +515,18 @@ int falqon_sequence_logprob(const void* logits, int dtype, int64_t rows, int64_t
   const int parts = parts_for(rows, vocab, dtype);
   SeqArgs a{};
   float2* part = reinterpret_cast<float2*>(static_cast<uint8_t*>(scratch) + kCounterBytes);
-  a.targets = targets;
   a.cu = cu_rows;
   a.rows = rows;
-  a.vocab = vocab;
-  a.ld = ld;
-  a.seqs = n_seq;
+  float* target_logit = reinterpret_cast<float*>(part + rows * parts);
   a.part = part;
   a.parts = parts;
+  a.target_logit = target_logit;
   a.logp = logp;
   a.seq_logp = seq_logp;
   a.average = average != 0;
-  const cudaError_t e = launch_row_stats(logits, dtype, rows, vocab, ld, targets, parts, part, static_cast<unsigned int*>(scratch), status, st);
+  const cudaError_t e = launch_row_stats(logits, dtype, rows, vocab, ld, targets, parts, part, target_logit, static_cast<unsigned int*>(scratch), status, st);
   if (e != cudaSuccess) return FALQON_ERR_CUDA;
-  const dim3 grid(static_cast<unsigned>(n_seq)), block(kSeqThreads);
-  return finish(dtype == FALQON_BF16
-                    ? launch_pdl(sequence_kernel<bf16_t, false>, grid, block, 0, st, 1, a, static_cast<const bf16_t*>(logits))
-                    : launch_pdl(sequence_kernel<float, false>, grid, block, 0, st, 1, a, static_cast<const float*>(logits)));
+  return finish(launch_pdl(sequence_kernel<false>, dim3(static_cast<unsigned>(n_seq)), dim3(sequence_threads(rows, n_seq)), 0, st, 1, a));
 }
 
 static bool preference_ok(const falqon_preference* p) {
@@ -452,16 +551,15 @@ int falqon_preference_forward(const falqon_preference* p, const void* logits, co
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int parts = parts_for(p->rows, p->vocab, p->dtype);
   float2* stats = reinterpret_cast<float2*>(row_stats);
-  float2* part = parts == 1 && stats != nullptr ? stats : reinterpret_cast<float2*>(static_cast<uint8_t*>(scratch) + kCounterBytes);
+  float2* const own = reinterpret_cast<float2*>(static_cast<uint8_t*>(scratch) + kCounterBytes);
+  float2* part = parts == 1 && stats != nullptr ? stats : own;
+  float* target_logit = reinterpret_cast<float*>(own + p->rows * parts);
   SeqArgs a{};
-  a.targets = targets;
   a.cu = cu_rows;
   a.rows = p->rows;
-  a.vocab = p->vocab;
-  a.ld = p->ld;
-  a.seqs = 2 * p->pairs;
   a.part = part;
   a.parts = parts;
+  a.target_logit = target_logit;
   a.stats = part == stats ? nullptr : stats;
   a.logp = logp;
   a.seq_logp = seq_logp;
@@ -476,12 +574,9 @@ int falqon_preference_forward(const falqon_preference* p, const void* logits, co
   a.margin = p->margin;
   a.smoothing = p->label_smoothing;
   a.nll_weight = p->nll_weight;
-  const cudaError_t e = launch_row_stats(logits, p->dtype, p->rows, p->vocab, p->ld, targets, parts, part, a.counter, status, st);
+  const cudaError_t e = launch_row_stats(logits, p->dtype, p->rows, p->vocab, p->ld, targets, parts, part, target_logit, a.counter, status, st);
   if (e != cudaSuccess) return FALQON_ERR_CUDA;
-  const dim3 grid(static_cast<unsigned>(p->pairs)), block(kSeqThreads);
-  return finish(p->dtype == FALQON_BF16
-                    ? launch_pdl(sequence_kernel<bf16_t, true>, grid, block, 0, st, 1, a, static_cast<const bf16_t*>(logits))
-                    : launch_pdl(sequence_kernel<float, true>, grid, block, 0, st, 1, a, static_cast<const float*>(logits)));
+  return finish(launch_pdl(sequence_kernel<true>, dim3(static_cast<unsigned>(p->pairs)), dim3(sequence_threads(p->rows, p->pairs)), 0, st, 1, a));
 }
 
 int falqon_preference_backward(const falqon_preference* p, const void* logits, const int64_t* targets, const float* row_stats,

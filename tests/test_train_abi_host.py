@@ -152,8 +152,8 @@ def test_preference_refusals(fq, tr):
 def test_scratch_sizes(tr):
     """A split row needs more scratch than a whole one, never less than one part per row."""
     size = tr.lib.falqon_preference_scratch_bytes
-    assert size(4096, 32000, 0) == 256 + 4096 * 8
-    assert size(1, 32000, 0) > 256 + 8
+    assert 4096 * 8 < size(4096, 32000, 0) < 4096 * 16
+    assert size(1, 32000, 0) > 8 * 8
     norm = tr.lib.falqon_block_norm_scratch_bytes
     assert norm(plan(tr, rows=4096, cols=4096, rows_per_gate=4096)) >= 2 * 4096 * 4
     assert norm(plan(tr, rows=4096, cols=64, rows_per_gate=1)) >= 4096 * 64 * 4         # a sum for every gate row
