@@ -15,7 +15,7 @@
 namespace falqon {
 namespace {
 
-constexpr int kNormUnits = 148;    // CTAs that share the rows of a backward
+constexpr int kNormUnits = 148;    // a CTA per SM
 
 struct NormArgs {
   const void *h, *y, *post_gain, *pre_gain, *gate;
@@ -1082,6 +1082,11 @@ struct Split {
   }
 };
 
+bool staged(int64_t cols) { return cols % 16 == 0; }
+// CTAs that share a backward's rows: one per SM where rows stream through its shared memory; four where every row is fetched when it
+// is due and only other CTAs' rows cover the wait (613 x 1011 fp32: 41 us with one, 20 with four).
+int64_t backward_units(int64_t cols) { return staged(cols) ? kNormUnits : 4 * kNormUnits; }
+
 NormArgs common(const falqon_block_norm* p) {
   NormArgs a{};
   a.post_gain = p->post_gain;
@@ -1119,7 +1124,6 @@ int with_items(int items, F go) {
 
 // The staged kernels' shape.  set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
 constexpr int kSmemLimit = 226 * 1024;    // dynamic; the kernels have a few bytes of their own besides
-bool staged(int64_t cols) { return cols % 16 == 0; }
 int spans_for(int64_t cols) { return cols <= 2 * 512 * 8 ? 2 : 4; }
 // set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
 bool make_shape(int64_t cols, int64_t rows_per_cta, int set_bytes, int red, int smem_limit, Shape* sh, size_t* smem) {
@@ -1237,7 +1241,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
 
 size_t falqon_block_norm_scratch_bytes(const falqon_block_norm* p) {
   if (!plan_ok(p)) return 0;
-  const Split s(p, kNormUnits);
+  const Split s(p, backward_units(p->cols));
   return static_cast<size_t>(s.units + s.ctas) * static_cast<size_t>(p->cols) * sizeof(float);
 }
 
@@ -1257,7 +1261,7 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
       !ok16(dh_out) || !ok16(h) || !ok16(h_codes) || !ok16(y) || !ok16(y_codes) || !ok16(dh) || !ok16(dy) || !ok16(dpost_gain) ||
       !ok16(dpre_gain) || !ok16(dgate) || (amax_dy != nullptr && dy == nullptr))
     return FALQON_ERR_INVALID_ARG;
-  const Split s(p, kNormUnits);
+  const Split s(p, backward_units(p->cols));
   const bool sums_s = dpost_gain != nullptr || dgate != nullptr, sums_p = dpre_gain != nullptr;
   if ((sums_s || sums_p) && (scratch == nullptr || !ok16(scratch) || scratch_bytes < falqon_block_norm_scratch_bytes(p)))
     return FALQON_ERR_WORKSPACE;

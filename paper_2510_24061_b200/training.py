@@ -68,11 +68,17 @@ def _dtype(t: torch.Tensor) -> int:
     return code
 
 
-def _on_device(*tensors):
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _on_device(*tensors) -> int:
+    """The current stream's handle, the tensors being checked to lie on the current device.  (A third of a small call's time was the
+    stream object that torch.cuda.current_stream() makes: the handle alone is enough here.)"""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor on {t.device} where the current device is cuda:{dev}")
+    return _raw_stream(dev)
 
 
 def _like(t: Optional[torch.Tensor], ref: torch.Tensor, name: str):
@@ -103,15 +109,16 @@ class Checkpoint(NamedTuple):
 
     @staticmethod
     def empty(rows: int, cols: int, device) -> "Checkpoint":
-        return Checkpoint(torch.empty((rows, cols), dtype=torch.uint8, device=device),
-                          torch.empty((rows, -(-cols // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=device))
+        blocks = -(-cols // CHECKPOINT_BLOCK)
+        return Checkpoint(torch.empty_strided((rows, cols), (cols, 1), dtype=torch.uint8, device=device),
+                          torch.empty_strided((rows, blocks), (blocks, 1), dtype=torch.uint8, device=device))
 
 
 def _checkpoint(ck: Checkpoint, shape, name: str):
     rows, cols = shape
-    if (ck.codes.dtype != torch.uint8 or ck.scales.dtype != torch.uint8 or tuple(ck.codes.shape) != (rows, cols)
-            or tuple(ck.scales.shape) != (rows, -(-cols // CHECKPOINT_BLOCK)) or not ck.codes.is_contiguous()
-            or not ck.scales.is_contiguous()):
+    codes, scales = ck
+    if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape != shape
+            or scales.shape != (rows, -(-cols // CHECKPOINT_BLOCK)) or not codes.is_contiguous() or not scales.is_contiguous()):
         raise ValueError(f"{name} must be a Checkpoint of a [{rows}, {cols}] tensor")
 
 
@@ -120,9 +127,9 @@ def checkpoint_save(x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkp
     _matrix(x, "x")
     out = Checkpoint.empty(*x.shape, x.device) if out is None else out
     _checkpoint(out, x.shape, "out")
-    _on_device(x, *out)
+    stream = _on_device(x, *out)
     fq._check("falqon_checkpoint_save", lib.falqon_checkpoint_save(x.data_ptr(), _dtype(x), *x.shape, out.codes.data_ptr(),
-                                                                    out.scales.data_ptr(), fq._stream()))
+                                                                    out.scales.data_ptr(), stream))
     return out
 
 
@@ -133,9 +140,9 @@ def checkpoint_load(ck: Checkpoint, dtype: torch.dtype = torch.bfloat16, out: Op
     out = torch.empty(ck.codes.shape, dtype=dtype, device=ck.codes.device) if out is None else out
     _matrix(out, "out")
     _need(out.shape == ck.codes.shape, "out has another shape than the checkpoint")
-    _on_device(*ck, out)
+    stream = _on_device(*ck, out)
     fq._check("falqon_checkpoint_load", lib.falqon_checkpoint_load(ck.codes.data_ptr(), ck.scales.data_ptr(), *out.shape,
-                                                                    out.data_ptr(), _dtype(out), fq._stream()))
+                                                                    out.data_ptr(), _dtype(out), stream))
     return out
 
 
@@ -147,7 +154,7 @@ def gate_forward(g: torch.Tensor, u: torch.Tensor, save: bool = True, z: Optiona
     _like(u, g, "u")
     _like(z, g, "z")
     _vector(amax, 1, torch.float32, "amax")
-    _on_device(g, u, z, amax)
+    stream = _on_device(g, u, z, amax)
     z = torch.empty_like(g) if z is None else z
     kg = ku = None
     ptrs = (None,) * 4
@@ -155,7 +162,7 @@ def gate_forward(g: torch.Tensor, u: torch.Tensor, save: bool = True, z: Optiona
         kg, ku = Checkpoint.empty(*g.shape, g.device), Checkpoint.empty(*g.shape, g.device)
         ptrs = (kg.codes.data_ptr(), kg.scales.data_ptr(), ku.codes.data_ptr(), ku.scales.data_ptr())
     fq._check("falqon_gate_forward", lib.falqon_gate_forward(g.data_ptr(), u.data_ptr(), _dtype(g), *g.shape, z.data_ptr(), *ptrs,
-                                                              _ptr(amax), fq._stream()))
+                                                              _ptr(amax), stream))
     return z, kg, ku
 
 
@@ -170,13 +177,12 @@ def gate_backward(g: Checkpoint, u: Checkpoint, dz: torch.Tensor, dg: Optional[t
     _like(du, dz, "du")
     _vector(amax_dg, 1, torch.float32, "amax_dg")
     _vector(amax_du, 1, torch.float32, "amax_du")
-    _on_device(*g, *u, dz, dg, du, amax_dg, amax_du)
+    stream = _on_device(*g, *u, dz, dg, du, amax_dg, amax_du)
     dg = torch.empty_like(dz) if dg is None else dg
     du = torch.empty_like(dz) if du is None else du
     fq._check("falqon_gate_backward",
               lib.falqon_gate_backward(g.codes.data_ptr(), g.scales.data_ptr(), u.codes.data_ptr(), u.scales.data_ptr(), dz.data_ptr(),
-                                       _dtype(dz), *dz.shape, dg.data_ptr(), du.data_ptr(), _ptr(amax_dg), _ptr(amax_du),
-                                       fq._stream()))
+                                       _dtype(dz), *dz.shape, dg.data_ptr(), du.data_ptr(), _ptr(amax_dg), _ptr(amax_du), stream))
     return dg, du
 
 
@@ -203,8 +209,10 @@ def _norm_plan(rows, cols, dtype, post, pre, post_gain, pre_gain, gate, rows_per
     gain_dtype = torch.float32 if gain is None else gain.dtype
     _need(post or post_gain is None, "post_gain without the norm after the block")
     _need(pre or pre_gain is None, "pre_gain without the norm before the next block")
-    _vector(post_gain, cols, gain_dtype, "post_gain")
-    _vector(pre_gain, cols, gain_dtype, "pre_gain")
+    if post_gain is not None:
+        _vector(post_gain, cols, gain_dtype, "post_gain")
+    if pre_gain is not None:
+        _vector(pre_gain, cols, gain_dtype, "pre_gain")
     rows_per_gate = rows if rows_per_gate is None else rows_per_gate
     _need(rows_per_gate >= 1, "rows_per_gate must be at least 1")
     if gate is not None:
@@ -224,12 +232,17 @@ def block_norm_forward(h: Optional[torch.Tensor], y: torch.Tensor, *, post: bool
         x = rmsnorm(h_out) * (gain_offset + pre_gain)   (with pre)
     A gain or gate that is None is 1.  save: h and y are kept in 8 bits for the backward."""
     _matrix(y, "y")
-    for t, name in ((h, "h"), (h_out, "h_out"), (x, "x")):
-        _like(t, y, name)
-    _vector(amax_x, 1, torch.float32, "amax_x")
+    if h is not None:
+        _like(h, y, "h")
+    if h_out is not None:
+        _like(h_out, y, "h_out")
+    if x is not None:
+        _like(x, y, "x")
+    if amax_x is not None:
+        _vector(amax_x, 1, torch.float32, "amax_x")
     rows, cols = y.shape
     plan = _norm_plan(rows, cols, _dtype(y), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
-    _on_device(h, y, h_out, x, amax_x, post_gain, pre_gain, gate)
+    stream = _on_device(h, y, h_out, x, amax_x, post_gain, pre_gain, gate)
     h_out = torch.empty_like(y) if h_out is None else h_out
     x = torch.empty_like(y) if x is None and pre else x
     inv_post = torch.empty(rows, dtype=torch.float32, device=y.device) if post else None
@@ -240,7 +253,7 @@ def block_norm_forward(h: Optional[torch.Tensor], y: torch.Tensor, *, post: bool
               lib.falqon_block_norm_forward(C.byref(plan), _ptr(h), y.data_ptr(), h_out.data_ptr(), _ptr(x), _ptr(inv_post), _ptr(inv_pre),
                                             *((None, None) if kh is None else (kh.codes.data_ptr(), kh.scales.data_ptr())),
                                             *((None, None) if ky is None else (ky.codes.data_ptr(), ky.scales.data_ptr())),
-                                            _ptr(amax_x), fq._stream()))
+                                            _ptr(amax_x), stream))
     return BlockNormOut(h_out, x if pre else None, inv_post, inv_pre, kh, ky)
 
 
@@ -259,25 +272,32 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
     _matrix(ref, "dx")
     rows, cols = ref.shape
     for t, name in ((dh_out, "dh_out"), (dh, "dh"), (dy, "dy")):
-        _like(t, ref, name)
+        if t is not None:
+            _like(t, ref, name)
     coded = isinstance(y, Checkpoint)
     _need(h is None or isinstance(h, Checkpoint) == coded, "h and y are saved in the same way")
-    saved = []
-    for t, name in ((h, "h"), (y, "y")):
-        if coded:
-            if t is not None:
-                _checkpoint(t, ref.shape, name)
-                _on_device(*t)
-            saved += [None] + ([None, None] if t is None else [t.codes.data_ptr(), t.scales.data_ptr()])
-        else:
-            _like(t, ref, name)
-            _on_device(t)
-            saved += [_ptr(t), None, None]
-    _need(not post or inv_post is not None, "inv_post of the forward is needed")
-    _need(not pre or inv_pre is not None, "inv_pre of the forward is needed")
-    _vector(inv_post, rows, torch.float32, "inv_post")
-    _vector(inv_pre, rows, torch.float32, "inv_pre")
-    _vector(amax_dy, 1, torch.float32, "amax_dy")
+    if coded:
+        _checkpoint(y, ref.shape, "y")
+        saved = [None, None, None, None, y.codes.data_ptr(), y.scales.data_ptr()]
+        kept = y
+        if h is not None:
+            _checkpoint(h, ref.shape, "h")
+            saved[1], saved[2] = h.codes.data_ptr(), h.scales.data_ptr()
+            kept = (*y, *h)
+    else:
+        _like(y, ref, "y")
+        if h is not None:
+            _like(h, ref, "h")
+        saved = [_ptr(h), None, None, y.data_ptr(), None, None]
+        kept = (h, y)
+    if post:
+        _need(inv_post is not None, "inv_post of the forward is needed")
+        _vector(inv_post, rows, torch.float32, "inv_post")
+    if pre:
+        _need(inv_pre is not None, "inv_pre of the forward is needed")
+        _vector(inv_pre, rows, torch.float32, "inv_pre")
+    if amax_dy is not None:
+        _vector(amax_dy, 1, torch.float32, "amax_dy")
     plan = _norm_plan(rows, cols, _dtype(ref), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
     dev = ref.device
     dh = torch.empty_like(ref) if dh is None and h is not None else dh
@@ -291,10 +311,10 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
         if scratch is None:
             scratch = torch.empty(size, dtype=torch.uint8, device=dev)
         size = scratch.numel() * scratch.element_size()
-    _on_device(dx, dh_out, inv_post, inv_pre, post_gain, pre_gain, gate, dh, dy, scratch, amax_dy)
+    stream = _on_device(dx, dh_out, inv_post, inv_pre, post_gain, pre_gain, gate, dh, dy, scratch, amax_dy, *kept)
     fq._check("falqon_block_norm_backward",
               lib.falqon_block_norm_backward(C.byref(plan), _ptr(dx), _ptr(dh_out), *saved, _ptr(inv_post), _ptr(inv_pre), _ptr(dh), dy.data_ptr(),
-                                             _ptr(dpost), _ptr(dpre), _ptr(dgate), _ptr(amax_dy), _ptr(scratch), size, fq._stream()))
+                                             _ptr(dpost), _ptr(dpre), _ptr(dgate), _ptr(amax_dy), _ptr(scratch), size, stream))
     return BlockNormGrad(dh, dy, dpost, dpre, dgate)
 
 
@@ -355,13 +375,13 @@ def sequence_logprob(logits: torch.Tensor, targets: torch.Tensor, cu_rows: torch
     _vector(targets, rows, torch.int64, "targets")
     _vector(cu_rows, n + 1, torch.int64, "cu_rows")
     scratch = _scratch(logits, scratch)
-    _on_device(logits, targets, cu_rows, scratch)
+    stream = _on_device(logits, targets, cu_rows, scratch)
     logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
     seq = torch.empty(n, dtype=torch.float32, device=logits.device)
     fq._check("falqon_sequence_logprob",
               lib.falqon_sequence_logprob(logits.data_ptr(), _dtype(logits), rows, logits.shape[1], _pitch(logits), targets.data_ptr(),
                                           cu_rows.data_ptr(), n, int(average), logp.data_ptr(), seq.data_ptr(), scratch.data_ptr(),
-                                          scratch.numel() * scratch.element_size(), fq._stream()))
+                                          scratch.numel() * scratch.element_size(), stream))
     return seq, logp
 
 
@@ -378,14 +398,15 @@ def preference_forward(spec: PreferenceLoss, logits: torch.Tensor, targets: torc
     _vector(ref_logp, n, torch.float32, "ref_logp")
     plan = _preference(spec, logits, n // 2)
     scratch = _scratch(logits, scratch)
-    _on_device(logits, targets, cu_rows, ref_logp, scratch)
-    e = lambda *shape: torch.empty(shape, dtype=torch.float32, device=logits.device)  # noqa: E731
-    loss, pair_loss, seq, logp = e(), e(n // 2), e(n), e(rows)
-    stats, dlogp = (e(rows, 2), e(rows)) if need_grad else (None, None)
+    stream = _on_device(logits, targets, cu_rows, ref_logp, scratch)
+    f32, dev, empty = torch.float32, logits.device, torch.empty
+    loss, pair_loss = empty((), dtype=f32, device=dev), empty(n // 2, dtype=f32, device=dev)
+    seq, logp = empty(n, dtype=f32, device=dev), empty(rows, dtype=f32, device=dev)
+    stats, dlogp = (torch.empty_strided((rows, 2), (2, 1), dtype=f32, device=dev), empty(rows, dtype=f32, device=dev)) if need_grad else (None, None)
     fq._check("falqon_preference_forward",
               lib.falqon_preference_forward(C.byref(plan), logits.data_ptr(), targets.data_ptr(), cu_rows.data_ptr(), _ptr(ref_logp),
                                             loss.data_ptr(), pair_loss.data_ptr(), seq.data_ptr(), logp.data_ptr(), _ptr(stats), _ptr(dlogp),
-                                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), fq._stream()))
+                                            scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
     return PreferenceOut(loss, pair_loss, seq, logp, stats, dlogp, spec)
 
 
@@ -400,13 +421,13 @@ def preference_backward(logits: torch.Tensor, targets: torch.Tensor, out: Prefer
     _vector(dloss, 1, torch.float32, "dloss")
     _vector(amax, 1, torch.float32, "amax")
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        dlogits = torch.empty_strided(logits.shape, (logits.shape[1], 1), dtype=logits.dtype, device=logits.device)
     else:
         _logits_ok(dlogits, "dlogits")
         _need(dlogits.shape == logits.shape and dlogits.dtype == logits.dtype, "dlogits must be like logits")
     plan = _preference(out.spec, logits, out.pair_loss.numel())
-    _on_device(logits, targets, out.row_stats, out.dlogp, dloss, dlogits, amax)
+    stream = _on_device(logits, targets, out.row_stats, out.dlogp, dloss, dlogits, amax)
     fq._check("falqon_preference_backward",
               lib.falqon_preference_backward(C.byref(plan), logits.data_ptr(), targets.data_ptr(), out.row_stats.data_ptr(),
-                                             out.dlogp.data_ptr(), _ptr(dloss), dlogits.data_ptr(), _pitch(dlogits), _ptr(amax), fq._stream()))
+                                             out.dlogp.data_ptr(), _ptr(dloss), dlogits.data_ptr(), _pitch(dlogits), _ptr(amax), stream))
     return dlogits
