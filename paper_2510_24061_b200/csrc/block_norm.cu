@@ -244,10 +244,6 @@ __device__ __forceinline__ void read_span(const uint8_t* src, int lane, f2 (&x)[
     x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
   }
 }
-// f: the scale, or its product with a factor of the row (a power of two times a factor is exact).
-__device__ __forceinline__ void read_codes(const uint8_t* src, int lane, float f, f2 (&x)[4]) {
-  mx8_decode8(*reinterpret_cast<const uint2*>(src + lane * 8), f, x);
-}
 // cp.async.wait_group takes a constant: at most depth - 1 younger groups may be open.
 __device__ __forceinline__ void wait_stage(int depth) {
   switch (depth) {
@@ -258,51 +254,37 @@ __device__ __forceinline__ void wait_stage(int depth) {
   }
 }
 
-// Sums over a row group of up to 16 warps; every thread gets them.  `red`: the group's kSumFloats<kN>, two halves used in turn so that
-// one barrier per call is enough.  Within a warp two sums share their shuffles (after one exchange, even lanes add up the
-// first and odd lanes the second); across warps one lane takes one warp's part of one sum.
-template <int kN>
-constexpr int kSumFloats = 2 * 16 * kN;
-template <int kN>
-__device__ __forceinline__ void group_sums(float (&v)[kN], float* red, int& phase, int warp, int lane, int warps, int barrier) {
-  static_assert(kN == 1 || kN == 3, "");
+// The sum over a row group of up to 16 warps; every thread gets it.  `red`: the group's kSumFloats, zero before the first call (a warp
+// that is not there adds 0): two halves used in turn, so that one barrier per call is enough.
+constexpr int kSumFloats = 2 * 16;
+__device__ __forceinline__ float group_sum(float v, float* red, int& phase, int warp, int lane, int warps, int barrier) {
   constexpr uint32_t all = 0xFFFFFFFFu;
-  float* buf = red + phase * 16 * kN;
-  if constexpr (kN == 3) {
-    const bool odd = (lane & 1) != 0;
-    const float other = __shfl_xor_sync(all, odd ? v[0] : v[1], 1);
-    float ab = (odd ? v[1] : v[0]) + other, c = v[2] + __shfl_xor_sync(all, v[2], 1);
 #pragma unroll
-    for (int o = 16; o > 1; o >>= 1) {
-      ab += __shfl_xor_sync(all, ab, o);
-      c += __shfl_xor_sync(all, c, o);
-    }
-    if (warps == 1) {
-      v[0] = __shfl_sync(all, ab, 0);
-      v[1] = __shfl_sync(all, ab, 1);
-      v[2] = c;
-      return;
-    }
-    if (lane < 2) buf[lane * 16 + warp] = ab;
-    if (lane == 2) buf[32 + warp] = c;
-  } else {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v[0] += __shfl_xor_sync(all, v[0], o);
-    if (warps == 1) return;
-    if (lane == 0) buf[warp] = v[0];
-  }
-  phase ^= 1;
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(all, v, o);
+  if (warps == 1) return v;
+  float* buf = red + phase;
+  phase ^= 16;
+  if (lane == 0) buf[warp] = v;
   asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(warps * 32) : "memory");
-  const int k = lane >> 3, w = lane & 7;                       // eight lanes to a sum
-  float t = 0.0f;
-  if (k < kN) {
-    if (w < warps) t = buf[k * 16 + w];
-    if (w + 8 < warps) t += buf[k * 16 + w + 8];
-  }
+  const bool many = warps > 8;
+  v = buf[lane & (many ? 15 : 7)];
+  if (many) v += __shfl_xor_sync(all, v, 8);
 #pragma unroll
-  for (int o = 4; o > 0; o >>= 1) t += __shfl_xor_sync(all, t, o);
-#pragma unroll
-  for (int i = 0; i < kN; ++i) v[i] = __shfl_sync(all, t, i * 8);
+  for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(all, v, o);
+  return v;
+}
+// Clears a CTA's reduction space.
+__device__ __forceinline__ void clear_sums(float* red, int floats) {
+  for (int i = threadIdx.x; i < floats; i += blockDim.x) red[i] = 0.0f;
+  __syncthreads();
+}
+
+// A load that leaves the value as it is where there is nothing to fetch: no branch, so nothing waits for it before its use.
+__device__ __forceinline__ void fetch_if(bool there, float& v, const float* p) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q ld.global.cg.f32 %0, [%1];\n\t}" : "+f"(v) : "l"(p), "r"(static_cast<int>(there)));
+}
+__device__ __forceinline__ void fetch_if(bool there, uint32_t& v, const uint8_t* p) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q ld.global.cg.u8 %0, [%1];\n\t}" : "+r"(v) : "l"(p), "r"(static_cast<int>(there)));
 }
 
 // Eight weights of columns c .. c + 7.
@@ -417,8 +399,9 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
   const int64_t blocks_per_row = (cols + kMx8Block - 1) / kMx8Block;
   uint8_t* ring = smem + static_cast<size_t>(threadIdx.x >> 5) * sh.depth * sh.warp_stage;
   float* const tail = reinterpret_cast<float*>(smem + static_cast<size_t>(blockDim.x >> 5) * sh.depth * sh.warp_stage);
-  float* red = tail + me.group * kSumFloats<1>;
-  float* wsm = tail + sh.groups * kSumFloats<1>;
+  clear_sums(tail, sh.groups * kSumFloats);
+  float* red = tail + me.group * kSumFloats;
+  float* wsm = tail + sh.groups * kSumFloats;
   constexpr int kSpan = 256 * sizeof(T);                       // bytes of a span; a stage holds [span][y, h]
   const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
   const f2 inv_cols = twice(a.inv_cols), res_scale = twice(a.res_scale);
@@ -468,11 +451,9 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
       __syncwarp();                                            // the warp has read its stage
       issue(row + sh.depth * sh.groups, stage);
       stage = stage + 1 == sh.depth ? 0 : stage + 1;
-      float sum[1], ip = 1.0f;
+      float ip = 1.0f;
       if (post) {
-        sum[0] = halves(ss);
-        group_sums<1>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-        ip = rsqrtf(sum[0] + a.eps);
+        ip = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
         if (me.warp == 0 && lane == 0) a.inv_post[row] = ip;
       }
       ss = 0;
@@ -490,9 +471,7 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
         if (has_out) write8(static_cast<T*>(a.h_out) + at + i * 256, H[i]);
       }
       if (pre) {
-        sum[0] = halves(ss);
-        group_sums<1>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-        const float iq = rsqrtf(sum[0] + a.eps);
+        const float iq = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
         if (me.warp == 0 && lane == 0) a.inv_pre[row] = iq;
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
@@ -509,236 +488,32 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
-// The row groups' column sums, added in group order through shared memory (over the ring, which is idle then), to out[cols].
-template <int kNv>
-__device__ __forceinline__ void sum_groups(const f2 (&v)[kNv][4], float* out, uint8_t* smem, const Shape& sh, const Seat& me) {
-  float* all = reinterpret_cast<float*>(smem) + me.group * sh.cols;            // [groups][cols]
-  if (sh.groups > 1) __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kNv; ++i) {
-    const int c = me.column<kNv>() + i * 256;
-    if (c >= sh.cols) continue;
-    ulonglong2* to = reinterpret_cast<ulonglong2*>((sh.groups > 1 ? all : out) + c);
-    to[0] = make_ulonglong2(v[i][0], v[i][1]);
-    to[1] = make_ulonglong2(v[i][2], v[i][3]);
-  }
-  if (sh.groups == 1) return;
-  __syncthreads();
-  for (int c = threadIdx.x; c < sh.cols; c += blockDim.x) {
-    float t = 0.0f;
-    for (int g = 0; g < sh.groups; ++g) t += reinterpret_cast<const float*>(smem)[g * sh.cols + c];
-    out[c] = t;
-  }
-  __syncthreads();
-}
-
-// In the terms of the file's head, with H in the place of xh = H * iq:  t = iq * dx * w;  g = dh_out + t;  b = q * yh;
-//   A = mean(t * H), B = sum b * g, C = sum b * H:  d = g - k1 * H with k1 = iq^2 * A;  dy = ip * (q * d - yh * k2), k2 = (B - k1 * C) / cols.
-// kNv = 2 keeps g and H of the row in registers between the sums and the results (yh is read again); kNv = 4 computes all again.
-template <typename T, bool kCoded, int kNv>
-__global__ void __launch_bounds__(512) norm_backward_rows_kernel(const NormArgs a, const Shape sh) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  pdl_trigger();
-  pdl_wait();
-  const bool has_h = (kCoded ? a.h_codes_in != nullptr : a.h != nullptr), has_dx = a.dx != nullptr, has_g = a.dh_out != nullptr;
-  const bool post = a.post, pre = a.pre, want_dh = a.dh != nullptr, want_dy = a.dy != nullptr;
-  const Seat me(sh);
-  const int cols = sh.cols, lane = me.lane, c0 = me.column<kNv>();
-  const int64_t blocks_per_row = (cols + kMx8Block - 1) / kMx8Block;
-  uint8_t* ring = smem + static_cast<size_t>(threadIdx.x >> 5) * sh.depth * sh.warp_stage;
-  float* const tail = reinterpret_cast<float*>(smem + static_cast<size_t>(blockDim.x >> 5) * sh.depth * sh.warp_stage);
-  float* red = tail + me.group * kSumFloats<3>;
-  float* wsm = tail + sh.groups * kSumFloats<3>;               // [2][cols]: q and w
-  constexpr int kSpan = 256 * sizeof(T), kSaved = kCoded ? 256 : kSpan;         // a stage holds [span][dx, dh_out, h, y]
-  constexpr int kSet = 2 * kSpan + 2 * kSaved;
-  constexpr bool kKeep = kNv <= 2;
-  constexpr int kKept = kKeep ? kNv : 1;
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
-  const f2 res_scale = twice(a.res_scale);
-  Largest<T> largest;
-  int phase = 0;
-  f2 P[kNv][4];
-#pragma unroll
-  for (int i = 0; i < kNv; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) P[i][k] = 0;
-
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const Unit u(a, unit);
-    const auto issue = [&](int row, int stage) {
-      if (row < u.last) {
-        const uint32_t dst = smem_u32(ring) + stage * sh.warp_stage;
-        const int64_t at = static_cast<int64_t>(row) * cols + me.warp * kNv * 256;
-        const T *dx = static_cast<const T*>(a.dx) + at, *g = static_cast<const T*>(a.dh_out) + at;
-        const T *h = static_cast<const T*>(a.h) + at, *y = static_cast<const T*>(a.y) + at;
-        const uint8_t* half = lane < 16 ? a.h_codes_in : a.y_codes_in;          // lanes 0..15 copy h's codes, 16..31 y's
-        const uint8_t* codes = half + at + (lane & 15) * 16;
-#pragma unroll
-        for (int i = 0; i < kNv; ++i) {
-          const int col0 = (me.warp * kNv + i) * 256;
-          if (has_dx) copy_span<T>(dst + i * kSet, dx + i * 256, col0, cols, lane);
-          if (has_g) copy_span<T>(dst + i * kSet + kSpan, g + i * 256, col0, cols, lane);
-          if (kCoded) {
-            if ((half != nullptr && col0 + (lane & 15) * 16 < cols)) cp_async16(dst + i * kSet + 2 * kSpan + lane * 16, codes + i * 256);
-          } else {
-            if (has_h) copy_span<T>(dst + i * kSet + 2 * kSpan, h + i * 256, col0, cols, lane);
-            copy_span<T>(dst + i * kSet + 2 * kSpan + kSaved, y + i * 256, col0, cols, lane);
-          }
-        }
-      }
-      cp_async_commit();
-    };
-    for (int s = 0; s < sh.depth; ++s) issue(u.first + me.group + s * sh.groups, s);
-    f2 S[kNv][4];
-#pragma unroll
-    for (int i = 0; i < kNv; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) S[i][k] = 0;
-    // what else a row needs, fetched one row ahead (scales as bytes: nothing waits for them before their row)
-    float ip_next = 1.0f, iq_next = 0.0f;
-    uint32_t eh_next[kNv], ey_next[kNv];
-    const auto fetch = [&](int next) {
-      const int64_t row = min(next, u.last - 1);               // no branch: the values would have to be waited for where it joins
-      if (post) ip_next = ld_stream(a.inv_post + row);
-      if (pre) iq_next = ld_stream(a.inv_pre + row);
-      if (kCoded) {
-        const int64_t block = row * blocks_per_row + (c0 >> 5);
-#pragma unroll
-        for (int i = 0; i < kNv; ++i) {
-          if (c0 + i * 256 >= cols) continue;
-          ey_next[i] = ld_stream(a.y_scales_in + block + i * 8);
-          if (has_h) eh_next[i] = ld_stream(a.h_scales_in + block + i * 8);
-        }
-      }
-    };
-    if (u.first < u.last) fetch(u.first + me.group);
-    if (sh.weights_in_smem) fill_weights(a, u.gate, wsm, cols);
-    const Weights weights{a, wsm, u.gate, cols, sh.weights_in_smem};
-    int stage = 0;
-    for (int row = u.first + me.group; row < u.last; row += sh.groups) {
-      const int64_t at = static_cast<int64_t>(row) * cols + c0;
-      const float ip = ip_next, iq = iq_next;
-      float fh[kNv], fy[kNv];
-#pragma unroll
-      for (int i = 0; i < kNv; ++i) fh[i] = scale_of(eh_next[i]), fy[i] = scale_of(ey_next[i]) * ip;
-      wait_stage(sh.depth);
-      __syncwarp();
-      fetch(row + sh.groups);
-      const uint8_t* src = ring + stage * sh.warp_stage;
-      const auto read_yh = [&](int i, f2 (&yh)[4]) {
-        const uint8_t* set = src + i * kSet + 2 * kSpan + kSaved;
-        if constexpr (kCoded) {
-          read_codes(set, lane, fy[i], yh);
-        } else {
-          read_span<T>(set, lane, yh);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) yh[k] = mul2(yh[k], twice(ip));
-        }
-      };
-      // dxi = iq * dx, t = dxi * w, g, H and b of one span
-      const auto values = [&](int i, f2 (&dxi)[4], f2 (&t)[4], f2 (&g)[4], f2 (&H)[4], f2 (&b)[4]) {
-        const uint8_t* set = src + i * kSet;
-        const int c = c0 + i * 256;
-        f2 yh[4];
-        read_yh(i, yh);
-        weights.get(0, c, b);
-        if (has_h) {
-          if constexpr (kCoded) read_codes(set + 2 * kSpan, lane, fh[i], H);
-          else read_span<T>(set + 2 * kSpan, lane, H);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          b[k] = mul2(b[k], yh[k]);
-          H[k] = has_h ? fma2(H[k], res_scale, b[k]) : b[k];
-          g[k] = dxi[k] = t[k] = 0;
-        }
-        if (has_g) read_span<T>(set + kSpan, lane, g);
-        if (has_dx) {
-          read_span<T>(set, lane, dxi);
-          weights.get(1, c, t);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            dxi[k] = mul2(dxi[k], twice(iq));
-            t[k] = mul2(dxi[k], t[k]);
-            g[k] = add2(g[k], t[k]);
-          }
-        }
-      };
-      f2 sums[3] = {0, 0, 0}, dxi[4], t[4], b[4], g[kKept][4], H[kKept][4];
-#pragma unroll
-      for (int i = 0; i < kNv; ++i) {
-        const int j = kKeep ? i : 0;
-        if (c0 + i * 256 >= cols) continue;
-        values(i, dxi, t, g[j], H[j], b);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          sums[0] = fma2(t[k], H[j][k], sums[0]);
-          sums[1] = fma2(b[k], g[j][k], sums[1]);
-          sums[2] = fma2(b[k], H[j][k], sums[2]);
-          P[i][k] = fma2(dxi[k], H[j][k], P[i][k]);
-        }
-      }
-      float sum[3] = {halves(sums[0]), halves(sums[1]), halves(sums[2])};
-      group_sums<3>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-      const float k1 = iq * iq * (sum[0] * a.inv_cols);
-      const float k2 = post ? (sum[1] - k1 * sum[2]) * a.inv_cols : 0.0f;
-#pragma unroll
-      for (int i = 0; i < kNv; ++i) {
-        const int j = kKeep ? i : 0;
-        if (c0 + i * 256 >= cols) continue;
-        if (!kKeep) values(i, dxi, t, g[j], H[j], b);
-        f2 q[4], yh[4];
-        weights.get(0, c0 + i * 256, q);
-        read_yh(i, yh);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f2 d = fma2(H[j][k], twice(-k1), g[j][k]);
-          S[i][k] = fma2(d, yh[k], S[i][k]);
-          q[k] = mul2(fma2(yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
-          yh[k] = mul2(d, res_scale);
-        }
-        if (want_dh) write8(static_cast<T*>(a.dh) + at + i * 256, yh);
-        if (want_dy) largest.see(write8(static_cast<T*>(a.dy) + at + i * 256, q));
-      }
-      __syncwarp();                                            // the warp has read its stage
-      issue(row + sh.depth * sh.groups, stage);
-      stage = stage + 1 == sh.depth ? 0 : stage + 1;
-    }
-    if (a.part_s != nullptr) sum_groups<kNv>(S, a.part_s + unit * cols, smem, sh, me);
-  }
-  if (a.part_p != nullptr) sum_groups<kNv>(P, a.part_p + static_cast<int64_t>(blockIdx.x) * cols, smem, sh, me);
-  if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
-}
-
 // ---- the usual call: both norms, a residual, every result, rows of 512 columns per warp (512, 1024, .. 8192)
 // The same work as the two kernels above with nothing left to test in the row loop and offsets that advance by a row: they are
 // bound by the instructions a row takes, and tests and address arithmetic were half of them.
 constexpr int kFullDepth = 2;                                  // two rows ahead per group cover the latency
 
-template <typename T>
-__device__ __forceinline__ void copy_lane(uint32_t dst, const T* src, int lane) {   // 512 columns; src: the lane's first value
-  if constexpr (sizeof(T) == 2) {
-    cp_async16(dst, src);
-    cp_async16(dst + 512, src + 256);
-  } else {                                                     // 128 columns per instruction: src is 4 * lane values from the first
+template <typename T, int kNv>
+__device__ __forceinline__ void copy_lane(uint32_t dst, const T* src) {   // kNv spans of 256 columns; src: the lane's first value
+  constexpr int n = 16 / sizeof(T) * 32;                       // columns per instruction
 #pragma unroll
-    for (int j = 0; j < 4; ++j) cp_async16(dst + 512 * j, src + 128 * j);
-  }
+  for (int j = 0; j < kNv * 256 / n; ++j) cp_async16(dst + 512 * j, src + n * j);
 }
 
-template <typename T, bool kCodes>
-__global__ void __launch_bounds__(512, 2) norm_forward_full_kernel(const NormArgs a, const Shape sh) {
+template <typename T, bool kCodes, int kNv>
+__global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kernel(const NormArgs a, const Shape sh) {
   extern __shared__ __align__(16) uint8_t smem[];
   pdl_trigger();
   pdl_wait();
-  constexpr int kSpan = 256 * sizeof(T), kStage = 4 * kSpan;   // a stage holds [y, h][span]
+  constexpr int kSpan = 256 * sizeof(T), kStage = 2 * kNv * kSpan;   // a stage holds [y, h][span]
   const Seat me(sh);
-  const int cols = sh.cols, lane = me.lane, c0 = me.column<2>(), groups = sh.groups;
+  const int cols = sh.cols, lane = me.lane, c0 = me.column<kNv>(), groups = sh.groups;
   const uint8_t* ring = smem + (threadIdx.x >> 5) * (kFullDepth * kStage);
   const uint32_t ring_lane = smem_u32(ring) + lane * 16;
   float* const tail = reinterpret_cast<float*>(smem + (blockDim.x >> 5) * (kFullDepth * kStage));
-  float* red = tail + me.group * kSumFloats<1>;
-  float* wsm = tail + groups * kSumFloats<1>;
+  clear_sums(tail, sh.groups * kSumFloats);
+  float* red = tail + me.group * kSumFloats;
+  float* wsm = tail + groups * kSumFloats;
   const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
   const int64_t step = static_cast<int64_t>(groups) * cols;
   const int lane_shift = sizeof(T) == 2 ? 0 : -4 * lane;       // from a lane's first column to what it copies
@@ -749,8 +524,8 @@ __global__ void __launch_bounds__(512, 2) norm_forward_full_kernel(const NormArg
     int row = u.first + me.group;
     int64_t at = static_cast<int64_t>(row) * cols + c0;
     const auto copy = [&](int64_t from, uint32_t dst) {
-      copy_lane<T>(dst, static_cast<const T*>(a.y) + from + lane_shift, lane);
-      copy_lane<T>(dst + 2 * kSpan, static_cast<const T*>(a.h) + from + lane_shift, lane);
+      copy_lane<T, kNv>(dst, static_cast<const T*>(a.y) + from + lane_shift);
+      copy_lane<T, kNv>(dst + kNv * kSpan, static_cast<const T*>(a.h) + from + lane_shift);
     };
     if (row < u.last) copy(at, ring_lane);
     cp_async_commit();
@@ -762,11 +537,11 @@ __global__ void __launch_bounds__(512, 2) norm_forward_full_kernel(const NormArg
       cp_async_wait<kFullDepth - 1>();
       __syncwarp();
       const uint8_t* src = ring + stage;
-      f2 y[2][4], H[2][4], ss = 0;
+      f2 y[kNv][4], H[kNv][4], ss = 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kNv; ++i) {
         read_span<T>(src + i * kSpan, lane, y[i]);
-        read_span<T>(src + (2 + i) * kSpan, lane, H[i]);
+        read_span<T>(src + (kNv + i) * kSpan, lane, H[i]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) ss = fma2(mul2(y[i][k], twice(a.inv_cols)), y[i][k], ss);
       }
@@ -775,17 +550,15 @@ __global__ void __launch_bounds__(512, 2) norm_forward_full_kernel(const NormArg
       cp_async_commit();
       if (kCodes) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kNv; ++i) {
           put_codes8(H[i], a.h_codes + at + i * 256, a.h_scales + (at >> 5) + i * 8, true, lane);
           put_codes8(y[i], a.y_codes + at + i * 256, a.y_scales + (at >> 5) + i * 8, true, lane);
         }
       }
-      float sum[1] = {halves(ss)};
-      group_sums<1>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-      const float ip = rsqrtf(sum[0] + a.eps);
+      const float ip = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
       ss = 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kNv; ++i) {
         f2 q[4];
         weights_of(wsm, c0 + i * 256, q);
 #pragma unroll
@@ -795,166 +568,326 @@ __global__ void __launch_bounds__(512, 2) norm_forward_full_kernel(const NormArg
         }
         write8(static_cast<T*>(a.h_out) + at + i * 256, H[i]);
       }
-      sum[0] = halves(ss);
-      group_sums<1>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-      const float iq = rsqrtf(sum[0] + a.eps);
+      const float iq = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
       if (c0 == 0) {
         a.inv_post[row] = ip;
         a.inv_pre[row] = iq;
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kNv; ++i) {
         f2 w[4];
         weights_of(wsm, cols + c0 + i * 256, w);
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = mul2(mul2(H[i][k], twice(iq)), w[k]);
-        largest.see(write8(static_cast<T*>(a.x) + at + i * 256, w));
+        const Vec8<T> o = write8(static_cast<T*>(a.x) + at + i * 256, w);
+        if (a.amax != nullptr) largest.see(o);
       }
     }
   }
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
-template <typename T, bool kCoded>
-__global__ void __launch_bounds__(512) norm_backward_full_kernel(const NormArgs a, const Shape sh) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  pdl_trigger();
-  pdl_wait();
-  constexpr int kSpan = 256 * sizeof(T), kSaved = kCoded ? 256 : kSpan;
-  constexpr int kStage = 4 * kSpan + 4 * kSaved;               // a stage holds [dx, dh_out][span] and [span][h, y] codes or [h, y][span]
-  constexpr int kH = 4 * kSpan, kY = kH + (kCoded ? 256 : 2 * kSpan), kNext = kCoded ? 512 : kSpan;   // from a span's saved values to the next's
-  const Seat me(sh);
-  const int cols = sh.cols, lane = me.lane, c0 = me.column<2>(), groups = sh.groups;
-  const uint8_t* ring = smem + (threadIdx.x >> 5) * (kFullDepth * kStage);
-  const uint32_t ring_lane = smem_u32(ring) + lane * 16;
-  float* const tail = reinterpret_cast<float*>(smem + (blockDim.x >> 5) * (kFullDepth * kStage));
-  float* red = tail + me.group * kSumFloats<3>;
-  float* wsm = tail + groups * kSumFloats<3>;                  // [2][cols]: q and w
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
-  const int64_t step = static_cast<int64_t>(groups) * cols;
-  const int lane_shift = sizeof(T) == 2 ? 0 : -4 * lane;       // from a lane's first column to what it copies
-  const uint8_t* codes = (lane < 16 ? a.h_codes_in : a.y_codes_in) + (lane & 15) * 16 - lane * 8;   // lanes 0..15 copy h's codes, 16..31 y's
-  Largest<T> largest;
-  int phase = 0;
-  f2 P[2][4];
+// ---- backward, widths that are multiples of 16: runs of rows through shared memory
+// A CTA brings R neighbouring rows of all four tensors into shared memory by bulk copies (a run of rows is one run of bytes), two runs
+// in turn.  First its warps share the rows, for the three sums of each; then they share the columns ("stripes" of 256, eight to a
+// lane), every warp going through all rows of the run with its columns' weights and sums in registers.  So a row's reduction is
+// a part of a warp's, there are two barriers per run instead of one per row, and no thread holds a row's values while it waits.  The
+// values are formed twice, from shared memory.  In the terms of the file's head, with H in the place of xh = H * iq:
+//   t = iq * dx * w;  g = dh_out + t;  b = q * yh;  A = sum t * H, B = sum b * g, C = sum b * H
+//   d = g - k1 * H with k1 = iq^2 * A / cols;  dy = ip * (q * d - yh * k2) with k2 = (B - k1 * C) / cols
+// (Rows in registers from the sums to the results, a barrier per row: 57 us at 4096 x 4096 from checkpoints, 150 us at 8192 x 5120.)
+constexpr int kMaxRun = 32;                                    // a lane per row
+constexpr int kScaleBytes = 4;                                 // of a run, per thread
+struct Run {
+  int cols, stripes, warps, run, parts, part_spans, split, stripe_warps, buffers, weights_in_smem, blocks_per_row;
+  int area, saved_area, buffer;                                // bytes: of a run of dx, of h or y, of a buffer
+};
+// Shared memory behind the buffers.
+struct RunTail {
+  float* wsm;                                                  // [2][cols]
+  float4* red;                                                 // [run][parts]
+  uint8_t* scales;                                             // [2][h, y][run * blocks_per_row]
+  uint32_t full;                                               // mbarriers, one per buffer
+};
+__device__ __host__ __forceinline__ size_t run_tail_bytes(const Run& r) {
+  return 16 + static_cast<size_t>(r.run) * r.parts * 16 + (static_cast<size_t>(4) * r.run * r.blocks_per_row + 15) / 16 * 16 + (r.weights_in_smem ? static_cast<size_t>(r.cols) * 8 : 0);
+}
+
+// One lane's eight columns of one row.
+template <typename T, bool kCoded, bool kFull>
+struct RowValues {
+  f2 yh[4], H[4], b[4];
+  bool has_h, has_dx, has_g;
+  __device__ __forceinline__ RowValues(const NormArgs& a)
+      : has_h(kFull || (kCoded ? a.h_codes_in != nullptr : a.h != nullptr)), has_dx(kFull || a.dx != nullptr), has_g(kFull || a.dh_out != nullptr) {}
+  // src: the lane's place in the run's dx; value columns from it are `at`
+  __device__ __forceinline__ void saved(const uint8_t* h, const uint8_t* y, uint32_t eh, uint32_t ey, float ip, float res_scale, const f2 (&q)[4]) {
+    if constexpr (kCoded) {
+      mx8_decode8(*reinterpret_cast<const uint2*>(y), scale_of(ey) * ip, yh);
+      if (has_h) {
+        const uint2 c = *reinterpret_cast<const uint2*>(h);
+        decode4(c.x, H[0], H[1]);
+        decode4(c.y, H[2], H[3]);
+      }
+    } else {
+      read8<T>(y, yh);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+      for (int k = 0; k < 4; ++k) yh[k] = mul2(yh[k], twice(ip));
+      if (has_h) read8<T>(h, H);
+    }
+    const f2 f = twice(kCoded ? scale_of(eh) * res_scale : res_scale);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      b[k] = mul2(q[k], yh[k]);
+      H[k] = has_h ? fma2(H[k], f, b[k]) : b[k];
+    }
+  }
+  template <typename U>
+  static __device__ __forceinline__ void read8(const uint8_t* p, f2 (&x)[4]) {
+    if constexpr (sizeof(U) == 2) {
+      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
+    } else {
+      const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(p)[0], hi = reinterpret_cast<const ulonglong2*>(p)[1];
+      x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
+    }
+  }
+  // g = dh_out + t with t = dxi * w, dxi = iq * dx
+  __device__ __forceinline__ void grads(const uint8_t* dx, const uint8_t* dh, float iq, const f2 (&w)[4], f2 (&dxi)[4], f2 (&t)[4], f2 (&g)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) dxi[k] = t[k] = g[k] = 0;
+    if (has_g) read8<T>(dh, g);
+    if (has_dx) {
+      read8<T>(dx, dxi);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        dxi[k] = mul2(dxi[k], twice(iq));
+        t[k] = mul2(dxi[k], w[k]);
+        g[k] = add2(g[k], t[k]);
+      }
+    }
+  }
+};
+
+// The sums of one stripe's columns over the warps that shared its rows, added in their order through shared memory, to out[cols].
+template <int kNv>
+__device__ __forceinline__ void store_stripes(const f2 (&v)[kNv][4], float* out, float* space, const Run& sh, int stripe, int member) {
+  const int lane = threadIdx.x & 31;
+  if (sh.split > 1) __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kNv; ++i) {
+    const int c = (stripe + i) * 256 + lane * 8;
+    if (member >= sh.split || c >= sh.cols) continue;
+    ulonglong2* to = reinterpret_cast<ulonglong2*>((sh.split > 1 ? space + member * sh.cols : out) + c);
+    to[0] = make_ulonglong2(v[i][0], v[i][1]);
+    to[1] = make_ulonglong2(v[i][2], v[i][3]);
+  }
+  if (sh.split == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < sh.cols; c += blockDim.x) {
+    float t = 0.0f;
+    for (int m = 0; m < sh.split; ++m) t += space[m * sh.cols + c];
+    out[c] = t;
+  }
+  fence_proxy_async_smem();                                    // bulk copies write here next
+  __syncthreads();
+}
+
+template <typename T, bool kCoded, int kNv, bool kFull, int kThreads>
+__global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormArgs a, const Run sh, int* status) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cols = sh.cols;
+  RunTail tail;
+  {
+    uint8_t* p = smem + static_cast<size_t>(sh.buffers) * sh.buffer;
+    tail.full = smem_u32(p);
+    tail.red = reinterpret_cast<float4*>(p + 16);
+    tail.scales = p + 16 + static_cast<size_t>(sh.run) * sh.parts * 16;
+    tail.wsm = reinterpret_cast<float*>(tail.scales + (static_cast<size_t>(4) * sh.run * sh.blocks_per_row + 15) / 16 * 16);
+  }
+  if (tid == 0) {
+    for (int b = 0; b < sh.buffers; ++b) mbar_init(tail.full + 8 * b, 1);
+    mbar_fence_init();
+  }
+  __syncthreads();
+  pdl_wait();
+  const bool post = kFull || a.post, pre = kFull || a.pre, want_dh = kFull || a.dh != nullptr, want_dy = kFull || a.dy != nullptr;
+  RowValues<T, kCoded, kFull> v(a);
+  const int stripe = (warp % sh.stripe_warps) * kNv, member = warp / sh.stripe_warps;
+  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const int half = sh.run * sh.blocks_per_row;                 // scale bytes of one tensor's run
+  Largest<T> largest;
+  uint32_t parity = 0;                                         // of each buffer's next wait, a bit
+  f2 P[kNv][4];
+#pragma unroll
+  for (int i = 0; i < kNv; ++i)
 #pragma unroll
     for (int k = 0; k < 4; ++k) P[i][k] = 0;
 
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const Unit u(a, unit);
-    int row = u.first + me.group;
-    int64_t at = static_cast<int64_t>(row) * cols + c0;
-    const auto copy = [&](int64_t from, uint32_t dst) {
-      copy_lane<T>(dst, static_cast<const T*>(a.dx) + from + lane_shift, lane);
-      copy_lane<T>(dst + 2 * kSpan, static_cast<const T*>(a.dh_out) + from + lane_shift, lane);
-      if constexpr (kCoded) {
-        cp_async16(dst + kH, codes + from);
-        cp_async16(dst + kH + kNext, codes + from + 256);
-      } else {
-        copy_lane<T>(dst + kH, static_cast<const T*>(a.h) + from + lane_shift, lane);
-        copy_lane<T>(dst + kY, static_cast<const T*>(a.y) + from + lane_shift, lane);
+    const int runs = (u.last - u.first + sh.run - 1) / sh.run;
+    const auto bring = [&](int c, int b) {                     // one thread: the c-th run into buffer b
+      if (c >= runs) return;
+      const int row = u.first + c * sh.run, n = min(sh.run, u.last - row);
+      const int64_t at = static_cast<int64_t>(row) * cols;
+      const uint32_t dst = smem_u32(smem) + b * sh.buffer, bar = tail.full + 8 * b, bytes = n * cols * static_cast<int>(sizeof(T));
+      const uint32_t saved = kCoded ? n * cols : bytes;
+      mbar_expect_tx(bar, (v.has_dx ? bytes : 0) + (v.has_g ? bytes : 0) + (v.has_h ? saved : 0) + saved);
+      if (v.has_dx) bulk_load_1d(dst, static_cast<const T*>(a.dx) + at, bytes, bar);
+      if (v.has_g) bulk_load_1d(dst + sh.area, static_cast<const T*>(a.dh_out) + at, bytes, bar);
+      const uint8_t *h = kCoded ? a.h_codes_in : static_cast<const uint8_t*>(a.h), *y = kCoded ? a.y_codes_in : static_cast<const uint8_t*>(a.y);
+      constexpr int kBytes = kCoded ? 1 : sizeof(T);
+      if (v.has_h) bulk_load_1d(dst + 2 * sh.area, h + at * kBytes, saved, bar);
+      bulk_load_1d(dst + 2 * sh.area + sh.saved_area, y + at * kBytes, saved, bar);
+    };
+    if (tid == 0)
+      for (int b = 0; b < sh.buffers; ++b) bring(b, b);
+    // what else a run needs, fetched one run ahead: a lane's row's factors, and the scales
+    float ip_next = 1.0f, iq_next = 0.0f;
+    uint32_t scale_next[kScaleBytes] = {0u, 0u, 0u, 0u};
+    const auto fetch = [&](int c) {
+      const int row = u.first + c * sh.run, n = min(sh.run, u.last - row);
+      if (post) fetch_if(lane < n, ip_next, a.inv_post + row + lane);
+      if (pre) fetch_if(lane < n, iq_next, a.inv_pre + row + lane);
+      if (kCoded) {
+        const int count = n * sh.blocks_per_row;
+        const int64_t at = static_cast<int64_t>(row) * sh.blocks_per_row;
+#pragma unroll
+        for (int j = 0; j < kScaleBytes; ++j) {
+          const int i = tid + j * blockDim.x;                  // h's bytes of the run, then y's
+          const bool of_y = i >= half;
+          const int k = of_y ? i - half : i;
+          fetch_if(i < 2 * half && k < count && (of_y || v.has_h), scale_next[j], (of_y ? a.y_scales_in : a.h_scales_in) + at + k);
+        }
       }
     };
-    if (row < u.last) copy(at, ring_lane);
-    cp_async_commit();
-    if (row + groups < u.last) copy(at + step, ring_lane + kStage);
-    cp_async_commit();
-    f2 S[2][4];
+    const auto keep = [&](int b) {
+      if (!kCoded) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < kScaleBytes; ++j)
+        if (tid + j * static_cast<int>(blockDim.x) < 2 * half) tail.scales[b * 2 * half + tid + j * blockDim.x] = static_cast<uint8_t>(scale_next[j]);
+    };
+    fetch(0);
+    keep(0);
+    if (sh.weights_in_smem) fill_weights(a, u.gate, tail.wsm, cols); else __syncthreads();
+    const Weights weights{a, tail.wsm, u.gate, cols, sh.weights_in_smem};
+    f2 S[kNv][4], q[4], w[4];
+#pragma unroll
+    for (int i = 0; i < kNv; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) S[i][k] = 0;
-    // what else a row needs, fetched one row ahead without a branch (where branches join, the values would be waited for)
-    float ip_next, iq_next;
-    uint32_t eh_next[2], ey_next[2];
-    const auto fetch = [&](int64_t r, int64_t first) {
-      ip_next = ld_stream(a.inv_post + r);
-      iq_next = ld_stream(a.inv_pre + r);
-      if (kCoded) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          ey_next[i] = ld_stream(a.y_scales_in + (first >> 5) + i * 8);
-          eh_next[i] = ld_stream(a.h_scales_in + (first >> 5) + i * 8);
+
+    for (int c = 0, b = 0; c < runs; ++c, b = b + 1 == sh.buffers ? 0 : b + 1) {
+      const int row0 = u.first + c * sh.run, n = min(sh.run, u.last - row0);
+      const float ip_lane = ip_next, iq_lane = iq_next;
+      if (c + 1 < runs) fetch(c + 1);
+      mbar_wait(tail.full + 8 * b, parity >> b & 1, status);
+      parity ^= 1u << b;
+      const uint8_t* buf = smem + b * sh.buffer;
+      const uint8_t* sc = tail.scales + (c & 1) * 2 * half;
+      // a lane's columns of run row r: v, and dxi, t, g
+      const auto form = [&](int r, int col, float ip, float iq, f2 (&dxi)[4], f2 (&t)[4], f2 (&g)[4]) {
+        const int at = r * cols + col;
+        uint32_t eh = 0, ey = 0;
+        if (kCoded) {
+          const int block = r * sh.blocks_per_row + (col >> 5);
+          ey = sc[half + block];
+          eh = sc[block];
         }
-      }
-    };
-    if (row < u.last) fetch(row, at);
-    fill_weights(a, u.gate, wsm, cols);
-    int stage = 0;
-    for (; row < u.last; row += groups, at += step, stage ^= kStage) {
-      const float ip = ip_next, iq = iq_next;
-      float fh[2], fy[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) fh[i] = kCoded ? scale_of(eh_next[i]) * a.res_scale : a.res_scale, fy[i] = kCoded ? scale_of(ey_next[i]) * ip : ip;
-      cp_async_wait<kFullDepth - 1>();
-      __syncwarp();
-      const bool more = row + groups < u.last;
-      fetch(more ? row + groups : row, more ? at + step : at);
-      const uint8_t* src = ring + stage;
-      const auto saved = [&](const uint8_t* p, f2 (&x)[4]) {   // not yet multiplied by its factor
-        if constexpr (kCoded) {
-          const uint2 q = *reinterpret_cast<const uint2*>(p + lane * 8);
-          decode4(q.x, x[0], x[1]);
-          decode4(q.y, x[2], x[3]);
-        } else {
-          read_span<T>(p, lane, x);
-        }
+        constexpr int kBytes = kCoded ? 1 : sizeof(T);
+        const uint8_t* h = buf + 2 * sh.area + at * kBytes;
+        v.saved(h, h + sh.saved_area, eh, ey, ip, a.res_scale, q);
+        v.grads(buf + at * sizeof(T), buf + sh.area + at * sizeof(T), iq, w, dxi, t, g);
       };
-      f2 sums[3] = {0, 0, 0}, g[2][4], H[2][4];
+      // the rows' sums, `parts` warps to a row
+      for (int task = warp; task < n * sh.parts; task += sh.warps) {
+        const int r = task / sh.parts, part = task - r * sh.parts;
+        const float ip = __shfl_sync(0xFFFFFFFFu, ip_lane, r), iq = __shfl_sync(0xFFFFFFFFu, iq_lane, r);
+        f2 sums[3] = {0, 0, 0};
+        const int end = min((part + 1) * sh.part_spans, sh.stripes);
+        for (int span = part * sh.part_spans; span < end; ++span) {
+          const int col = span * 256 + lane * 8;
+          if (!kFull && col >= cols) break;
+          f2 dxi[4], t[4], g[4];
+          weights.get(0, col, q);
+          weights.get(1, col, w);
+          form(r, col, ip, iq, dxi, t, g);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        f2 b[4], t[4], dxi[4];
-        saved(src + kY + i * kNext, b);
-        weights_of(wsm, c0 + i * 256, t);
-        saved(src + kH + i * kNext, H[i]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          b[k] = mul2(mul2(b[k], twice(fy[i])), t[k]);
-          H[i][k] = fma2(H[i][k], twice(fh[i]), b[k]);
+          for (int k = 0; k < 4; ++k) {
+            sums[0] = fma2(t[k], v.H[k], sums[0]);
+            sums[1] = fma2(v.b[k], g[k], sums[1]);
+            sums[2] = fma2(v.b[k], v.H[k], sums[2]);
+          }
         }
-        read_span<T>(src + i * kSpan, lane, dxi);
-        read_span<T>(src + (2 + i) * kSpan, lane, g[i]);
-        weights_of(wsm, cols + c0 + i * 256, t);
+        __syncwarp();
+        float s[3] = {halves(sums[0]), halves(sums[1]), halves(sums[2])};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          dxi[k] = mul2(dxi[k], twice(iq));
-          t[k] = mul2(dxi[k], t[k]);
-          g[i][k] = add2(g[i][k], t[k]);
-          sums[0] = fma2(t[k], H[i][k], sums[0]);
-          sums[1] = fma2(b[k], g[i][k], sums[1]);
-          sums[2] = fma2(b[k], H[i][k], sums[2]);
-          P[i][k] = fma2(dxi[k], H[i][k], P[i][k]);
+        for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+          for (int k = 0; k < 3; ++k) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], o);
+        }
+        if (lane == 0) tail.red[task] = make_float4(s[0], s[1], s[2], 0.0f);
+      }
+      __syncthreads();
+      float k1_lane = 0.0f, k2_lane = 0.0f;                    // of the lane's row
+      if (lane < n) {
+        float s[3] = {0.0f, 0.0f, 0.0f};
+        for (int p = 0; p < sh.parts; ++p) {
+          const float4 x = tail.red[lane * sh.parts + p];
+          s[0] += x.x, s[1] += x.y, s[2] += x.z;
+        }
+        k1_lane = iq_lane * iq_lane * (s[0] * a.inv_cols);
+        k2_lane = post ? (s[1] - k1_lane * s[2]) * a.inv_cols : 0.0f;
+      }
+      // the results, a stripe of columns to a warp
+      if (kNv == 1) {
+        const int col = stripe * 256 + lane * 8;
+        if (kFull || col < cols) {
+          weights.get(0, col, q);
+          weights.get(1, col, w);
         }
       }
-      float sum[3] = {halves(sums[0]), halves(sums[1]), halves(sums[2])};
-      group_sums<3>(sum, red, phase, me.warp, lane, me.warps, me.group + 1);
-      const float k1 = iq * iq * (sum[0] * a.inv_cols);
-      const float k2 = (sum[1] - k1 * sum[2]) * a.inv_cols;
+      for (int r = member < sh.split ? member : n; r < n; r += sh.split) {
+        const float ip = __shfl_sync(0xFFFFFFFFu, ip_lane, r), iq = __shfl_sync(0xFFFFFFFFu, iq_lane, r);
+        const float k1 = __shfl_sync(0xFFFFFFFFu, k1_lane, r), k2 = __shfl_sync(0xFFFFFFFFu, k2_lane, r);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        f2 q[4], yh[4];
-        weights_of(wsm, c0 + i * 256, q);
-        saved(src + kY + i * kNext, yh);
+        for (int i = 0; i < kNv; ++i) {
+          const int col = (stripe + i) * 256 + lane * 8;
+          if (kNv == 1 ? !kFull && col >= cols : col >= cols) continue;
+          if (kNv > 1) {
+            weights.get(0, col, q);
+            weights.get(1, col, w);
+          }
+          f2 dxi[4], t[4], g[4];
+          form(r, col, ip, iq, dxi, t, g);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f2 d = fma2(H[i][k], twice(-k1), g[i][k]);
-          yh[k] = mul2(yh[k], twice(fy[i]));
-          S[i][k] = fma2(d, yh[k], S[i][k]);
-          q[k] = mul2(fma2(yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
-          yh[k] = mul2(d, twice(a.res_scale));
+          for (int k = 0; k < 4; ++k) {
+            P[i][k] = fma2(dxi[k], v.H[k], P[i][k]);
+            const f2 d = fma2(v.H[k], twice(-k1), g[k]);
+            S[i][k] = fma2(d, v.yh[k], S[i][k]);
+            g[k] = mul2(d, twice(a.res_scale));
+            t[k] = mul2(fma2(v.yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
+          }
+          const int64_t at = static_cast<int64_t>(row0 + r) * cols + col;
+          if (want_dh) write8(static_cast<T*>(a.dh) + at, g);
+          if (want_dy) {
+            const Vec8<T> o = write8(static_cast<T*>(a.dy) + at, t);
+            if (a.amax != nullptr) largest.see(o);
+          }
         }
-        write8(static_cast<T*>(a.dh) + at + i * 256, yh);
-        largest.see(write8(static_cast<T*>(a.dy) + at + i * 256, q));
       }
-      __syncwarp();                                            // the warp has read its stage
-      if (row + kFullDepth * groups < u.last) copy(at + kFullDepth * step, ring_lane + stage);
-      cp_async_commit();
+      if (c + 1 < runs) keep((c + 1) & 1);
+      __syncthreads();                                         // the buffer is read, the next run's scales are there
+      if (tid == 0) bring(c + sh.buffers, b);
     }
-    if (a.part_s != nullptr) sum_groups<2>(S, a.part_s + unit * cols, smem, sh, me);
+    if (a.part_s != nullptr) store_stripes<kNv>(S, a.part_s + unit * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
+    else __syncthreads();
   }
-  if (a.part_p != nullptr) sum_groups<2>(P, a.part_p + static_cast<int64_t>(blockIdx.x) * cols, smem, sh, me);
+  if (a.part_p != nullptr) store_stripes<kNv>(P, a.part_p + static_cast<int64_t>(blockIdx.x) * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
@@ -1142,11 +1075,12 @@ bool make_shape(int64_t cols, int64_t rows_per_cta, int set_bytes, int red, int 
   return sh->depth >= 1;
 }
 
-bool whole_spans(int64_t cols) { return cols % 512 == 0 && cols <= 8192; }
+constexpr int kFullSpans = 4;
+bool whole_spans(int64_t cols) { return cols % (256 * kFullSpans) == 0 && cols <= 8192; }
 // Shape of the usual call's kernels: a fixed depth and the weights in shared memory, or false.
-bool make_full_shape(int64_t cols, int64_t rows_per_cta, int stage_bytes, int red, Shape* sh, size_t* smem) {
+bool make_full_shape(int64_t cols, int nv, int64_t rows_per_cta, int stage_bytes, int red, Shape* sh, size_t* smem) {
   sh->cols = static_cast<int>(cols);
-  sh->group_threads = static_cast<int>(cols / 16);
+  sh->group_threads = static_cast<int>(cols / (8 * nv));
   sh->groups = 512 / sh->group_threads;
   if (sh->groups > rows_per_cta) sh->groups = static_cast<int>(rows_per_cta < 1 ? 1 : rows_per_cta);
   *smem = static_cast<size_t>(sh->groups * sh->group_threads / 32) * kFullDepth * stage_bytes + sh->groups * red * 4 + static_cast<size_t>(cols) * 8;
@@ -1163,26 +1097,72 @@ int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
   Shape sh;
   size_t smem;
   if (kNv == 2 && whole_spans(a.cols) && a.h != nullptr && a.h_out != nullptr && a.post && a.pre && (a.h_codes != nullptr) == (a.y_codes != nullptr) &&
-      make_full_shape(a.cols, a.rows_per_piece, 4 * 256 * sizeof(T), kSumFloats<1>, &sh, &smem))
-    return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true>, done[0], a, sh, smem, ctas, stream)
-                                : start_rows(norm_forward_full_kernel<T, false>, done[1], a, sh, smem, ctas, stream);
+      make_full_shape(a.cols, kFullSpans, a.rows_per_piece, 2 * kFullSpans * 256 * sizeof(T), kSumFloats, &sh, &smem))
+    return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true, kFullSpans>, done[0], a, sh, smem, ctas, stream)
+                                : start_rows(norm_forward_full_kernel<T, false, kFullSpans>, done[1], a, sh, smem, ctas, stream);
   const int limit = kNv == 2 ? kSmemLimit / 2 - 1024 : kSmemLimit;       // two CTAs per SM
-  if (!make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats<1>, limit, &sh, &smem) &&
-      !make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats<1>, kSmemLimit, &sh, &smem))
+  if (!make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem) &&
+      !make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, kSmemLimit, &sh, &smem))
     return FALQON_ERR_UNSUPPORTED;
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
 }
-template <typename T, bool kCoded, int kNv>
-int launch_backward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
-  static DeviceMask done[2];
-  Shape sh;
+// How a backward's runs are cut: warps, rows per run, and the shared memory it takes; false where not even one row fits.
+bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_bytes, int* spans, Run* r, size_t* smem) {
+  r->cols = static_cast<int>(cols);
+  r->stripes = static_cast<int>((cols + 255) / 256);
+  r->blocks_per_row = static_cast<int>((cols + kMx8Block - 1) / kMx8Block);
+  *spans = r->stripes <= 24 ? 1 : r->stripes <= 32 ? 2 : 4;
+  r->stripe_warps = (r->stripes + *spans - 1) / *spans;
+  r->warps = r->stripe_warps < 16 ? 16 : r->stripe_warps;
+  r->split = r->warps / r->stripe_warps;
+  const int row = static_cast<int>(cols) * (2 * value_bytes + 2 * saved_bytes);
+  for (int attempt = 0; attempt < 3; ++attempt) {              // two buffers and the weights; without the weights; one buffer
+    r->weights_in_smem = attempt == 0;
+    r->buffers = attempt < 2 ? 2 : 1;
+    int run = (kSmemLimit - (r->weights_in_smem ? r->cols * 8 : 0)) / (r->buffers * row);
+    if (run > kMaxRun) run = kMaxRun;
+    if (run > rows_per_piece) run = static_cast<int>(rows_per_piece);
+    for (; run >= 1; --run) {
+      r->run = run;
+      r->parts = r->warps / run;
+      if (r->parts > r->stripes) r->parts = r->stripes;
+      if (r->parts < 1) r->parts = 1;
+      r->part_spans = (r->stripes + r->parts - 1) / r->parts;
+      r->area = run * r->cols * value_bytes;
+      r->saved_area = run * r->cols * saved_bytes;
+      r->buffer = (2 * r->area + 2 * r->saved_area + 127) / 128 * 128;
+      *smem = static_cast<size_t>(r->buffers) * r->buffer + run_tail_bytes(*r);
+      const size_t sums = static_cast<size_t>(r->split) * r->cols * sizeof(float);   // store_stripes, over the buffers
+      if (*smem <= static_cast<size_t>(kSmemLimit) && 2 * run * r->blocks_per_row <= kScaleBytes * 32 * r->warps &&
+          (r->split == 1 || sums <= static_cast<size_t>(r->buffers) * r->buffer))
+        return true;
+    }
+  }
+  return false;
+}
+template <typename T, bool kCoded, int kNv, bool kFull, int kThreads>
+int start_run(const NormArgs& a, const Run& r, size_t smem, int64_t ctas, int* status, cudaStream_t stream) {
+  static DeviceMask done{0};
+  if (set_max_dynamic_smem(norm_backward_run_kernel<T, kCoded, kNv, kFull, kThreads>, kSmemLimit, done) != cudaSuccess) return FALQON_ERR_CUDA;
+  return finish(launch_pdl(norm_backward_run_kernel<T, kCoded, kNv, kFull, kThreads>, dim3(static_cast<unsigned>(ctas)), dim3(32u * r.warps), smem, stream, 1, a, r,
+                           status));
+}
+template <typename T, bool kCoded>
+int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStream_t stream) {
+  Run r;
   size_t smem;
-  const int set = 2 * 256 * sizeof(T) + 2 * 256 * (kCoded ? 1 : sizeof(T));
-  if (kNv == 2 && whole_spans(a.cols) && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr && a.post && a.pre &&
-      a.dh != nullptr && a.dy != nullptr && make_full_shape(a.cols, a.rows_per_piece, 2 * set, kSumFloats<3>, &sh, &smem))
-    return start_rows(norm_backward_full_kernel<T, kCoded>, done[0], a, sh, smem, ctas, stream);
-  if (!make_shape(a.cols, a.rows_per_piece, set, kSumFloats<3>, kSmemLimit, &sh, &smem)) return FALQON_ERR_UNSUPPORTED;
-  return start_rows(norm_backward_rows_kernel<T, kCoded, kNv>, done[1], a, sh, smem, ctas, stream);
+  int spans;
+  if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded ? 1 : sizeof(T), &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
+  // the usual call: both norms, both gradients in and out, a residual, whole stripes
+  const bool full = a.cols % 256 == 0 && r.weights_in_smem && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr &&
+                    a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
+  if (spans == 1 && r.warps <= 16)
+    return full ? start_run<T, kCoded, 1, true, 512>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 512>(a, r, smem, ctas, status, stream);
+  if (spans == 1)
+    return full ? start_run<T, kCoded, 1, true, 768>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 768>(a, r, smem, ctas, status, stream);
+  if (spans == 2)
+    return full ? start_run<T, kCoded, 2, true, 512>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 2, false, 512>(a, r, smem, ctas, status, stream);
+  return start_run<T, kCoded, 4, false, 512>(a, r, smem, ctas, status, stream);
 }
 template <typename F>
 int with_spans(int64_t cols, F go) {
@@ -1218,7 +1198,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
   a.y_scales = y_scales;
   a.amax = a.pre ? amax_x : nullptr;
   if (staged(a.cols)) {
-    const Split s(p, spans_for(a.cols) == 2 ? 2 * kNormUnits : kNormUnits);
+    const Split s(p, !whole_spans(a.cols) && spans_for(a.cols) == 2 ? 2 * kNormUnits : kNormUnits);   // as many CTAs as are resident
     NormArgs b = a;
     s.put(&b);
     const int rc = with_spans(a.cols, [&](auto n) {
@@ -1283,12 +1263,14 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
   a.part_p = sums_p ? static_cast<float*>(scratch) + s.units * a.cols : nullptr;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int rc = FALQON_ERR_UNSUPPORTED;
-  if (staged(a.cols))
-    rc = with_spans(a.cols, [&](auto n) {
-      if (p->dtype == FALQON_BF16)
-        return coded ? launch_backward_rows<bf16_t, true, n.value>(a, s.ctas, st) : launch_backward_rows<bf16_t, false, n.value>(a, s.ctas, st);
-      return coded ? launch_backward_rows<float, true, n.value>(a, s.ctas, st) : launch_backward_rows<float, false, n.value>(a, s.ctas, st);
-    });
+  if (staged(a.cols)) {
+    int* status = device_status_ptr();
+    if (status == nullptr) return FALQON_ERR_CUDA;
+    if (p->dtype == FALQON_BF16)
+      rc = coded ? launch_backward_runs<bf16_t, true>(a, s.ctas, status, st) : launch_backward_runs<bf16_t, false>(a, s.ctas, status, st);
+    else
+      rc = coded ? launch_backward_runs<float, true>(a, s.ctas, status, st) : launch_backward_runs<float, false>(a, s.ctas, status, st);
+  }
   if (rc == FALQON_ERR_UNSUPPORTED) {                          // any other width, or rows that do not fit the ring
     const int items = items_for(a.cols);
     const dim3 grid(static_cast<unsigned>(s.ctas)), block(static_cast<unsigned>(((a.cols + items - 1) / items + 31) / 32 * 32));
