@@ -593,8 +593,8 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kerne
 // lane), every warp going through all rows of the run with its columns' weights and sums in registers.  So a row's reduction is
 // a part of a warp's, there are two barriers per run instead of one per row, and no thread holds a row's values while it waits.  The
 // values are formed twice, from shared memory.  In the terms of the file's head, with H in the place of xh = H * iq:
-//   t = iq * dx * w;  g = dh_out + t;  b = q * yh;  A = sum t * H, B = sum b * g, C = sum b * H
-//   d = g - k1 * H with k1 = iq^2 * A / cols;  dy = ip * (q * d - yh * k2) with k2 = (B - k1 * C) / cols
+//   t = dx * w;  g = dh_out + iq * t;  b = q * yh;  A = sum t * H, B = sum b * g, C = sum b * H
+//   d = g - k1 * H with k1 = iq^3 * A / cols;  dy = ip * (q * d - yh * k2) with k2 = (B - k1 * C) / cols
 // (Rows in registers from the sums to the results, a barrier per row: 57 us at 4096 x 4096 from checkpoints, 150 us at 8192 x 5120.)
 constexpr int kMaxRun = 32;                                    // a lane per row
 constexpr int kScaleBytes = 4;                                 // of a run, per thread
@@ -613,62 +613,40 @@ __device__ __host__ __forceinline__ size_t run_tail_bytes(const Run& r) {
   return 16 + static_cast<size_t>(r.run) * r.parts * 16 + (static_cast<size_t>(4) * r.run * r.blocks_per_row + 15) / 16 * 16 + (r.weights_in_smem ? static_cast<size_t>(r.cols) * 8 : 0);
 }
 
-// One lane's eight columns of one row.
-template <typename T, bool kCoded, bool kFull>
-struct RowValues {
-  f2 yh[4], H[4], b[4];
-  bool has_h, has_dx, has_g;
-  __device__ __forceinline__ RowValues(const NormArgs& a)
-      : has_h(kFull || (kCoded ? a.h_codes_in != nullptr : a.h != nullptr)), has_dx(kFull || a.dx != nullptr), has_g(kFull || a.dh_out != nullptr) {}
-  // src: the lane's place in the run's dx; value columns from it are `at`
-  __device__ __forceinline__ void saved(const uint8_t* h, const uint8_t* y, uint32_t eh, uint32_t ey, float ip, float res_scale, const f2 (&q)[4]) {
-    if constexpr (kCoded) {
-      mx8_decode8(*reinterpret_cast<const uint2*>(y), scale_of(ey) * ip, yh);
-      if (has_h) {
-        const uint2 c = *reinterpret_cast<const uint2*>(h);
-        decode4(c.x, H[0], H[1]);
-        decode4(c.y, H[2], H[3]);
-      }
-    } else {
-      read8<T>(y, yh);
+// Eight values of a run in shared memory.
+template <typename T>
+__device__ __forceinline__ void read8(uint32_t at, f2 (&x)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
 #pragma unroll
-      for (int k = 0; k < 4; ++k) yh[k] = mul2(yh[k], twice(ip));
-      if (has_h) read8<T>(h, H);
-    }
-    const f2 f = twice(kCoded ? scale_of(eh) * res_scale : res_scale);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      b[k] = mul2(q[k], yh[k]);
-      H[k] = has_h ? fma2(H[k], f, b[k]) : b[k];
-    }
+    for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
+  } else {
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[0]), "=l"(x[1]) : "r"(at));
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[2]), "=l"(x[3]) : "r"(at + 16));
   }
-  template <typename U>
-  static __device__ __forceinline__ void read8(const uint8_t* p, f2 (&x)[4]) {
-    if constexpr (sizeof(U) == 2) {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
-    } else {
-      const ulonglong2 lo = reinterpret_cast<const ulonglong2*>(p)[0], hi = reinterpret_cast<const ulonglong2*>(p)[1];
-      x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
-    }
+}
+// The same of a saved tensor, not yet multiplied by its scale.
+template <typename T, bool kCoded>
+__device__ __forceinline__ void read_saved(uint32_t at, f2 (&x)[4]) {
+  if constexpr (kCoded) {
+    uint32_t w[2];
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    decode4(w[0], x[0], x[1]);
+    decode4(w[1], x[2], x[3]);
+  } else {
+    read8<T>(at, x);
   }
-  // g = dh_out + t with t = dxi * w, dxi = iq * dx
-  __device__ __forceinline__ void grads(const uint8_t* dx, const uint8_t* dh, float iq, const f2 (&w)[4], f2 (&dxi)[4], f2 (&t)[4], f2 (&g)[4]) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) dxi[k] = t[k] = g[k] = 0;
-    if (has_g) read8<T>(dh, g);
-    if (has_dx) {
-      read8<T>(dx, dxi);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        dxi[k] = mul2(dxi[k], twice(iq));
-        t[k] = mul2(dxi[k], w[k]);
-        g[k] = add2(g[k], t[k]);
-      }
-    }
-  }
+}
+__device__ __forceinline__ uint32_t read_byte(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
+  return v;
+}
+// Where a lane's eight columns of a row lie in shared memory: dx (dh_out is `area` further), h (y `saved_area` further), the scale of h
+// (y's `half` further).
+struct Spot {
+  uint32_t dx, h, scale;
 };
 
 // The sums of one stripe's columns over the warps that shared its rows, added in their order through shared memory, to out[cols].
@@ -715,7 +693,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
   __syncthreads();
   pdl_wait();
   const bool post = kFull || a.post, pre = kFull || a.pre, want_dh = kFull || a.dh != nullptr, want_dy = kFull || a.dy != nullptr;
-  RowValues<T, kCoded, kFull> v(a);
+  const bool has_h = kFull || (kCoded ? a.h_codes_in != nullptr : a.h != nullptr), has_dx = kFull || a.dx != nullptr, has_g = kFull || a.dh_out != nullptr;
   const int stripe = (warp % sh.stripe_warps) * kNv, member = warp / sh.stripe_warps;
   const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
   const int half = sh.run * sh.blocks_per_row;                 // scale bytes of one tensor's run
@@ -736,12 +714,12 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
       const int64_t at = static_cast<int64_t>(row) * cols;
       const uint32_t dst = smem_u32(smem) + b * sh.buffer, bar = tail.full + 8 * b, bytes = n * cols * static_cast<int>(sizeof(T));
       const uint32_t saved = kCoded ? n * cols : bytes;
-      mbar_expect_tx(bar, (v.has_dx ? bytes : 0) + (v.has_g ? bytes : 0) + (v.has_h ? saved : 0) + saved);
-      if (v.has_dx) bulk_load_1d(dst, static_cast<const T*>(a.dx) + at, bytes, bar);
-      if (v.has_g) bulk_load_1d(dst + sh.area, static_cast<const T*>(a.dh_out) + at, bytes, bar);
+      mbar_expect_tx(bar, (has_dx ? bytes : 0) + (has_g ? bytes : 0) + (has_h ? saved : 0) + saved);
+      if (has_dx) bulk_load_1d(dst, static_cast<const T*>(a.dx) + at, bytes, bar);
+      if (has_g) bulk_load_1d(dst + sh.area, static_cast<const T*>(a.dh_out) + at, bytes, bar);
       const uint8_t *h = kCoded ? a.h_codes_in : static_cast<const uint8_t*>(a.h), *y = kCoded ? a.y_codes_in : static_cast<const uint8_t*>(a.y);
       constexpr int kBytes = kCoded ? 1 : sizeof(T);
-      if (v.has_h) bulk_load_1d(dst + 2 * sh.area, h + at * kBytes, saved, bar);
+      if (has_h) bulk_load_1d(dst + 2 * sh.area, h + at * kBytes, saved, bar);
       bulk_load_1d(dst + 2 * sh.area + sh.saved_area, y + at * kBytes, saved, bar);
     };
     if (tid == 0)
@@ -761,7 +739,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
           const int i = tid + j * blockDim.x;                  // h's bytes of the run, then y's
           const bool of_y = i >= half;
           const int k = of_y ? i - half : i;
-          fetch_if(i < 2 * half && k < count && (of_y || v.has_h), scale_next[j], (of_y ? a.y_scales_in : a.h_scales_in) + at + k);
+          fetch_if(i < 2 * half && k < count && (of_y || has_h), scale_next[j], (of_y ? a.y_scales_in : a.h_scales_in) + at + k);
         }
       }
     };
@@ -773,8 +751,17 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
     };
     fetch(0);
     keep(0);
-    if (sh.weights_in_smem) fill_weights(a, u.gate, tail.wsm, cols); else __syncthreads();
+    if (kFull || sh.weights_in_smem) fill_weights(a, u.gate, tail.wsm, cols); else __syncthreads();
     const Weights weights{a, tail.wsm, u.gate, cols, sh.weights_in_smem};
+    const auto get = [&](int col, f2 (&q)[4], f2 (&w)[4]) {
+      if (kFull) {                                             // then they are in shared memory
+        weights_of(tail.wsm, col, q);
+        weights_of(tail.wsm, cols + col, w);
+      } else {
+        weights.get(0, col, q);
+        weights.get(1, col, w);
+      }
+    };
     f2 S[kNv][4], q[4], w[4];
 #pragma unroll
     for (int i = 0; i < kNv; ++i)
@@ -787,41 +774,64 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
       if (c + 1 < runs) fetch(c + 1);
       mbar_wait(tail.full + 8 * b, parity >> b & 1, status);
       parity ^= 1u << b;
-      const uint8_t* buf = smem + b * sh.buffer;
-      const uint8_t* sc = tail.scales + (c & 1) * 2 * half;
-      // a lane's columns of run row r: v, and dxi, t, g
-      const auto form = [&](int r, int col, float ip, float iq, f2 (&dxi)[4], f2 (&t)[4], f2 (&g)[4]) {
+      constexpr int kBytes = kCoded ? 1 : sizeof(T);
+      const auto spot = [&](int r, int col) {
         const int at = r * cols + col;
-        uint32_t eh = 0, ey = 0;
-        if (kCoded) {
-          const int block = r * sh.blocks_per_row + (col >> 5);
-          ey = sc[half + block];
-          eh = sc[block];
+        const uint32_t buf = smem_u32(smem) + b * sh.buffer;
+        return Spot{buf + at * static_cast<int>(sizeof(T)), buf + 2 * sh.area + at * kBytes,
+                    smem_u32(tail.scales) + (c & 1) * 2 * half + r * sh.blocks_per_row + (col >> 5)};
+      };
+      // of a lane's columns: yh (y times its scale and ip), b = q * yh, H, and t = dx * w with g = dh_out + iq * t
+      const auto form = [&](const Spot& p, float ip, float iq, f2 (&yh)[4], f2 (&b4)[4], f2 (&H)[4], f2 (&dx)[4], f2 (&t)[4], f2 (&g)[4]) {
+        const float fy = kCoded ? scale_of(read_byte(p.scale + half)) * ip : ip, fh = kCoded ? scale_of(read_byte(p.scale)) * a.res_scale : a.res_scale;
+        read_saved<T, kCoded>(p.h + sh.saved_area, yh);
+        if (has_h) read_saved<T, kCoded>(p.h, H);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          yh[k] = mul2(yh[k], twice(fy));
+          b4[k] = mul2(q[k], yh[k]);
+          H[k] = has_h ? fma2(H[k], twice(fh), b4[k]) : b4[k];
         }
-        constexpr int kBytes = kCoded ? 1 : sizeof(T);
-        const uint8_t* h = buf + 2 * sh.area + at * kBytes;
-        v.saved(h, h + sh.saved_area, eh, ey, ip, a.res_scale, q);
-        v.grads(buf + at * sizeof(T), buf + sh.area + at * sizeof(T), iq, w, dxi, t, g);
+        if (has_g) {
+          read8<T>(p.dx + sh.area, g);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) g[k] = 0;
+        }
+        if (has_dx) {
+          read8<T>(p.dx, dx);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            t[k] = mul2(dx[k], w[k]);
+            g[k] = fma2(t[k], twice(iq), g[k]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) dx[k] = t[k] = 0;
+        }
       };
       // the rows' sums, `parts` warps to a row
       for (int task = warp; task < n * sh.parts; task += sh.warps) {
         const int r = task / sh.parts, part = task - r * sh.parts;
         const float ip = __shfl_sync(0xFFFFFFFFu, ip_lane, r), iq = __shfl_sync(0xFFFFFFFFu, iq_lane, r);
         f2 sums[3] = {0, 0, 0};
-        const int end = min((part + 1) * sh.part_spans, sh.stripes);
-        for (int span = part * sh.part_spans; span < end; ++span) {
-          const int col = span * 256 + lane * 8;
-          if (!kFull && col >= cols) break;
-          f2 dxi[4], t[4], g[4];
-          weights.get(0, col, q);
-          weights.get(1, col, w);
-          form(r, col, ip, iq, dxi, t, g);
+        int col = part * sh.part_spans * 256 + lane * 8;
+        const int end = kFull ? min((part + 1) * sh.part_spans * 256, cols) : min((part + 1) * sh.part_spans * 256 + lane * 8, cols);
+        Spot p = spot(r, col);
+#pragma unroll 2
+        for (; col < end; col += 256) {
+          f2 yh[4], b4[4], H[4], dx[4], t[4], g[4];
+          get(col, q, w);
+          form(p, ip, iq, yh, b4, H, dx, t, g);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            sums[0] = fma2(t[k], v.H[k], sums[0]);
-            sums[1] = fma2(v.b[k], g[k], sums[1]);
-            sums[2] = fma2(v.b[k], v.H[k], sums[2]);
+            sums[0] = fma2(t[k], H[k], sums[0]);
+            sums[1] = fma2(b4[k], g[k], sums[1]);
+            sums[2] = fma2(b4[k], H[k], sums[2]);
           }
+          p.dx += 256 * sizeof(T);
+          p.h += 256 * kBytes;
+          p.scale += 8;
         }
         __syncwarp();
         float s[3] = {halves(sums[0]), halves(sums[1]), halves(sums[2])};
@@ -840,45 +850,47 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
           const float4 x = tail.red[lane * sh.parts + p];
           s[0] += x.x, s[1] += x.y, s[2] += x.z;
         }
-        k1_lane = iq_lane * iq_lane * (s[0] * a.inv_cols);
+        k1_lane = iq_lane * iq_lane * (iq_lane * s[0] * a.inv_cols);
         k2_lane = post ? (s[1] - k1_lane * s[2]) * a.inv_cols : 0.0f;
       }
       // the results, a stripe of columns to a warp
-      if (kNv == 1) {
-        const int col = stripe * 256 + lane * 8;
-        if (kFull || col < cols) {
-          weights.get(0, col, q);
-          weights.get(1, col, w);
-        }
+      const int col0 = stripe * 256 + lane * 8;
+      if (kNv == 1 && (kFull || col0 < cols)) {
+        get(col0, q, w);
       }
-      for (int r = member < sh.split ? member : n; r < n; r += sh.split) {
+      int r = member < sh.split ? member : n;
+      Spot p = spot(r, col0);
+      int64_t at = static_cast<int64_t>(row0 + r) * cols + col0;
+      const int64_t ahead = static_cast<int64_t>(sh.split) * cols;
+      for (; r < n; r += sh.split, at += ahead) {
         const float ip = __shfl_sync(0xFFFFFFFFu, ip_lane, r), iq = __shfl_sync(0xFFFFFFFFu, iq_lane, r);
         const float k1 = __shfl_sync(0xFFFFFFFFu, k1_lane, r), k2 = __shfl_sync(0xFFFFFFFFu, k2_lane, r);
 #pragma unroll
         for (int i = 0; i < kNv; ++i) {
-          const int col = (stripe + i) * 256 + lane * 8;
+          const int col = col0 + i * 256;
           if (kNv == 1 ? !kFull && col >= cols : col >= cols) continue;
           if (kNv > 1) {
-            weights.get(0, col, q);
-            weights.get(1, col, w);
+            get(col, q, w);
           }
-          f2 dxi[4], t[4], g[4];
-          form(r, col, ip, iq, dxi, t, g);
+          f2 yh[4], b4[4], H[4], dx[4], t[4], g[4];
+          form(Spot{p.dx + i * 256 * static_cast<int>(sizeof(T)), p.h + i * 256 * kBytes, p.scale + i * 8}, ip, iq, yh, b4, H, dx, t, g);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            P[i][k] = fma2(dxi[k], v.H[k], P[i][k]);
-            const f2 d = fma2(v.H[k], twice(-k1), g[k]);
-            S[i][k] = fma2(d, v.yh[k], S[i][k]);
+            P[i][k] = fma2(mul2(dx[k], twice(iq)), H[k], P[i][k]);
+            const f2 d = fma2(H[k], twice(-k1), g[k]);
+            S[i][k] = fma2(d, yh[k], S[i][k]);
             g[k] = mul2(d, twice(a.res_scale));
-            t[k] = mul2(fma2(v.yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
+            t[k] = mul2(fma2(yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
           }
-          const int64_t at = static_cast<int64_t>(row0 + r) * cols + col;
-          if (want_dh) write8(static_cast<T*>(a.dh) + at, g);
+          if (want_dh) write8(static_cast<T*>(a.dh) + at + i * 256, g);
           if (want_dy) {
-            const Vec8<T> o = write8(static_cast<T*>(a.dy) + at, t);
+            const Vec8<T> o = write8(static_cast<T*>(a.dy) + at + i * 256, t);
             if (a.amax != nullptr) largest.see(o);
           }
         }
+        p.dx += sh.split * cols * static_cast<int>(sizeof(T));
+        p.h += sh.split * cols * kBytes;
+        p.scale += sh.split * sh.blocks_per_row;
       }
       if (c + 1 < runs) keep((c + 1) & 1);
       __syncthreads();                                         // the buffer is read, the next run's scales are there
@@ -1158,6 +1170,8 @@ int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStrea
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
   if (spans == 1 && r.warps <= 16)
     return full ? start_run<T, kCoded, 1, true, 512>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 512>(a, r, smem, ctas, status, stream);
+  if (spans == 1 && r.warps <= 20)
+    return full ? start_run<T, kCoded, 1, true, 640>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 640>(a, r, smem, ctas, status, stream);
   if (spans == 1)
     return full ? start_run<T, kCoded, 1, true, 768>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 768>(a, r, smem, ctas, status, stream);
   if (spans == 2)
