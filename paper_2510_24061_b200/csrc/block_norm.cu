@@ -587,6 +587,204 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kerne
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
+// ---- any width: the same rings and runs with single values
+// Rows begin anywhere, so a copy takes the 16-byte pieces that cover its values (of the neighbouring rows' values a few come along and
+// are not looked at), and in shared memory lanes read single values: value e of a lane in a span is column 32 * e + lane, so that
+// neighbouring lanes read and write neighbouring values, and every e is one block of a checkpoint.
+__device__ __forceinline__ float single_at(uint32_t at, bf16_t) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+  return bf16_bits_to_float(v);
+}
+__device__ __forceinline__ float single_at(uint32_t at, float) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint32_t byte_at(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
+  return v;
+}
+// A lane's eight values of a span whose first lies at `at`; `left`: columns from it to the row's end.
+template <typename T>
+__device__ __forceinline__ void read_singles(uint32_t at, int left, int lane, f2 (&x)[4]) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e * 32 + lane < left ? single_at(at + (e * 32 + lane) * static_cast<int>(sizeof(T)), T{}) : 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(v[2 * k], v[2 * k + 1]);
+}
+// The same of eight codes: not yet multiplied by their scales.
+__device__ __forceinline__ void read_single_codes(uint32_t at, int left, int lane, f2 (&x)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = 64 * k + lane < left ? byte_at(at + 64 * k + lane) : 0u, hi = 64 * k + 32 + lane < left ? byte_at(at + 64 * k + 32 + lane) : 0u;
+    const float2 f = e4m3x2_to_float2(lo | hi << 8);
+    x[k] = pack_f32x2(f.x, f.y);
+  }
+}
+__device__ __forceinline__ void read_single_weights(const float* w, int left, int lane, f2 (&x)[4]) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e * 32 + lane < left ? w[e * 32 + lane] : 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = pack_f32x2(v[2 * k], v[2 * k + 1]);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t write_singles(T* p, int left, int lane, const f2 (&x)[4]) {   // the largest |value| stored, as bits
+  uint32_t m = 0u;
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e * 32 + lane < left) m = max(m, store1(p + e * 32 + lane, v[e]));
+  return m;
+}
+__device__ __forceinline__ void put_single_codes(const f2 (&x)[4], int left, int lane, uint8_t* codes, uint8_t* scales) {
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t e8 = mx8_exponent(__reduce_max_sync(0xFFFFFFFFu, abs_bits(v[e])));
+    if (e * 32 + lane < left) codes[e * 32 + lane] = mx8_encode1(v[e], mx8_encode_factor(e8));
+    if (lane == 0 && e * 32 < left) scales[e] = static_cast<uint8_t>(e8);
+  }
+}
+// The 16-byte pieces that cover the 256 values from `at` on, of a tensor of `total` values; returns nothing: the first value lies
+// offset_of(at) bytes behind dst.
+template <typename T>
+__device__ __forceinline__ uint32_t offset_of(int64_t at) {
+  return static_cast<uint32_t>(at * static_cast<int64_t>(sizeof(T))) & 15u;
+}
+template <typename T>
+__device__ __forceinline__ void copy_loose(uint32_t dst, const T* base, int64_t at, int64_t total, int lane) {
+  const int64_t from = at * static_cast<int64_t>(sizeof(T)) & ~static_cast<int64_t>(15), end = total * static_cast<int64_t>(sizeof(T));
+#pragma unroll
+  for (int ch = lane; ch < 256 * static_cast<int>(sizeof(T)) / 16 + 1; ch += 32) {
+    const int64_t left = end - (from + ch * 16);
+    if (left <= 0) break;
+    const int bytes = left < 16 ? static_cast<int>(left) : 16;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + ch * 16), "l"(reinterpret_cast<const uint8_t*>(base) + from + ch * 16), "r"(bytes)
+                 : "memory");
+  }
+}
+__device__ __forceinline__ void fill_weights_singly(const NormArgs& a, int64_t group, float* wsm, int cols) {
+  __syncthreads();
+  for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+    const float q = a.post ? weight_at(a.post_gain, c, a) : 1.0f;
+    wsm[c] = a.gate != nullptr ? q * gain_at(a.gate, group * cols + c, a.gain_f32) : q;
+    wsm[cols + c] = a.pre ? weight_at(a.pre_gain, c, a) : 1.0f;
+  }
+  __syncthreads();
+}
+
+template <typename T, int kNv>
+__global__ void __launch_bounds__(512) norm_forward_loose_kernel(const NormArgs a, const Shape sh) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  pdl_trigger();
+  pdl_wait();
+  const bool has_h = a.h != nullptr;
+  const Seat me(sh);
+  const int cols = sh.cols, lane = me.lane, c0 = me.warp * kNv * 256;
+  const int64_t blocks_per_row = (cols + kMx8Block - 1) / kMx8Block, total = a.rows * cols;
+  const uint32_t ring = smem_u32(smem) + (threadIdx.x >> 5) * sh.depth * sh.warp_stage;
+  float* const tail = reinterpret_cast<float*>(smem + static_cast<size_t>(blockDim.x >> 5) * sh.depth * sh.warp_stage);
+  clear_sums(tail, sh.groups * kSumFloats);
+  float* red = tail + me.group * kSumFloats;
+  float* wsm = tail + sh.groups * kSumFloats;
+  constexpr int kSpan = 256 * sizeof(T) + 16;                  // bytes of a span and what comes along; a stage holds [span][y, h]
+  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const f2 inv_cols = twice(a.inv_cols);
+  int phase = 0;
+  uint32_t mx = 0;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const Unit u(a, unit);
+    const auto issue = [&](int row, int stage) {
+      if (row < u.last) {
+        const uint32_t dst = ring + stage * sh.warp_stage;
+#pragma unroll
+        for (int i = 0; i < kNv; ++i) {
+          if (c0 + i * 256 >= cols) continue;
+          const int64_t at = static_cast<int64_t>(row) * cols + c0 + i * 256;
+          copy_loose(dst + i * 2 * kSpan, static_cast<const T*>(a.y), at, total, lane);
+          if (has_h) copy_loose(dst + (i * 2 + 1) * kSpan, static_cast<const T*>(a.h), at, total, lane);
+        }
+      }
+      cp_async_commit();
+    };
+    for (int s = 0; s < sh.depth; ++s) issue(u.first + me.group + s * sh.groups, s);
+    fill_weights_singly(a, u.gate, wsm, cols);
+    int stage = 0;
+    for (int row = u.first + me.group; row < u.last; row += sh.groups) {
+      const int64_t at = static_cast<int64_t>(row) * cols + c0;
+      wait_stage(sh.depth);
+      __syncwarp();
+      const uint32_t src = ring + stage * sh.warp_stage;
+      f2 y[kNv][4], H[kNv][4], ss = 0;
+#pragma unroll
+      for (int i = 0; i < kNv; ++i) {
+        const int left = cols - c0 - i * 256;                  // of a span beyond the row: none
+        const uint32_t off = offset_of<T>(at + i * 256);
+        read_singles<T>(src + i * 2 * kSpan + off, left, lane, y[i]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) H[i][k] = 0;
+        if (has_h) read_singles<T>(src + (i * 2 + 1) * kSpan + off, left, lane, H[i]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ss = fma2(mul2(y[i][k], inv_cols), y[i][k], ss);
+      }
+      __syncwarp();                                            // the warp has read its stage
+      issue(row + sh.depth * sh.groups, stage);
+      stage = stage + 1 == sh.depth ? 0 : stage + 1;
+#pragma unroll
+      for (int i = 0; i < kNv; ++i) {
+        const int left = cols - c0 - i * 256;
+        if (left <= 0) continue;
+        const int64_t block = row * blocks_per_row + (c0 + i * 256) / kMx8Block;
+        if (a.h_codes != nullptr) put_single_codes(H[i], left, lane, a.h_codes + at + i * 256, a.h_scales + block);
+        if (a.y_codes != nullptr) put_single_codes(y[i], left, lane, a.y_codes + at + i * 256, a.y_scales + block);
+      }
+      float ip = 1.0f;
+      if (a.post) {
+        ip = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
+        if (me.warp == 0 && lane == 0) a.inv_post[row] = ip;
+      }
+      ss = 0;
+#pragma unroll
+      for (int i = 0; i < kNv; ++i) {
+        const int left = cols - c0 - i * 256;
+        if (left <= 0) continue;
+        f2 q[4];
+        read_single_weights(wsm + c0 + i * 256, left, lane, q);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f2 n = mul2(mul2(y[i][k], twice(ip)), q[k]);
+          H[i][k] = has_h ? fma2(twice(a.res_scale), H[i][k], n) : n;
+          ss = fma2(mul2(H[i][k], inv_cols), H[i][k], ss);
+        }
+        if (a.h_out != nullptr) write_singles(static_cast<T*>(a.h_out) + at + i * 256, left, lane, H[i]);
+      }
+      if (a.pre) {
+        const float iq = rsqrtf(group_sum(halves(ss), red, phase, me.warp, lane, me.warps, me.group + 1) + a.eps);
+        if (me.warp == 0 && lane == 0) a.inv_pre[row] = iq;
+#pragma unroll
+        for (int i = 0; i < kNv; ++i) {
+          const int left = cols - c0 - i * 256;
+          if (left <= 0) continue;
+          f2 w[4];
+          read_single_weights(wsm + cols + c0 + i * 256, left, lane, w);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = mul2(mul2(H[i][k], twice(iq)), w[k]);
+          mx = max(mx, write_singles(static_cast<T*>(a.x) + at + i * 256, left, lane, w));
+        }
+      }
+    }
+  }
+  if (a.amax != nullptr) raise_amax(mx, a.amax);
+}
+
 // ---- backward, widths that are multiples of 16: runs of rows through shared memory
 // A CTA brings R neighbouring rows of all four tensors into shared memory by bulk copies (a run of rows is one run of bytes), two runs
 // in turn.  First its warps share the rows, for the three sums of each; then they share the columns ("stripes" of 256, eight to a
@@ -649,13 +847,53 @@ struct Spot {
   uint32_t dx, h, scale;
 };
 
+// kLoose: the 16-byte pieces that cover n rows from `row` on, into a run's buffer, as bulk copies by one lane; values in a last piece
+// that the tensor does not fill are copied singly by the warp (they are read after a barrier or more).
+template <typename V>
+__device__ __forceinline__ uint32_t loose_bytes(int64_t at, int64_t count, int64_t total) {   // of the whole pieces
+  const int64_t from = at * static_cast<int64_t>(sizeof(V)) & ~static_cast<int64_t>(15), whole = total * static_cast<int64_t>(sizeof(V)) & ~static_cast<int64_t>(15);
+  const int64_t end = ((at + count) * static_cast<int64_t>(sizeof(V)) + 15) & ~static_cast<int64_t>(15);
+  return static_cast<uint32_t>(max(min(end, whole) - from, static_cast<int64_t>(0)));
+}
+template <typename V>
+__device__ __forceinline__ void loose_copy(uint8_t* dst, const V* base, int64_t at, int64_t count, int64_t total, uint32_t bar, int lane) {
+  const uint8_t* src = reinterpret_cast<const uint8_t*>(base);
+  const int64_t from = at * static_cast<int64_t>(sizeof(V)) & ~static_cast<int64_t>(15);
+  const uint32_t bytes = loose_bytes<V>(at, count, total);
+  if (lane == 0 && bytes > 0) bulk_load_1d(smem_u32(dst), src + from, bytes, bar);
+  const int64_t rest = (at + count) * static_cast<int64_t>(sizeof(V)) - (from + bytes);       // bytes, less than 16
+  if (lane < rest / static_cast<int64_t>(sizeof(V)))
+    reinterpret_cast<V*>(dst + bytes)[lane] = ld_stream(reinterpret_cast<const V*>(src + from + bytes) + lane);
+}
+template <typename T, bool kCoded>
+__device__ __forceinline__ void bring_loose(const NormArgs& a, const Run& sh, int row, int n, bool has_h, bool has_dx, bool has_g, uint8_t* buf, uint32_t bar) {
+  using V = std::conditional_t<sizeof(T) == 2, uint16_t, float>;
+  using S = std::conditional_t<kCoded, uint8_t, V>;
+  const int lane = threadIdx.x & 31;
+  const int64_t at = static_cast<int64_t>(row) * sh.cols, count = static_cast<int64_t>(n) * sh.cols, total = a.rows * sh.cols;
+  const S* h = static_cast<const S*>(kCoded ? static_cast<const void*>(a.h_codes_in) : a.h);
+  const S* y = static_cast<const S*>(kCoded ? static_cast<const void*>(a.y_codes_in) : a.y);
+  if (lane == 0)
+    mbar_expect_tx(bar, (has_dx + has_g) * loose_bytes<V>(at, count, total) + (1 + has_h) * loose_bytes<S>(at, count, total));
+  __syncwarp();
+  if (has_dx) loose_copy(buf, static_cast<const V*>(a.dx), at, count, total, bar, lane);
+  if (has_g) loose_copy(buf + sh.area, static_cast<const V*>(a.dh_out), at, count, total, bar, lane);
+  if (has_h) loose_copy(buf + 2 * sh.area, h, at, count, total, bar, lane);
+  loose_copy(buf + 2 * sh.area + sh.saved_area, y, at, count, total, bar, lane);
+}
+
 // The sums of one stripe's columns over the warps that shared its rows, added in their order through shared memory, to out[cols].
-template <int kNv>
+template <int kNv, bool kLoose>
 __device__ __forceinline__ void store_stripes(const f2 (&v)[kNv][4], float* out, float* space, const Run& sh, int stripe, int member) {
   const int lane = threadIdx.x & 31;
   if (sh.split > 1) __syncthreads();
 #pragma unroll
   for (int i = 0; i < kNv; ++i) {
+    if (kLoose) {
+      const int c = (stripe + i) * 256;
+      if (member < sh.split && c < sh.cols) write_singles((sh.split > 1 ? space + member * sh.cols : out) + c, sh.cols - c, lane, v[i]);
+      continue;
+    }
     const int c = (stripe + i) * 256 + lane * 8;
     if (member >= sh.split || c >= sh.cols) continue;
     ulonglong2* to = reinterpret_cast<ulonglong2*>((sh.split > 1 ? space + member * sh.cols : out) + c);
@@ -673,7 +911,7 @@ __device__ __forceinline__ void store_stripes(const f2 (&v)[kNv][4], float* out,
   __syncthreads();
 }
 
-template <typename T, bool kCoded, int kNv, bool kFull, int kThreads>
+template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose, int kThreads>
 __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormArgs a, const Run sh, int* status) {
   extern __shared__ __align__(128) uint8_t smem[];
   pdl_trigger();
@@ -697,6 +935,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
   const int stripe = (warp % sh.stripe_warps) * kNv, member = warp / sh.stripe_warps;
   const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
   const int half = sh.run * sh.blocks_per_row;                 // scale bytes of one tensor's run
+  const int lane_col = kLoose ? 0 : lane * 8;                  // of a span: the lane's first column, or where all lanes begin
+  uint32_t mx = 0;
   Largest<T> largest;
   uint32_t parity = 0;                                         // of each buffer's next wait, a bit
   f2 P[kNv][4];
@@ -708,8 +948,10 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const Unit u(a, unit);
     const int runs = (u.last - u.first + sh.run - 1) / sh.run;
-    const auto bring = [&](int c, int b) {                     // one thread: the c-th run into buffer b
+    const auto bring = [&](int c, int b) {                     // one thread (kLoose: one warp): the c-th run into buffer b
       if (c >= runs) return;
+      if constexpr (kLoose) return bring_loose<T, kCoded>(a, sh, u.first + c * sh.run, min(sh.run, u.last - (u.first + c * sh.run)), has_h, has_dx, has_g,
+                                                          smem + b * sh.buffer, tail.full + 8 * b);
       const int row = u.first + c * sh.run, n = min(sh.run, u.last - row);
       const int64_t at = static_cast<int64_t>(row) * cols;
       const uint32_t dst = smem_u32(smem) + b * sh.buffer, bar = tail.full + 8 * b, bytes = n * cols * static_cast<int>(sizeof(T));
@@ -722,7 +964,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
       if (has_h) bulk_load_1d(dst + 2 * sh.area, h + at * kBytes, saved, bar);
       bulk_load_1d(dst + 2 * sh.area + sh.saved_area, y + at * kBytes, saved, bar);
     };
-    if (tid == 0)
+    const bool courier = kLoose ? warp == 0 : tid == 0;
+    if (courier)
       for (int b = 0; b < sh.buffers; ++b) bring(b, b);
     // what else a run needs, fetched one run ahead: a lane's row's factors, and the scales
     float ip_next = 1.0f, iq_next = 0.0f;
@@ -751,10 +994,15 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
     };
     fetch(0);
     keep(0);
-    if (kFull || sh.weights_in_smem) fill_weights(a, u.gate, tail.wsm, cols); else __syncthreads();
+    if (kLoose) fill_weights_singly(a, u.gate, tail.wsm, cols);
+    else if (kFull || sh.weights_in_smem) fill_weights(a, u.gate, tail.wsm, cols);
+    else __syncthreads();
     const Weights weights{a, tail.wsm, u.gate, cols, sh.weights_in_smem};
     const auto get = [&](int col, f2 (&q)[4], f2 (&w)[4]) {
-      if (kFull) {                                             // then they are in shared memory
+      if (kLoose) {
+        read_single_weights(tail.wsm + col, cols - col, lane, q);
+        read_single_weights(tail.wsm + cols + col, cols - col, lane, w);
+      } else if (kFull) {                                      // then they are in shared memory
         weights_of(tail.wsm, col, q);
         weights_of(tail.wsm, cols + col, w);
       } else {
@@ -775,14 +1023,53 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
       mbar_wait(tail.full + 8 * b, parity >> b & 1, status);
       parity ^= 1u << b;
       constexpr int kBytes = kCoded ? 1 : sizeof(T);
+      const int64_t run_at = static_cast<int64_t>(row0) * cols;
+      const uint32_t off_v = kLoose ? offset_of<T>(run_at) : 0u, off_s = kLoose ? (kCoded ? offset_of<uint8_t>(run_at) : off_v) : 0u;
       const auto spot = [&](int r, int col) {
         const int at = r * cols + col;
         const uint32_t buf = smem_u32(smem) + b * sh.buffer;
-        return Spot{buf + at * static_cast<int>(sizeof(T)), buf + 2 * sh.area + at * kBytes,
+        return Spot{buf + off_v + at * static_cast<int>(sizeof(T)), buf + off_s + 2 * sh.area + at * kBytes,
                     smem_u32(tail.scales) + (c & 1) * 2 * half + r * sh.blocks_per_row + (col >> 5)};
       };
       // of a lane's columns: yh (y times its scale and ip), b = q * yh, H, and t = dx * w with g = dh_out + iq * t
-      const auto form = [&](const Spot& p, float ip, float iq, f2 (&yh)[4], f2 (&b4)[4], f2 (&H)[4], f2 (&dx)[4], f2 (&t)[4], f2 (&g)[4]) {
+      // (kLoose: of a span's columns, of which `left` lie in the row)
+      const auto form = [&](const Spot& p, int left, float ip, float iq, f2 (&yh)[4], f2 (&b4)[4], f2 (&H)[4], f2 (&dx)[4], f2 (&t)[4], f2 (&g)[4]) {
+        if constexpr (kLoose) {
+          f2 fy[4], fh[4];
+          if (kCoded) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const bool one = 64 * k < left, two = 64 * k + 32 < left;
+              fy[k] = pack_f32x2(one ? scale_of(byte_at(p.scale + half + 2 * k)) * ip : 0.0f, two ? scale_of(byte_at(p.scale + half + 2 * k + 1)) * ip : 0.0f);
+              fh[k] = has_h ? pack_f32x2(one ? scale_of(byte_at(p.scale + 2 * k)) * a.res_scale : 0.0f,
+                                         two ? scale_of(byte_at(p.scale + 2 * k + 1)) * a.res_scale : 0.0f) : 0;
+            }
+            read_single_codes(p.h + sh.saved_area, left, lane, yh);
+            if (has_h) read_single_codes(p.h, left, lane, H);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) fy[k] = twice(ip), fh[k] = twice(a.res_scale);
+            read_singles<T>(p.h + sh.saved_area, left, lane, yh);
+            if (has_h) read_singles<T>(p.h, left, lane, H);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            yh[k] = mul2(yh[k], fy[k]);
+            b4[k] = mul2(q[k], yh[k]);
+            H[k] = has_h ? fma2(H[k], fh[k], b4[k]) : b4[k];
+            g[k] = dx[k] = t[k] = 0;
+          }
+          if (has_g) read_singles<T>(p.dx + sh.area, left, lane, g);
+          if (has_dx) {
+            read_singles<T>(p.dx, left, lane, dx);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              t[k] = mul2(dx[k], w[k]);
+              g[k] = fma2(t[k], twice(iq), g[k]);
+            }
+          }
+          return;
+        }
         const float fy = kCoded ? scale_of(read_byte(p.scale + half)) * ip : ip, fh = kCoded ? scale_of(read_byte(p.scale)) * a.res_scale : a.res_scale;
         read_saved<T, kCoded>(p.h + sh.saved_area, yh);
         if (has_h) read_saved<T, kCoded>(p.h, H);
@@ -815,14 +1102,14 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
         const int r = task / sh.parts, part = task - r * sh.parts;
         const float ip = __shfl_sync(0xFFFFFFFFu, ip_lane, r), iq = __shfl_sync(0xFFFFFFFFu, iq_lane, r);
         f2 sums[3] = {0, 0, 0};
-        int col = part * sh.part_spans * 256 + lane * 8;
-        const int end = kFull ? min((part + 1) * sh.part_spans * 256, cols) : min((part + 1) * sh.part_spans * 256 + lane * 8, cols);
+        int col = part * sh.part_spans * 256 + lane_col;
+        const int end = kFull || kLoose ? min((part + 1) * sh.part_spans * 256, cols) : min((part + 1) * sh.part_spans * 256 + lane * 8, cols);
         Spot p = spot(r, col);
-#pragma unroll 2
+#pragma unroll 1
         for (; col < end; col += 256) {
           f2 yh[4], b4[4], H[4], dx[4], t[4], g[4];
           get(col, q, w);
-          form(p, ip, iq, yh, b4, H, dx, t, g);
+          form(p, cols - col, ip, iq, yh, b4, H, dx, t, g);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             sums[0] = fma2(t[k], H[k], sums[0]);
@@ -854,7 +1141,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
         k2_lane = post ? (s[1] - k1_lane * s[2]) * a.inv_cols : 0.0f;
       }
       // the results, a stripe of columns to a warp
-      const int col0 = stripe * 256 + lane * 8;
+      const int col0 = stripe * 256 + lane_col;
       if (kNv == 1 && (kFull || col0 < cols)) {
         get(col0, q, w);
       }
@@ -873,7 +1160,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
             get(col, q, w);
           }
           f2 yh[4], b4[4], H[4], dx[4], t[4], g[4];
-          form(Spot{p.dx + i * 256 * static_cast<int>(sizeof(T)), p.h + i * 256 * kBytes, p.scale + i * 8}, ip, iq, yh, b4, H, dx, t, g);
+          form(Spot{p.dx + i * 256 * static_cast<int>(sizeof(T)), p.h + i * 256 * kBytes, p.scale + i * 8}, cols - col, ip, iq, yh, b4, H, dx, t, g);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             P[i][k] = fma2(mul2(dx[k], twice(iq)), H[k], P[i][k]);
@@ -881,6 +1168,11 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
             S[i][k] = fma2(d, yh[k], S[i][k]);
             g[k] = mul2(d, twice(a.res_scale));
             t[k] = mul2(fma2(yh[k], twice(-k2), mul2(q[k], d)), twice(ip));
+          }
+          if constexpr (kLoose) {
+            if (want_dh) write_singles(static_cast<T*>(a.dh) + at + i * 256, cols - col, lane, g);
+            if (want_dy) mx = max(mx, write_singles(static_cast<T*>(a.dy) + at + i * 256, cols - col, lane, t));
+            continue;
           }
           if (want_dh) write8(static_cast<T*>(a.dh) + at + i * 256, g);
           if (want_dy) {
@@ -894,13 +1186,14 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
       }
       if (c + 1 < runs) keep((c + 1) & 1);
       __syncthreads();                                         // the buffer is read, the next run's scales are there
-      if (tid == 0) bring(c + sh.buffers, b);
+      if (courier) bring(c + sh.buffers, b);
+      if (kLoose && sh.buffers == 1) __syncthreads();          // single values among what was brought
     }
-    if (a.part_s != nullptr) store_stripes<kNv>(S, a.part_s + unit * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
+    if (a.part_s != nullptr) store_stripes<kNv, kLoose>(S, a.part_s + unit * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
     else __syncthreads();
   }
-  if (a.part_p != nullptr) store_stripes<kNv>(P, a.part_p + static_cast<int64_t>(blockIdx.x) * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
-  if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
+  if (a.part_p != nullptr) store_stripes<kNv, kLoose>(P, a.part_p + static_cast<int64_t>(blockIdx.x) * cols, reinterpret_cast<float*>(smem), sh, stripe, member);
+  if (a.amax != nullptr) raise_amax(kLoose ? mx : largest.bits(), a.amax);
 }
 
 // The gradients of gains and gate from the partial column sums.  A CTA takes 32 columns (a row of them is eight lanes of four), a warp
@@ -1028,10 +1321,6 @@ struct Split {
 };
 
 bool staged(int64_t cols) { return cols % 16 == 0; }
-// CTAs that share a backward's rows: one per SM where rows stream through its shared memory; four where every row is fetched when it
-// is due and only other CTAs' rows cover the wait (613 x 1011 fp32: 41 us with one, 20 with four).
-int64_t backward_units(int64_t cols) { return staged(cols) ? kNormUnits : 4 * kNormUnits; }
-
 NormArgs common(const falqon_block_norm* p) {
   NormArgs a{};
   a.post_gain = p->post_gain;
@@ -1072,9 +1361,9 @@ constexpr int kSmemLimit = 226 * 1024;    // dynamic; the kernels have a few byt
 int spans_for(int64_t cols) { return cols <= 2 * 512 * 8 ? 2 : 4; }
 // set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
 bool make_shape(int64_t cols, int64_t rows_per_cta, int set_bytes, int red, int smem_limit, Shape* sh, size_t* smem) {
-  const int nv = spans_for(cols), vec = static_cast<int>(cols / 8);
+  const int nv = spans_for(cols), vec = static_cast<int>((cols + 7) / 8);
   sh->cols = static_cast<int>(cols);
-  sh->group_threads = (vec + 32 * nv - 1) / (32 * nv) * 32;
+  sh->group_threads = (vec + 32 * nv - 1) / (32 * nv) * 32;   // a warp to nv spans of 256 columns
   sh->groups = 512 / sh->group_threads;
   if (sh->groups > rows_per_cta) sh->groups = static_cast<int>(rows_per_cta < 1 ? 1 : rows_per_cta);
   sh->warp_stage = nv * set_bytes;
@@ -1119,7 +1408,7 @@ int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
 }
 // How a backward's runs are cut: warps, rows per run, and the shared memory it takes; false where not even one row fits.
-bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_bytes, int* spans, Run* r, size_t* smem) {
+bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_bytes, bool loose, int* spans, Run* r, size_t* smem) {
   r->cols = static_cast<int>(cols);
   r->stripes = static_cast<int>((cols + 255) / 256);
   r->blocks_per_row = static_cast<int>((cols + kMx8Block - 1) / kMx8Block);
@@ -1129,7 +1418,8 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
   r->split = r->warps / r->stripe_warps;
   const int row = static_cast<int>(cols) * (2 * value_bytes + 2 * saved_bytes);
   for (int attempt = 0; attempt < 3; ++attempt) {              // two buffers and the weights; without the weights; one buffer
-    r->weights_in_smem = attempt == 0;
+    if (loose && attempt == 1) continue;
+    r->weights_in_smem = loose || attempt == 0;
     r->buffers = attempt < 2 ? 2 : 1;
     int run = (kSmemLimit - (r->weights_in_smem ? r->cols * 8 : 0)) / (r->buffers * row);
     if (run > kMaxRun) run = kMaxRun;
@@ -1140,8 +1430,8 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
       if (r->parts > r->stripes) r->parts = r->stripes;
       if (r->parts < 1) r->parts = 1;
       r->part_spans = (r->stripes + r->parts - 1) / r->parts;
-      r->area = run * r->cols * value_bytes;
-      r->saved_area = run * r->cols * saved_bytes;
+      r->area = loose ? (run * r->cols * value_bytes + 47) / 16 * 16 : run * r->cols * value_bytes;
+      r->saved_area = loose ? (run * r->cols * saved_bytes + 47) / 16 * 16 : run * r->cols * saved_bytes;
       r->buffer = (2 * r->area + 2 * r->saved_area + 127) / 128 * 128;
       *smem = static_cast<size_t>(r->buffers) * r->buffer + run_tail_bytes(*r);
       const size_t sums = static_cast<size_t>(r->split) * r->cols * sizeof(float);   // store_stripes, over the buffers
@@ -1152,31 +1442,41 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
   }
   return false;
 }
-template <typename T, bool kCoded, int kNv, bool kFull, int kThreads>
+template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose, int kThreads>
 int start_run(const NormArgs& a, const Run& r, size_t smem, int64_t ctas, int* status, cudaStream_t stream) {
   static DeviceMask done{0};
-  if (set_max_dynamic_smem(norm_backward_run_kernel<T, kCoded, kNv, kFull, kThreads>, kSmemLimit, done) != cudaSuccess) return FALQON_ERR_CUDA;
-  return finish(launch_pdl(norm_backward_run_kernel<T, kCoded, kNv, kFull, kThreads>, dim3(static_cast<unsigned>(ctas)), dim3(32u * r.warps), smem, stream, 1, a, r,
-                           status));
+  const auto kernel = norm_backward_run_kernel<T, kCoded, kNv, kFull, kLoose, kThreads>;
+  if (set_max_dynamic_smem(kernel, kSmemLimit, done) != cudaSuccess) return FALQON_ERR_CUDA;
+  return finish(launch_pdl(kernel, dim3(static_cast<unsigned>(ctas)), dim3(32u * r.warps), smem, stream, 1, a, r, status));
 }
 template <typename T, bool kCoded>
 int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStream_t stream) {
   Run r;
   size_t smem;
   int spans;
-  if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded ? 1 : sizeof(T), &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
+  const bool loose = !staged(a.cols);
+  if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded ? 1 : sizeof(T), loose, &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
   // the usual call: both norms, both gradients in and out, a residual, whole stripes
   const bool full = a.cols % 256 == 0 && r.weights_in_smem && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr &&
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
-  if (spans == 1 && r.warps <= 16)
-    return full ? start_run<T, kCoded, 1, true, 512>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 512>(a, r, smem, ctas, status, stream);
-  if (spans == 1 && r.warps <= 20)
-    return full ? start_run<T, kCoded, 1, true, 640>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 640>(a, r, smem, ctas, status, stream);
-  if (spans == 1)
-    return full ? start_run<T, kCoded, 1, true, 768>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 1, false, 768>(a, r, smem, ctas, status, stream);
-  if (spans == 2)
-    return full ? start_run<T, kCoded, 2, true, 512>(a, r, smem, ctas, status, stream) : start_run<T, kCoded, 2, false, 512>(a, r, smem, ctas, status, stream);
-  return start_run<T, kCoded, 4, false, 512>(a, r, smem, ctas, status, stream);
+  const auto go = [&](auto kind) {                             // 0: any call, 1: the usual call, 2: any width
+    constexpr bool kFull = decltype(kind)::value == 1, kLoose = decltype(kind)::value == 2;
+    if (spans == 1 && r.warps <= 16) return start_run<T, kCoded, 1, kFull, kLoose, 512>(a, r, smem, ctas, status, stream);
+    if (spans == 1 && r.warps <= 20) return start_run<T, kCoded, 1, kFull, kLoose, 640>(a, r, smem, ctas, status, stream);
+    if (spans == 1) return start_run<T, kCoded, 1, kFull, kLoose, 768>(a, r, smem, ctas, status, stream);
+    if (spans == 2) return start_run<T, kCoded, 2, kFull, kLoose, 512>(a, r, smem, ctas, status, stream);
+    return start_run<T, kCoded, 4, false, kLoose, 512>(a, r, smem, ctas, status, stream);
+  };
+  if (loose) return go(std::integral_constant<int, 2>{});
+  return full ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 0>{});
+}
+template <typename T, int kNv>
+int launch_forward_loose(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
+  static DeviceMask done{0};
+  Shape sh;
+  size_t smem;
+  if (!make_shape(a.cols, a.rows_per_piece, 2 * (256 * sizeof(T) + 16), kSumFloats, kSmemLimit, &sh, &smem) || !sh.weights_in_smem) return FALQON_ERR_UNSUPPORTED;
+  return start_rows(norm_forward_loose_kernel<T, kNv>, done, a, sh, smem, ctas, stream);
 }
 template <typename F>
 int with_spans(int64_t cols, F go) {
@@ -1221,6 +1521,16 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
     });
     if (rc != FALQON_ERR_UNSUPPORTED) return rc;
   }
+  if (!staged(a.cols)) {
+    const Split s(p, kNormUnits);
+    NormArgs b = a;
+    s.put(&b);
+    const int rc = with_spans(a.cols, [&](auto n) {
+      return p->dtype == FALQON_BF16 ? launch_forward_loose<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
+                                     : launch_forward_loose<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
+    });
+    if (rc != FALQON_ERR_UNSUPPORTED) return rc;
+  }
   const int items = items_for(a.cols);
   const unsigned threads = static_cast<unsigned>(((a.cols + items - 1) / items + 31) / 32 * 32);
   const int64_t cap = static_cast<int64_t>(sm_count()) * 16;
@@ -1235,7 +1545,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
 
 size_t falqon_block_norm_scratch_bytes(const falqon_block_norm* p) {
   if (!plan_ok(p)) return 0;
-  const Split s(p, backward_units(p->cols));
+  const Split s(p, kNormUnits);
   return static_cast<size_t>(s.units + s.ctas) * static_cast<size_t>(p->cols) * sizeof(float);
 }
 
@@ -1255,7 +1565,7 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
       !ok16(dh_out) || !ok16(h) || !ok16(h_codes) || !ok16(y) || !ok16(y_codes) || !ok16(dh) || !ok16(dy) || !ok16(dpost_gain) ||
       !ok16(dpre_gain) || !ok16(dgate) || (amax_dy != nullptr && dy == nullptr))
     return FALQON_ERR_INVALID_ARG;
-  const Split s(p, backward_units(p->cols));
+  const Split s(p, kNormUnits);
   const bool sums_s = dpost_gain != nullptr || dgate != nullptr, sums_p = dpre_gain != nullptr;
   if ((sums_s || sums_p) && (scratch == nullptr || !ok16(scratch) || scratch_bytes < falqon_block_norm_scratch_bytes(p)))
     return FALQON_ERR_WORKSPACE;
@@ -1277,7 +1587,7 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
   a.part_p = sums_p ? static_cast<float*>(scratch) + s.units * a.cols : nullptr;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int rc = FALQON_ERR_UNSUPPORTED;
-  if (staged(a.cols)) {
+  {
     int* status = device_status_ptr();
     if (status == nullptr) return FALQON_ERR_CUDA;
     if (p->dtype == FALQON_BF16)
