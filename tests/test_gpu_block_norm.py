@@ -24,6 +24,8 @@ CASES = [
     (9, 8192, 9, True, True, True, True), (6, 11008, 2, True, True, True, True), (5, 16384, 5, True, True, True, True),
     (7, 16383, 3, True, True, True, True), (257, 256, 1, True, True, True, True), (20, 96, 0, False, False, True, False),
     (700, 1536, 64, True, True, True, True), (16, 128, 16, False, True, False, False),
+    (1, 4095, 1, True, True, True, True), (17, 2049, 6, True, True, True, True), (5, 5111, 2, True, False, True, True), (3, 8191, 3, False, True, True, False),
+    (2, 9, 2, True, True, False, True), (400, 33, 0, True, True, True, True), (2, 6160, 1, True, True, True, True), (3, 12300, 3, True, True, True, True),
 ]
 IDS = [f"{c[0]}x{c[1]}" for c in CASES]
 
