@@ -17,7 +17,7 @@ namespace falqon {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kSeqThreads = 512;
+constexpr int kSeqThreads = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxParts = 64;              // parts of one row
 constexpr float kNotCounted = -1.0f;       // in the place of a row's (first part's) sum, which is never negative
@@ -118,18 +118,20 @@ struct Running {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
+// kTeam threads to a row or a part of one: a CTA, or a warp where rows are short (then parts == 1).
+template <typename T, int kTeam>
+__global__ void __launch_bounds__(kRowThreads) row_stats_kernel(int64_t rows, const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
                                                                 int parts, float2* out, float* target_logit, unsigned int* counter, int* status) {
   __shared__ float red_m[kRowThreads / 32], red_s[kRowThreads / 32];
   pdl_trigger();
   pdl_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0u;   // for the kernel after this one
-  const int64_t row = blockIdx.x / parts;
-  const int part = static_cast<int>(blockIdx.x - row * parts);
+  const int64_t team = static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam, row = team / parts;
+  const int part = static_cast<int>(team - row * parts), tid = threadIdx.x % kTeam;
+  if (kTeam < kRowThreads && row >= rows) return;
   const int64_t target = ld_stream(targets + row);
   if (target < 0 || target >= vocab) {
-    if (part == 0 && threadIdx.x == 0) {
+    if (part == 0 && tid == 0) {
       out[row * parts] = make_float2(0.0f, kNotCounted);
       if (target >= vocab) atomicExch(status, FALQON_ERR_INVALID_ARG);
     }
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits,
   }
   const T* p = logits + row * ld;
   float at_target = 0.0f;                  // fetched here, beside the stream, and not in a gather of the next kernel
-  if (part == 0 && threadIdx.x == 0) at_target = load1(p + target);
+  if (part == 0 && tid == 0) at_target = load1(p + target);
   const Span sp = span_of(p, vocab);
   Running r;
   const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
@@ -145,15 +147,15 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits,
   f2 sum = 0;                              // the running sum, two halves of it
   constexpr int kUnroll = 4;
   constexpr uint32_t kNone = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;   // -inf: adds nothing
-  for (int64_t v = begin + threadIdx.x; v < end; v += kUnroll * kRowThreads) {
+  for (int64_t v = begin + tid; v < end; v += kUnroll * kTeam) {
     uint4 q[kUnroll];
-    if (v + (kUnroll - 1) * kRowThreads < end) {
+    if (v + (kUnroll - 1) * kTeam < end) {
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kRowThreads);
+      for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kTeam);
     } else {
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j)
-        q[j] = v + j * kRowThreads < end ? ld_stream(body + v + j * kRowThreads) : make_uint4(kNone, kNone, kNone, kNone);
+        q[j] = v + j * kTeam < end ? ld_stream(body + v + j * kTeam) : make_uint4(kNone, kNone, kNone, kNone);
     }
     const float top = largest_of(q, kUnroll, T{});
     if (top > r.m) {                       // seldom after the first vectors
@@ -171,22 +173,24 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(const T* logits,
   }
   r.s = halves(sum);
   if (part == 0) {
-    if (static_cast<int>(threadIdx.x) < sp.head) r.add(load1(p + threadIdx.x));
-    if (threadIdx.x < vocab - sp.tail) r.add(load1(p + sp.tail + threadIdx.x));
+    if (tid < sp.head) r.add(load1(p + tid));
+    if (tid < vocab - sp.tail) r.add(load1(p + sp.tail + tid));
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const float om = __shfl_xor_sync(0xFFFFFFFFu, r.m, o), os = __shfl_xor_sync(0xFFFFFFFFu, r.s, o);
     r.join(om, os);
   }
-  if ((threadIdx.x & 31) == 0) {
-    red_m[threadIdx.x >> 5] = r.m;
-    red_s[threadIdx.x >> 5] = r.s;
+  if (kTeam > 32) {
+    if ((tid & 31) == 0) {
+      red_m[tid >> 5] = r.m;
+      red_s[tid >> 5] = r.s;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
 #pragma unroll
-    for (int w = 1; w < kRowThreads / 32; ++w) r.join(red_m[w], red_s[w]);
+    for (int w = 1; w < kTeam / 32; ++w) r.join(red_m[w], red_s[w]);
     out[row * parts + part] = make_float2(r.m, r.s);
     if (part == 0) target_logit[row] = at_target;
   }
@@ -235,23 +239,20 @@ __device__ __forceinline__ Sums cta_sums(Sums v, Sums* red) {
   return warp_sums(static_cast<int>(threadIdx.x) < warps ? red[threadIdx.x] : Sums{0.0, 0.0, 0u, 0u});
 }
 
-// The log-probability of one row (0 and false: not counted) from its parts.
-__device__ __forceinline__ bool row_logp(const SeqArgs& a, int64_t row, float& lp) {
-  const float x = ld_stream(a.target_logit + row);   // anything where the row is not counted
-  const float2* part = a.part + row * a.parts;
-  const float2 head = ld_stream(part);
+// The log-probability of one row (0 and false: not counted) from its target's logit, its first part and the others.
+__device__ __forceinline__ bool row_logp(const SeqArgs& a, int64_t row, float x, const float2& head, float& lp) {
+  lp = 0.0f;
+  if (head.y == kNotCounted) return false;           // the other parts were not written
   Running r{head.x, head.y};
-  constexpr int kAhead = 8;
+  const float2* part = a.part + row * a.parts;
+  constexpr int kAhead = 4;
   for (int i = 1; i < a.parts; i += kAhead) {
     float2 q[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) q[j] = i + j < a.parts ? ld_stream(part + i + j) : make_float2(-INFINITY, 0.0f);
-    if (head.y == kNotCounted) break;                // the other parts were not written
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) r.join(q[j].x, q[j].y);
   }
-  lp = 0.0f;
-  if (head.y == kNotCounted) return false;
   if (a.stats != nullptr) a.stats[row] = make_float2(r.m, r.s);
   lp = (x - r.m) - logf(r.s);
   return true;
@@ -292,18 +293,33 @@ __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) 
   uint64_t seen = 0;                       // which of the thread's first 64 rows are counted
   int turn = 0;
   Sums t{0.0, 0.0, 0u, 0u};
-  for (int64_t row = begin + threadIdx.x; row < end; row += blockDim.x, ++turn) {
-    float lp;
-    const bool counted = row_logp(a, row, lp);
-    if (a.logp != nullptr) a.logp[row] = lp;
-    if (!counted) continue;
-    if (turn < 64) seen |= 1ull << turn;
-    if (kPairs && row >= mid) {
-      t.second += static_cast<double>(lp);
-      ++t.n_second;
-    } else {
-      t.first += static_cast<double>(lp);
-      ++t.n_first;
+  constexpr int kRows = 4;                 // a thread's rows in flight
+  for (int64_t row0 = begin + threadIdx.x; row0 < end; row0 += kRows * blockDim.x) {
+    float x[kRows];
+    float2 head[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      const int64_t row = row0 + j * blockDim.x;
+      if (row >= end) break;
+      x[j] = ld_stream(a.target_logit + row);        // anything where the row is not counted
+      head[j] = ld_stream(a.part + row * a.parts);
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j, ++turn) {
+      const int64_t row = row0 + j * blockDim.x;
+      if (row >= end) break;
+      float lp;
+      const bool counted = row_logp(a, row, x[j], head[j], lp);
+      if (a.logp != nullptr) a.logp[row] = lp;
+      if (!counted) continue;
+      if (turn < 64) seen |= 1ull << turn;
+      if (kPairs && row >= mid) {
+        t.second += static_cast<double>(lp);
+        ++t.n_second;
+      } else {
+        t.first += static_cast<double>(lp);
+        ++t.n_first;
+      }
     }
   }
   t = cta_sums(t, red);
@@ -372,86 +388,88 @@ __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) 
 }
 
 // kSame: logits and dlogits rows have the same offset from a 16-byte boundary, so vectors can be stored; else single values are.
-template <typename T, bool kSame>
-__global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
+template <typename T, bool kSame, int kTeam>
+__global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(int64_t rows, const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
                                                                  int parts, const float2* stats, const float* dlogp, const float* dloss,
                                                                  T* out, int64_t ld_out, float* amax) {
   pdl_trigger();
   pdl_wait();
   constexpr int n = Row<T>::kN;
   // the last rows first: of what the forward has read, they are still in L2
-  const int64_t task = static_cast<int64_t>(gridDim.x) - 1 - blockIdx.x, row = task / parts;
-  const int part = static_cast<int>(task - row * parts);
-  const float c = ld_stream(dlogp + row) * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
-  const T* p = logits + row * ld;
-  T* o = out + row * ld_out;
-  const Span sp = span_of(p, vocab);
-  const int64_t begin = sp.body * part / parts, end = sp.body * (part + 1) / parts;
-  const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
-  const bool zero = c == 0.0f;
-  const float2 st = zero ? make_float2(0.0f, 1.0f) : ld_stream(stats + row);
-  const int64_t target = zero ? -1 : ld_stream(targets + row);
-  const float f = -c / st.y;
+  const int64_t task = rows * parts - 1 - (static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam), row = task / parts;
+  const int part = static_cast<int>(task - row * parts), tid = threadIdx.x % kTeam;
   uint32_t mx = 0;
-  const auto one = [&](int64_t i) {
-    const float g = zero ? 0.0f : __fmaf_rn(f, exp_of(load1(p + i) - st.x), i == target ? c : 0.0f);
-    mx = max(mx, store1(o + i, g));
-  };
-  // one vector: its values' gradients
-  const auto put = [&](int64_t v, const uint4& q) {
-    const int64_t at = sp.head + v * n;
-    f2 x[Row<T>::kPairs];
-    if (zero) {
+  if (task >= 0) {
+    const float c = ld_stream(dlogp + row) * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
+    const T* p = logits + row * ld;
+    T* o = out + row * ld_out;
+    const Span sp = span_of(p, vocab);
+    const int64_t begin = sp.body * part / parts, end = sp.body * (part + 1) / parts;
+    const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
+    const bool zero = c == 0.0f;
+    const float2 st = zero ? make_float2(0.0f, 1.0f) : ld_stream(stats + row);
+    const int64_t target = zero ? -1 : ld_stream(targets + row);
+    const float f = -c / st.y;
+    const auto one = [&](int64_t i) {
+      const float g = zero ? 0.0f : __fmaf_rn(f, exp_of(load1(p + i) - st.x), i == target ? c : 0.0f);
+      mx = max(mx, store1(o + i, g));
+    };
+    // one vector: its values' gradients
+    const auto put = [&](int64_t v, const uint4& q) {
+      const int64_t at = sp.head + v * n;
+      f2 x[Row<T>::kPairs];
+      if (zero) {
 #pragma unroll
-      for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = 0;
-    } else {
-      expand(q, x, T{});
+        for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = 0;
+      } else {
+        expand(q, x, T{});
 #pragma unroll
-      for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = mul2(twice(f), exp_of2(x[k], twice(-st.x)));
-      if (target >= at && target < at + n) {
+        for (int k = 0; k < Row<T>::kPairs; ++k) x[k] = mul2(twice(f), exp_of2(x[k], twice(-st.x)));
+        if (target >= at && target < at + n) {
 #pragma unroll
-        for (int k = 0; k < Row<T>::kPairs; ++k) {
-          if (at + 2 * k == target) x[k] = add2(x[k], pack_f32x2(c, 0.0f));
-          if (at + 2 * k + 1 == target) x[k] = add2(x[k], pack_f32x2(0.0f, c));
+          for (int k = 0; k < Row<T>::kPairs; ++k) {
+            if (at + 2 * k == target) x[k] = add2(x[k], pack_f32x2(c, 0.0f));
+            if (at + 2 * k + 1 == target) x[k] = add2(x[k], pack_f32x2(0.0f, c));
+          }
         }
       }
-    }
-    const uint4 w = shrink(x, T{});
-    if (kSame) {
-      *reinterpret_cast<uint4*>(o + at) = w;
-      if (amax != nullptr) {
-        expand(w, x, T{});
+      const uint4 w = shrink(x, T{});
+      if (kSame) {
+        *reinterpret_cast<uint4*>(o + at) = w;
+        if (amax != nullptr) {
+          expand(w, x, T{});
+#pragma unroll
+          for (int k = 0; k < Row<T>::kPairs; ++k) {
+            float lo, hi;
+            unpack_f32x2(x[k], lo, hi);
+            mx = max(mx, max(abs_bits(lo), abs_bits(hi)));
+          }
+        }
+      } else {
 #pragma unroll
         for (int k = 0; k < Row<T>::kPairs; ++k) {
           float lo, hi;
           unpack_f32x2(x[k], lo, hi);
-          mx = max(mx, max(abs_bits(lo), abs_bits(hi)));
+          mx = max(mx, max(store1(o + at + 2 * k, lo), store1(o + at + 2 * k + 1, hi)));
         }
       }
-    } else {
+    };
+    constexpr int kUnroll = 4;
+    int64_t v = begin + tid;
+    for (; v + (kUnroll - 1) * kTeam < end; v += kUnroll * kTeam) {
+      uint4 q[kUnroll];
+      if (!zero) {
 #pragma unroll
-      for (int k = 0; k < Row<T>::kPairs; ++k) {
-        float lo, hi;
-        unpack_f32x2(x[k], lo, hi);
-        mx = max(mx, max(store1(o + at + 2 * k, lo), store1(o + at + 2 * k + 1, hi)));
+        for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kTeam);
       }
-    }
-  };
-  constexpr int kUnroll = 4;
-  int64_t v = begin + threadIdx.x;
-  for (; v + (kUnroll - 1) * kRowThreads < end; v += kUnroll * kRowThreads) {
-    uint4 q[kUnroll];
-    if (!zero) {
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) q[j] = ld_stream(body + v + j * kRowThreads);
+      for (int j = 0; j < kUnroll; ++j) put(v + j * kTeam, q[j]);
     }
-#pragma unroll
-    for (int j = 0; j < kUnroll; ++j) put(v + j * kRowThreads, q[j]);
-  }
-  for (; v < end; v += kRowThreads) put(v, zero ? make_uint4(0u, 0u, 0u, 0u) : ld_stream(body + v));
-  if (part == 0) {
-    if (static_cast<int>(threadIdx.x) < sp.head) one(threadIdx.x);
-    if (threadIdx.x < vocab - sp.tail) one(sp.tail + threadIdx.x);
+    for (; v < end; v += kTeam) put(v, zero ? make_uint4(0u, 0u, 0u, 0u) : ld_stream(body + v));
+    if (part == 0) {
+      if (tid < sp.head) one(tid);
+      if (tid < vocab - sp.tail) one(sp.tail + tid);
+    }
   }
   if (amax != nullptr) raise_amax(mx, amax);
 }
@@ -477,17 +495,26 @@ int parts_for(int64_t rows, int64_t vocab, int dtype) {
 
 // A thread per row of the average sequence (or pair), a warp at least.
 unsigned sequence_threads(int64_t rows, int64_t ctas) {
-  const int64_t t = (rows / ctas + 31) / 32 * 32;
+  const int64_t t = (rows / ctas + 31) / 32 * 32;            // (a pair's rows vary: a thread takes several where they are more)
   return static_cast<unsigned>(t < 32 ? 32 : t > kSeqThreads ? kSeqThreads : t);
 }
 
+// A warp to a row where a CTA's threads would not even have a vector each.  Loss and gradient of 12000 x 1500 bf16: 82 us by CTAs, 36 by
+// warps; of 1500 x 8000, which is beyond this rule, 27 by CTAs, 35 by warps.
+bool by_warps(int64_t vocab, int dtype, int parts) { return parts == 1 && vocab / (dtype == FALQON_BF16 ? 8 : 4) < kRowThreads; }
+
+template <typename T>
+cudaError_t launch_row_stats(const void* logits, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts, bool warps, float2* out,
+                             float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
+  const int64_t per = warps ? kRowThreads / 32 : 1;
+  return launch_pdl(warps ? row_stats_kernel<T, 32> : row_stats_kernel<T, kRowThreads>, dim3(static_cast<unsigned>((rows * parts + per - 1) / per)),
+                    dim3(kRowThreads), 0, stream, 1, rows, static_cast<const T*>(logits), vocab, ld, targets, parts, out, target_logit, counter, status);
+}
 cudaError_t launch_row_stats(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts,
                              float2* out, float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(rows * parts)), block(kRowThreads);
-  return dtype == FALQON_BF16 ? launch_pdl(row_stats_kernel<bf16_t>, grid, block, 0, stream, 1, static_cast<const bf16_t*>(logits), vocab,
-                                           ld, targets, parts, out, target_logit, counter, status)
-                              : launch_pdl(row_stats_kernel<float>, grid, block, 0, stream, 1, static_cast<const float*>(logits), vocab,
-                                           ld, targets, parts, out, target_logit, counter, status);
+  const bool warps = by_warps(vocab, dtype, parts);
+  return dtype == FALQON_BF16 ? launch_row_stats<bf16_t>(logits, rows, vocab, ld, targets, parts, warps, out, target_logit, counter, status, stream)
+                              : launch_row_stats<float>(logits, rows, vocab, ld, targets, parts, warps, out, target_logit, counter, status, stream);
 }
 
 }  // namespace
@@ -588,21 +615,22 @@ int falqon_preference_backward(const falqon_preference* p, const void* logits, c
     return FALQON_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int parts = parts_for(p->rows, p->vocab, p->dtype);
-  const dim3 grid(static_cast<unsigned>(p->rows * parts)), block(kRowThreads);
+  const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 &&
+                    (ld_out - p->ld) % (p->dtype == FALQON_BF16 ? 8 : 4) == 0;
+  const bool warps = by_warps(p->vocab, p->dtype, parts);
+  const int64_t per = warps ? kRowThreads / 32 : 1;
   const float2* stats = reinterpret_cast<const float2*>(row_stats);
   const auto go = [&](auto kernel, auto* typed) {
     using T = std::remove_pointer_t<decltype(typed)>;
-    return finish(launch_pdl(kernel, grid, block, 0, st, 1, static_cast<const T*>(logits), p->vocab, p->ld, targets, parts, stats, dlogp,
-                             dloss, typed, ld_out, amax_out));
+    return finish(launch_pdl(kernel, dim3(static_cast<unsigned>((p->rows * parts + per - 1) / per)), dim3(kRowThreads), 0, st, 1, p->rows,
+                             static_cast<const T*>(logits), p->vocab, p->ld, targets, parts, stats, dlogp, dloss, typed, ld_out, amax_out));
   };
-  const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 &&
-                    (ld_out - p->ld) % (p->dtype == FALQON_BF16 ? 8 : 4) == 0;
-  if (p->dtype == FALQON_BF16) {
-    bf16_t* t = static_cast<bf16_t*>(dlogits);
-    return same ? go(logit_grad_kernel<bf16_t, true>, t) : go(logit_grad_kernel<bf16_t, false>, t);
-  }
-  float* t = static_cast<float*>(dlogits);
-  return same ? go(logit_grad_kernel<float, true>, t) : go(logit_grad_kernel<float, false>, t);
+  const auto pick = [&](auto* typed) {
+    using T = std::remove_pointer_t<decltype(typed)>;
+    if (warps) return same ? go(logit_grad_kernel<T, true, 32>, typed) : go(logit_grad_kernel<T, false, 32>, typed);
+    return same ? go(logit_grad_kernel<T, true, kRowThreads>, typed) : go(logit_grad_kernel<T, false, kRowThreads>, typed);
+  };
+  return p->dtype == FALQON_BF16 ? pick(static_cast<bf16_t*>(dlogits)) : pick(static_cast<float*>(dlogits));
 }
 
 }  // extern "C"
