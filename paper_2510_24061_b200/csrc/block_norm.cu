@@ -61,10 +61,13 @@ __device__ __forceinline__ void cta_sums(float (&v)[kN], float* red, int& phase)
   }
 }
 
-// ---- any width: a thread holds kItems single columns tid, tid + threads, ...; a checkpoint's block is a warp
+// ---- rows that do not fit in shared memory beside their weights (fp32 beyond 9640 columns backward and 13900 forward, if not a
+// multiple of 16 wide; fp32 beyond 14464 backward in any case): a CTA takes a row at a time, a thread kItems single columns tid,
+// tid + threads, .. in registers, and a checkpoint's block is a warp.  Nothing is fetched ahead: 2 to 6 times the staged kernels' time.
+constexpr int kItems = 16;   // of up to 1024 threads: FALQON_NORM_MAX_COLS
 // Squares are divided by the width before they are added, so that only a mean beyond fp32's range overflows.
-template <typename T, int kItems>
-__global__ void __launch_bounds__(1024) norm_forward_kernel(const NormArgs a) {
+template <typename T>
+__global__ void __launch_bounds__(1024, 1) norm_forward_kernel(const NormArgs a) {
   __shared__ float red[2 * 32];
   pdl_trigger();
   pdl_wait();
@@ -135,8 +138,8 @@ __device__ __forceinline__ float saved_at(const void* plain, const uint8_t* code
   return mx8_decode1(ld_stream(codes + base + c), mx8_decode_factor(ld_stream(scales + scale_base + (c >> 5))));
 }
 
-template <typename T, int kItems>
-__global__ void __launch_bounds__(1024) norm_backward_kernel(const NormArgs a) {
+template <typename T>
+__global__ void __launch_bounds__(1024, 1) norm_backward_kernel(const NormArgs a) {
   __shared__ float red[2 * 3 * 32];
   pdl_trigger();
   pdl_wait();
@@ -211,12 +214,12 @@ __global__ void __launch_bounds__(1024) norm_backward_kernel(const NormArgs a) {
   if (a.amax != nullptr) raise_amax(mx, a.amax);
 }
 
-// ---- widths that are multiples of 16: rows stream through shared memory
+// ---- forward, widths that are multiples of 16: rows stream through shared memory
 // A row belongs to a group of whole warps; a warp has kNv neighbouring spans of 256 columns, a lane eight columns of each.
 // Every warp copies its own spans of the next rows with 16-byte asynchronous copies into a ring of `depth` stages that only
-// it reads, so the copies in flight cost no registers and no barrier.  Two rows at a time (two groups of 256 threads at 4096
-// columns): while one group waits for its row's sums, the other computes.  Arithmetic is two values per instruction (f32x2,
-// each half an ordinary rounded operation), since a row's instructions, not its bytes, were the limit without it.
+// it reads, so the copies in flight cost no registers and no barrier.  Several rows at a time: while one group waits for its
+// row's sums, the others compute.  Arithmetic is two values per instruction (f32x2, each half an ordinary rounded operation),
+// since a row's instructions, not its bytes, were the limit without it.
 struct Shape {
   int cols, group_threads, groups, depth, warp_stage;   // groups: rows a CTA works on at a time; warp_stage: bytes of a warp's stage
   int weights_in_smem;
@@ -488,9 +491,11 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
-// ---- the usual call: both norms, a residual, every result, rows of 512 columns per warp (512, 1024, .. 8192)
-// The same work as the two kernels above with nothing left to test in the row loop and offsets that advance by a row: they are
-// bound by the instructions a row takes, and tests and address arithmetic were half of them.
+// ---- forward, the usual call: both norms, a residual, every result, rows of 1024 columns per warp (1024, 2048, .. 8192)
+// The same work with nothing left to test in the row loop and offsets that advance by a row; four spans a lane (a row of 4096 columns
+// is 128 threads, four rows a CTA), so that a row's two reductions are shared by 1024 columns a warp.  HBM-bound as far as
+// instructions allow: 4096 x 4096 bf16 with both checkpoints 37 us (4.6 TB/s of what it must move; two spans a lane and two CTAs per
+// SM 42), 8192 x 8192 without 96 us (5.6 TB/s).
 constexpr int kFullDepth = 2;                                  // two rows ahead per group cover the latency
 
 template <typename T, int kNv>
@@ -1339,22 +1344,7 @@ NormArgs common(const falqon_block_norm* p) {
   return a;
 }
 
-// The smallest number of columns per thread that keeps a row within 256 threads, or 16 with up to 1024 threads.
-int items_for(int64_t cols) {
-  int items = 1;
-  while (items < 16 && cols > items * 256) items *= 2;
-  return items;
-}
-template <typename F>
-int with_items(int items, F go) {
-  switch (items) {
-    case 1: return go(std::integral_constant<int, 1>{});
-    case 2: return go(std::integral_constant<int, 2>{});
-    case 4: return go(std::integral_constant<int, 4>{});
-    case 8: return go(std::integral_constant<int, 8>{});
-    default: return go(std::integral_constant<int, 16>{});
-  }
-}
+unsigned item_threads(int64_t cols) { return static_cast<unsigned>(((cols + kItems - 1) / kItems + 31) / 32 * 32); }
 
 // The staged kernels' shape.  set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
 constexpr int kSmemLimit = 226 * 1024;    // dynamic; the kernels have a few bytes of their own besides
@@ -1531,16 +1521,10 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
     });
     if (rc != FALQON_ERR_UNSUPPORTED) return rc;
   }
-  const int items = items_for(a.cols);
-  const unsigned threads = static_cast<unsigned>(((a.cols + items - 1) / items + 31) / 32 * 32);
-  const int64_t cap = static_cast<int64_t>(sm_count()) * 16;
-  const unsigned grid = static_cast<unsigned>(a.rows < cap ? a.rows : cap);
-  return with_items(items, [&](auto n) {
-    return finish(p->dtype == FALQON_BF16 ? launch_pdl(norm_forward_kernel<bf16_t, n.value>, dim3(grid), dim3(threads), 0,
-                                                       static_cast<cudaStream_t>(stream), 1, a)
-                                          : launch_pdl(norm_forward_kernel<float, n.value>, dim3(grid), dim3(threads), 0,
-                                                       static_cast<cudaStream_t>(stream), 1, a));
-  });
+  const int64_t cap = static_cast<int64_t>(sm_count()) * 2;
+  const dim3 grid(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), block(item_threads(a.cols));
+  return finish(launch_pdl(p->dtype == FALQON_BF16 ? norm_forward_kernel<bf16_t> : norm_forward_kernel<float>, grid, block, 0,
+                           static_cast<cudaStream_t>(stream), 1, a));
 }
 
 size_t falqon_block_norm_scratch_bytes(const falqon_block_norm* p) {
@@ -1595,14 +1579,9 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
     else
       rc = coded ? launch_backward_runs<float, true>(a, s.ctas, status, st) : launch_backward_runs<float, false>(a, s.ctas, status, st);
   }
-  if (rc == FALQON_ERR_UNSUPPORTED) {                          // any other width, or rows that do not fit the ring
-    const int items = items_for(a.cols);
-    const dim3 grid(static_cast<unsigned>(s.ctas)), block(static_cast<unsigned>(((a.cols + items - 1) / items + 31) / 32 * 32));
-    rc = with_items(items, [&](auto n) {
-      return finish(p->dtype == FALQON_BF16 ? launch_pdl(norm_backward_kernel<bf16_t, n.value>, grid, block, 0, st, 1, a)
-                                            : launch_pdl(norm_backward_kernel<float, n.value>, grid, block, 0, st, 1, a));
-    });
-  }
+  if (rc == FALQON_ERR_UNSUPPORTED)
+    rc = finish(launch_pdl(p->dtype == FALQON_BF16 ? norm_backward_kernel<bf16_t> : norm_backward_kernel<float>, dim3(static_cast<unsigned>(s.ctas)),
+                           dim3(item_threads(a.cols)), 0, st, 1, a));
   if (rc != FALQON_OK || (!sums_s && !sums_p)) return rc;
   FinishArgs f{};
   f.part_s = a.part_s;
