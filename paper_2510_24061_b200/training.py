@@ -56,6 +56,25 @@ PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "ipo": 2}
 _DTYPES = {torch.bfloat16: fq.BF16, torch.float32: fq.F32}
 
 
+def _new(*shape: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """An uninitialised contiguous tensor on the current device.  The four outputs of a one-row norm take 5.8 us by torch.empty and
+    torch.empty_like, of 17 us for the whole call, and 3.8 us by the allocator entry that torch's generated code uses, where torch has
+    it: it skips the parsing of a device and its guard."""
+    if _empty_cuda is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    stride = (shape[1], 1) if len(shape) == 2 else (1,) * len(shape)
+    return _empty_cuda(shape, stride, dtype)
+
+
+def _new_checkpoint(x: torch.Tensor) -> "Checkpoint":
+    rows, cols = x.shape
+    return Checkpoint(_new(rows, cols, dtype=torch.uint8, device=x.device),
+                      _new(rows, (cols + CHECKPOINT_BLOCK - 1) // CHECKPOINT_BLOCK, dtype=torch.uint8, device=x.device))
+
+
+_empty_cuda = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+
+
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
@@ -125,9 +144,10 @@ def _checkpoint(ck: Checkpoint, shape, name: str):
 def checkpoint_save(x: torch.Tensor, out: Optional[Checkpoint] = None) -> Checkpoint:
     """falqon_checkpoint_save: x [rows, cols] in 8 bits."""
     _matrix(x, "x")
-    out = Checkpoint.empty(*x.shape, x.device) if out is None else out
+    stream = _on_device(x)
+    out = _new_checkpoint(x) if out is None else out
     _checkpoint(out, x.shape, "out")
-    stream = _on_device(x, *out)
+    _on_device(*out)
     fq._check("falqon_checkpoint_save", lib.falqon_checkpoint_save(x.data_ptr(), _dtype(x), *x.shape, out.codes.data_ptr(),
                                                                     out.scales.data_ptr(), stream))
     return out
@@ -155,11 +175,11 @@ def gate_forward(g: torch.Tensor, u: torch.Tensor, save: bool = True, z: Optiona
     _like(z, g, "z")
     _vector(amax, 1, torch.float32, "amax")
     stream = _on_device(g, u, z, amax)
-    z = torch.empty_like(g) if z is None else z
+    z = _new(*g.shape, dtype=g.dtype, device=g.device) if z is None else z
     kg = ku = None
     ptrs = (None,) * 4
     if save:
-        kg, ku = Checkpoint.empty(*g.shape, g.device), Checkpoint.empty(*g.shape, g.device)
+        kg, ku = _new_checkpoint(g), _new_checkpoint(g)
         ptrs = (kg.codes.data_ptr(), kg.scales.data_ptr(), ku.codes.data_ptr(), ku.scales.data_ptr())
     fq._check("falqon_gate_forward", lib.falqon_gate_forward(g.data_ptr(), u.data_ptr(), _dtype(g), *g.shape, z.data_ptr(), *ptrs,
                                                               _ptr(amax), stream))
@@ -178,8 +198,8 @@ def gate_backward(g: Checkpoint, u: Checkpoint, dz: torch.Tensor, dg: Optional[t
     _vector(amax_dg, 1, torch.float32, "amax_dg")
     _vector(amax_du, 1, torch.float32, "amax_du")
     stream = _on_device(*g, *u, dz, dg, du, amax_dg, amax_du)
-    dg = torch.empty_like(dz) if dg is None else dg
-    du = torch.empty_like(dz) if du is None else du
+    dg = _new(*dz.shape, dtype=dz.dtype, device=dz.device) if dg is None else dg
+    du = _new(*dz.shape, dtype=dz.dtype, device=dz.device) if du is None else du
     fq._check("falqon_gate_backward",
               lib.falqon_gate_backward(g.codes.data_ptr(), g.scales.data_ptr(), u.codes.data_ptr(), u.scales.data_ptr(), dz.data_ptr(),
                                        _dtype(dz), *dz.shape, dg.data_ptr(), du.data_ptr(), _ptr(amax_dg), _ptr(amax_du), stream))
@@ -243,12 +263,13 @@ def block_norm_forward(h: Optional[torch.Tensor], y: torch.Tensor, *, post: bool
     rows, cols = y.shape
     plan = _norm_plan(rows, cols, _dtype(y), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
     stream = _on_device(h, y, h_out, x, amax_x, post_gain, pre_gain, gate)
-    h_out = torch.empty_like(y) if h_out is None else h_out
-    x = torch.empty_like(y) if x is None and pre else x
-    inv_post = torch.empty(rows, dtype=torch.float32, device=y.device) if post else None
-    inv_pre = torch.empty(rows, dtype=torch.float32, device=y.device) if pre else None
-    kh = Checkpoint.empty(rows, cols, y.device) if save and h is not None else None
-    ky = Checkpoint.empty(rows, cols, y.device) if save else None
+    dtype, dev = y.dtype, y.device
+    h_out = _new(rows, cols, dtype=dtype, device=dev) if h_out is None else h_out
+    x = _new(rows, cols, dtype=dtype, device=dev) if x is None and pre else x
+    inv_post = _new(rows, dtype=torch.float32, device=dev) if post else None
+    inv_pre = _new(rows, dtype=torch.float32, device=dev) if pre else None
+    kh = _new_checkpoint(y) if save and h is not None else None
+    ky = _new_checkpoint(y) if save else None
     fq._check("falqon_block_norm_forward",
               lib.falqon_block_norm_forward(C.byref(plan), _ptr(h), y.data_ptr(), h_out.data_ptr(), _ptr(x), _ptr(inv_post), _ptr(inv_pre),
                                             *((None, None) if kh is None else (kh.codes.data_ptr(), kh.scales.data_ptr())),
@@ -299,19 +320,19 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
     if amax_dy is not None:
         _vector(amax_dy, 1, torch.float32, "amax_dy")
     plan = _norm_plan(rows, cols, _dtype(ref), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
-    dev = ref.device
-    dh = torch.empty_like(ref) if dh is None and h is not None else dh
-    dy = torch.empty_like(ref) if dy is None else dy
-    dpost = torch.empty(cols, dtype=torch.float32, device=dev) if need_gains and post_gain is not None else None
-    dpre = torch.empty(cols, dtype=torch.float32, device=dev) if need_gains and pre_gain is not None else None
-    dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev) if need_gains and gate is not None else None
+    stream = _on_device(dx, dh_out, inv_post, inv_pre, post_gain, pre_gain, gate, dh, dy, scratch, amax_dy, *kept)
+    dev, dtype, f32 = ref.device, ref.dtype, torch.float32
+    dh = _new(rows, cols, dtype=dtype, device=dev) if dh is None and h is not None else dh
+    dy = _new(rows, cols, dtype=dtype, device=dev) if dy is None else dy
+    dpost = _new(cols, dtype=f32, device=dev) if need_gains and post_gain is not None else None
+    dpre = _new(cols, dtype=f32, device=dev) if need_gains and pre_gain is not None else None
+    dgate = torch.empty(gate.shape, dtype=f32, device=dev) if need_gains and gate is not None else None
     size = 0
     if dpost is not None or dpre is not None or dgate is not None:
         size = lib.falqon_block_norm_scratch_bytes(C.byref(plan))
         if scratch is None:
-            scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+            scratch = _new(size, dtype=torch.uint8, device=dev)
         size = scratch.numel() * scratch.element_size()
-    stream = _on_device(dx, dh_out, inv_post, inv_pre, post_gain, pre_gain, gate, dh, dy, scratch, amax_dy, *kept)
     fq._check("falqon_block_norm_backward",
               lib.falqon_block_norm_backward(C.byref(plan), _ptr(dx), _ptr(dh_out), *saved, _ptr(inv_post), _ptr(inv_pre), _ptr(dh), dy.data_ptr(),
                                              _ptr(dpost), _ptr(dpre), _ptr(dgate), _ptr(amax_dy), _ptr(scratch), size, stream))
@@ -362,7 +383,7 @@ def _scratch(logits: torch.Tensor, scratch: Optional[torch.Tensor]) -> torch.Ten
     size = lib.falqon_preference_scratch_bytes(logits.shape[0], logits.shape[1], _dtype(logits))
     if size == 0:
         raise fq.FalqonError("falqon_preference_scratch_bytes", fq.ERR_INVALID_ARG)
-    return torch.empty(size, dtype=torch.uint8, device=logits.device)
+    return _new(size, dtype=torch.uint8, device=logits.device)
 
 
 def sequence_logprob(logits: torch.Tensor, targets: torch.Tensor, cu_rows: torch.Tensor, average: bool = False,
@@ -374,10 +395,9 @@ def sequence_logprob(logits: torch.Tensor, targets: torch.Tensor, cu_rows: torch
     _need(n >= 1, "cu_rows must hold at least two entries")
     _vector(targets, rows, torch.int64, "targets")
     _vector(cu_rows, n + 1, torch.int64, "cu_rows")
-    scratch = _scratch(logits, scratch)
     stream = _on_device(logits, targets, cu_rows, scratch)
-    logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    seq = torch.empty(n, dtype=torch.float32, device=logits.device)
+    scratch = _scratch(logits, scratch)
+    logp, seq = _new(rows, dtype=torch.float32, device=logits.device), _new(n, dtype=torch.float32, device=logits.device)
     fq._check("falqon_sequence_logprob",
               lib.falqon_sequence_logprob(logits.data_ptr(), _dtype(logits), rows, logits.shape[1], _pitch(logits), targets.data_ptr(),
                                           cu_rows.data_ptr(), n, int(average), logp.data_ptr(), seq.data_ptr(), scratch.data_ptr(),
@@ -397,12 +417,11 @@ def preference_forward(spec: PreferenceLoss, logits: torch.Tensor, targets: torc
     _vector(cu_rows, n + 1, torch.int64, "cu_rows")
     _vector(ref_logp, n, torch.float32, "ref_logp")
     plan = _preference(spec, logits, n // 2)
-    scratch = _scratch(logits, scratch)
     stream = _on_device(logits, targets, cu_rows, ref_logp, scratch)
-    f32, dev, empty = torch.float32, logits.device, torch.empty
-    loss, pair_loss = empty((), dtype=f32, device=dev), empty(n // 2, dtype=f32, device=dev)
-    seq, logp = empty(n, dtype=f32, device=dev), empty(rows, dtype=f32, device=dev)
-    stats, dlogp = (torch.empty_strided((rows, 2), (2, 1), dtype=f32, device=dev), empty(rows, dtype=f32, device=dev)) if need_grad else (None, None)
+    scratch = _scratch(logits, scratch)
+    f32, dev = torch.float32, logits.device
+    loss, pair_loss, seq, logp = (_new(*shape, dtype=f32, device=dev) for shape in ((), (n // 2,), (n,), (rows,)))
+    stats, dlogp = (_new(rows, 2, dtype=f32, device=dev), _new(rows, dtype=f32, device=dev)) if need_grad else (None, None)
     fq._check("falqon_preference_forward",
               lib.falqon_preference_forward(C.byref(plan), logits.data_ptr(), targets.data_ptr(), cu_rows.data_ptr(), _ptr(ref_logp),
                                             loss.data_ptr(), pair_loss.data_ptr(), seq.data_ptr(), logp.data_ptr(), _ptr(stats), _ptr(dlogp),
@@ -415,18 +434,18 @@ def preference_backward(logits: torch.Tensor, targets: torch.Tensor, out: Prefer
     """falqon_preference_backward: d loss / d logits times dloss (fp32 [1] on the device; None: 1).  dlogits may be logits itself."""
     _logits_ok(logits, "logits")
     _need(out.row_stats is not None, "the forward was called without need_grad")
+    stream = _on_device(logits, targets, out.row_stats, out.dlogp, dloss, dlogits, amax)
     _vector(targets, logits.shape[0], torch.int64, "targets")
     _vector(out.dlogp, logits.shape[0], torch.float32, "out.dlogp")
     _vector(out.row_stats, 2 * logits.shape[0], torch.float32, "out.row_stats")
     _vector(dloss, 1, torch.float32, "dloss")
     _vector(amax, 1, torch.float32, "amax")
     if dlogits is None:
-        dlogits = torch.empty_strided(logits.shape, (logits.shape[1], 1), dtype=logits.dtype, device=logits.device)
+        dlogits = _new(*logits.shape, dtype=logits.dtype, device=logits.device)
     else:
         _logits_ok(dlogits, "dlogits")
         _need(dlogits.shape == logits.shape and dlogits.dtype == logits.dtype, "dlogits must be like logits")
     plan = _preference(out.spec, logits, out.pair_loss.numel())
-    stream = _on_device(logits, targets, out.row_stats, out.dlogp, dloss, dlogits, amax)
     fq._check("falqon_preference_backward",
               lib.falqon_preference_backward(C.byref(plan), logits.data_ptr(), targets.data_ptr(), out.row_stats.data_ptr(),
                                              out.dlogp.data_ptr(), _ptr(dloss), dlogits.data_ptr(), _pitch(dlogits), _ptr(amax), stream))
