@@ -26,7 +26,8 @@ struct NormArgs {
   float *inv_post, *inv_pre;                 // written by the forward, read by the backward
   float *amax;
   float *part_s, *part_p;                    // [units][cols] each, nullable: column sums S and dwpre
-  int64_t rows, cols, rows_per_gate, pieces, rows_per_piece;
+  int64_t rows, cols, rows_per_gate, rows_per_piece;
+  int units, pieces;                         // all units; those of a gate group
   float res_scale, gain_offset, eps, inv_cols;
   int post, pre, gain_f32;
 };
@@ -37,6 +38,17 @@ __device__ __forceinline__ float gain_at(const void* p, int64_t i, int f32) {
 __device__ __forceinline__ float weight_at(const void* p, int64_t i, const NormArgs& a) {
   return p == nullptr ? 1.0f : a.gain_offset + gain_at(p, i, a.gain_f32);
 }
+
+// The rows of a unit, which is a run of the rows of one gate group (32-bit division: a 64-bit one is a hundred instructions).
+struct Unit {
+  int gate, first, last;                                       // rows < 2^31
+  __device__ __forceinline__ Unit(const NormArgs& a, int unit) {
+    gate = unit / a.pieces;
+    const int64_t begin = gate * a.rows_per_gate + (unit - gate * a.pieces) * a.rows_per_piece;
+    first = static_cast<int>(min(begin, a.rows));
+    last = static_cast<int>(min(min(begin + a.rows_per_piece, (gate + 1) * a.rows_per_gate), a.rows));
+  }
+};
 
 // Sums over the CTA (whole warps); every thread gets them.  `red`: 32 * kN floats; `phase` alternates so that one barrier per
 // call is enough (2 buffers).
@@ -146,14 +158,12 @@ __global__ void __launch_bounds__(1024, 1) norm_backward_kernel(const NormArgs a
   int phase = 0;
   uint32_t mx = 0;
   const int64_t blocks_per_row = (a.cols + kMx8Block - 1) / kMx8Block;
-  const int64_t groups = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
   float P[kItems];
 #pragma unroll
   for (int i = 0; i < kItems; ++i) P[i] = 0.0f;
-  for (int64_t unit = blockIdx.x; unit < groups * a.pieces; unit += gridDim.x) {
-    const int64_t group = unit / a.pieces;
-    const int64_t first = group * a.rows_per_gate + (unit - group * a.pieces) * a.rows_per_piece;
-    const int64_t last = min(min(first + a.rows_per_piece, (group + 1) * a.rows_per_gate), a.rows);
+  for (int64_t unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
+    const Unit u(a, static_cast<int>(unit));
+    const int64_t group = u.gate, first = u.first, last = u.last;
     float S[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) S[i] = 0.0f;
@@ -367,7 +377,7 @@ __device__ __forceinline__ void put_codes8(const f2 (&x)[4], uint8_t* codes, uin
   if ((lane & 3) == 0) *scale = static_cast<uint8_t>(e8);
 }
 
-// What a thread knows of its place, and the rows of a unit: unit = (gate group, run of its rows).
+// What a thread knows of its place.
 struct Seat {
   int lane, group, warp, warps;
   __device__ __forceinline__ explicit Seat(const Shape& sh) {
@@ -380,16 +390,6 @@ struct Seat {
   template <int kNv>
   __device__ __forceinline__ int column() const { return warp * kNv * 256 + lane * 8; }   // its first; span i is 256 * i further
 };
-struct Unit {
-  int gate, first, last;                                       // rows < 2^31
-  __device__ __forceinline__ Unit(const NormArgs& a, int64_t unit) {
-    gate = static_cast<int>(unit / a.pieces);
-    const int64_t begin = gate * a.rows_per_gate + (unit - gate * a.pieces) * a.rows_per_piece;
-    first = static_cast<int>(min(begin, a.rows));
-    last = static_cast<int>(min(min(begin + a.rows_per_piece, (gate + 1) * a.rows_per_gate), a.rows));
-  }
-};
-
 template <typename T, int kNv>
 __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kernel(const NormArgs a, const Shape sh) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
   float* red = tail + me.group * kSumFloats;
   float* wsm = tail + sh.groups * kSumFloats;
   constexpr int kSpan = 256 * sizeof(T);                       // bytes of a span; a stage holds [span][y, h]
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const int units = a.units;
   const f2 inv_cols = twice(a.inv_cols), res_scale = twice(a.res_scale);
   int phase = 0;
   Largest<T> largest;
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kerne
   clear_sums(tail, sh.groups * kSumFloats);
   float* red = tail + me.group * kSumFloats;
   float* wsm = tail + groups * kSumFloats;
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const int units = a.units;
   const int64_t step = static_cast<int64_t>(groups) * cols;
   const int lane_shift = sizeof(T) == 2 ? 0 : -4 * lane;       // from a lane's first column to what it copies
   int phase = 0;
@@ -701,7 +701,7 @@ __global__ void __launch_bounds__(512) norm_forward_loose_kernel(const NormArgs 
   float* red = tail + me.group * kSumFloats;
   float* wsm = tail + sh.groups * kSumFloats;
   constexpr int kSpan = 256 * sizeof(T) + 16;                  // bytes of a span and what comes along; a stage holds [span][y, h]
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const int units = a.units;
   const f2 inv_cols = twice(a.inv_cols);
   int phase = 0;
   uint32_t mx = 0;
@@ -938,7 +938,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
   const bool post = kFull || a.post, pre = kFull || a.pre, want_dh = kFull || a.dh != nullptr, want_dy = kFull || a.dy != nullptr;
   const bool has_h = kFull || (kCoded ? a.h_codes_in != nullptr : a.h != nullptr), has_dx = kFull || a.dx != nullptr, has_g = kFull || a.dh_out != nullptr;
   const int stripe = (warp % sh.stripe_warps) * kNv, member = warp / sh.stripe_warps;
-  const int64_t units = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate * a.pieces;
+  const int units = a.units;
   const int half = sh.run * sh.blocks_per_row;                 // scale bytes of one tensor's run
   const int lane_col = kLoose ? 0 : lane * 8;                  // of a span: the lane's first column, or where all lanes begin
   uint32_t mx = 0;
@@ -1202,35 +1202,38 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
 }
 
 // The gradients of gains and gate from the partial column sums.  A CTA takes 32 columns (a row of them is eight lanes of four), a warp
-// four partial rows at a time; a team of warps shares a gate group's rows, so that few groups use all warps too.  All loads of a
-// sum are in flight at once and every addition has its place: the order never changes.
+// four partial rows at a time; a team of warps shares a gate group's rows, so that few groups use all warps too.  The loads of both
+// sums, and of the next groups', are in flight before the first addition, and every addition has its place: the order never changes.
 constexpr int kFinishWarps = 16;
 struct FinishArgs {
   const float *part_s, *part_p;
   const void *post_gain, *gate;
   float *dpost_gain, *dpre_gain, *dgate;
-  int64_t cols, groups, pieces, ctas;
+  int64_t cols;
+  int groups, pieces, ctas;      // of part_s: groups * pieces rows; of part_p: a row per CTA
   float gain_offset;
-  int post, gain_f32, team;      // team: warps to a group, a power of two
+  int post, gain_f32, team, batches;   // team: warps to a group, a power of two; batches: of as many groups as there are teams
 };
 __device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ float4 shfl4(float4 a, int o) {
   constexpr uint32_t all = 0xFFFFFFFFu;
   return make_float4(__shfl_xor_sync(all, a.x, o), __shfl_xor_sync(all, a.y, o), __shfl_xor_sync(all, a.z, o), __shfl_xor_sync(all, a.w, o));
 }
-// Rows from, from + 4 * team, .. of n (a lane's row is from + lane / 8), four columns; kVec: columns are a multiple of four.
+// The sum of rows from, from + stride, .. of n (a lane's row is that of its eighth of the warp), of four columns from c on.
+// kVec: the columns are a multiple of four.
 template <bool kVec>
-__device__ __forceinline__ float4 partial_sum(const float* p, int64_t from, int64_t n, int64_t stride, int64_t cols, int64_t c) {
-  constexpr int kAhead = 4;
-  float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int64_t r = from; r < n; r += kAhead * stride) {
-    float4 v[kAhead];
+struct PartialSum {
+  static constexpr int kAhead = 4;
+  const float* p;
+  int row, n, stride;
+  float4 v[kAhead];
+  __device__ __forceinline__ void fetch(int64_t cols, int64_t c) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const int64_t row = r + j * stride;
-      if (row >= n || c >= cols) continue;
-      const float* q = p + row * cols + c;
+      const int at = row + j * stride;
+      if (at >= n || c >= cols) continue;
+      const float* q = p + at * cols + c;
       if (kVec) {
         v[j] = ld_stream(reinterpret_cast<const float4*>(q));
       } else {
@@ -1240,58 +1243,76 @@ __device__ __forceinline__ float4 partial_sum(const float* p, int64_t from, int6
         if (c + 3 < cols) v[j].w = ld_stream(q + 3);
       }
     }
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) t = add4(t, v[j]);
   }
-  t = add4(t, shfl4(t, 8));
-  return add4(t, shfl4(t, 16));
-}
+  __device__ __forceinline__ void start(const float* from, int first, int rows, int step, int64_t cols, int64_t c) {
+    p = from;
+    row = first;
+    n = rows;
+    stride = step;
+    fetch(cols, c);
+  }
+  __device__ __forceinline__ float4 finish(int64_t cols, int64_t c) {
+    float4 t = add4(add4(v[0], v[1]), add4(v[2], v[3]));
+    for (row += kAhead * stride; row < n; row += kAhead * stride) {
+      fetch(cols, c);
+      t = add4(t, add4(add4(v[0], v[1]), add4(v[2], v[3])));
+    }
+    t = add4(t, shfl4(t, 8));
+    return add4(t, shfl4(t, 16));
+  }
+};
 template <bool kVec>
 __global__ void __launch_bounds__(32 * kFinishWarps) norm_finish_kernel(const FinishArgs a) {
   __shared__ float4 red_s[kFinishWarps][8], red_p[kFinishWarps][8];
   pdl_trigger();
-  pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, column = threadIdx.x & 31;
-  const int64_t c4 = static_cast<int64_t>(blockIdx.x) * 32 + (lane & 7) * 4, c = static_cast<int64_t>(blockIdx.x) * 32 + column;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t c4 = static_cast<int64_t>(blockIdx.x) * 32 + (lane & 7) * 4, c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
   const int teams = kFinishWarps / a.team, team = warp / a.team, member = warp % a.team;
-  if (a.part_p != nullptr) {
-    const float4 t = partial_sum<kVec>(a.part_p, warp * 4 + (lane >> 3), a.ctas, 4 * kFinishWarps, a.cols, c4);
-    if (lane < 8) red_p[warp][lane] = t;
-  }
+  pdl_wait();
+  PartialSum<kVec> sp, ss;
+  if (a.part_p != nullptr) sp.start(a.part_p, warp * 4 + (lane >> 3), a.ctas, 4 * kFinishWarps, a.cols, c4);
+  const auto start_group = [&](int g) {
+    if (g < a.groups)
+      ss.start(a.part_s + static_cast<int64_t>(g) * a.pieces * a.cols, member * 4 + (lane >> 3), a.pieces, 4 * a.team, a.cols, c4);
+  };
+  if (a.batches > 0) start_group(team);
   const bool in = c < a.cols;
   const float wpost = in && a.post && a.post_gain != nullptr ? a.gain_offset + gain_at(a.post_gain, c, a.gain_f32) : 1.0f;
   float dpost = 0.0f;                                          // of the warp's groups: warp w adds up groups w, w + teams, ..
-  const int64_t batches = a.part_s != nullptr ? (a.groups + teams - 1) / teams : 0;
-  for (int64_t batch = 0; batch < batches; ++batch) {
-    const int64_t g = batch * teams + team;
+  if (a.part_p != nullptr) {
+    const float4 t = sp.finish(a.cols, c4);
+    if (lane < 8) red_p[warp][lane] = t;
+  }
+  for (int batch = 0; batch < a.batches; ++batch) {
+    const int g = batch * teams + team, mine = batch * teams + warp;   // warp w < teams finishes team w's group
+    const bool ends = warp < teams && mine < a.groups && in;
+    const float gate = ends && a.gate != nullptr ? gain_at(a.gate, mine * a.cols + c, a.gain_f32) : 1.0f;
     if (g < a.groups) {
-      const float4 t = partial_sum<kVec>(a.part_s + g * a.pieces * a.cols, member * 4 + (lane >> 3), a.pieces, 4 * a.team, a.cols, c4);
+      const float4 t = ss.finish(a.cols, c4);
       if (lane < 8) red_s[warp][lane] = t;
+      start_group(g + teams);
     }
     if (a.team > 1) __syncthreads(); else __syncwarp();
-    const int64_t mine = batch * teams + warp;                 // warp w < teams finishes team w's group
-    if (warp < teams && mine < a.groups && in) {
+    if (ends) {
       float s = 0.0f;
-      for (int m = 0; m < a.team; ++m) s += reinterpret_cast<const float*>(red_s[warp * a.team + m])[column];
+      for (int m = 0; m < a.team; ++m) s += reinterpret_cast<const float*>(red_s[warp * a.team + m])[lane];
       if (a.dgate != nullptr) a.dgate[mine * a.cols + c] = wpost * s;
-      dpost = __fmaf_rn(a.gate != nullptr ? gain_at(a.gate, mine * a.cols + c, a.gain_f32) : 1.0f, s, dpost);
+      dpost = __fmaf_rn(gate, s, dpost);
     }
     if (a.team > 1) __syncthreads(); else __syncwarp();
   }
+  reinterpret_cast<float*>(red_s[warp])[lane] = dpost;         // the warp's own place in every batch, or that of a member it has read
   __syncthreads();
-  if (warp == 0 && in && a.dpre_gain != nullptr) {
+  if (warp == 0 && in && a.dpost_gain != nullptr) {
+    float s = 0.0f;
+    for (int w = 0; w < teams; ++w) s += reinterpret_cast<const float*>(red_s[w])[lane];
+    a.dpost_gain[c] = s;
+  }
+  if (warp == 1 && in && a.dpre_gain != nullptr) {
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kFinishWarps; ++w) s += reinterpret_cast<const float*>(red_p[w])[column];
+    for (int w = 0; w < kFinishWarps; ++w) s += reinterpret_cast<const float*>(red_p[w])[lane];
     a.dpre_gain[c] = s;
-  }
-  if (a.dpost_gain == nullptr) return;
-  reinterpret_cast<float*>(red_s[warp])[column] = dpost;
-  __syncthreads();
-  if (warp == 0 && in) {
-    float s = 0.0f;
-    for (int w = 0; w < teams; ++w) s += reinterpret_cast<const float*>(red_s[w])[column];
-    a.dpost_gain[c] = s;
   }
 }
 
@@ -1320,7 +1341,8 @@ struct Split {
   }
   void put(NormArgs* a) const {
     a->rows_per_gate = rows_per_gate;
-    a->pieces = pieces;
+    a->units = static_cast<int>(units);
+    a->pieces = static_cast<int>(pieces);
     a->rows_per_piece = rows_per_piece;
   }
 };
@@ -1346,7 +1368,6 @@ NormArgs common(const falqon_block_norm* p) {
 
 unsigned item_threads(int64_t cols) { return static_cast<unsigned>(((cols + kItems - 1) / kItems + 31) / 32 * 32); }
 
-// The staged kernels' shape.  set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
 constexpr int kSmemLimit = 226 * 1024;    // dynamic; the kernels have a few bytes of their own besides
 int spans_for(int64_t cols) { return cols <= 2 * 512 * 8 ? 2 : 4; }
 // set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
@@ -1592,13 +1613,14 @@ int falqon_block_norm_backward(const falqon_block_norm* p, const void* dx, const
   f.dpre_gain = dpre_gain;
   f.dgate = dgate;
   f.cols = a.cols;
-  f.groups = s.groups;
-  f.pieces = s.pieces;
-  f.ctas = s.ctas;
+  f.groups = static_cast<int>(s.groups);
+  f.pieces = static_cast<int>(s.pieces);
+  f.ctas = static_cast<int>(s.ctas);
   f.gain_offset = a.gain_offset;
   f.post = a.post;
   f.gain_f32 = a.gain_f32;
   for (f.team = kFinishWarps; f.team > 1 && f.team * s.groups > kFinishWarps;) f.team /= 2;
+  f.batches = sums_s ? (f.groups + kFinishWarps / f.team - 1) / (kFinishWarps / f.team) : 0;
   return finish(launch_pdl(a.cols % 4 == 0 ? norm_finish_kernel<true> : norm_finish_kernel<false>, dim3(static_cast<unsigned>((a.cols + 31) / 32)),
                            dim3(32 * kFinishWarps), 0, st, 1, f));
 }

@@ -116,18 +116,37 @@ struct Running {
     raise(om);
     s += os * exp_of(om - base());
   }
+  // Those of a warp's lanes together: every sum brought to the largest maximum once, then added.
+  __device__ __forceinline__ void join_warp() {
+    float top;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(top) : "f"(m));
+    const float own = m;
+    m = top;
+    s *= exp_of(own - base());
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  }
+};
+
+// The vectors of a part, blockIdx.y: `chunk` of them, the last part's to the row's end.
+struct Part {
+  int64_t begin, end;
+  __device__ __forceinline__ Part(const Span& sp, int64_t chunk) {
+    begin = static_cast<int64_t>(blockIdx.y) * chunk;
+    end = blockIdx.y == gridDim.y - 1 ? sp.body : min(begin + chunk, sp.body);
+  }
 };
 
 // kTeam threads to a row or a part of one: a CTA, or a warp where rows are short (then parts == 1).
 template <typename T, int kTeam>
 __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(int64_t rows, const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
-                                                                int parts, float2* out, float* target_logit, unsigned int* counter, int* status) {
+                                                                int64_t chunk, float2* out, float* target_logit, unsigned int* counter, int* status) {
   __shared__ float red_m[kRowThreads / 32], red_s[kRowThreads / 32];
   pdl_trigger();
   pdl_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0u;   // for the kernel after this one
-  const int64_t team = static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam, row = team / parts;
-  const int part = static_cast<int>(team - row * parts), tid = threadIdx.x % kTeam;
+  const int part = blockIdx.y, parts = gridDim.y, tid = threadIdx.x % kTeam;
+  if (blockIdx.x == 0 && part == 0 && threadIdx.x == 0) *counter = 0u;   // for the kernel after this one
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam;
   if (kTeam < kRowThreads && row >= rows) return;
   const int64_t target = ld_stream(targets + row);
   if (target < 0 || target >= vocab) {
@@ -143,7 +162,7 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(int64_t rows, co
   const Span sp = span_of(p, vocab);
   Running r;
   const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
-  const int64_t begin = sp.body * part / parts, end = sp.body * (part + 1) / parts;
+  const auto [begin, end] = Part(sp, chunk);
   f2 sum = 0;                              // the running sum, two halves of it
   constexpr int kUnroll = 4;
   constexpr uint32_t kNone = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;   // -inf: adds nothing
@@ -176,21 +195,20 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(int64_t rows, co
     if (tid < sp.head) r.add(load1(p + tid));
     if (tid < vocab - sp.tail) r.add(load1(p + sp.tail + tid));
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float om = __shfl_xor_sync(0xFFFFFFFFu, r.m, o), os = __shfl_xor_sync(0xFFFFFFFFu, r.s, o);
-    r.join(om, os);
-  }
+  r.join_warp();
   if (kTeam > 32) {
     if ((tid & 31) == 0) {
       red_m[tid >> 5] = r.m;
       red_s[tid >> 5] = r.s;
     }
     __syncthreads();
+    if (tid >= 32) return;
+    const bool one = tid < kTeam / 32;
+    r.m = one ? red_m[tid] : -INFINITY;
+    r.s = one ? red_s[tid] : 0.0f;
+    r.join_warp();
   }
   if (tid == 0) {
-#pragma unroll
-    for (int w = 1; w < kTeam / 32; ++w) r.join(red_m[w], red_s[w]);
     out[row * parts + part] = make_float2(r.m, r.s);
     if (part == 0) target_logit[row] = at_target;
   }
@@ -390,21 +408,21 @@ __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) 
 // kSame: logits and dlogits rows have the same offset from a 16-byte boundary, so vectors can be stored; else single values are.
 template <typename T, bool kSame, int kTeam>
 __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(int64_t rows, const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
-                                                                 int parts, const float2* stats, const float* dlogp, const float* dloss,
+                                                                 int64_t chunk, const float2* stats, const float* dlogp, const float* dloss,
                                                                  T* out, int64_t ld_out, float* amax) {
   pdl_trigger();
   pdl_wait();
   constexpr int n = Row<T>::kN;
   // the last rows first: of what the forward has read, they are still in L2
-  const int64_t task = rows * parts - 1 - (static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam), row = task / parts;
-  const int part = static_cast<int>(task - row * parts), tid = threadIdx.x % kTeam;
+  const int64_t row = rows - 1 - (static_cast<int64_t>(blockIdx.x) * (kRowThreads / kTeam) + threadIdx.x / kTeam);
+  const int tid = threadIdx.x % kTeam;
   uint32_t mx = 0;
-  if (task >= 0) {
+  if (row >= 0) {
     const float c = ld_stream(dlogp + row) * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
     const T* p = logits + row * ld;
     T* o = out + row * ld_out;
     const Span sp = span_of(p, vocab);
-    const int64_t begin = sp.body * part / parts, end = sp.body * (part + 1) / parts;
+    const auto [begin, end] = Part(sp, chunk);
     const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
     const bool zero = c == 0.0f;
     const float2 st = zero ? make_float2(0.0f, 1.0f) : ld_stream(stats + row);
@@ -466,7 +484,7 @@ __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(int64_t rows, c
       for (int j = 0; j < kUnroll; ++j) put(v + j * kTeam, q[j]);
     }
     for (; v < end; v += kTeam) put(v, zero ? make_uint4(0u, 0u, 0u, 0u) : ld_stream(body + v));
-    if (part == 0) {
+    if (blockIdx.y == 0) {
       if (tid < sp.head) one(tid);
       if (tid < vocab - sp.tail) one(sp.tail + tid);
     }
@@ -493,6 +511,9 @@ int parts_for(int64_t rows, int64_t vocab, int dtype) {
   return static_cast<int>(parts < 1 ? 1 : parts);
 }
 
+// Vectors of a part, of a row that begins on a 16-byte boundary; the others' have one less at the most.
+int64_t chunk_for(int64_t vocab, int dtype, int parts) { return (vocab / (dtype == FALQON_BF16 ? 8 : 4) + parts - 1) / parts; }
+
 // A thread per row of the average sequence (or pair), a warp at least.
 unsigned sequence_threads(int64_t rows, int64_t ctas) {
   const int64_t t = (rows / ctas + 31) / 32 * 32;            // (a pair's rows vary: a thread takes several where they are more)
@@ -506,9 +527,9 @@ bool by_warps(int64_t vocab, int dtype, int parts) { return parts == 1 && vocab 
 template <typename T>
 cudaError_t launch_row_stats(const void* logits, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts, bool warps, float2* out,
                              float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
-  const int64_t per = warps ? kRowThreads / 32 : 1;
-  return launch_pdl(warps ? row_stats_kernel<T, 32> : row_stats_kernel<T, kRowThreads>, dim3(static_cast<unsigned>((rows * parts + per - 1) / per)),
-                    dim3(kRowThreads), 0, stream, 1, rows, static_cast<const T*>(logits), vocab, ld, targets, parts, out, target_logit, counter, status);
+  const int64_t per = warps ? kRowThreads / 32 : 1, chunk = chunk_for(vocab, sizeof(T) == 2 ? FALQON_BF16 : FALQON_F32, parts);
+  return launch_pdl(warps ? row_stats_kernel<T, 32> : row_stats_kernel<T, kRowThreads>, dim3(static_cast<unsigned>((rows + per - 1) / per), parts),
+                    dim3(kRowThreads), 0, stream, 1, rows, static_cast<const T*>(logits), vocab, ld, targets, chunk, out, target_logit, counter, status);
 }
 cudaError_t launch_row_stats(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts,
                              float2* out, float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
@@ -618,12 +639,12 @@ int falqon_preference_backward(const falqon_preference* p, const void* logits, c
   const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 &&
                     (ld_out - p->ld) % (p->dtype == FALQON_BF16 ? 8 : 4) == 0;
   const bool warps = by_warps(p->vocab, p->dtype, parts);
-  const int64_t per = warps ? kRowThreads / 32 : 1;
+  const int64_t per = warps ? kRowThreads / 32 : 1, chunk = chunk_for(p->vocab, p->dtype, parts);
   const float2* stats = reinterpret_cast<const float2*>(row_stats);
   const auto go = [&](auto kernel, auto* typed) {
     using T = std::remove_pointer_t<decltype(typed)>;
-    return finish(launch_pdl(kernel, dim3(static_cast<unsigned>((p->rows * parts + per - 1) / per)), dim3(kRowThreads), 0, st, 1, p->rows,
-                             static_cast<const T*>(logits), p->vocab, p->ld, targets, parts, stats, dlogp, dloss, typed, ld_out, amax_out));
+    return finish(launch_pdl(kernel, dim3(static_cast<unsigned>((p->rows + per - 1) / per), parts), dim3(kRowThreads), 0, st, 1, p->rows,
+                             static_cast<const T*>(logits), p->vocab, p->ld, targets, chunk, stats, dlogp, dloss, typed, ld_out, amax_out));
   };
   const auto pick = [&](auto* typed) {
     using T = std::remove_pointer_t<decltype(typed)>;
