@@ -651,11 +651,19 @@ __device__ __forceinline__ void put_single_codes(const f2 (&x)[4], int left, int
   float v[8];
 #pragma unroll
   for (int k = 0; k < 4; ++k) unpack_f32x2(x[k], v[2 * k], v[2 * k + 1]);
+  uint32_t top = 0u;                                           // of block `lane`: lane e works out the scale of block e for all
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t e8 = mx8_exponent(__reduce_max_sync(0xFFFFFFFFu, abs_bits(v[e])));
-    if (e * 32 + lane < left) codes[e * 32 + lane] = mx8_encode1(v[e], mx8_encode_factor(e8));
-    if (lane == 0 && e * 32 < left) scales[e] = static_cast<uint8_t>(e8);
+    const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, abs_bits(v[e]));
+    if (lane == e) top = m;
+  }
+  const uint32_t e8 = mx8_exponent(top);
+  const float factor = mx8_encode_factor(e8);
+  if (lane < 8 && lane * 32 < left) scales[lane] = static_cast<uint8_t>(e8);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float f = __shfl_sync(0xFFFFFFFFu, factor, e);
+    if (e * 32 + lane < left) codes[e * 32 + lane] = mx8_encode1(v[e], f);
   }
 }
 // The 16-byte pieces that cover the 256 values from `at` on, of a tensor of `total` values; returns nothing: the first value lies
@@ -1370,11 +1378,20 @@ unsigned item_threads(int64_t cols) { return static_cast<unsigned>(((cols + kIte
 
 constexpr int kSmemLimit = 226 * 1024;    // dynamic; the kernels have a few bytes of their own besides
 int spans_for(int64_t cols) { return cols <= 2 * 512 * 8 ? 2 : 4; }
+int group_warps(int64_t cols, int nv) { return static_cast<int>((cols + 256 * nv - 1) / (256 * nv)); }
+// Of the any-width forward, which has one CTA per SM: four spans to a warp where more of its 16 warps are at work then, since a group is
+// whole (4096 x 5001 bf16 with both checkpoints: three groups of five warps 99 us, one of ten 129).
+int loose_spans(int64_t cols, int64_t rows_per_cta) {
+  const auto at_work = [&](int nv) {
+    const int64_t warps = group_warps(cols, nv), groups = 16 / warps;
+    return warps * (groups < rows_per_cta ? groups : rows_per_cta);
+  };
+  return at_work(4) > at_work(2) ? 4 : 2;
+}
 // set_bytes: of a span of 256 columns of every tensor; red: floats of reduction space per row group.
-bool make_shape(int64_t cols, int64_t rows_per_cta, int set_bytes, int red, int smem_limit, Shape* sh, size_t* smem) {
-  const int nv = spans_for(cols), vec = static_cast<int>((cols + 7) / 8);
+bool make_shape(int64_t cols, int nv, int64_t rows_per_cta, int set_bytes, int red, int smem_limit, Shape* sh, size_t* smem) {
   sh->cols = static_cast<int>(cols);
-  sh->group_threads = (vec + 32 * nv - 1) / (32 * nv) * 32;   // a warp to nv spans of 256 columns
+  sh->group_threads = 32 * group_warps(cols, nv);
   sh->groups = 512 / sh->group_threads;
   if (sh->groups > rows_per_cta) sh->groups = static_cast<int>(rows_per_cta < 1 ? 1 : rows_per_cta);
   sh->warp_stage = nv * set_bytes;
@@ -1413,8 +1430,8 @@ int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
     return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true, kFullSpans>, done[0], a, sh, smem, ctas, stream)
                                 : start_rows(norm_forward_full_kernel<T, false, kFullSpans>, done[1], a, sh, smem, ctas, stream);
   const int limit = kNv == 2 ? kSmemLimit / 2 - 1024 : kSmemLimit;       // two CTAs per SM
-  if (!make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem) &&
-      !make_shape(a.cols, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, kSmemLimit, &sh, &smem))
+  if (!make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem) &&
+      !make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, kSmemLimit, &sh, &smem))
     return FALQON_ERR_UNSUPPORTED;
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
 }
@@ -1486,12 +1503,12 @@ int launch_forward_loose(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
   static DeviceMask done{0};
   Shape sh;
   size_t smem;
-  if (!make_shape(a.cols, a.rows_per_piece, 2 * (256 * sizeof(T) + 16), kSumFloats, kSmemLimit, &sh, &smem) || !sh.weights_in_smem) return FALQON_ERR_UNSUPPORTED;
+  if (!make_shape(a.cols, kNv, a.rows_per_piece, 2 * (256 * sizeof(T) + 16), kSumFloats, kSmemLimit, &sh, &smem) || !sh.weights_in_smem) return FALQON_ERR_UNSUPPORTED;
   return start_rows(norm_forward_loose_kernel<T, kNv>, done, a, sh, smem, ctas, stream);
 }
 template <typename F>
-int with_spans(int64_t cols, F go) {
-  return spans_for(cols) == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+int with_spans(int spans, F go) {
+  return spans == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
@@ -1526,7 +1543,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
     const Split s(p, !whole_spans(a.cols) && spans_for(a.cols) == 2 ? 2 * kNormUnits : kNormUnits);   // as many CTAs as are resident
     NormArgs b = a;
     s.put(&b);
-    const int rc = with_spans(a.cols, [&](auto n) {
+    const int rc = with_spans(spans_for(a.cols), [&](auto n) {
       return p->dtype == FALQON_BF16 ? launch_forward_rows<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
                                      : launch_forward_rows<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
     });
@@ -1536,7 +1553,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
     const Split s(p, kNormUnits);
     NormArgs b = a;
     s.put(&b);
-    const int rc = with_spans(a.cols, [&](auto n) {
+    const int rc = with_spans(loose_spans(a.cols, s.rows_per_piece), [&](auto n) {
       return p->dtype == FALQON_BF16 ? launch_forward_loose<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
                                      : launch_forward_loose<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
     });

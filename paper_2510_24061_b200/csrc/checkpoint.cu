@@ -360,7 +360,7 @@ __device__ __forceinline__ void spread_factors(const Spread& p, const Rows& r, f
 }
 
 template <typename T, bool kGate>
-__global__ void __launch_bounds__(kThreads) ragged_encode_kernel(const T* g, const T* u, T* z, const Rows r, uint8_t* g_codes, uint8_t* g_scales,
+__global__ void __launch_bounds__(kThreads, 4) ragged_encode_kernel(const T* g, const T* u, T* z, const Rows r, uint8_t* g_codes, uint8_t* g_scales,
                                                                  uint8_t* u_codes, uint8_t* u_scales, float* amax) {
   __shared__ uint32_t top[kGate ? 2 : 1][kTileBlocks];
   pdl_trigger();
@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kThreads) ragged_load_kernel(T* x, const Rows 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) ragged_gate_backward_kernel(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes,
+__global__ void __launch_bounds__(kThreads, 4) ragged_gate_backward_kernel(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes,
                                                                         const uint8_t* u_scales, const T* dz, T* dg, T* du, const Rows r,
                                                                         float* amax_dg, float* amax_du) {
   pdl_trigger();
