@@ -666,8 +666,8 @@ __device__ __forceinline__ void put_single_codes(const f2 (&x)[4], int left, int
     if (e * 32 + lane < left) codes[e * 32 + lane] = mx8_encode1(v[e], f);
   }
 }
-// The 16-byte pieces that cover the 256 values from `at` on, of a tensor of `total` values; returns nothing: the first value lies
-// offset_of(at) bytes behind dst.
+// Copies the 16-byte pieces that cover the 256 values from `at` on, of a tensor of `total` values: the first value lies offset_of(at)
+// bytes behind dst then.
 template <typename T>
 __device__ __forceinline__ uint32_t offset_of(int64_t at) {
   return static_cast<uint32_t>(at * static_cast<int64_t>(sizeof(T))) & 15u;
@@ -849,11 +849,6 @@ __device__ __forceinline__ void read_saved(uint32_t at, f2 (&x)[4]) {
     read8<T>(at, x);
   }
 }
-__device__ __forceinline__ uint32_t read_byte(uint32_t at) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
-  return v;
-}
 // Where a lane's eight columns of a row lie in shared memory: dx (dh_out is `area` further), h (y `saved_area` further), the scale of h
 // (y's `half` further).
 struct Spot {
@@ -924,8 +919,8 @@ __device__ __forceinline__ void store_stripes(const f2 (&v)[kNv][4], float* out,
   __syncthreads();
 }
 
-template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose, int kThreads>
-__global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormArgs a, const Run sh, int* status) {
+template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose>
+__global__ void __launch_bounds__(512) norm_backward_run_kernel(const NormArgs a, const Run sh, int* status) {
   extern __shared__ __align__(128) uint8_t smem[];
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cols = sh.cols;
@@ -1083,7 +1078,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_run_kernel(const NormA
           }
           return;
         }
-        const float fy = kCoded ? scale_of(read_byte(p.scale + half)) * ip : ip, fh = kCoded ? scale_of(read_byte(p.scale)) * a.res_scale : a.res_scale;
+        const float fy = kCoded ? scale_of(byte_at(p.scale + half)) * ip : ip, fh = kCoded ? scale_of(byte_at(p.scale)) * a.res_scale : a.res_scale;
         read_saved<T, kCoded>(p.h + sh.saved_area, yh);
         if (has_h) read_saved<T, kCoded>(p.h, H);
 #pragma unroll
@@ -1435,14 +1430,17 @@ int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
     return FALQON_ERR_UNSUPPORTED;
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
 }
-// How a backward's runs are cut: warps, rows per run, and the shared memory it takes; false where not even one row fits.
+// How a backward's runs are cut: stripes per warp, rows per run, and the shared memory it takes; false where not even one row fits.
 bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_bytes, bool loose, int* spans, Run* r, size_t* smem) {
   r->cols = static_cast<int>(cols);
   r->stripes = static_cast<int>((cols + 255) / 256);
   r->blocks_per_row = static_cast<int>((cols + kMx8Block - 1) / kMx8Block);
-  *spans = r->stripes <= 24 ? 1 : r->stripes <= 32 ? 2 : 4;
+  // As few stripes to a warp as 16 warps can take: their weights and sums are registers, and more warps than 16 have too few of them.
+  // From checkpoints, bf16: 4096 x 4096 with one 54 us, with two 59; 8192 x 6144 with two 139, with one and 24 warps 195; 4096 x 11008 with
+  // three 218, with four 262.
+  *spans = (r->stripes + 15) / 16;
   r->stripe_warps = (r->stripes + *spans - 1) / *spans;
-  r->warps = r->stripe_warps < 16 ? 16 : r->stripe_warps;
+  r->warps = 16;
   r->split = r->warps / r->stripe_warps;
   const int row = static_cast<int>(cols) * (2 * value_bytes + 2 * saved_bytes);
   for (int attempt = 0; attempt < 3; ++attempt) {              // two buffers and the weights; without the weights; one buffer
@@ -1470,10 +1468,10 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
   }
   return false;
 }
-template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose, int kThreads>
+template <typename T, bool kCoded, int kNv, bool kFull, bool kLoose>
 int start_run(const NormArgs& a, const Run& r, size_t smem, int64_t ctas, int* status, cudaStream_t stream) {
   static DeviceMask done{0};
-  const auto kernel = norm_backward_run_kernel<T, kCoded, kNv, kFull, kLoose, kThreads>;
+  const auto kernel = norm_backward_run_kernel<T, kCoded, kNv, kFull, kLoose>;
   if (set_max_dynamic_smem(kernel, kSmemLimit, done) != cudaSuccess) return FALQON_ERR_CUDA;
   return finish(launch_pdl(kernel, dim3(static_cast<unsigned>(ctas)), dim3(32u * r.warps), smem, stream, 1, a, r, status));
 }
@@ -1489,11 +1487,10 @@ int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStrea
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
   const auto go = [&](auto kind) {                             // 0: any call, 1: the usual call, 2: any width
     constexpr bool kFull = decltype(kind)::value == 1, kLoose = decltype(kind)::value == 2;
-    if (spans == 1 && r.warps <= 16) return start_run<T, kCoded, 1, kFull, kLoose, 512>(a, r, smem, ctas, status, stream);
-    if (spans == 1 && r.warps <= 20) return start_run<T, kCoded, 1, kFull, kLoose, 640>(a, r, smem, ctas, status, stream);
-    if (spans == 1) return start_run<T, kCoded, 1, kFull, kLoose, 768>(a, r, smem, ctas, status, stream);
-    if (spans == 2) return start_run<T, kCoded, 2, kFull, kLoose, 512>(a, r, smem, ctas, status, stream);
-    return start_run<T, kCoded, 4, false, kLoose, 512>(a, r, smem, ctas, status, stream);
+    if (spans == 1) return start_run<T, kCoded, 1, kFull, kLoose>(a, r, smem, ctas, status, stream);
+    if (spans == 2) return start_run<T, kCoded, 2, kFull, kLoose>(a, r, smem, ctas, status, stream);
+    if (spans == 3) return start_run<T, kCoded, 3, false, kLoose>(a, r, smem, ctas, status, stream);
+    return start_run<T, kCoded, 4, false, kLoose>(a, r, smem, ctas, status, stream);
   };
   if (loose) return go(std::integral_constant<int, 2>{});
   return full ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 0>{});
