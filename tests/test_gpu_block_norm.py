@@ -26,6 +26,7 @@ CASES = [
     (700, 1536, 64, True, True, True, True), (16, 128, 16, False, True, False, False),
     (1, 4095, 1, True, True, True, True), (17, 2049, 6, True, True, True, True), (5, 5111, 2, True, False, True, True), (3, 8191, 3, False, True, True, False),
     (2, 9, 2, True, True, False, True), (400, 33, 0, True, True, True, True), (2, 6160, 1, True, True, True, True), (3, 12300, 3, True, True, True, True),
+    (310, 9001, 155, True, True, True, True), (450, 5001, 225, True, True, True, True), (160, 8208, 0, True, True, True, True),
 ]
 IDS = [f"{c[0]}x{c[1]}" for c in CASES]
 
