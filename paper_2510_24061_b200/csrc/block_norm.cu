@@ -75,7 +75,8 @@ __device__ __forceinline__ void cta_sums(float (&v)[kN], float* red, int& phase)
 
 // ---- rows that do not fit in shared memory beside their weights (fp32 beyond 9640 columns backward and 13900 forward, if not a
 // multiple of 16 wide; fp32 beyond 14464 backward in any case): a CTA takes a row at a time, a thread kItems single columns tid,
-// tid + threads, .. in registers, and a checkpoint's block is a warp.  Nothing is fetched ahead: 2 to 6 times the staged kernels' time.
+// tid + threads, .. in registers, and a checkpoint's block is a warp.  Nothing is fetched ahead: bf16 4096 x 4096 would take 357 us forward and 1300
+// backward from checkpoints, where the staged kernels take 37 and 54.
 constexpr int kItems = 16;   // of up to 1024 threads: FALQON_NORM_MAX_COLS
 // Squares are divided by the width before they are added, so that only a mean beyond fp32's range overflows.
 template <typename T>
@@ -494,8 +495,8 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
 // ---- forward, the usual call: both norms, a residual, every result, rows of 1024 columns per warp (1024, 2048, .. 8192)
 // The same work with nothing left to test in the row loop and offsets that advance by a row; four spans a lane (a row of 4096 columns
 // is 128 threads, four rows a CTA), so that a row's two reductions are shared by 1024 columns a warp.  HBM-bound as far as
-// instructions allow: 4096 x 4096 bf16 with both checkpoints 37 us (4.6 TB/s of what it must move; two spans a lane and two CTAs per
-// SM 42), 8192 x 8192 without 96 us (5.6 TB/s).
+// instructions allow: 4096 x 4096 bf16 with both checkpoints 36.5 us (4.6 TB/s of what it must move; two spans a lane and two CTAs per
+// SM 42; the kernel above, for any call, 52), 8192 x 8192 without 98 us (5.5 TB/s; the kernel above 149).
 constexpr int kFullDepth = 2;                                  // two rows ahead per group cover the latency
 
 template <typename T, int kNv>
@@ -595,7 +596,9 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kerne
 // ---- any width: the same rings and runs with single values
 // Rows begin anywhere, so a copy takes the 16-byte pieces that cover its values (of the neighbouring rows' values a few come along and
 // are not looked at), and in shared memory lanes read single values: value e of a lane in a span is column 32 * e + lane, so that
-// neighbouring lanes read and write neighbouring values, and every e is one block of a checkpoint.
+// neighbouring lanes read and write neighbouring values, and every e is one block of a checkpoint.  Bound by instructions, single values
+// taking eight times the accesses: bf16 4096 x 4095 with checkpoints 78 us forward and 108 backward, where 4096 x 4096 takes 37 and 54
+// (and by these kernels about as long as 4095).
 __device__ __forceinline__ float single_at(uint32_t at, bf16_t) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
@@ -806,7 +809,9 @@ __global__ void __launch_bounds__(512) norm_forward_loose_kernel(const NormArgs 
 // values are formed twice, from shared memory.  In the terms of the file's head, with H in the place of xh = H * iq:
 //   t = dx * w;  g = dh_out + iq * t;  b = q * yh;  A = sum t * H, B = sum b * g, C = sum b * H
 //   d = g - k1 * H with k1 = iq^3 * A / cols;  dy = ip * (q * d - yh * k2) with k2 = (B - k1 * C) / cols
-// (Rows in registers from the sums to the results, a barrier per row: 57 us at 4096 x 4096 from checkpoints, 150 us at 8192 x 5120.)
+// Bound by instructions, since every value is decoded and formed twice (issued on 48 % of cycles by 16 warps, the most whose registers and
+// shared memory fit): 4096 x 4096 from checkpoints 54 us with the finish below (3.1 TB/s of what it must move), 8192 x 5120 from bf16 121 us
+// (4.2 TB/s).  Rows in registers from the sums to the results, a barrier per row: 57 and 150 us.
 constexpr int kMaxRun = 32;                                    // a lane per row
 constexpr int kScaleBytes = 4;                                 // of a run, per thread
 struct Run {
@@ -1207,6 +1212,7 @@ __global__ void __launch_bounds__(512) norm_backward_run_kernel(const NormArgs a
 // The gradients of gains and gate from the partial column sums.  A CTA takes 32 columns (a row of them is eight lanes of four), a warp
 // four partial rows at a time; a team of warps shares a gate group's rows, so that few groups use all warps too.  The loads of both
 // sums, and of the next groups', are in flight before the first addition, and every addition has its place: the order never changes.
+// 7 us behind a backward of 4096 columns, of which the partial sums' bytes are one; the rest is the launch and three dependent loads.
 constexpr int kFinishWarps = 16;
 struct FinishArgs {
   const float *part_s, *part_p;
@@ -1223,7 +1229,7 @@ __device__ __forceinline__ float4 shfl4(float4 a, int o) {
   return make_float4(__shfl_xor_sync(all, a.x, o), __shfl_xor_sync(all, a.y, o), __shfl_xor_sync(all, a.z, o), __shfl_xor_sync(all, a.w, o));
 }
 // The sum of rows from, from + stride, .. of n (a lane's row is that of its eighth of the warp), of four columns from c on.
-// kVec: the columns are a multiple of four.
+// kVec: the columns are a multiple of four (8192 x 5120 in 16 gate groups: the whole backward 121 us, 123 by single values).
 template <bool kVec>
 struct PartialSum {
   static constexpr int kAhead = 4;
@@ -1482,7 +1488,7 @@ int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStrea
   int spans;
   const bool loose = !staged(a.cols);
   if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded ? 1 : sizeof(T), loose, &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
-  // the usual call: both norms, both gradients in and out, a residual, whole stripes
+  // the usual call: both norms, both gradients in and out, a residual, whole stripes (4096 x 4096 from checkpoints 57 us, as any call 74, side by side)
   const bool full = a.cols % 256 == 0 && r.weights_in_smem && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr &&
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
   const auto go = [&](auto kind) {                             // 0: any call, 1: the usual call, 2: any width

@@ -4,7 +4,11 @@
 //   logit_grad_kernel  dlogits = dlogp * ([v == target] - exp(x - m) / sum)
 // exp(x - m) is taken as 2^((x - m) * log2 e) with the difference formed first: exact near the maximum whatever its size, and
 // a row of the type's lowest values (a mask over the whole vocabulary) does not overflow on the way.
-// HBM-bound: the forward reads each counted row once, the backward reads it again and writes every row once.
+// HBM-bound: the forward reads each counted row once, the backward reads it again and writes every row once.  A row is a CTA's, so that
+// all its vectors are in flight together and one row's reduction passes under the others' loads: 4096 x 32000 bf16, of which 3080 rows
+// are counted, 38 us (5.2 TB/s; two special-function instructions and eight others per pair of values are issued on 54 % of cycles, and
+// deeper prefetching, 2 or 8 vectors a turn, or a turn ahead, did not help).  The gradient of 16384 x 32000 runs at 6.6 TB/s.  The
+// sequences' kernel is a chain of dependent loads, 5 us at any size.
 #include <cfloat>
 #include <type_traits>
 
@@ -405,7 +409,8 @@ __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) 
   }
 }
 
-// kSame: logits and dlogits rows have the same offset from a 16-byte boundary, so vectors can be stored; else single values are.
+// kSame: logits and dlogits rows have the same offset from a 16-byte boundary, so vectors can be stored; else single values are (the
+// whole step of 16384 x 32000 bf16: 410 us with vectors, 1456 with single values).
 template <typename T, bool kSame, int kTeam>
 __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(int64_t rows, const T* logits, int64_t vocab, int64_t ld, const int64_t* targets,
                                                                  int64_t chunk, const float2* stats, const float* dlogp, const float* dloss,
@@ -502,7 +507,8 @@ bool sizes_ok(int64_t rows, int64_t vocab, int dtype) {
          (dtype == FALQON_BF16 || dtype == FALQON_F32);
 }
 
-// Into how many parts a row is cut: none where the rows alone fill the GPU, and no part below two vectors per thread.
+// Into how many parts a row is cut: none where the rows alone fill the GPU, and no part below two vectors per thread.  Loss and gradient
+// of 300 x 128000 bf16: 43 us by four parts, 58 by whole rows.
 int parts_for(int64_t rows, int64_t vocab, int dtype) {
   const int64_t want = (148 * 8 + rows - 1) / rows;
   const int64_t most = vocab / (dtype == FALQON_BF16 ? 8 : 4) / (2 * kRowThreads);
@@ -514,7 +520,8 @@ int parts_for(int64_t rows, int64_t vocab, int dtype) {
 // Vectors of a part, of a row that begins on a 16-byte boundary; the others' have one less at the most.
 int64_t chunk_for(int64_t vocab, int dtype, int parts) { return (vocab / (dtype == FALQON_BF16 ? 8 : 4) + parts - 1) / parts; }
 
-// A thread per row of the average sequence (or pair), a warp at least.
+// A thread per row of the average sequence (or pair), a warp at least (1500 x 8000 bf16, four pairs, loss and gradient: 26.7 us, with 1024
+// threads 28.0).
 unsigned sequence_threads(int64_t rows, int64_t ctas) {
   const int64_t t = (rows / ctas + 31) / 32 * 32;            // (a pair's rows vary: a thread takes several where they are more)
   return static_cast<unsigned>(t < 32 ? 32 : t > kSeqThreads ? kSeqThreads : t);
