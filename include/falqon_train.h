@@ -45,10 +45,11 @@ int falqon_gate_backward(const uint8_t *g_codes, const uint8_t *g_scales, const 
  *   h_out = res_scale * h + gate * n                         y: what the block gave, h: the residual stream before it
  *   x     = h_out * inv_pre[t] * (gain_offset + pre_gain)    inv_pre[t] = 1 / sqrt(mean(h_out[t]^2) + eps)  (FALQON_NORM_PRE: the next block's input)
  * x and inv_pre come from h_out before its rounding.  A NULL gain or gate is 1 (without gain_offset); a NULL h leaves the
- * residual term out.  cols <= FALQON_NORM_MAX_COLS. */
+ * residual term out.  rows <= FALQON_NORM_MAX_ROWS, cols <= FALQON_NORM_MAX_COLS. */
 #define FALQON_NORM_POST 1
 #define FALQON_NORM_PRE 2
 #define FALQON_NORM_MAX_COLS 16384
+#define FALQON_NORM_MAX_ROWS 2147482624 /* 2^31 - 1024: the kernels count rows in 32 bits and look up to 64 rows ahead */
 
 typedef struct { /* host struct */
   int64_t rows, cols;

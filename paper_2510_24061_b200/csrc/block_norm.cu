@@ -41,7 +41,7 @@ __device__ __forceinline__ float weight_at(const void* p, int64_t i, const NormA
 
 // The rows of a unit, which is a run of the rows of one gate group (32-bit division: a 64-bit one is a hundred instructions).
 struct Unit {
-  int gate, first, last;                                       // rows < 2^31
+  int gate, first, last;                                       // at most FALQON_NORM_MAX_ROWS, so that a row number plus what is looked ahead (64) fits
   __device__ __forceinline__ Unit(const NormArgs& a, int unit) {
     gate = unit / a.pieces;
     const int64_t begin = gate * a.rows_per_gate + (unit - gate * a.pieces) * a.rows_per_piece;
@@ -1329,7 +1329,7 @@ inline bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) =
 int finish(cudaError_t e) { return e == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA; }
 
 bool plan_ok(const falqon_block_norm* p) {
-  return p != nullptr && p->rows >= 1 && p->rows < (1ll << 31) && p->cols >= 1 && p->cols <= FALQON_NORM_MAX_COLS &&
+  return p != nullptr && p->rows >= 1 && p->rows <= FALQON_NORM_MAX_ROWS && p->cols >= 1 && p->cols <= FALQON_NORM_MAX_COLS &&
          p->rows_per_gate >= 1 && (p->dtype == FALQON_BF16 || p->dtype == FALQON_F32) &&
          (p->gain_dtype == FALQON_BF16 || p->gain_dtype == FALQON_F32) && (p->flags & ~(FALQON_NORM_POST | FALQON_NORM_PRE)) == 0 &&
          p->eps >= 0.0f && p->res_scale == p->res_scale && p->gain_offset == p->gain_offset && ok16(p->post_gain) &&

@@ -50,7 +50,7 @@ for _name, (_res, _args) in _SIGNATURES.items():
     getattr(lib, _name).restype = _res
     getattr(lib, _name).argtypes = _args
 
-NORM_POST, NORM_PRE, NORM_MAX_COLS = 1, 2, 16384
+NORM_POST, NORM_PRE, NORM_MAX_COLS, NORM_MAX_ROWS = 1, 2, 16384, (1 << 31) - 1024
 CHECKPOINT_BLOCK = 32
 PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "ipo": 2}
 _DTYPES = {torch.bfloat16: fq.BF16, torch.float32: fq.F32}
