@@ -63,8 +63,8 @@ typedef struct { /* host struct */
   const void *gate;       /* device, nullable                                                                          */
 } falqon_block_norm;
 
-/* h_out may be NULL with FALQON_NORM_PRE (only x is wanted) and may alias h or y; x, inv_pre / inv_post are needed with
- * their flag and ignored without it.  h_codes, h_scales / y_codes, y_scales (nullable, in pairs): checkpoints of h / y. */
+/* h_out may be NULL with FALQON_NORM_PRE (only x is wanted) and may alias h or y; x is not h_out; x, inv_pre / inv_post are
+ * needed with their flag and ignored without it.  h_codes, h_scales / y_codes, y_scales (nullable, in pairs): checkpoints of h / y. */
 int falqon_block_norm_forward(const falqon_block_norm *p, const void *h, const void *y, void *h_out, void *x, float *inv_post,
                               float *inv_pre, uint8_t *h_codes, uint8_t *h_scales, uint8_t *y_codes, uint8_t *y_scales,
                               float *amax_x, falqon_stream stream);

@@ -1529,7 +1529,7 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
   if (y == nullptr || !ok16(h) || !ok16(y) || !ok16(h_out) || !ok16(x) || !ok16(h_codes) || !ok16(y_codes) ||
       (h_codes != nullptr) != (h_scales != nullptr) || (y_codes != nullptr) != (y_scales != nullptr) ||
       (h_codes != nullptr && h == nullptr) || (a.post && inv_post == nullptr) || (a.pre && (x == nullptr || inv_pre == nullptr)) ||
-      (!a.pre && h_out == nullptr))
+      (!a.pre && h_out == nullptr) || (a.pre && x == h_out))
     return FALQON_ERR_INVALID_ARG;
   a.h = h;
   a.y = y;

@@ -43,3 +43,10 @@ def test_rows_beyond_what_the_kernels_can_count_are_refused(fq, tr):
         assert tr.lib.falqon_block_norm_backward(p, FAKE, FAKE, FAKE, None, None, FAKE, None, None, FAKE, FAKE, FAKE, 2 * FAKE, FAKE, FAKE, FAKE, None, FAKE, 1 << 40,
                                                  None) == fq.ERR_INVALID_ARG
     assert tr.lib.falqon_block_norm_scratch_bytes(plan(tr, rows=limit, cols=1, rows_per_gate=limit)) > 0
+
+
+def test_two_results_in_one_buffer_are_refused(fq, tr):
+    """h_out and x written to the same place would leave a mixture of the two: refused, as dh = dy is in the backward."""
+    fwd = tr.lib.falqon_block_norm_forward
+    assert fwd(plan(tr), FAKE, 2 * FAKE, 3 * FAKE, 3 * FAKE, FAKE, FAKE, *(None,) * 6) == fq.ERR_INVALID_ARG
+    assert fwd(plan(tr), FAKE, 2 * FAKE, FAKE, FAKE, FAKE, FAKE, *(None,) * 6) == fq.ERR_INVALID_ARG           # h_out in place of h, and x there too
