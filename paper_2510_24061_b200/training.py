@@ -97,7 +97,7 @@ def _on_device(*tensors) -> int:
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor on {t.device} where the current device is cuda:{dev}")
-    return _raw_stream(dev)
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _like(t: Optional[torch.Tensor], ref: torch.Tensor, name: str):

@@ -50,3 +50,14 @@ def test_two_results_in_one_buffer_are_refused(fq, tr):
     fwd = tr.lib.falqon_block_norm_forward
     assert fwd(plan(tr), FAKE, 2 * FAKE, 3 * FAKE, 3 * FAKE, FAKE, FAKE, *(None,) * 6) == fq.ERR_INVALID_ARG
     assert fwd(plan(tr), FAKE, 2 * FAKE, FAKE, FAKE, FAKE, FAKE, *(None,) * 6) == fq.ERR_INVALID_ARG           # h_out in place of h, and x there too
+
+
+def test_the_stream_is_found_without_torchs_private_entry(tr, monkeypatch):
+    """The handle comes from a private entry of torch where it has one, else from the public stream object."""
+    class Stream:
+        cuda_stream = 0x5EED
+
+    monkeypatch.setattr(tr.torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(tr.torch.cuda, "current_stream", lambda dev: Stream())
+    monkeypatch.setattr(tr, "_raw_stream", None)
+    assert tr._on_device() == 0x5EED
