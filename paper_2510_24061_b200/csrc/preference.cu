@@ -423,13 +423,13 @@ __global__ void __launch_bounds__(kRowThreads) logit_grad_kernel(int64_t rows, c
   const int tid = threadIdx.x % kTeam;
   uint32_t mx = 0;
   if (row >= 0) {
-    const float c = ld_stream(dlogp + row) * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
+    const float own = ld_stream(dlogp + row), c = own * (dloss != nullptr ? ld_stream(dloss) : 1.0f);
     const T* p = logits + row * ld;
     T* o = out + row * ld_out;
     const Span sp = span_of(p, vocab);
     const auto [begin, end] = Part(sp, chunk);
     const uint4* body = reinterpret_cast<const uint4*>(p + sp.head);
-    const bool zero = c == 0.0f;
+    const bool zero = own == 0.0f || c == 0.0f;                // a row that is not counted stays so under an infinite or NaN dloss
     const float2 st = zero ? make_float2(0.0f, 1.0f) : ld_stream(stats + row);
     const int64_t target = zero ? -1 : ld_stream(targets + row);
     const float f = -c / st.y;
