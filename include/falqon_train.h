@@ -114,14 +114,14 @@ int falqon_sequence_logprob(const void *logits, int dtype, int64_t rows, int64_t
                             size_t scratch_bytes, falqon_stream stream);
 
 /* ref_logp [2 * pairs] (nullable: 0).  Results: loss [1], pair_loss [pairs], seq_logp [2 * pairs], logp [rows]; and for the
- * gradient (both or neither) row_stats [rows][2], 8-byte aligned: the row's maximum and its sum of exp(logit - maximum) (not
- * written where the row is not counted), and dlogp [rows]: d loss / d logp of the row, 0 where it is not counted. */
+ * gradient (both or neither) row_stats [rows][2], 8-byte aligned: the row's maximum and its sum of exp(logit - maximum) (of no
+ * meaning where the row is not counted), and dlogp [rows]: d loss / d logp of the row, 0 where it is not counted. */
 int falqon_preference_forward(const falqon_preference *p, const void *logits, const int64_t *targets, const int64_t *cu_rows,
                               const float *ref_logp, float *loss, float *pair_loss, float *seq_logp, float *logp,
                               float *row_stats, float *dlogp, void *scratch, size_t scratch_bytes, falqon_stream stream);
 
 /* dlogits[row][v] = dloss * dlogp[row] * ([v == target] - softmax(logits[row])[v]), row pitch ld_out; a row whose dlogp is 0
- * gets zeros and is not read.  dloss: device [1], nullable (1).  dlogits may be logits (ld_out == ld). */
+ * gets zeros and is not read, whatever dloss is.  dloss: device [1], nullable (1).  dlogits may be logits (ld_out == ld). */
 int falqon_preference_backward(const falqon_preference *p, const void *logits, const int64_t *targets, const float *row_stats,
                                const float *dlogp, const float *dloss, void *dlogits, int64_t ld_out, float *amax_out,
                                falqon_stream stream);
