@@ -72,36 +72,44 @@ struct Coded {
   }
 };
 
-// 1 / (1 + exp(-x)).  For bf16 results two special-function instructions (a few 2^-22, the results' rounding is 2^-8); fp32 results
-// take expf and the reciprocal, within 2 units in the last place.
-template <typename T>
-__device__ __forceinline__ float sigmoid_of(float x) {
-  float e, r;
-  if constexpr (sizeof(T) == 2) {
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * -1.4426950408889634f));
-  } else {
-    e = expf(-x);
-  }
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return r;
+// 1 / (1 + exp(-x)) of two values.  As it stands exp(-x) overflows at x = -88.8 and the reciprocal is subnormal, and flushed, from -87.4 on,
+// where x times it is still a normal number; so it is taken in forms that stay in range:
+//   fp32 results   t = exp(-|x|): 1 / (1 + t) or t / (1 + t), with expf and the reciprocal instruction, 4 units of 2^-23 at most
+//   bf16 results   2^-24 / (2^-24 + exp(-x) * 2^-24), the last product formed in the exponent, from the special-function unit: |x| * 2^-23
+//                  from the exponent's rounding and 8 * 2^-23 from the rest (the results' rounding is 2^-8)
+__device__ __forceinline__ f2 sigmoid2(f2 x, bf16_t) {
+  constexpr float kShift = 24.0f, kScale = 0x1p-24f;
+  float a, b, r, q;
+  unpack_f32x2(fma2(x, twice(-1.4426950408889634f), twice(-kShift)), a, b);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+  unpack_f32x2(add2(pack_f32x2(a, b), twice(kScale)), a, b);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(b));
+  return mul2(pack_f32x2(r, q), twice(kScale));
 }
-template <typename T>
-__device__ __forceinline__ f2 sigmoid2(f2 x) {
+__device__ __forceinline__ float sigmoid1(float x) {
+  const float t = expf(-fabsf(x));
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + t));
+  return x < 0.0f ? t * r : r;
+}
+__device__ __forceinline__ f2 sigmoid2(f2 x, float) {
   float lo, hi;
   unpack_f32x2(x, lo, hi);
-  return pack_f32x2(sigmoid_of<T>(lo), sigmoid_of<T>(hi));
+  return pack_f32x2(sigmoid1(lo), sigmoid1(hi));
 }
 
 template <typename T>
 __device__ __forceinline__ void gate8(const f2 (&g)[4], const f2 (&u)[4], f2 (&z)[4]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) z[k] = mul2(mul2(g[k], sigmoid2<T>(g[k])), u[k]);
+  for (int k = 0; k < 4; ++k) z[k] = mul2(mul2(g[k], sigmoid2(g[k], T{})), u[k]);
 }
 template <typename T>
 __device__ __forceinline__ void gate_grad8(const f2 (&g)[4], const f2 (&u)[4], const f2 (&dz)[4], f2 (&dg)[4], f2 (&du)[4]) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const f2 s = sigmoid2<T>(g[k]), gs = mul2(g[k], s);
+    const f2 s = sigmoid2(g[k], T{}), gs = mul2(g[k], s);
     du[k] = mul2(dz[k], gs);
     // s * (1 + g * (1 - s)) = s + g * s * (1 - s)
     dg[k] = mul2(mul2(dz[k], u[k]), fma2(gs, fma2(s, twice(-1.0f), twice(1.0f)), s));
