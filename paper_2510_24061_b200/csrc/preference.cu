@@ -296,8 +296,24 @@ __device__ __forceinline__ void clear_rows(const SeqArgs& a, int64_t begin, int6
   }
 }
 
-__device__ __forceinline__ float log_sigmoid(float d) { return fminf(d, 0.0f) - log1pf(expf(-fabsf(d))); }
-__device__ __forceinline__ float logistic(float d) { return 1.0f / (1.0f + expf(-d)); }
+// log sigmoid and sigmoid of d and of -d.  q = exp(-|d|) is taken in 32 bits, its argument's rounding made good to the first order, so that
+// every value has a few units of 2^-23 of its own size; what is added to large numbers is added in 64 bits.  (The 64-bit functions would
+// be hundreds of instructions in a kernel that is one dependent chain.)
+struct Sigmoids {
+  double log_of, log_of_minus;
+  float of, of_minus;
+  __device__ __forceinline__ explicit Sigmoids(double d) {
+    const double size = fabs(d) > 256.0 ? 256.0 : fabs(d);   // exp(-256) is 0 in 32 bits; a NaN stays one
+    const float near = static_cast<float>(size);
+    const float e = expf(-near), q = __fmaf_rn(-e, static_cast<float>(size - static_cast<double>(near)), e);
+    const double tail = static_cast<double>(log1pf(q));
+    log_of = (d < 0.0 ? d : 0.0) - tail;
+    log_of_minus = (d > 0.0 ? -d : 0.0) - tail;
+    const float large = 1.0f / (1.0f + q), small = q * large;
+    of = d < 0.0 ? small : large;
+    of_minus = d < 0.0 ? large : small;
+  }
+};
 
 template <bool kPairs>
 __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) {
@@ -349,38 +365,39 @@ __global__ void __launch_bounds__(kSeqThreads) sequence_kernel(const SeqArgs a) 
   }
   t = cta_sums(t, red);
   if (threadIdx.x < 32) {
-    const float n1 = static_cast<float>(max(t.n_first, 1u)), n2 = static_cast<float>(max(t.n_second, 1u));
-    const float chosen = static_cast<float>(t.first) / (a.average ? n1 : 1.0f);
+    const double n1 = max(t.n_first, 1u), n2 = max(t.n_second, 1u);
+    const double chosen = a.average ? t.first / n1 : t.first;
     if constexpr (!kPairs) {
-      if (threadIdx.x == 0) a.seq_logp[first] = chosen;
+      if (threadIdx.x == 0) a.seq_logp[first] = static_cast<float>(chosen);
     } else {
-      const float rejected = static_cast<float>(t.second) / (a.average ? n2 : 1.0f);
-      // u in 64 bits where it is a difference of sums of many rows
-      const float u = a.average ? (chosen - ref[0]) - (rejected - ref[1])
-                                : static_cast<float>((t.first - static_cast<double>(ref[0])) - (t.second - static_cast<double>(ref[1])));
-      const float beta = a.beta, d = __fmaf_rn(beta, u, -a.margin);
-      float l, du;
+      // 64 bits up to the results: u, d and the squared loss are differences of numbers much larger than themselves
+      const double rejected = a.average ? t.second / n2 : t.second;
+      const double u = (chosen - static_cast<double>(ref[0])) - (rejected - static_cast<double>(ref[1]));
+      const double beta = a.beta, d = beta * u - a.margin;
+      double l, du;
       if (a.kind == FALQON_PREFERENCE_SIGMOID) {
-        const float eps = a.smoothing;     // a term of weight 0 is left out: its logarithm may be infinite
-        l = (eps < 1.0f ? -(1.0f - eps) * log_sigmoid(d) : 0.0f) - (eps > 0.0f ? eps * log_sigmoid(-d) : 0.0f);
-        du = beta * (eps * logistic(d) - (1.0f - eps) * logistic(-d));
+        const double eps = a.smoothing;    // a term of weight 0 is left out: its logarithm may be infinite
+        const Sigmoids s(d);
+        l = (eps < 1.0 ? -(1.0 - eps) * s.log_of : 0.0) - (eps > 0.0 ? eps * s.log_of_minus : 0.0);
+        du = beta * (eps * s.of - (1.0 - eps) * s.of_minus);
       } else if (a.kind == FALQON_PREFERENCE_HINGE) {
-        l = d < 1.0f ? 1.0f - d : d >= 1.0f ? 0.0f : d;     // a NaN stays one
-        du = d < 1.0f ? -beta : d >= 1.0f ? 0.0f : d;
+        l = d < 1.0 ? 1.0 - d : d >= 1.0 ? 0.0 : d;     // a NaN stays one
+        du = d < 1.0 ? -beta : d >= 1.0 ? 0.0 : d;
       } else {
-        const float v = u - a.margin - 0.5f / beta;
+        const double v = u - a.margin - 0.5 / beta;
         l = v * v;
-        du = 2.0f * v;
+        du = 2.0 * v;
       }
-      const float pairs = static_cast<float>(gridDim.x), nll = a.nll_weight / n1;
-      if (nll != 0.0f) l = __fmaf_rn(-nll, static_cast<float>(t.first), l);
+      const double pairs = gridDim.x, nll = a.nll_weight == 0.0f ? 0.0 : static_cast<double>(a.nll_weight) / n1;
+      if (nll != 0.0) l -= nll * t.first;
       if (threadIdx.x == 0) {
-        a.seq_logp[first] = chosen;
-        a.seq_logp[first + 1] = rejected;
-        a.pair_loss[blockIdx.x] = l;
-        if (gridDim.x == 1) *a.loss = l;
-        s_coef[0] = ((a.average ? du / n1 : du) - nll) / pairs;
-        s_coef[1] = -(a.average ? du / n2 : du) / pairs;
+        const float out = static_cast<float>(l);
+        a.seq_logp[first] = static_cast<float>(chosen);
+        a.seq_logp[first + 1] = static_cast<float>(rejected);
+        a.pair_loss[blockIdx.x] = out;
+        if (gridDim.x == 1) *a.loss = out;
+        s_coef[0] = static_cast<float>(((a.average ? du / n1 : du) - nll) / pairs);
+        s_coef[1] = static_cast<float>(-(a.average ? du / n2 : du) / pairs);
       }
     }
   }

@@ -68,3 +68,64 @@ def test_fp32_bits(tr, rows, vocab, spread):
     tol = unit * c.abs() * (p * (each + total[:, None] + 3) + one * 2) + 2.0 ** -126       # a product below the normal numbers is flushed
     err = (grad - c * (one - p)).abs()
     assert (err <= tol).all(), float((err / tol).max())
+
+
+def pairs_from(logp, targets, cu, ref, spec):
+    """seq_logp, pair_loss and dlogp in 64 bits from the rows' log-probabilities as the call returned them."""
+    f = lambda v: float(torch.tensor(v, dtype=torch.float32))  # noqa: E731
+    beta, margin, eps, weight = f(spec.beta), f(spec.margin), f(spec.label_smoothing), f(spec.nll_weight)
+    counted, n, total = targets >= 0, [], []
+    for a, b in zip(cu, cu[1:]):
+        n.append(max(int(counted[a:b].sum()), 1))
+        total.append(logp[a:b].sum())
+    total, n = torch.stack(total), torch.tensor(n, dtype=torch.float64)
+    seq = total / n if spec.average else total
+    u = (seq - ref)[0::2] - (seq - ref)[1::2]
+    D = beta * u - margin
+    sp = torch.nn.functional.softplus
+    if spec.kind == "sigmoid":
+        # softplus in torch returns D itself beyond a threshold of 20, so its second term is added
+        tail = torch.log1p(torch.exp(-D.abs()))
+        l = (1 - eps) * (torch.relu(-D) + tail) + eps * (torch.relu(D) + tail)
+        du = beta * (eps * torch.sigmoid(D) - (1 - eps) * torch.sigmoid(-D))
+    elif spec.kind == "hinge":
+        l, du = torch.relu(1 - D), torch.where(D < 1, -beta, 0.0).double()
+    else:
+        l, du = (u - margin - 0.5 / beta) ** 2, 2 * (u - margin - 0.5 / beta)
+    nll = weight / n[0::2]
+    coef = torch.stack(((du / n[0::2] if spec.average else du) - nll, -(du / n[1::2] if spec.average else du)), 1).view(-1) / len(u)
+    dlogp = torch.zeros_like(logp)
+    for i, (a, b) in enumerate(zip(cu, cu[1:])):
+        dlogp[a:b] = torch.where(counted[a:b], coef[i], 0.0)
+    return seq, l - nll * total[0::2], dlogp, l, (du.abs() + (nll if spec.average else nll)), D
+
+
+@pytest.mark.parametrize("average", [False, True])
+@pytest.mark.parametrize("kind,smoothing", [("sigmoid", 0.0), ("sigmoid", 0.1), ("hinge", 0.0), ("ipo", 0.0)])
+def test_the_pairs_arithmetic_is_rounded_once(tr, kind, smoothing, average):
+    """From the returned logp on: sums, differences and results are 64 bits and rounded once (2^-24); the sigmoid's exponential, logarithm and
+    reciprocal are 32 bits and enter with 4 * 2^-23 of their own values.  References lie close to the policy's own sums, as early in training,
+    so that u is small beside them; margins bring the loss near its bends."""
+    lens = [int(v) for v in torch.randint(1, 60, (64,), generator=torch.Generator().manual_seed(3))]
+    cu = torch.tensor([0] + lens).cumsum(0)
+    rows, vocab = int(cu[-1]), 200
+    gen = torch.Generator().manual_seed(4)
+    logits = torch.randn((rows, vocab), generator=gen) * 2
+    targets = torch.randint(0, vocab, (rows,), generator=gen)
+    targets[torch.rand(rows, generator=gen) < 0.25] = -100
+    first, _ = tr.sequence_logprob(logits.cuda(), targets.cuda(), cu.cuda(), average=average)
+    ref = (first.cpu() + torch.randn(64, generator=gen) * 0.05).contiguous()
+    for beta, margin, nll in ((0.1, 0.0, 0.0), (2.0, 0.9, 0.0), (30.0, 0.0, 0.3), (0.5, -12.0, 0.0), (0.5, 60.0, 0.0)):
+        spec = tr.PreferenceLoss(kind, beta, margin, smoothing, average, nll)
+        out = tr.preference_forward(spec, logits.cuda(), targets.cuda(), cu.cuda(), ref.cuda())
+        seq, loss, dlogp, l, size, D = pairs_from(out.logp.cpu().double(), targets, cu.tolist(), ref.double(), spec)
+        soft = (4 * 2.0 ** -23 if kind == "sigmoid" else 0.0)
+        once = 2.0 ** -24 * (1 + 2.0 ** -20)
+        assert ((out.seq_logp.cpu().double() - seq).abs() <= once * seq.abs() + 2.0 ** -149).all()
+        err, tol = (out.pair_loss.cpu().double() - loss).abs(), once * loss.abs() + soft * l.abs() + 2.0 ** -126 + 2.0 ** -48 * seq.abs().max()
+        assert (err <= tol).all(), (beta, margin, float((err / tol).max()))
+        per = (size / len(size)).repeat_interleave(2)
+        bound = torch.cat([per[i].expand(b - a) for i, (a, b) in enumerate(zip(cu.tolist(), cu.tolist()[1:]))])
+        err, tol = (out.dlogp.cpu().double() - dlogp).abs(), once * dlogp.abs() + soft * bound + 2.0 ** -126 + 2.0 ** -48 * seq.abs().max()
+        assert (err <= tol).all(), (beta, margin, float((err / tol).max()))
+        assert abs(out.loss.item() - float(loss.mean())) <= 2.0 ** -23 * float(loss.abs().mean()) + soft * float(l.mean()) + 2.0 ** -48 * float(seq.abs().max())
