@@ -1447,7 +1447,6 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
   *spans = (r->stripes + 15) / 16;
   r->stripe_warps = (r->stripes + *spans - 1) / *spans;
   r->warps = 16;
-  r->split = r->warps / r->stripe_warps;
   const int row = static_cast<int>(cols) * (2 * value_bytes + 2 * saved_bytes);
   for (int attempt = 0; attempt < 3; ++attempt) {              // two buffers and the weights; without the weights; one buffer
     if (loose && attempt == 1) continue;
@@ -1458,6 +1457,8 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
     if (run > rows_per_piece) run = static_cast<int>(rows_per_piece);
     for (; run >= 1; --run) {
       r->run = run;
+      r->split = r->warps / r->stripe_warps;                   // a row of the run each; so their sums, 4 bytes a column, fit over the buffers
+      if (r->split > run) r->split = run;
       r->parts = r->warps / run;
       if (r->parts > r->stripes) r->parts = r->stripes;
       if (r->parts < 1) r->parts = 1;
@@ -1466,9 +1467,7 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
       r->saved_area = loose ? (run * r->cols * saved_bytes + 47) / 16 * 16 : run * r->cols * saved_bytes;
       r->buffer = (2 * r->area + 2 * r->saved_area + 127) / 128 * 128;
       *smem = static_cast<size_t>(r->buffers) * r->buffer + run_tail_bytes(*r);
-      const size_t sums = static_cast<size_t>(r->split) * r->cols * sizeof(float);   // store_stripes, over the buffers
-      if (*smem <= static_cast<size_t>(kSmemLimit) && 2 * run * r->blocks_per_row <= kScaleBytes * 32 * r->warps &&
-          (r->split == 1 || sums <= static_cast<size_t>(r->buffers) * r->buffer))
+      if (*smem <= static_cast<size_t>(kSmemLimit) && 2 * run * r->blocks_per_row <= kScaleBytes * 32 * r->warps)
         return true;
     }
   }

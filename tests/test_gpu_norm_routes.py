@@ -1,0 +1,37 @@
+"""Which kernels the block norms launch: the staged ones wherever a row fits in shared memory, on every CTA that can be resident."""
+import pytest
+import torch
+
+from tests.launches import launched
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tr():
+    from paper_2510_24061_b200 import training
+    return training
+
+
+def one(n, v=1.0):
+    return torch.full((n,), v, device="cuda")
+
+
+def backward_call(tr, rows, cols, rpg, dtype, coded, gains=True):
+    h, y, dx, dh_out = (torch.randn((rows, cols), device="cuda").to(dtype) for _ in range(4))
+    gates = -(-rows // rpg)
+    kw = dict(post_gain=one(cols), pre_gain=one(cols), gate=torch.rand((gates, cols), device="cuda"), rows_per_gate=rpg, res_scale=0.5)
+    out = tr.block_norm_forward(h, y, save=coded, **kw)
+    saved = (out.saved_h, out.saved_y) if coded else (h, y)
+    return lambda: tr.block_norm_backward(dx, dh_out, *saved, out.inv_post, out.inv_pre, need_gains=gains, **kw)
+
+
+@pytest.mark.parametrize("gains", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("coded", [True, False])
+@pytest.mark.parametrize("rows,cols,rpg", [(724, 256, 724), (1, 1024, 1), (300, 64, 300), (37, 40, 5), (257, 256, 1), (16, 128, 16), (1000, 1024, 1), (200, 512, 200),
+                                           (150, 97, 150), (5, 1, 5), (1, 16, 1), (400, 33, 100)])
+def test_short_runs_of_narrow_rows_are_staged(tr, rows, cols, rpg, dtype, coded, gains):
+    """Few rows per CTA, and rows of one to a few spans: the warps that could share a run's columns are more than its rows."""
+    names = [n for n, _, _ in launched(backward_call(tr, rows, cols, rpg, dtype, coded, gains)) if "norm_backward" in n]
+    assert len(names) == 1 and "norm_backward_run_kernel" in names[0]
