@@ -73,10 +73,11 @@ __device__ __forceinline__ void cta_sums(float (&v)[kN], float* red, int& phase)
   }
 }
 
-// ---- rows that do not fit in shared memory beside their weights (fp32 beyond 9640 columns backward and 13900 forward, if not a
-// multiple of 16 wide; fp32 beyond 14464 backward in any case): a CTA takes a row at a time, a thread kItems single columns tid,
-// tid + threads, .. in registers, and a checkpoint's block is a warp.  Nothing is fetched ahead: bf16 4096 x 4096 would take 357 us forward and 1300
-// backward from checkpoints, where the staged kernels take 37 and 54.
+// ---- rows that do not fit in shared memory: a CTA takes a row at a time, a thread kItems single columns tid, tid + threads, .. in registers,
+// and a checkpoint's block is a warp.  Nothing is fetched ahead: bf16 4096 x 4096 would take 357 us forward and 1300 backward from
+// checkpoints, where the staged kernels take 37 and 54.  The widest rows that are staged, of multiples of 16 / of other widths:
+//   forward   bf16 all / all;  fp32 all / 14335
+//   backward  bf16 from checkpoints all / 16350, from bf16 all / 14431;  fp32 from checkpoints all / 12742, from fp32 14432 / 9624
 constexpr int kItems = 16;   // of up to 1024 threads: FALQON_NORM_MAX_COLS
 // Squares are divided by the width before they are added, so that only a mean beyond fp32's range overflows.
 template <typename T>
@@ -817,6 +818,7 @@ constexpr int kScaleBytes = 4;                                 // of a run, per 
 struct Run {
   int cols, stripes, warps, run, parts, part_spans, split, stripe_warps, buffers, weights_in_smem, blocks_per_row;
   int area, saved_area, buffer;                                // bytes: of a run of dx, of h or y, of a buffer
+  int scale_bytes;                                             // of all scales; 0 where h and y are saved as they are
 };
 // Shared memory behind the buffers.
 struct RunTail {
@@ -826,7 +828,7 @@ struct RunTail {
   uint32_t full;                                               // mbarriers, one per buffer
 };
 __device__ __host__ __forceinline__ size_t run_tail_bytes(const Run& r) {
-  return 16 + static_cast<size_t>(r.run) * r.parts * 16 + (static_cast<size_t>(4) * r.run * r.blocks_per_row + 15) / 16 * 16 + (r.weights_in_smem ? static_cast<size_t>(r.cols) * 8 : 0);
+  return 16 + static_cast<size_t>(r.run) * r.parts * 16 + r.scale_bytes + (r.weights_in_smem ? static_cast<size_t>(r.cols) * 8 : 0);
 }
 
 // Eight values of a run in shared memory.
@@ -935,7 +937,7 @@ __global__ void __launch_bounds__(512) norm_backward_run_kernel(const NormArgs a
     tail.full = smem_u32(p);
     tail.red = reinterpret_cast<float4*>(p + 16);
     tail.scales = p + 16 + static_cast<size_t>(sh.run) * sh.parts * 16;
-    tail.wsm = reinterpret_cast<float*>(tail.scales + (static_cast<size_t>(4) * sh.run * sh.blocks_per_row + 15) / 16 * 16);
+    tail.wsm = reinterpret_cast<float*>(tail.scales + sh.scale_bytes);
   }
   if (tid == 0) {
     for (int b = 0; b < sh.buffers; ++b) mbar_init(tail.full + 8 * b, 1);
@@ -1437,7 +1439,8 @@ int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
 }
 // How a backward's runs are cut: stripes per warp, rows per run, and the shared memory it takes; false where not even one row fits.
-bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_bytes, bool loose, int* spans, Run* r, size_t* smem) {
+bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, bool coded, bool loose, int* spans, Run* r, size_t* smem) {
+  const int saved_bytes = coded ? 1 : value_bytes;
   r->cols = static_cast<int>(cols);
   r->stripes = static_cast<int>((cols + 255) / 256);
   r->blocks_per_row = static_cast<int>((cols + kMx8Block - 1) / kMx8Block);
@@ -1466,8 +1469,9 @@ bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, int saved_b
       r->area = loose ? (run * r->cols * value_bytes + 47) / 16 * 16 : run * r->cols * value_bytes;
       r->saved_area = loose ? (run * r->cols * saved_bytes + 47) / 16 * 16 : run * r->cols * saved_bytes;
       r->buffer = (2 * r->area + 2 * r->saved_area + 127) / 128 * 128;
+      r->scale_bytes = coded ? (4 * run * r->blocks_per_row + 15) / 16 * 16 : 0;
       *smem = static_cast<size_t>(r->buffers) * r->buffer + run_tail_bytes(*r);
-      if (*smem <= static_cast<size_t>(kSmemLimit) && 2 * run * r->blocks_per_row <= kScaleBytes * 32 * r->warps)
+      if (*smem <= static_cast<size_t>(kSmemLimit) && (!coded || 2 * run * r->blocks_per_row <= kScaleBytes * 32 * r->warps))
         return true;
     }
   }
@@ -1486,7 +1490,7 @@ int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStrea
   size_t smem;
   int spans;
   const bool loose = !staged(a.cols);
-  if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded ? 1 : sizeof(T), loose, &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
+  if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded, loose, &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
   // the usual call: both norms, both gradients in and out, a residual, whole stripes (4096 x 4096 from checkpoints 57 us, as any call 74, side by side)
   const bool full = a.cols % 256 == 0 && r.weights_in_smem && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr &&
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;

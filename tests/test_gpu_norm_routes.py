@@ -35,3 +35,30 @@ def test_short_runs_of_narrow_rows_are_staged(tr, rows, cols, rpg, dtype, coded,
     """Few rows per CTA, and rows of one to a few spans: the warps that could share a run's columns are more than its rows."""
     names = [n for n, _, _ in launched(backward_call(tr, rows, cols, rpg, dtype, coded, gains)) if "norm_backward" in n]
     assert len(names) == 1 and "norm_backward_run_kernel" in names[0]
+
+
+# saved values, width, whether rows of it are staged: both sides of each limit
+LIMITS = [("bf16", True, 16350, True), ("bf16", True, 16351, False), ("bf16", True, 16384, True), ("bf16", False, 14431, True), ("bf16", False, 14433, False),
+          ("bf16", False, 16384, True), ("f32", True, 12742, True), ("f32", True, 12743, False), ("f32", True, 16384, True), ("f32", False, 14336, True),
+          ("f32", False, 14432, True), ("f32", False, 14448, False), ("f32", False, 9623, True), ("f32", False, 9625, False)]
+
+
+@pytest.mark.parametrize("dtype,coded,cols,staged", LIMITS)
+def test_the_widest_rows(tr, dtype, coded, cols, staged):
+    """On each side of the widths up to which a row is staged: the kernel, and the gradients against 64 bits."""
+    from tests import test_gpu_block_norm as norm
+    from tests import train_oracle as orc
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    names = [n for n, _, _ in launched(backward_call(tr, 3, cols, 2, dt, coded)) if "norm_backward" in n]
+    assert len(names) == 1 and ("norm_backward_run_kernel" in names[0]) == staged
+    t, kw = norm.inputs(3, cols, 2, True, True, True, True, dt, torch.float32, cols)
+    g, kg = {k: v.cuda() for k, v in t.items()}, norm.on_gpu(kw)
+    out = tr.block_norm_forward(g["h"], g["y"], save=coded, **kg)
+    saved = (out.saved_h, out.saved_y) if coded else (g["h"], g["y"])
+    got = tr.block_norm_backward(g["dx"], g["dh_out"], *saved, out.inv_post, out.inv_pre, **kg)
+    hd, yd = (torch.from_numpy(orc.decode(v.codes.cpu().numpy(), v.scales.cpu().numpy())) if coded else orc.d(v) for v in saved)
+    ref = norm.reference(3, cols, kw).backward(orc.d(t["dx"]), orc.d(t["dh_out"]), hd, yd, orc.d(out.inv_post), orc.d(out.inv_pre))
+    for name in ("dh", "dy"):
+        norm.close(getattr(got, name), *ref[name], dt, 64)
+    for name in ("dpost_gain", "dpre_gain", "dgate"):
+        norm.close(getattr(got, name), *ref[name], torch.float32, 64 + 3)
