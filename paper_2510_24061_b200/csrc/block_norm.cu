@@ -1423,20 +1423,28 @@ int start_rows(K kernel, DeviceMask& done, const NormArgs& a, const Shape& sh, s
   if (set_max_dynamic_smem(kernel, kSmemLimit, done) != cudaSuccess) return FALQON_ERR_CUDA;
   return finish(launch_pdl(kernel, dim3(static_cast<unsigned>(ctas)), dim3(static_cast<unsigned>(sh.groups * sh.group_threads)), smem, stream, 1, a, sh));
 }
+// Each kernel with as many CTAs as are resident: one per SM, or two of norm_forward_rows_kernel with two spans a lane (4096 x 5120 bf16 with the
+// norm before the next block only: 52 us, one per SM 73; fp32 with both norms: 73 and 84; fp32 4096 x 1024 and norms after the block only at
+// 4096 are the other way, by 5 to 7 %).
 template <typename T, int kNv>
-int launch_forward_rows(const NormArgs& a, int64_t ctas, cudaStream_t stream) {
+int launch_forward_rows(const falqon_block_norm* p, NormArgs a, cudaStream_t stream) {
   static DeviceMask done[3];
   Shape sh;
   size_t smem;
-  if (kNv == 2 && whole_spans(a.cols) && a.h != nullptr && a.h_out != nullptr && a.post && a.pre && (a.h_codes != nullptr) == (a.y_codes != nullptr) &&
-      make_full_shape(a.cols, kFullSpans, a.rows_per_piece, 2 * kFullSpans * 256 * sizeof(T), kSumFloats, &sh, &smem))
-    return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true, kFullSpans>, done[0], a, sh, smem, ctas, stream)
-                                : start_rows(norm_forward_full_kernel<T, false, kFullSpans>, done[1], a, sh, smem, ctas, stream);
+  if (kNv == 2 && whole_spans(a.cols) && a.h != nullptr && a.h_out != nullptr && a.post && a.pre && (a.h_codes != nullptr) == (a.y_codes != nullptr)) {
+    const Split s(p, kNormUnits);
+    s.put(&a);
+    if (make_full_shape(a.cols, kFullSpans, a.rows_per_piece, 2 * kFullSpans * 256 * sizeof(T), kSumFloats, &sh, &smem))
+      return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true, kFullSpans>, done[0], a, sh, smem, s.ctas, stream)
+                                  : start_rows(norm_forward_full_kernel<T, false, kFullSpans>, done[1], a, sh, smem, s.ctas, stream);
+  }
+  const Split s(p, kNv == 2 ? 2 * kNormUnits : kNormUnits);
+  s.put(&a);
   const int limit = kNv == 2 ? kSmemLimit / 2 - 1024 : kSmemLimit;       // two CTAs per SM
   if (!make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem) &&
       !make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, kSmemLimit, &sh, &smem))
     return FALQON_ERR_UNSUPPORTED;
-  return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, ctas, stream);
+  return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, s.ctas, stream);
 }
 // How a backward's runs are cut: stripes per warp, rows per run, and the shared memory it takes; false where not even one row fits.
 bool make_run(int64_t cols, int64_t rows_per_piece, int value_bytes, bool coded, bool loose, int* spans, Run* r, size_t* smem) {
@@ -1546,12 +1554,9 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
   a.y_scales = y_scales;
   a.amax = a.pre ? amax_x : nullptr;
   if (staged(a.cols)) {
-    const Split s(p, !whole_spans(a.cols) && spans_for(a.cols) == 2 ? 2 * kNormUnits : kNormUnits);   // as many CTAs as are resident
-    NormArgs b = a;
-    s.put(&b);
     const int rc = with_spans(spans_for(a.cols), [&](auto n) {
-      return p->dtype == FALQON_BF16 ? launch_forward_rows<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
-                                     : launch_forward_rows<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
+      return p->dtype == FALQON_BF16 ? launch_forward_rows<bf16_t, n.value>(p, a, static_cast<cudaStream_t>(stream))
+                                     : launch_forward_rows<float, n.value>(p, a, static_cast<cudaStream_t>(stream));
     });
     if (rc != FALQON_ERR_UNSUPPORTED) return rc;
   }

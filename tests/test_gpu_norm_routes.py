@@ -62,3 +62,35 @@ def test_the_widest_rows(tr, dtype, coded, cols, staged):
         norm.close(getattr(got, name), *ref[name], dt, 64)
     for name in ("dpost_gain", "dpre_gain", "dgate"):
         norm.close(getattr(got, name), *ref[name], torch.float32, 64 + 3)
+
+
+FORMS = {"both": {}, "post only": dict(pre=False), "pre only": dict(post=False), "no residual": dict(h=False), "frozen": dict(gate=False)}
+
+
+def forward_call(tr, rows, cols, dtype, form, save):
+    kw = dict(FORMS[form])
+    h, y = (torch.randn((rows, cols), device="cuda").to(dtype) for _ in range(2))
+    if not kw.pop("h", True):
+        h = None
+    gate = torch.rand((1, cols), device="cuda") if kw.pop("gate", True) else None
+    if kw.get("post", True):
+        kw["post_gain"] = one(cols)
+    if kw.get("pre", True):
+        kw["pre_gain"] = one(cols)
+    return lambda: tr.block_norm_forward(h, y, gate=gate, save=save, **kw)
+
+
+@pytest.mark.parametrize("save", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("cols", [1024, 4096, 4112, 5120, 8192, 9216, 4095])
+def test_every_forward_fills_the_gpu(tr, cols, form, dtype, save):
+    """As many CTAs as are resident: 148, one to an SM, or 296 of the kernel whose threads take two spans (it is compiled for two to an SM)."""
+    (name, ctas, _), = [v for v in launched(forward_call(tr, 2000, cols, dtype, form, save)) if "norm_forward" in v[0]]
+    rows = 2000
+    two = "norm_forward_rows_kernel" in name and cols <= 8192
+    per = -(-rows // (296 if two else 148))
+    assert ctas == -(-rows // per)
+    usual = form in ("both", "frozen") and cols % 1024 == 0 and cols <= 8192
+    if dtype == torch.bfloat16 and cols % 16 == 0:
+        assert ("norm_forward_full_kernel" in name) == usual
