@@ -80,8 +80,8 @@ __device__ __forceinline__ void cta_sums(float (&v)[kN], float* red, int& phase)
 //   backward  bf16 from checkpoints all / 16350, from bf16 all / 14431;  fp32 from checkpoints all / 12742, from fp32 14432 / 9624
 constexpr int kItems = 16;   // of up to 1024 threads: FALQON_NORM_MAX_COLS
 // Squares are divided by the width before they are added, so that only a mean beyond fp32's range overflows.
-template <typename T>
-__global__ void __launch_bounds__(1024, 1) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(1024, 1) norm_forward_f32_kernel(const NormArgs a) {
+  using T = float;                                             // bf16 rows always fit
   __shared__ float red[2 * 32];
   pdl_trigger();
   pdl_wait();
@@ -499,6 +499,7 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
 // instructions allow: 4096 x 4096 bf16 with both checkpoints 36.5 us (4.6 TB/s of what it must move; two spans a lane and two CTAs per
 // SM 42; the kernel above, for any call, 52), 8192 x 8192 without 98 us (5.5 TB/s; the kernel above 149).
 constexpr int kFullDepth = 2;                                  // two rows ahead per group cover the latency
+constexpr int kFullSpans = 4;
 
 template <typename T, int kNv>
 __device__ __forceinline__ void copy_lane(uint32_t dst, const T* src) {   // kNv spans of 256 columns; src: the lane's first value
@@ -507,11 +508,12 @@ __device__ __forceinline__ void copy_lane(uint32_t dst, const T* src) {   // kNv
   for (int j = 0; j < kNv * 256 / n; ++j) cp_async16(dst + 512 * j, src + n * j);
 }
 
-template <typename T, bool kCodes, int kNv>
-__global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_full_kernel(const NormArgs a, const Shape sh) {
+template <typename T, bool kCodes>
+__global__ void __launch_bounds__(512, 1) norm_forward_full_kernel(const NormArgs a, const Shape sh) {
   extern __shared__ __align__(16) uint8_t smem[];
   pdl_trigger();
   pdl_wait();
+  constexpr int kNv = kFullSpans;
   constexpr int kSpan = 256 * sizeof(T), kStage = 2 * kNv * kSpan;   // a stage holds [y, h][span]
   const Seat me(sh);
   const int cols = sh.cols, lane = me.lane, c0 = me.column<kNv>(), groups = sh.groups;
@@ -1407,7 +1409,6 @@ bool make_shape(int64_t cols, int nv, int64_t rows_per_cta, int set_bytes, int r
   return sh->depth >= 1;
 }
 
-constexpr int kFullSpans = 4;
 bool whole_spans(int64_t cols) { return cols % (256 * kFullSpans) == 0 && cols <= 8192; }
 // Shape of the usual call's kernels: a fixed depth and the weights in shared memory, or false.
 bool make_full_shape(int64_t cols, int nv, int64_t rows_per_cta, int stage_bytes, int red, Shape* sh, size_t* smem) {
@@ -1435,15 +1436,13 @@ int launch_forward_rows(const falqon_block_norm* p, NormArgs a, cudaStream_t str
     const Split s(p, kNormUnits);
     s.put(&a);
     if (make_full_shape(a.cols, kFullSpans, a.rows_per_piece, 2 * kFullSpans * 256 * sizeof(T), kSumFloats, &sh, &smem))
-      return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true, kFullSpans>, done[0], a, sh, smem, s.ctas, stream)
-                                  : start_rows(norm_forward_full_kernel<T, false, kFullSpans>, done[1], a, sh, smem, s.ctas, stream);
+      return a.h_codes != nullptr ? start_rows(norm_forward_full_kernel<T, true>, done[0], a, sh, smem, s.ctas, stream)
+                                  : start_rows(norm_forward_full_kernel<T, false>, done[1], a, sh, smem, s.ctas, stream);
   }
   const Split s(p, kNv == 2 ? 2 * kNormUnits : kNormUnits);
   s.put(&a);
   const int limit = kNv == 2 ? kSmemLimit / 2 - 1024 : kSmemLimit;       // two CTAs per SM
-  if (!make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem) &&
-      !make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, kSmemLimit, &sh, &smem))
-    return FALQON_ERR_UNSUPPORTED;
+  if (!make_shape(a.cols, kNv, a.rows_per_piece, 2 * 256 * sizeof(T), kSumFloats, limit, &sh, &smem)) return FALQON_ERR_UNSUPPORTED;   // of no width
   return start_rows(norm_forward_rows_kernel<T, kNv>, done[2], a, sh, smem, s.ctas, stream);
 }
 // How a backward's runs are cut: stripes per warp, rows per run, and the shared memory it takes; false where not even one row fits.
@@ -1553,27 +1552,22 @@ int falqon_block_norm_forward(const falqon_block_norm* p, const void* h, const v
   a.y_codes = y_codes;
   a.y_scales = y_scales;
   a.amax = a.pre ? amax_x : nullptr;
-  if (staged(a.cols)) {
-    const int rc = with_spans(spans_for(a.cols), [&](auto n) {
+  if (staged(a.cols))
+    return with_spans(spans_for(a.cols), [&](auto n) {
       return p->dtype == FALQON_BF16 ? launch_forward_rows<bf16_t, n.value>(p, a, static_cast<cudaStream_t>(stream))
                                      : launch_forward_rows<float, n.value>(p, a, static_cast<cudaStream_t>(stream));
     });
-    if (rc != FALQON_ERR_UNSUPPORTED) return rc;
-  }
-  if (!staged(a.cols)) {
-    const Split s(p, kNormUnits);
-    NormArgs b = a;
-    s.put(&b);
-    const int rc = with_spans(loose_spans(a.cols, s.rows_per_piece), [&](auto n) {
-      return p->dtype == FALQON_BF16 ? launch_forward_loose<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
-                                     : launch_forward_loose<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
-    });
-    if (rc != FALQON_ERR_UNSUPPORTED) return rc;
-  }
+  const Split s(p, kNormUnits);
+  NormArgs b = a;
+  s.put(&b);
+  const int rc = with_spans(loose_spans(a.cols, s.rows_per_piece), [&](auto n) {
+    return p->dtype == FALQON_BF16 ? launch_forward_loose<bf16_t, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream))
+                                   : launch_forward_loose<float, n.value>(b, s.ctas, static_cast<cudaStream_t>(stream));
+  });
+  if (rc != FALQON_ERR_UNSUPPORTED || p->dtype == FALQON_BF16) return rc;
   const int64_t cap = static_cast<int64_t>(sm_count()) * 2;
   const dim3 grid(static_cast<unsigned>(a.rows < cap ? a.rows : cap)), block(item_threads(a.cols));
-  return finish(launch_pdl(p->dtype == FALQON_BF16 ? norm_forward_kernel<bf16_t> : norm_forward_kernel<float>, grid, block, 0,
-                           static_cast<cudaStream_t>(stream), 1, a));
+  return finish(launch_pdl(norm_forward_f32_kernel, grid, block, 0, static_cast<cudaStream_t>(stream), 1, a));
 }
 
 size_t falqon_block_norm_scratch_bytes(const falqon_block_norm* p) {

@@ -94,3 +94,23 @@ def test_every_forward_fills_the_gpu(tr, cols, form, dtype, save):
     usual = form in ("both", "frozen") and cols % 1024 == 0 and cols <= 8192
     if dtype == torch.bfloat16 and cols % 16 == 0:
         assert ("norm_forward_full_kernel" in name) == usual
+
+
+@pytest.mark.parametrize("dtype,cols,staged", [("bf16", 16383, True), ("f32", 14335, True), ("f32", 14337, False), ("f32", 16384, True)])
+def test_the_widest_rows_forward(tr, dtype, cols, staged):
+    """Only fp32 rows of odd widths ever leave the staged kernels, on either side of their limit; results against 64 bits."""
+    from tests import test_gpu_block_norm as norm
+    from tests import train_oracle as orc
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    t, kw = norm.inputs(3, cols, 2, True, True, True, True, dt, torch.float32, cols)
+    h, y, kg = t["h"].cuda(), t["y"].cuda(), norm.on_gpu(kw)
+    (name, _, _), = launched(lambda: tr.block_norm_forward(h, y, save=True, **kg))
+    assert ("norm_forward_f32_kernel" not in name) == staged
+    out = tr.block_norm_forward(h, y, save=True, **kg)
+    ref = norm.reference(3, cols, kw)
+    H, x = ref.forward(orc.d(t["h"]), orc.d(t["y"]))
+    norm.close(out.h_out, H, ref.H_size, dt, 32)
+    spread = 1 + (ref.H_size ** 2).mean(1, keepdim=True) / ((H ** 2).mean(1, keepdim=True) + kw["eps"])
+    norm.close(out.x, x, ref.H_size * ref.iq * ref.w2.abs() * spread, dt, 64)
+    e, vals = orc.encode(t["y"].double().numpy())
+    assert (out.saved_y.scales.cpu().numpy() == e).all() and (orc.e4m3_values()[out.saved_y.codes.cpu().numpy()] == vals).all()
