@@ -540,11 +540,12 @@ int parts_for(int64_t rows, int64_t vocab, int dtype) {
 // Vectors of a part, of a row that begins on a 16-byte boundary; the others' have one less at the most.
 int64_t chunk_for(int64_t vocab, int dtype, int parts) { return (vocab / (dtype == FALQON_BF16 ? 8 : 4) + parts - 1) / parts; }
 
-// A thread per row of the average sequence (or pair), a warp at least (1500 x 8000 bf16, four pairs, loss and gradient: 26.7 us, with 1024
-// threads 28.0).
+// A thread per row of the average sequence (or pair): 1500 x 8000 bf16, four pairs, loss and gradient 26.7 us, with 1024 threads 28.0.  Four warps
+// at least, since sequences differ and a thread takes several rows of a long one: 699 pairs of 2 rows and one of 8000, 1000 columns, 46 us, from
+// one warp on 135, from eight on 40, which 4096 pairs of 10 rows pay with 81 us, against 69 and 68.
 unsigned sequence_threads(int64_t rows, int64_t ctas) {
-  const int64_t t = (rows / ctas + 31) / 32 * 32;            // (a pair's rows vary: a thread takes several where they are more)
-  return static_cast<unsigned>(t < 32 ? 32 : t > kSeqThreads ? kSeqThreads : t);
+  const int64_t t = (rows / ctas + 31) / 32 * 32;
+  return static_cast<unsigned>(t < 128 ? 128 : t > kSeqThreads ? kSeqThreads : t);
 }
 
 // A warp to a row where a CTA's threads would not even have a vector each.  Loss and gradient of 12000 x 1500 bf16: 82 us by CTAs, 36 by

@@ -129,3 +129,51 @@ def test_the_pairs_arithmetic_is_rounded_once(tr, kind, smoothing, average):
         err, tol = (out.dlogp.cpu().double() - dlogp).abs(), once * dlogp.abs() + soft * bound + 2.0 ** -126 + 2.0 ** -48 * seq.abs().max()
         assert (err <= tol).all(), (beta, margin, float((err / tol).max()))
         assert abs(out.loss.item() - float(loss.mean())) <= 2.0 ** -23 * float(loss.abs().mean()) + soft * float(l.mean()) + 2.0 ** -48 * float(seq.abs().max())
+
+
+def check_skewed(tr, lens, vocab, seed, average, threads=None):
+    """logp, seq_logp, dlogp and the gradient where sequences differ much in length, rows counted and not in turn."""
+    cu = torch.tensor([0] + lens).cumsum(0)
+    rows, gen = sum(lens), torch.Generator().manual_seed(seed)
+    logits = torch.randn((rows, vocab), generator=gen) * 2
+    targets = torch.randint(0, vocab, (rows,), generator=gen)
+    targets[torch.rand(rows, generator=gen) < 0.4] = -100
+    spec = tr.PreferenceLoss("sigmoid", 0.01, 0.0, 0.1, average, 0.2)
+    call = lambda: tr.preference_forward(spec, logits.cuda(), targets.cuda(), cu.cuda())  # noqa: E731
+    out = call()
+    if threads is not None:
+        from tests.launches import launched
+        dev = logits.cuda(), targets.cuda(), cu.cuda()
+        (used,) = [t for n, _, t in launched(lambda: tr.preference_forward(spec, *dev)) if "sequence_kernel" in n]
+        assert used == threads
+    ref = torch.zeros(len(lens), dtype=torch.float64)
+    logp = torch.where(targets >= 0, torch.log_softmax(logits.double(), 1)[torch.arange(rows), targets.clamp(min=0)], 0.0)
+    assert float((out.logp.cpu().double() - logp).abs().max()) <= 2.0 ** -18                # a few units of 2^-23 of |d| + lse, below 20
+    seq, loss, dlogp, l, size, _ = pairs_from(out.logp.cpu().double(), targets, cu.tolist(), ref, spec)
+    soft, once = 4 * 2.0 ** -23, 2.0 ** -24 * (1 + 2.0 ** -20)
+    assert ((out.seq_logp.cpu().double() - seq).abs() <= once * seq.abs() + 2.0 ** -149).all()
+    assert ((out.pair_loss.cpu().double() - loss).abs() <= once * loss.abs() + soft * l.abs() + 2.0 ** -40).all()
+    got = out.dlogp.cpu().double()
+    assert ((got == 0) == (targets < 0)).all()
+    per = (size / len(size)).repeat_interleave(2).repeat_interleave(torch.tensor(lens))
+    assert ((got - dlogp).abs() <= once * dlogp.abs() + soft * per + 2.0 ** -126).all()
+    grad = tr.preference_backward(logits.cuda(), targets.cuda(), out).cpu().double()
+    one = torch.zeros((rows, vocab), dtype=torch.float64)
+    one[torch.arange(rows), targets.clamp(min=0)] = 1.0
+    want = got[:, None] * (one - torch.softmax(logits.double(), 1))
+    assert ((grad - want).abs() <= 2.0 ** -18 * got.abs()[:, None]).all()
+
+
+@pytest.mark.parametrize("average", [False, True])
+def test_many_short_pairs_and_one_long(tr, average):
+    """The CTA of a pair is sized by the average: it has to stay able to walk a long one."""
+    check_skewed(tr, [1, 1] * 699 + [2300, 2100], 40, 5, average, threads=128)
+    check_skewed(tr, [1, 0, 700, 3] + [2, 1] * 40, 2100, 6, average, threads=128)
+
+
+@pytest.mark.parametrize("average", [False, True])
+def test_more_rows_than_a_thread_remembers(tr, average):
+    """A thread keeps the marks of its first 64 rows and reads the others' again: 64 * 128 rows and more in one pair of many, and 64 * 1024 in
+    the only pair."""
+    check_skewed(tr, [1, 1] * 500 + [5000, 4500], 12, 7, average, threads=128)
+    check_skewed(tr, [36000, 35001], 7, 8, average, threads=1024)
