@@ -548,9 +548,20 @@ unsigned sequence_threads(int64_t rows, int64_t ctas) {
   return static_cast<unsigned>(t < 128 ? 128 : t > kSeqThreads ? kSeqThreads : t);
 }
 
-// A warp to a row where a CTA's threads would not even have a vector each.  Loss and gradient of 12000 x 1500 bf16: 82 us by CTAs, 36 by
-// warps; of 1500 x 8000, which is beyond this rule, 27 by CTAs, 35 by warps.
-bool by_warps(int64_t vocab, int dtype, int parts) { return parts == 1 && vocab / (dtype == FALQON_BF16 ? 8 : 4) < kRowThreads; }
+// A warp to a row where rows are short and enough of them, a CTA otherwise; by the 16-byte vectors of a row.  A CTA takes 5 us per 1000 rows
+// whatever their length; a warp, which has a few loads in flight only, needs ten or more beside it on its SM.  Loss and gradient, bf16, by
+// warps / by CTAs:
+//               1000 columns   2000        4000        6000        8000        12000
+//   300 rows     12.4 / 11.8   14.5 / 12.4 16.5 / 12.4 18.6 / 12.4 20.6 / 14.4
+//   1000 rows    12.4 / 14.4   14.2 / 15.1 16.5 / 16.5 23.5 / 17.3 28.7 / 20.8
+//   2400 rows    14.4 / 19.3   16.5 / 21.4 24.7 / 25.4 30.3 / 28.8 35.9 / 33.5 47.8 / 41.3
+//   4000 rows    16.5 / 24.7   20.7 / 30.8 29.0 / 34.9 37.3 / 41.3 45.8 / 49.4
+//   12000 rows   30.7 / 63.5   40.6 / 72.4 67.2 / 92.5 92.2 / 112  118 / 126
+//   16000 rows   36.5 / 81.2   50.5 / 96.8 84.2 / 124  115 / 149   147 / 164   208 / 221
+bool by_warps(int64_t rows, int64_t vocab, int dtype) {
+  const int64_t vecs = vocab / (dtype == FALQON_BF16 ? 8 : 4);
+  return vecs < 1024 && (rows >= 4000 || (vecs < 512 && 2 * vecs <= rows));            // then a row has one part
+}
 
 template <typename T>
 cudaError_t launch_row_stats(const void* logits, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts, bool warps, float2* out,
@@ -561,7 +572,7 @@ cudaError_t launch_row_stats(const void* logits, int64_t rows, int64_t vocab, in
 }
 cudaError_t launch_row_stats(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const int64_t* targets, int parts,
                              float2* out, float* target_logit, unsigned int* counter, int* status, cudaStream_t stream) {
-  const bool warps = by_warps(vocab, dtype, parts);
+  const bool warps = by_warps(rows, vocab, dtype);
   return dtype == FALQON_BF16 ? launch_row_stats<bf16_t>(logits, rows, vocab, ld, targets, parts, warps, out, target_logit, counter, status, stream)
                               : launch_row_stats<float>(logits, rows, vocab, ld, targets, parts, warps, out, target_logit, counter, status, stream);
 }
@@ -666,7 +677,7 @@ int falqon_preference_backward(const falqon_preference* p, const void* logits, c
   const int parts = parts_for(p->rows, p->vocab, p->dtype);
   const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 &&
                     (ld_out - p->ld) % (p->dtype == FALQON_BF16 ? 8 : 4) == 0;
-  const bool warps = by_warps(p->vocab, p->dtype, parts);
+  const bool warps = by_warps(p->rows, p->vocab, p->dtype);
   const int64_t per = warps ? kRowThreads / 32 : 1, chunk = chunk_for(p->vocab, p->dtype, parts);
   const float2* stats = reinterpret_cast<const float2*>(row_stats);
   const auto go = [&](auto kernel, auto* typed) {

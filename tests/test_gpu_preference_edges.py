@@ -177,3 +177,25 @@ def test_more_rows_than_a_thread_remembers(tr, average):
     the only pair."""
     check_skewed(tr, [1, 1] * 500 + [5000, 4500], 12, 7, average, threads=128)
     check_skewed(tr, [36000, 35001], 7, 8, average, threads=1024)
+
+
+@pytest.mark.parametrize("dtype,k", [(torch.bfloat16, 1), (torch.float32, 2)])
+@pytest.mark.parametrize("rows,vocab,warps", [(300, 2000, False), (300, 1000, True), (1000, 3990, True), (1000, 4100, False), (3990, 6000, False), (4000, 8100, True),
+                                              (4000, 8200, False), (12000, 2500, True), (49, 1000, False), (2, 6, True)])
+def test_a_warp_or_a_cta_to_a_row(tr, rows, vocab, warps, dtype, k):
+    """Both passes by the same rule, which looks at rows and columns."""
+    from tests.launches import launched
+    logits = torch.zeros((rows, vocab // k), dtype=dtype, device="cuda")
+    targets, cu = torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.tensor([0, rows // 2, rows], device="cuda")
+    def call():
+        out = tr.preference_forward(tr.PreferenceLoss(), logits, targets, cu)
+        return tr.preference_backward(logits, targets, out), out
+    used = {n: c for n, c, _ in launched(call) if "row_stats" in n or "logit_grad" in n}
+    assert len(used) == 2
+    for name, ctas in used.items():
+        assert ("Li32E" in name) == warps and (ctas == -(-rows // 8)) == warps, name
+
+
+@pytest.mark.parametrize("rows,vocab", [(1000, 2040), (4100, 2051), (4000, 4090)])
+def test_longer_rows_by_warps(tr, rows, vocab):
+    check_skewed(tr, [rows // 3, rows - rows // 3], vocab, vocab, False)
