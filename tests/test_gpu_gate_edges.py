@@ -84,3 +84,16 @@ def test_infinite_gates(tr):
         back = tr.checkpoint_load(kg, torch.float32).cpu()
         assert torch.isnan(back[0, :32]).all() and torch.isnan(back[1, 32:64]).all() and torch.isfinite(back[0, 32:]).all()
         assert np.array_equal(kg.scales.cpu().numpy() == 255, np.array([[1, 0, 0], [0, 1, 0]], dtype=bool))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols", [(300, 1024), (33, 1000), (65, 1011), (1, 7), (700, 33)])
+def test_backward_with_either_gradient_in_place(tr, rows, cols, dtype):
+    gen = torch.Generator().manual_seed(cols)
+    kg, ku = (tr.checkpoint_save(torch.randn((rows, cols), generator=gen).cuda()) for _ in range(2))
+    dz = torch.randn((rows, cols), generator=gen).to(dtype).cuda()
+    want = tr.gate_backward(kg, ku, dz)
+    for which in ("dg", "du"):
+        into = dz.clone()
+        got = tr.gate_backward(kg, ku, into, **{which: into})
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and got[which == "du"].data_ptr() == into.data_ptr()
