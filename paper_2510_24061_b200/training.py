@@ -10,7 +10,7 @@ Tensors are contiguous (logits may have a row pitch), on the current device, bf1
 from __future__ import annotations
 
 import ctypes as C
-from typing import NamedTuple, Optional, Union
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -216,6 +216,9 @@ class BlockNormOut(NamedTuple):
     saved_y: Optional[Checkpoint]
 
 
+_GAINS = ("post_gain", "pre_gain", "gate")
+
+
 class BlockNormGrad(NamedTuple):
     dh: Optional[torch.Tensor]
     dy: Optional[torch.Tensor]
@@ -245,13 +248,16 @@ def block_norm_forward(h: Optional[torch.Tensor], y: torch.Tensor, *, post: bool
                        post_gain: Optional[torch.Tensor] = None, pre_gain: Optional[torch.Tensor] = None,
                        gate: Optional[torch.Tensor] = None, rows_per_gate: Optional[int] = None, res_scale: float = 1.0,
                        gain_offset: float = 0.0, eps: float = 1e-6, save: bool = False, h_out: Optional[torch.Tensor] = None,
-                       x: Optional[torch.Tensor] = None, amax_x: Optional[torch.Tensor] = None) -> BlockNormOut:
+                       x: Optional[torch.Tensor] = None, amax_x: Optional[torch.Tensor] = None, need_h_out: bool = True) -> BlockNormOut:
     """falqon_block_norm_forward.  y [rows, cols]: what the block gave; h: the residual stream before it (None: there is none).
         n = rmsnorm(y) * (gain_offset + post_gain)      (n = y without post)
         h_out = res_scale * h + gate * n                gate [ceil(rows / rows_per_gate), cols], one row per rows_per_gate rows
         x = rmsnorm(h_out) * (gain_offset + pre_gain)   (with pre)
-    A gain or gate that is None is 1.  save: h and y are kept in 8 bits for the backward."""
+    A gain or gate that is None is 1.  save: h and y are kept in 8 bits for the backward.  need_h_out False (with pre): only x is wanted,
+    as before the head."""
     _matrix(y, "y")
+    if not need_h_out:
+        _need(pre and h_out is None, "a call without h_out is one with the norm before the next block and no h_out given")
     if h is not None:
         _like(h, y, "h")
     if h_out is not None:
@@ -264,14 +270,15 @@ def block_norm_forward(h: Optional[torch.Tensor], y: torch.Tensor, *, post: bool
     plan = _norm_plan(rows, cols, _dtype(y), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
     stream = _on_device(h, y, h_out, x, amax_x, post_gain, pre_gain, gate)
     dtype, dev = y.dtype, y.device
-    h_out = _new(rows, cols, dtype=dtype, device=dev) if h_out is None else h_out
+    h_out = _new(rows, cols, dtype=dtype, device=dev) if h_out is None and need_h_out else h_out
     x = _new(rows, cols, dtype=dtype, device=dev) if x is None and pre else x
     inv_post = _new(rows, dtype=torch.float32, device=dev) if post else None
     inv_pre = _new(rows, dtype=torch.float32, device=dev) if pre else None
     kh = _new_checkpoint(y) if save and h is not None else None
     ky = _new_checkpoint(y) if save else None
     fq._check("falqon_block_norm_forward",
-              lib.falqon_block_norm_forward(C.byref(plan), _ptr(h), y.data_ptr(), h_out.data_ptr(), _ptr(x), _ptr(inv_post), _ptr(inv_pre),
+              lib.falqon_block_norm_forward(C.byref(plan), _ptr(h), y.data_ptr(), h_out.data_ptr() if h_out is not None else None, _ptr(x), _ptr(inv_post),
+                                            _ptr(inv_pre),
                                             *((None, None) if kh is None else (kh.codes.data_ptr(), kh.scales.data_ptr())),
                                             *((None, None) if ky is None else (ky.codes.data_ptr(), ky.scales.data_ptr())),
                                             _ptr(amax_x), stream))
@@ -283,10 +290,11 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
                         post: bool = True, pre: bool = True, post_gain: Optional[torch.Tensor] = None,
                         pre_gain: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
                         rows_per_gate: Optional[int] = None, res_scale: float = 1.0, gain_offset: float = 0.0, eps: float = 1e-6,
-                        need_gains: bool = True, dh: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
-                        scratch: Optional[torch.Tensor] = None, amax_dy: Optional[torch.Tensor] = None) -> BlockNormGrad:
+                        need_gains: Union[bool, Sequence[str]] = True, need_dy: bool = True, dh: Optional[torch.Tensor] = None,
+                        dy: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None, amax_dy: Optional[torch.Tensor] = None) -> BlockNormGrad:
     """falqon_block_norm_backward.  dx, dh_out: gradients of x (None without pre) and h_out (None: 0); h, y: the forward's inputs,
-    as tensors or as its checkpoints; need_gains False: gains and gate are frozen and get no gradient.  dh or dy may be dx or dh_out."""
+    as tensors or as its checkpoints; need_gains False: gains and gate are frozen and get no gradient, or the names of those that do
+    ("post_gain", "pre_gain", "gate"); need_dy False: the block itself is frozen.  dh or dy may be dx or dh_out."""
     ref = dx if dx is not None else dh_out
     _need(ref is not None, "a backward needs dx or dh_out")
     _need(pre == (dx is not None), "dx goes with the norm before the next block")
@@ -319,14 +327,20 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
         _vector(inv_pre, rows, torch.float32, "inv_pre")
     if amax_dy is not None:
         _vector(amax_dy, 1, torch.float32, "amax_dy")
+    if not need_dy:
+        _need(dy is None and amax_dy is None, "dy or its absmax given where it is not wanted")
+    of_post = of_pre = of_gate = need_gains is True
+    if need_gains is not True and need_gains is not False:
+        _need(not isinstance(need_gains, str) and set(need_gains) <= set(_GAINS), f"need_gains must be a bool or some of {_GAINS}")
+        of_post, of_pre, of_gate = (name in need_gains for name in _GAINS)
     plan = _norm_plan(rows, cols, _dtype(ref), post, pre, post_gain, pre_gain, gate, rows_per_gate, res_scale, gain_offset, eps)
     stream = _on_device(dx, dh_out, inv_post, inv_pre, post_gain, pre_gain, gate, dh, dy, scratch, amax_dy, *kept)
     dev, dtype, f32 = ref.device, ref.dtype, torch.float32
     dh = _new(rows, cols, dtype=dtype, device=dev) if dh is None and h is not None else dh
-    dy = _new(rows, cols, dtype=dtype, device=dev) if dy is None else dy
-    dpost = _new(cols, dtype=f32, device=dev) if need_gains and post_gain is not None else None
-    dpre = _new(cols, dtype=f32, device=dev) if need_gains and pre_gain is not None else None
-    dgate = torch.empty(gate.shape, dtype=f32, device=dev) if need_gains and gate is not None else None
+    dy = _new(rows, cols, dtype=dtype, device=dev) if dy is None and need_dy else dy
+    dpost = _new(cols, dtype=f32, device=dev) if of_post and post_gain is not None else None
+    dpre = _new(cols, dtype=f32, device=dev) if of_pre and pre_gain is not None else None
+    dgate = torch.empty(gate.shape, dtype=f32, device=dev) if of_gate and gate is not None else None
     size = 0
     if dpost is not None or dpre is not None or dgate is not None:
         size = lib.falqon_block_norm_scratch_bytes(C.byref(plan))
@@ -334,7 +348,8 @@ def block_norm_backward(dx: Optional[torch.Tensor], dh_out: Optional[torch.Tenso
             scratch = _new(size, dtype=torch.uint8, device=dev)
         size = scratch.numel() * scratch.element_size()
     fq._check("falqon_block_norm_backward",
-              lib.falqon_block_norm_backward(C.byref(plan), _ptr(dx), _ptr(dh_out), *saved, _ptr(inv_post), _ptr(inv_pre), _ptr(dh), dy.data_ptr(),
+              lib.falqon_block_norm_backward(C.byref(plan), _ptr(dx), _ptr(dh_out), *saved, _ptr(inv_post), _ptr(inv_pre), _ptr(dh),
+                                             dy.data_ptr() if dy is not None else None,
                                              _ptr(dpost), _ptr(dpre), _ptr(dgate), _ptr(amax_dy), _ptr(scratch), size, stream))
     return BlockNormGrad(dh, dy, dpost, dpre, dgate)
 

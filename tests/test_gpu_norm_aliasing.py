@@ -46,3 +46,38 @@ def test_backward_in_place(tr, rows, cols, rpg, dtype, saved):
         got = tr.block_norm_backward(b["dx"], b["dh_out"], *kept, out.inv_post, out.inv_pre, dh=b.get(dh), dy=b.get(dy), **kw)
         for name, p, q in zip(want._fields, got, want):
             assert torch.equal(p, q), (dh, dy, name)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,rpg", SIZES)
+def test_forward_without_the_residual_stream(tr, rows, cols, rpg, dtype):
+    """Only x is wanted: what it is does not depend on it (another kernel may run: the same roundings in another order of the sums)."""
+    t, kw = inputs(rows, cols, rpg, True, True, True, True, dtype, torch.float32, 23)
+    ref = reference(rows, cols, kw)
+    H, x = ref.forward(orc.d(t["h"]), orc.d(t["y"]))
+    out = tr.block_norm_forward(t["h"].cuda(), t["y"].cuda(), need_h_out=False, save=True, **on_gpu(kw))
+    assert out.h_out is None and out.saved_h is not None
+    spread = 1 + (ref.H_size ** 2).mean(1, keepdim=True) / ((H ** 2).mean(1, keepdim=True) + kw["eps"])
+    close(out.x, x, ref.H_size * ref.iq * ref.w2.abs() * spread, dtype, 64)
+
+
+@pytest.mark.parametrize("saved", ["codes", "plain"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,rpg", SIZES)
+def test_backward_of_some_results(tr, rows, cols, rpg, dtype, saved):
+    """Every choice of gradients, each against 64 bits; what is not asked for is not there."""
+    t, kw = inputs(rows, cols, rpg, True, True, True, True, dtype, torch.float32, 24)
+    g, kg = {k: v.cuda() for k, v in t.items()}, on_gpu(kw)
+    out = tr.block_norm_forward(g["h"], g["y"], save=saved == "codes", **kg)
+    kept = (out.saved_h, out.saved_y) if saved == "codes" else (g["h"], g["y"])
+    hd, yd = (torch.from_numpy(orc.decode(v.codes.cpu().numpy(), v.scales.cpu().numpy())) if saved == "codes" else orc.d(v) for v in kept)
+    ref = reference(rows, cols, kw).backward(orc.d(t["dx"]), orc.d(t["dh_out"]), hd, yd, orc.d(out.inv_post), orc.d(out.inv_pre))
+    for need_dy, gains in ((False, True), (False, False), (True, ("gate",)), (True, ("pre_gain",)), (False, ("post_gain",)), (True, ("post_gain", "pre_gain"))):
+        got = tr.block_norm_backward(g["dx"], g["dh_out"], *kept, out.inv_post, out.inv_pre, need_dy=need_dy, need_gains=gains, **kg)
+        names = ("post_gain", "pre_gain", "gate") if gains is True else gains or ()
+        assert (got.dy is not None) == need_dy and [n for n in ("post_gain", "pre_gain", "gate") if getattr(got, "d" + n) is not None] == sorted(names, key=("post_gain", "pre_gain", "gate").index)
+        for name in ("dh", "dy"):
+            if getattr(got, name) is not None:
+                close(getattr(got, name), *ref[name], dtype, 64)
+        for name in names:
+            close(getattr(got, "d" + name), *ref["d" + name], torch.float32, 64 + min(rows, 700))

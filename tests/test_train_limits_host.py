@@ -61,3 +61,15 @@ def test_the_stream_is_found_without_torchs_private_entry(tr, monkeypatch):
     monkeypatch.setattr(tr.torch.cuda, "current_stream", lambda dev: Stream())
     monkeypatch.setattr(tr, "_raw_stream", None)
     assert tr._on_device() == 0x5EED
+
+
+def test_choices_of_results_are_checked(tr, monkeypatch):
+    monkeypatch.setattr(tr.torch.cuda, "current_device", lambda: 0)
+    x, inv = tr.torch.zeros((4, 64)), tr.torch.zeros(4)
+    one = tr.torch.zeros(1)
+    for call in (lambda: tr.block_norm_forward(x, x, pre=False, need_h_out=False), lambda: tr.block_norm_forward(x, x, h_out=x.clone(), need_h_out=False),
+                 lambda: tr.block_norm_backward(x, x, x, x, inv, inv, need_gains=("gain",)), lambda: tr.block_norm_backward(x, x, x, x, inv, inv, need_gains="gate"),
+                 lambda: tr.block_norm_backward(x, x, x, x, inv, inv, need_dy=False, dy=x.clone()),
+                 lambda: tr.block_norm_backward(x, x, x, x, inv, inv, need_dy=False, amax_dy=one)):
+        with pytest.raises(ValueError, match="wanted|need_gains|without h_out"):
+            call()
