@@ -5,6 +5,8 @@
 //              dwpre = sum_t dx * xh;  S_g = sum_{t in g} d * yh;  dgate_g = wpost * S_g;  dwpost = sum_g gate_g * S_g
 // The two means of a row's backward come out of ONE reduction, because the second is linear in the first:
 //   sum b * yh = sum q * yh * (dh_out + iq * a) - iq * mean(a * xh) * sum q * yh * xh.
+// Both forms are off by roundings of sum |q * yh * (dh_out + iq * a)|; so a row whose d nearly cancels, because dx is nearly along x and dh_out
+// is small, has a mean(b * yh) right to those terms' size and not to its own, as its d is itself.
 // Column sums: a CTA owns consecutive rows of one gate group and keeps its columns' sums in registers; the partial sums are
 // added in a fixed order by a second kernel, so every run gives the same bits.
 #include "../../include/falqon_train.h"
@@ -493,7 +495,7 @@ __global__ void __launch_bounds__(512, kNv == 2 ? 2 : 1) norm_forward_rows_kerne
   if (a.amax != nullptr) raise_amax(largest.bits(), a.amax);
 }
 
-// ---- forward, the usual call: both norms, a residual, every result, rows of 1024 columns per warp (1024, 2048, .. 8192)
+// ---- forward, the full call: both norms, a residual, every result, rows of 1024 columns per warp (1024, 2048, .. 8192)
 // The same work with nothing left to test in the row loop and offsets that advance by a row; four spans a lane (a row of 4096 columns
 // is 128 threads, four rows a CTA), so that a row's two reductions are shared by 1024 columns a warp.  HBM-bound as far as
 // instructions allow: 4096 x 4096 bf16 with both checkpoints 36.5 us (4.6 TB/s of what it must move; two spans a lane and two CTAs per
@@ -812,9 +814,10 @@ __global__ void __launch_bounds__(512) norm_forward_loose_kernel(const NormArgs 
 // values are formed twice, from shared memory.  In the terms of the file's head, with H in the place of xh = H * iq:
 //   t = dx * w;  g = dh_out + iq * t;  b = q * yh;  A = sum t * H, B = sum b * g, C = sum b * H
 //   d = g - k1 * H with k1 = iq^3 * A / cols;  dy = ip * (q * d - yh * k2) with k2 = (B - k1 * C) / cols
-// Bound by instructions, since every value is decoded and formed twice (issued on 48 % of cycles by 16 warps, the most whose registers and
-// shared memory fit): 4096 x 4096 from checkpoints 54 us with the finish below (3.1 TB/s of what it must move), 8192 x 5120 from bf16 121 us
-// (4.2 TB/s).  Rows in registers from the sums to the results, a barrier per row: 57 and 150 us.
+// Bound by instructions, since every value is decoded and formed twice, and by warps that the shares leave without work (issued on 48 % of
+// cycles by 16 warps, the most whose registers and shared memory fit: of 4096 columns from checkpoints a run is 3 rows, whose sums 12 warps share;
+// of 5120 columns, two stripes to a warp, 10 write the results): 4096 x 4096 from checkpoints 54 us with the finish below (3.1 TB/s of what it
+// must move), 8192 x 5120 from bf16 121 us (4.2 TB/s).  Rows in registers from the sums to the results, a barrier per row: 57 and 150 us.
 constexpr int kMaxRun = 32;                                    // a lane per row
 constexpr int kScaleBytes = 4;                                 // of a run, per thread
 struct Run {
@@ -1410,7 +1413,7 @@ bool make_shape(int64_t cols, int nv, int64_t rows_per_cta, int set_bytes, int r
 }
 
 bool whole_spans(int64_t cols) { return cols % (256 * kFullSpans) == 0 && cols <= 8192; }
-// Shape of the usual call's kernels: a fixed depth and the weights in shared memory, or false.
+// Shape of the full call's kernels: a fixed depth and the weights in shared memory, or false.
 bool make_full_shape(int64_t cols, int nv, int64_t rows_per_cta, int stage_bytes, int red, Shape* sh, size_t* smem) {
   sh->cols = static_cast<int>(cols);
   sh->group_threads = static_cast<int>(cols / (8 * nv));
@@ -1498,10 +1501,10 @@ int launch_backward_runs(const NormArgs& a, int64_t ctas, int* status, cudaStrea
   int spans;
   const bool loose = !staged(a.cols);
   if (!make_run(a.cols, a.rows_per_piece, sizeof(T), kCoded, loose, &spans, &r, &smem)) return FALQON_ERR_UNSUPPORTED;
-  // the usual call: both norms, both gradients in and out, a residual, whole stripes (4096 x 4096 from checkpoints 57 us, as any call 74, side by side)
+  // the full call: both norms, both gradients in and out, a residual, whole stripes (4096 x 4096 from checkpoints 57 us, as any call 74, side by side)
   const bool full = a.cols % 256 == 0 && r.weights_in_smem && (kCoded ? a.h_codes_in != nullptr : a.h != nullptr) && a.dx != nullptr && a.dh_out != nullptr &&
                     a.post && a.pre && a.dh != nullptr && a.dy != nullptr;
-  const auto go = [&](auto kind) {                             // 0: any call, 1: the usual call, 2: any width
+  const auto go = [&](auto kind) {                             // 0: any call, 1: the full call, 2: any width
     constexpr bool kFull = decltype(kind)::value == 1, kLoose = decltype(kind)::value == 2;
     if (spans == 1) return start_run<T, kCoded, 1, kFull, kLoose>(a, r, smem, ctas, status, stream);
     if (spans == 2) return start_run<T, kCoded, 2, kFull, kLoose>(a, r, smem, ctas, status, stream);

@@ -373,7 +373,7 @@ __device__ __forceinline__ void spread_factors(const Spread& p, const Rows& r, f
 }
 
 // Bound by instructions: finding and spreading the blocks' scales is most of them.  Four CTAs per SM cost a few spilled words and hide
-// the barriers and the shared-memory maxima: bf16 4096 x 11007 with both checkpoints 166 us, with three 208 (2.2 TB/s; 62 us at 11008).
+// the barriers and the shared-memory maxima: bf16 4096 x 11007 with both checkpoints 168 us, with three 208 (2.2 TB/s; 62 us at 11008).
 template <typename T, bool kGate>
 __global__ void __launch_bounds__(kThreads, 4) ragged_encode_kernel(const T* g, const T* u, T* z, const Rows r, uint8_t* g_codes, uint8_t* g_scales,
                                                                  uint8_t* u_codes, uint8_t* u_scales, float* amax) {
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) ragged_load_kernel(T* x, const Rows 
   }
 }
 
-// bf16 4096 x 11007: 88 us with four CTAs per SM (4.1 TB/s), 98 with three.
+// bf16 4096 x 11007: 89 us with four CTAs per SM (4.1 TB/s), 98 with three.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4) ragged_gate_backward_kernel(const uint8_t* g_codes, const uint8_t* g_scales, const uint8_t* u_codes,
                                                                         const uint8_t* u_scales, const T* dz, T* dg, T* du, const Rows r,
