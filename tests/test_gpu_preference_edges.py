@@ -89,7 +89,7 @@ def pairs_from(logp, targets, cu, ref, spec):
         l = (1 - eps) * (torch.relu(-D) + tail) + eps * (torch.relu(D) + tail)
         du = beta * (eps * torch.sigmoid(D) - (1 - eps) * torch.sigmoid(-D))
     elif spec.kind == "hinge":
-        l, du = torch.relu(1 - D), torch.where(D < 1, -beta, 0.0).double()
+        l, du = torch.relu(1 - D), torch.where(D < 1, -beta, torch.where(D >= 1, 0.0, D))      # the slope of a NaN is one
     else:
         l, du = (u - margin - 0.5 / beta) ** 2, 2 * (u - margin - 0.5 / beta)
     nll = weight / n[0::2]
@@ -97,7 +97,7 @@ def pairs_from(logp, targets, cu, ref, spec):
     dlogp = torch.zeros_like(logp)
     for i, (a, b) in enumerate(zip(cu, cu[1:])):
         dlogp[a:b] = torch.where(counted[a:b], coef[i], 0.0)
-    return seq, l - nll * total[0::2], dlogp, l, (du.abs() + (nll if spec.average else nll)), D
+    return seq, l - nll * total[0::2] if weight else l.clone(), dlogp, l, (du.abs() + (nll if spec.average else nll)), D
 
 
 @pytest.mark.parametrize("average", [False, True])
@@ -199,3 +199,27 @@ def test_a_warp_or_a_cta_to_a_row(tr, rows, vocab, warps, dtype, k):
 @pytest.mark.parametrize("rows,vocab", [(1000, 2040), (4100, 2051), (4000, 4090)])
 def test_longer_rows_by_warps(tr, rows, vocab):
     check_skewed(tr, [rows // 3, rows - rows // 3], vocab, vocab, False)
+
+
+@pytest.mark.parametrize("average", [False, True])
+@pytest.mark.parametrize("kind,smoothing", [("sigmoid", 0.0), ("sigmoid", 0.1), ("hinge", 0.0), ("ipo", 0.0)])
+def test_targets_that_cannot_be(tr, kind, smoothing, average):
+    """A target whose logit is -inf in the chosen, the rejected, both or neither sequence: infinite log-probabilities go through the pair's
+    arithmetic as through the formulas, and the other pairs are as without them."""
+    cu = torch.arange(0, 17, 2)
+    logits = torch.randn((16, 50), generator=torch.Generator().manual_seed(11))
+    targets = torch.arange(16) % 50
+    for row in (1, 6, 8, 10):                    # pair 0: chosen; pair 1: rejected; pair 2: both; pair 3: neither
+        logits[row, targets[row]] = float("-inf")
+    for nll in (0.0, 0.5):
+        spec = tr.PreferenceLoss(kind, 0.5, 0.25, smoothing, average, nll)
+        out = tr.preference_forward(spec, logits.cuda(), targets.cuda(), cu.cuda())
+        logp = out.logp.cpu().double()
+        assert torch.equal(torch.isinf(logp), torch.isin(torch.arange(16), torch.tensor([1, 6, 8, 10])))
+        seq, loss, dlogp, _, _, D = pairs_from(logp, targets, cu.tolist(), torch.zeros(8, dtype=torch.float64), spec)
+        if kind == "sigmoid" and smoothing == 0.0:
+            loss[1] = 0.0 + (-0.0 if nll == 0.0 else -nll / 2 * float(logp[4:6].sum()))     # 0 * inf of the other term is left out
+        assert torch.isinf(D[0]) and D[0] < 0 and torch.isinf(D[1]) and D[1] > 0 and torch.isnan(D[2]) and torch.isfinite(D[3])
+        for got, want in ((out.seq_logp, seq), (out.pair_loss, loss), (out.dlogp, dlogp)):
+            assert torch.allclose(got.cpu().double(), want, rtol=2.0 ** -21, atol=2.0 ** -30, equal_nan=True), (got, want)
+        assert torch.isnan(out.loss)
