@@ -1,0 +1,468 @@
+// The products of a linear layer held in 8 bits by blocks of 128 (include/falqon_dense.h), on the tensor cores:
+//   D[M][N] = sum over k of  a[i][k] * 2^(ea[i][k / 128] - 127) * b[j][k] * 2^(eb[j][k / 128] - 127)
+// The scales are powers of two, so the tensor core applies them itself (tcgen05.mma kind::mxf8f6f4.block_scale, whose blocks of 32
+// take the same byte four times) and a tile is accumulated in fp32 over all of K without leaving tensor memory; scales that are
+// not powers of two would have to be applied to every partial tile of 128 on its way through registers.
+//
+// Two CTAs of a cluster compute a tile of 256 x block_n (one tcgen05.mma cta_group::2), a persistent pair walking its tiles:
+//   warp 0        TMA producer: 128 rows of A and block_n / 2 rows of B per CTA and stage of 128 values of K
+//   warp 1        (leader) issues the MMAs
+//   warps 2..9    epilogue: tensor memory -> registers -> shared memory -> full 128-byte lines
+//   warps 10..13  scales: global memory -> tensor memory (tcgen05.st), four blocks of K at a time, the four bytes of a word
+// Tensor memory: the scales' ring takes 64 of the 512 columns, which leaves 448 for two accumulators of up to 256.  They overlap in
+// columns 192..255, and the epilogue reads those first: the next tile's MMAs start as soon as they are in registers, so that the
+// rest of the epilogue runs beside them.
+// The three products differ in how the codes lie (K-major or MN-major, no transposed copies) and in the strides of their scales.
+// Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
+#include <cuda.h>
+
+#include "../../include/falqon_dense.h"
+#include "gemm_common.cuh"
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace falqon {
+namespace {
+
+constexpr int kEpiWarps = 8, kScaleWarps = 4;
+constexpr int kThreads = 32 * (2 + kEpiWarps + kScaleWarps);
+constexpr uint32_t kStageBytes = 32 * 1024;          // 16 KB of A, up to 16 KB of B
+constexpr int kStages = 6;
+constexpr uint32_t kAccStride = 192;                 // the second accumulator's first column
+constexpr uint32_t kScaleCol0 = 448;                 // ring of kGroups entries of 4 (A) + 8 (B) columns
+constexpr int kGroups = 5;
+constexpr uint32_t kGroupCols = 12;
+constexpr int kGroupBlocks = 4;                      // blocks of K per entry: the bytes of a word
+constexpr uint32_t kStagingOff = kStages * kStageBytes;
+constexpr uint32_t kWordsOff = kStagingOff + kEpiWarps * 32 * 128;
+constexpr uint32_t kWordsBytes = 12 * 32 * 4;        // an entry's scale words, passed between the scale warps
+constexpr uint32_t kBarsOff = kWordsOff + kWordsBytes;
+constexpr uint32_t kSmem = kBarsOff + 256 + 1024;
+
+struct Scales {               // byte of row i and block kb: p[(i >> shift) * row + kb * block]
+  const uint8_t* p;
+  long long row, block;
+  int shift, rows;            // rows: how many i there are
+  bool words;                 // four blocks of a row are an aligned 32-bit word
+};
+
+struct ProductArgs {
+  int M, N, kblocks;
+  int m_tiles, n_tiles, block_n;
+  bool a_mn, b_mn;
+  uint32_t idesc;             // without N and the scale bytes
+  Scales sa, sb;
+  void* out;
+  bool bf16;
+  int* status;
+};
+
+__device__ __forceinline__ uint32_t scale_word(const Scales& s, int i, int kb, int kblocks) {
+  if (i >= s.rows) return 0x7F7F7F7Fu;        // rows that are not there: their codes are zero
+  const uint8_t* p = s.p + static_cast<long long>(i >> s.shift) * s.row + kb * s.block;
+  if (s.words) return ld_stream(reinterpret_cast<const uint32_t*>(p));
+  uint32_t w = 0u;
+#pragma unroll
+  for (int b = 0; b < kGroupBlocks; ++b)
+    if (kb + b < kblocks) w |= static_cast<uint32_t>(ld_stream(p + b * s.block)) << (8 * b);
+  return w;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw);
+  const uint32_t bars = base + kBarsOff;
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };
+  auto sf_full_bar = [&](int g) { return bars + 8u * (2 * kStages + g); };
+  auto sf_empty_bar = [&](int g) { return bars + 8u * (2 * kStages + kGroups + g); };
+  const uint32_t acc_full_bar = bars + 8u * (2 * kStages + 2 * kGroups), acc_empty_bar = acc_full_bar + 8u;
+  const uint32_t slot = acc_empty_bar + 8u;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensor_map(&map_a);
+    prefetch_tensor_map(&map_b);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);                       // the leader's expect_tx; the bytes of both CTAs
+      mbar_init(empty_bar(s), 1);                      // one commit to both CTAs
+    }
+    for (int g = 0; g < kGroups; ++g) {
+      mbar_init(sf_full_bar(g), 2 * kScaleWarps);      // the scale warps of both CTAs
+      mbar_init(sf_empty_bar(g), 1);
+    }
+    mbar_init(acc_full_bar, 1);
+    mbar_init(acc_empty_bar, 2 * kEpiWarps);
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(slot, kTmemCols);
+    tmem_relinquish_pair();
+  }
+  pdl_trigger();
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(gen + (slot - base));
+  pdl_wait();
+
+  const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  const int tiles = p.m_tiles * p.n_tiles;
+  bool aborted = false;
+  auto inst_n = [&](int n0) {        // columns of a tile: at the right edge rounded up to what a half may be
+    const int gran = p.b_mn ? 32 : 16;
+    return min(p.block_n, (p.N - n0 + gran - 1) / gran * gran);
+  };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    int stage = 0;
+    uint32_t phase = 0;
+    const uint32_t bytes = kATileBytes + (p.b_mn ? kMnChunkBytes : static_cast<uint32_t>(p.block_n >> 1) * kBlockKBytes);
+    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
+      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
+      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM;
+      const int bn0 = n0 + static_cast<int>(rank) * (inst_n(n0) >> 1);
+      for (int kb = 0; kb < p.kblocks; ++kb) {
+        if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) { aborted = true; break; }
+        if (elect_one()) {
+          if (leader) mbar_expect_tx(full_bar(stage), 2 * bytes);
+          const uint32_t fb = map_to_cta(full_bar(stage), 0);
+          const uint32_t a_dst = base + static_cast<uint32_t>(stage) * kStageBytes, b_dst = a_dst + kATileBytes;
+          if (p.a_mn) tma_load_2d_pair(a_dst, &map_a, fb, row0, kb * kBlockKBytes);
+          else        tma_load_2d_pair(a_dst, &map_a, fb, kb * kBlockKBytes, row0);
+          if (p.b_mn) tma_load_2d_pair(b_dst, &map_b, fb, bn0, kb * kBlockKBytes);
+          else        tma_load_2d_pair(b_dst, &map_b, fb, kb * kBlockKBytes, bn0);
+        }
+        __syncwarp();
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    for (int i = 0; i < kStages && !aborted; ++i) {   // the MMAs have let go of every stage before this CTA may leave
+      if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) aborted = true;
+      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    if (leader) {
+      int stage = 0, group = 0, acc = 0;
+      uint32_t phase = 0, sf_phase = 0, acc_phase = 0;
+      bool first = true;
+      const uint64_t a_desc0 = p.a_mn ? make_smem_desc(base, kMnChunkBytes, 1024) : make_smem_desc(base, 16, 1024);
+      const uint64_t b_desc0 = p.b_mn ? make_smem_desc(base + kATileBytes, kMnChunkBytes, 1024) : make_smem_desc(base + kATileBytes, 16, 1024);
+      const uint32_t a_step = (p.a_mn ? kUmmaK * 128 : kUmmaK) >> 4, b_step = (p.b_mn ? kUmmaK * 128 : kUmmaK) >> 4;
+      for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
+        const int n0 = (tile / p.m_tiles) * p.block_n;
+        const uint32_t idesc_n = p.idesc | (static_cast<uint32_t>(inst_n(n0) >> 3) << 17);
+        if (!first) {   // the tile before: its part of the overlap is in registers, everything older is stored
+          if (!mbar_wait_warp(acc_empty_bar, acc_phase, p.status)) { aborted = true; break; }
+          acc_phase ^= 1u;
+          tc_fence_after_sync();
+        }
+        first = false;
+        const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          const int byte = kb % kGroupBlocks;
+          if (byte == 0 && !mbar_wait_warp(sf_full_bar(group), sf_phase, p.status)) { aborted = true; break; }
+          if (!mbar_wait_warp(full_bar(stage), phase, p.status)) { aborted = true; break; }
+          tc_fence_after_sync();
+          const uint32_t off = (static_cast<uint32_t>(stage) * kStageBytes) >> 4;
+          const uint32_t sfa = tmem + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
+          const uint32_t idesc = idesc_n | (static_cast<uint32_t>(byte) << 29) | (static_cast<uint32_t>(byte) << 4);
+          const bool last = byte == kGroupBlocks - 1 || kb == p.kblocks - 1;
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kBlockKBytes / kUmmaK; ++k)
+              umma_mx8_pair(d, a_desc0 + off + k * a_step, b_desc0 + off + k * b_step, idesc, sfa, sfa + 4, (kb > 0 || k > 0) ? 1u : 0u);
+            umma_commit_pair(empty_bar(stage), 3);
+            if (last) umma_commit_pair(sf_empty_bar(group), 3);
+          }
+          __syncwarp();
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          if (last && ++group == kGroups) { group = 0; sf_phase ^= 1u; }
+        }
+        if (aborted) break;
+        if (elect_one()) umma_commit_pair(acc_full_bar, 3);
+        __syncwarp();
+        acc ^= 1;
+      }
+    }
+  } else if (warp >= 2 + kEpiWarps) {
+    // ------------------------------------------------------------ scales
+    const int q = warp & 3;                                   // this warp's quadrant of tensor memory
+    const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
+    uint32_t* words = reinterpret_cast<uint32_t*>(gen + kWordsOff);
+    int group = 0;
+    uint32_t phase = 0;
+    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
+      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
+      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM;
+      for (int kb = 0; kb < p.kblocks; kb += kGroupBlocks) {
+        // each warp fetches a quarter of the words (rows 32 q .. of A; two columns of B), all four write all of them
+        const uint32_t wa = scale_word(p.sa, row0 + 32 * q + lane, kb, p.kblocks);
+        const uint32_t wb0 = scale_word(p.sb, n0 + 32 * q + lane, kb, p.kblocks);
+        const uint32_t wb1 = p.block_n > 128 ? scale_word(p.sb, n0 + 128 + 32 * q + lane, kb, p.kblocks) : 0x7F7F7F7Fu;
+        words[q * 32 + lane] = wa;
+        words[(4 + q) * 32 + lane] = wb0;
+        words[(8 + q) * 32 + lane] = wb1;
+        asm volatile("bar.sync 1, %0;" ::"n"(kScaleWarps * 32) : "memory");
+        uint32_t va[4], vb[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) va[c] = words[c * 32 + lane];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) vb[c] = words[(4 + c) * 32 + lane];
+        aborted = !mbar_wait_warp(sf_empty_bar(group), phase ^ 1u, p.status);
+        if (!aborted) {
+          tc_fence_after_sync();
+          const uint32_t t = tmem + lane_base + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
+          tmem_st_32x32b_x4(t, va);
+          tmem_st_32x32b_x8(t + 4, vb);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_full_bar(group), 0));
+        }
+        // the words have been read; and all four warps leave together, or the barriers would be waited for in vain
+        uint32_t any;
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                     : "=r"(any) : "r"(static_cast<uint32_t>(aborted)), "n"(kScaleWarps * 32) : "memory");
+        aborted = any != 0;
+        if (aborted) break;
+        if (++group == kGroups) { group = 0; phase ^= 1u; }
+      }
+    }
+    // the MMAs have let go of every entry before this CTA may leave
+    for (int i = 0; i < kGroups && !aborted; ++i) {
+      if (!mbar_wait_warp(sf_empty_bar(group), phase ^ 1u, p.status)) aborted = true;
+      if (++group == kGroups) { group = 0; phase ^= 1u; }
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int chunks = (p.block_n + 63) / 64, low = (chunks + 1) / 2;       // chunks of 64 columns: half 0 takes [0, low) upwards,
+    const int count = half == 0 ? low : chunks - low;                       // half 1 [low, chunks) downwards: the overlap first
+    uint8_t* stage_out = gen + kStagingOff + (warp - 2) * 32 * 128;
+    const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
+    int acc = 0;
+    uint32_t full_phase = 0;
+    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
+      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
+      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM + quad * 32;
+      if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
+      full_phase ^= 1u;
+      tc_fence_after_sync();
+      const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
+      const int end = min(p.block_n, p.N - n0);
+      if (count == 0) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar, 0));
+      }
+      for (int i = 0; i < count; ++i) {
+        const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
+        uint32_t v0[32], v1[32];
+        __syncwarp();
+        tmem_ld_32x32b_x32(t + c0, v0);
+        tmem_ld_32x32b_x32(t + c0 + 32, v1);
+        tmem_ld_wait();
+        if (i == 0) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar, 0));
+        }
+        if (c0 >= end) continue;
+        uint8_t* my = stage_out + lane * 128;
+        const int sw = lane & 7;
+        // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
+        // so a piece lies inside or outside as a whole
+        auto flush = [&](int col, int per_piece, int esize) {
+          __syncwarp();
+          const int piece = lane & 7;
+          const bool in = col + piece * per_piece < end;
+#pragma unroll
+          for (int r0 = 0; r0 < 32; r0 += 4) {
+            const int r = r0 + (lane >> 3);
+            const uint4 val = *reinterpret_cast<const uint4*>(stage_out + r * 128 + ((piece ^ (r & 7)) << 4));
+            if (in && row0 + r < p.M)
+              *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (static_cast<long long>(row0 + r) * p.N + n0 + col + piece * per_piece) * esize) = val;
+          }
+          __syncwarp();
+        };
+        if (p.bf16) {
+          auto put = [&](const uint32_t (&v)[32], int first_piece) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint4 o;
+              o.x = pack_bf16x2(__uint_as_float(v[8 * j]), __uint_as_float(v[8 * j + 1]));
+              o.y = pack_bf16x2(__uint_as_float(v[8 * j + 2]), __uint_as_float(v[8 * j + 3]));
+              o.z = pack_bf16x2(__uint_as_float(v[8 * j + 4]), __uint_as_float(v[8 * j + 5]));
+              o.w = pack_bf16x2(__uint_as_float(v[8 * j + 6]), __uint_as_float(v[8 * j + 7]));
+              *reinterpret_cast<uint4*>(my + (((first_piece + j) ^ sw) << 4)) = o;
+            }
+          };
+          put(v0, 0);
+          put(v1, 4);
+          flush(c0, 8, 2);
+        } else {
+          auto put = [&](const uint32_t (&v)[32]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(my + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          };
+          put(v0);
+          flush(c0, 4, 4);
+          put(v1);
+          flush(c0 + 32, 4, 4);
+        }
+      }
+      acc ^= 1;
+    }
+  }
+
+  // ------------------------------------------------------------ common exit
+  if (aborted) {
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 200000ull) { }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem, kTmemCols);
+  }
+}
+
+struct Operand {
+  const uint8_t* codes;
+  int64_t rows, cols;     // as the codes lie
+  bool mn;                // contracted along its rows
+  int fmt;
+  Scales s;
+};
+
+cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
+  ProductArgs g{};
+  g.M = static_cast<int>(M);
+  g.N = static_cast<int>(N);
+  g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
+  g.m_tiles = static_cast<int>((M + 255) / 256);
+  const int64_t pairs_all = sm_count() / 2;
+  // The tile's width: what makes (waves of tiles) x (time of a tile) least; a tile's time goes with its width plus a constant part
+  // (A's rows, the pipeline's start).
+  int64_t best = 0;
+  for (int w = 256; w >= 64; w -= 32) {
+    const int64_t tiles = g.m_tiles * ((N + w - 1) / w), cost = ((tiles + pairs_all - 1) / pairs_all) * (w + 48);
+    if (best == 0 || cost < best) best = cost, g.block_n = w;
+  }
+  g.n_tiles = static_cast<int>((N + g.block_n - 1) / g.block_n);
+  g.a_mn = a.mn;
+  g.b_mn = b.mn;
+  // instruction descriptor of the block-scaled kinds: formats at 7 and 10, majors at 15 and 16, N / 8 at 17, E8M0 scales at 23,
+  // M / 16 at 24; the scale bytes of B at 4 and of A at 29
+  g.idesc = (static_cast<uint32_t>(a.fmt) << 7) | (static_cast<uint32_t>(b.fmt) << 10) | ((a.mn ? 1u : 0u) << 15) | ((b.mn ? 1u : 0u) << 16) |
+            (1u << 23) | (static_cast<uint32_t>(256 >> 4) << 24);
+  g.sa = a.s;
+  g.sb = b.s;
+  g.out = out;
+  g.bf16 = out_dt == FALQON_BF16;
+  g.status = device_status_ptr();
+  if (g.status == nullptr) return cudaErrorInvalidValue;
+  CUtensorMap ma, mb;
+  if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, 128)) return cudaErrorInvalidValue;
+  if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.block_n / 2))) return cudaErrorInvalidValue;
+  const int64_t tiles = static_cast<int64_t>(g.m_tiles) * g.n_tiles, pairs = tiles < pairs_all ? tiles : pairs_all;
+  static DeviceMask configured{0};
+  const cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(block_product_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, 2, ma, mb, g);
+}
+
+Scales scales_of(const uint8_t* p, int along, int64_t rows, int64_t cols, bool over_rows) {
+  // over_rows: the blocks of the contraction run down the rows and i counts columns; else they run along a row and i counts rows
+  const int64_t nb = (cols + 127) / 128;
+  Scales s{};
+  s.p = p;
+  s.rows = static_cast<int>(over_rows ? cols : rows);
+  if (along == FALQON_ALONG_ROW) s.row = nb, s.block = 1;
+  else if (along == FALQON_ALONG_COL) s.row = 1, s.block = cols;
+  else s.row = over_rows ? 1 : nb, s.block = over_rows ? nb : 1, s.shift = 7;
+  s.words = s.block == 1 && s.row % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 3) == 0;
+  return s;
+}
+
+bool ok16(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool fmt_ok(int f) { return f == FALQON_E4M3 || f == FALQON_E5M2; }
+// n and m multiples of 16; no dimension so long that a count of tiles or a coordinate leaves 31 bits
+bool layer_ok(int64_t T, int64_t n, int64_t m) {
+  constexpr int64_t kMost = int64_t{1} << 30;
+  return T >= 1 && n >= 16 && m >= 16 && n % 16 == 0 && m % 16 == 0 && T <= kMost && n <= kMost && m <= kMost;
+}
+bool tiles_ok(int64_t M, int64_t N) { return ((M + 255) / 256) <= (int64_t{1} << 29) / ((N + 63) / 64); }
+int finish(cudaError_t e) { return e == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA; }
+
+}  // namespace
+}  // namespace falqon
+
+using namespace falqon;
+
+extern "C" {
+
+int falqon_block_forward(const uint8_t* x_codes, const uint8_t* x_scales, falqon_fp8 x_fmt, const uint8_t* w_codes, const uint8_t* w_scales,
+                         falqon_fp8 w_fmt, int64_t T, int64_t n, int64_t m, void* y, int y_dtype, falqon_stream stream) {
+  if (!ok16(x_codes) || !ok16(w_codes) || !ok16(y) || x_scales == nullptr || w_scales == nullptr || !fmt_ok(x_fmt) || !fmt_ok(w_fmt) ||
+      (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
+    return FALQON_ERR_INVALID_ARG;
+  const Operand a{x_codes, T, n, false, x_fmt, scales_of(x_scales, FALQON_ALONG_ROW, T, n, false)};
+  const Operand b{w_codes, m, n, false, w_fmt, scales_of(w_scales, FALQON_TILE, m, n, false)};
+  return finish(launch_product(a, b, T, m, n, y, y_dtype, static_cast<cudaStream_t>(stream)));
+}
+
+int falqon_block_input_grad(const uint8_t* dy_codes, const uint8_t* dy_scales, falqon_fp8 dy_fmt, const uint8_t* w_codes,
+                            const uint8_t* w_scales, falqon_fp8 w_fmt, int64_t T, int64_t n, int64_t m, void* dx, int dx_dtype,
+                            falqon_stream stream) {
+  if (!ok16(dy_codes) || !ok16(w_codes) || !ok16(dx) || dy_scales == nullptr || w_scales == nullptr || !fmt_ok(dy_fmt) || !fmt_ok(w_fmt) ||
+      (dx_dtype != FALQON_BF16 && dx_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, n))
+    return FALQON_ERR_INVALID_ARG;
+  const Operand a{dy_codes, T, m, false, dy_fmt, scales_of(dy_scales, FALQON_ALONG_ROW, T, m, false)};
+  const Operand b{w_codes, m, n, true, w_fmt, scales_of(w_scales, FALQON_TILE, m, n, true)};
+  return finish(launch_product(a, b, T, n, m, dx, dx_dtype, static_cast<cudaStream_t>(stream)));
+}
+
+int falqon_block_weight_grad(const uint8_t* dy_codes, const uint8_t* dy_scales, falqon_fp8 dy_fmt, const uint8_t* x_codes,
+                             const uint8_t* x_scales, falqon_fp8 x_fmt, int64_t T, int64_t n, int64_t m, void* dw, int dw_dtype,
+                             falqon_stream stream) {
+  if (!ok16(dy_codes) || !ok16(x_codes) || !ok16(dw) || dy_scales == nullptr || x_scales == nullptr || !fmt_ok(dy_fmt) || !fmt_ok(x_fmt) ||
+      (dw_dtype != FALQON_BF16 && dw_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(m, n))
+    return FALQON_ERR_INVALID_ARG;
+  const Operand a{dy_codes, T, m, true, dy_fmt, scales_of(dy_scales, FALQON_ALONG_COL, T, m, true)};
+  const Operand b{x_codes, T, n, true, x_fmt, scales_of(x_scales, FALQON_ALONG_COL, T, n, true)};
+  return finish(launch_product(a, b, m, n, T, dw, dw_dtype, static_cast<cudaStream_t>(stream)));
+}
+
+size_t falqon_block_linear_scratch_bytes(int64_t T, int64_t n, int64_t m) {
+  if (!layer_ok(T, n, m) || !tiles_ok(T, m)) return 0;
+  return static_cast<size_t>(T * n + round_up(T * ((n + 127) / 128), 16));
+}
+
+int falqon_block_linear(const void* x, int x_dtype, const uint8_t* w_codes, const uint8_t* w_scales, falqon_fp8 w_fmt, int64_t T, int64_t n,
+                        int64_t m, void* y, int y_dtype, void* scratch, size_t scratch_bytes, falqon_stream stream) {
+  if (!ok16(x) || (x_dtype != FALQON_BF16 && x_dtype != FALQON_F32) || !ok16(w_codes) || !ok16(y) || w_scales == nullptr || !fmt_ok(w_fmt) ||
+      (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
+    return FALQON_ERR_INVALID_ARG;
+  if (!ok16(scratch) || scratch_bytes < falqon_block_linear_scratch_bytes(T, n, m)) return FALQON_ERR_WORKSPACE;
+  uint8_t* codes = static_cast<uint8_t*>(scratch);
+  uint8_t* scales = codes + T * n;
+  const int rc = falqon_block_quantize(x, x_dtype, T, n, n, FALQON_E4M3, FALQON_ALONG_ROW, codes, scales, stream);
+  if (rc != FALQON_OK) return rc;
+  return falqon_block_forward(codes, scales, FALQON_E4M3, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype, stream);
+}
+
+}  // extern "C"
