@@ -17,6 +17,7 @@
 #include <cuda.h>
 
 #include "../../include/falqon_dense.h"
+#include "block_linear.h"
 #include "gemm_common.cuh"
 #include "internal.h"
 #include "ptx.cuh"
@@ -57,15 +58,29 @@ struct ProductArgs {
   int* status;
 };
 
-__device__ __forceinline__ uint32_t scale_word(const Scales& s, int i, int kb, int kblocks) {
-  if (i >= s.rows) return 0x7F7F7F7Fu;        // rows that are not there: their codes are zero
-  const uint8_t* p = s.p + static_cast<long long>(i >> s.shift) * s.row + kb * s.block;
-  if (s.words) return ld_stream(reinterpret_cast<const uint32_t*>(p));
-  uint32_t w = 0u;
+// The four bytes of a row on their way: together in [0] where they are an aligned word, else one in each.  Nothing touches them
+// before they are needed -- putting them together at once would wait for each load.
+struct Bytes { uint32_t v[kGroupBlocks]; };
+
+__device__ __forceinline__ const uint8_t* scale_row(const Scales& s, int i) {
+  return i < s.rows ? s.p + static_cast<long long>(i >> s.shift) * s.row : nullptr;     // null: a row that is not there
+}
+__device__ __forceinline__ void scale_fetch(Bytes& w, const Scales& s, const uint8_t* row, int kb, int kblocks) {
+  if (row == nullptr) {
 #pragma unroll
-  for (int b = 0; b < kGroupBlocks; ++b)
-    if (kb + b < kblocks) w |= static_cast<uint32_t>(ld_stream(p + b * s.block)) << (8 * b);
-  return w;
+    for (int b = 0; b < kGroupBlocks; ++b) w.v[b] = 0u;          // its codes are zero, any scale that is not 255 will do
+    return;
+  }
+  const uint8_t* p = row + kb * s.block;
+  if (s.words) {
+    w.v[0] = ld_stream(reinterpret_cast<const uint32_t*>(p));
+    return;
+  }
+#pragma unroll
+  for (int b = 0; b < kGroupBlocks; ++b, p += s.block) w.v[b] = kb + b < kblocks ? ld_stream(p) : 0u;
+}
+__device__ __forceinline__ uint32_t scale_word(const Bytes& w, const Scales& s) {
+  return s.words ? w.v[0] : w.v[0] | w.v[1] << 8 | w.v[2] << 16 | w.v[3] << 24;
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -199,19 +214,41 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     const int q = warp & 3;                                   // this warp's quadrant of tensor memory
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
     uint32_t* words = reinterpret_cast<uint32_t*>(gen + kWordsOff);
+    // Each warp fetches a quarter of an entry's words (rows 32 q .. of A, two columns of B), all four write all of them.  kAhead
+    // entries' words are on their way, in registers that no copy touches before they are needed (a queue that moved them waited for
+    // each load: 4096 x 16384 x 4096 333 us).
+    constexpr int kAhead = 3;
+    struct Entry { Bytes a, b0, b1; };
+    int next_tile = pair, next_kb = 0;
+    const uint8_t *row_a = nullptr, *row_b0 = nullptr, *row_b1 = nullptr;
+    auto fetch = [&](Entry& w) {
+      if (next_tile >= tiles) return;
+      if (next_kb == 0) {
+        const int n_idx = next_tile / p.m_tiles, n0 = n_idx * p.block_n;
+        row_a = scale_row(p.sa, (next_tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM + 32 * q + lane);
+        row_b0 = scale_row(p.sb, n0 + 32 * q + lane);
+        row_b1 = p.block_n > 128 ? scale_row(p.sb, n0 + 128 + 32 * q + lane) : nullptr;
+      }
+      scale_fetch(w.a, p.sa, row_a, next_kb, p.kblocks);
+      scale_fetch(w.b0, p.sb, row_b0, next_kb, p.kblocks);
+      scale_fetch(w.b1, p.sb, row_b1, next_kb, p.kblocks);
+      next_kb += kGroupBlocks;
+      if (next_kb >= p.kblocks) next_kb = 0, next_tile += pairs;
+    };
     int group = 0;
     uint32_t phase = 0;
-    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
-      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
-      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM;
-      for (int kb = 0; kb < p.kblocks; kb += kGroupBlocks) {
-        // each warp fetches a quarter of the words (rows 32 q .. of A; two columns of B), all four write all of them
-        const uint32_t wa = scale_word(p.sa, row0 + 32 * q + lane, kb, p.kblocks);
-        const uint32_t wb0 = scale_word(p.sb, n0 + 32 * q + lane, kb, p.kblocks);
-        const uint32_t wb1 = p.block_n > 128 ? scale_word(p.sb, n0 + 128 + 32 * q + lane, kb, p.kblocks) : 0x7F7F7F7Fu;
-        words[q * 32 + lane] = wa;
-        words[(4 + q) * 32 + lane] = wb0;
-        words[(8 + q) * 32 + lane] = wb1;
+    Entry ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) fetch(ahead[j]);
+    const int steps = (tiles - pair + pairs - 1) / pairs * ((p.kblocks + kGroupBlocks - 1) / kGroupBlocks);
+    for (int step0 = 0; step0 < steps && !aborted; step0 += kAhead) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (step0 + j >= steps || aborted) break;
+        words[q * 32 + lane] = scale_word(ahead[j].a, p.sa);
+        words[(4 + q) * 32 + lane] = scale_word(ahead[j].b0, p.sb);
+        words[(8 + q) * 32 + lane] = scale_word(ahead[j].b1, p.sb);
+        fetch(ahead[j]);
         asm volatile("bar.sync 1, %0;" ::"n"(kScaleWarps * 32) : "memory");
         uint32_t va[4], vb[8];
 #pragma unroll
@@ -227,7 +264,8 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           tmem_st_wait();
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(sf_full_bar(group), 0));
+          // (a release at cluster scope would wait for the loads ahead, too: 281 us instead of 253)
+          if (lane == 0) mbar_arrive_remote(map_to_cta(sf_full_bar(group), 0));
         }
         // the words have been read; and all four warps leave together, or the barriers would be waited for in vain
         uint32_t any;
@@ -263,7 +301,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       if (count == 0) {
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar, 0));
+        if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, 0));
       }
       for (int i = 0; i < count; ++i) {
         const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
@@ -275,7 +313,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         if (i == 0) {
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty_bar, 0));
+          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, 0));
         }
         if (c0 >= end) continue;
         uint8_t* my = stage_out + lane * 128;
@@ -355,11 +393,11 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
   g.m_tiles = static_cast<int>((M + 255) / 256);
   const int64_t pairs_all = sm_count() / 2;
-  // The tile's width: what makes (waves of tiles) x (time of a tile) least; a tile's time goes with its width plus a constant part
-  // (A's rows, the pipeline's start).
+  // The tile's width: what makes (waves of tiles) x (time of a tile) least; a tile's time goes with the bytes that its
+  // operands bring through L2, 256 rows of A and w of B (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 less).
   int64_t best = 0;
   for (int w = 256; w >= 64; w -= 32) {
-    const int64_t tiles = g.m_tiles * ((N + w - 1) / w), cost = ((tiles + pairs_all - 1) / pairs_all) * (w + 48);
+    const int64_t tiles = g.m_tiles * ((N + w - 1) / w), cost = ((tiles + pairs_all - 1) / pairs_all) * (w + 256);
     if (best == 0 || cost < best) best = cost, g.block_n = w;
   }
   g.n_tiles = static_cast<int>((N + g.block_n - 1) / g.block_n);
@@ -420,6 +458,9 @@ int falqon_block_forward(const uint8_t* x_codes, const uint8_t* x_scales, falqon
   if (!ok16(x_codes) || !ok16(w_codes) || !ok16(y) || x_scales == nullptr || w_scales == nullptr || !fmt_ok(x_fmt) || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
+  if (T <= kMostFew)
+    return finish(launch_block_linear_codes(x_codes, x_scales, x_fmt, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
+                                            static_cast<cudaStream_t>(stream)));
   const Operand a{x_codes, T, n, false, x_fmt, scales_of(x_scales, FALQON_ALONG_ROW, T, n, false)};
   const Operand b{w_codes, m, n, false, w_fmt, scales_of(w_scales, FALQON_TILE, m, n, false)};
   return finish(launch_product(a, b, T, m, n, y, y_dtype, static_cast<cudaStream_t>(stream)));
@@ -448,7 +489,7 @@ int falqon_block_weight_grad(const uint8_t* dy_codes, const uint8_t* dy_scales, 
 }
 
 size_t falqon_block_linear_scratch_bytes(int64_t T, int64_t n, int64_t m) {
-  if (!layer_ok(T, n, m) || !tiles_ok(T, m)) return 0;
+  if (!layer_ok(T, n, m) || !tiles_ok(T, m) || block_linear_plain(T, n)) return 0;
   return static_cast<size_t>(T * n + round_up(T * ((n + 127) / 128), 16));
 }
 
@@ -457,6 +498,9 @@ int falqon_block_linear(const void* x, int x_dtype, const uint8_t* w_codes, cons
   if (!ok16(x) || (x_dtype != FALQON_BF16 && x_dtype != FALQON_F32) || !ok16(w_codes) || !ok16(y) || w_scales == nullptr || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
+  if (block_linear_plain(T, n))
+    return finish(launch_block_linear_plain(x, x_dtype == FALQON_BF16, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
+                                            static_cast<cudaStream_t>(stream)));
   if (!ok16(scratch) || scratch_bytes < falqon_block_linear_scratch_bytes(T, n, m)) return FALQON_ERR_WORKSPACE;
   uint8_t* codes = static_cast<uint8_t*>(scratch);
   uint8_t* scales = codes + T * n;

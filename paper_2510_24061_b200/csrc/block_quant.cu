@@ -30,124 +30,212 @@ struct QuantArgs {
   uint8_t *col_codes, *col_scales;   // along columns
 };
 
-// How a warp lies on its 16 rows of the tile.  Vectors: 16 lanes x 8 values a row, two rows at a time (16-byte loads, 8-byte stores).
-// Singles (rows that are not 16-byte aligned, or a width that is no multiple of eight): 32 lanes, values 32 apart, a row at a time.
-template <bool kVec>
-struct Lay {
-  static constexpr int kValues = kVec ? 8 : 4;           // of a lane in a row
-  static constexpr int kPasses = 64 / kValues;
-  static __device__ __forceinline__ int row(int lane, int pass) { return kVec ? 2 * pass + (lane >> 4) : pass; }
-  static __device__ __forceinline__ int col(int lane, int j) { return kVec ? (lane & 15) * 8 + j : lane + 32 * j; }
+// Maxima of eight columns: of bf16 as pairs in the type itself, of fp32 as bit patterns without the sign.
+template <typename T>
+struct ColMax;
+template <>
+struct ColMax<bf16_t> {
+  uint32_t m[4] = {0u, 0u, 0u, 0u};
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ __forceinline__ void see(const Vec8<bf16_t>& v) {
+    const uint32_t w[4] = {v.q.x, v.q.y, v.q.z, v.q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = larger(m[k], w[k] & 0x7FFF7FFFu);
+  }
+  __device__ __forceinline__ void across(int s) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = larger(m[k], __shfl_xor_sync(0xFFFFFFFFu, m[k], s));
+  }
+  __device__ __forceinline__ uint32_t bits(int j) const { return j & 1 ? m[j >> 1] & 0xFFFF0000u : m[j >> 1] << 16; }
+};
+template <>
+struct ColMax<float> {
+  uint32_t m[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+  __device__ __forceinline__ void see(const Vec8<float>& v) {
+    const float x[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = max(m[k], abs_bits(x[k]));
+  }
+  __device__ __forceinline__ void across(int s) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = max(m[k], __shfl_xor_sync(0xFFFFFFFFu, m[k], s));
+  }
+  __device__ __forceinline__ uint32_t bits(int j) const { return m[j]; }
 };
 
-template <typename T, int kFmt, bool kVec, bool kRow, bool kCol, bool kTile>
-__global__ void __launch_bounds__(kThreads)
+template <int kFmt, typename T>
+__device__ __forceinline__ uint2 codes8(const Vec8<T>& v, const float (&f)[8]) {
+  float x[8];
+  v.unpack(x);
+  return make_uint2(cvt_fp8x4<kFmt>(x[0] * f[0], x[1] * f[1], x[2] * f[2], x[3] * f[3]), cvt_fp8x4<kFmt>(x[4] * f[4], x[5] * f[5], x[6] * f[6], x[7] * f[7]));
+}
+
+// Rows of whole 16-byte vectors.  A warp lies on 16 rows of the tile, two at a time, 16 lanes x 8 values to a row; values stay as they
+// came (bf16: half the registers).
+template <typename T, int kFmt, bool kRow, bool kCol, bool kTile>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2)
 block_quant_kernel(const T* x, const QuantArgs a) {
-  using L = Lay<kVec>;
-  __shared__ uint32_t s_max[kWarps][kB];
+  constexpr int kPasses = 8;
+  __shared__ __align__(16) uint32_t s_max[kWarps][kB];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t tile_r = blockIdx.x / a.col_tiles, tile_c = blockIdx.x - tile_r * a.col_tiles;
-  const int64_t row0 = tile_r * kB + warp * 16, col0 = tile_c * kB;
-  const bool col_in = col0 + L::col(lane, 0) < a.cols;   // vectors are inside or outside as a whole
+  const int64_t row0 = tile_r * kB + warp * 16 + (lane >> 4), col = tile_c * kB + (lane & 15) * 8;
+  const bool col_in = col < a.cols;      // a vector is inside or outside as a whole
 
-  float v[L::kPasses][L::kValues];
+  Vec8<T> v[kPasses];
 #pragma unroll
-  for (int p = 0; p < L::kPasses; ++p) {
-    const int64_t r = row0 + L::row(lane, p);
-    const T* src = x + r * a.ld + col0;
-    if constexpr (kVec) {
-      Vec8<T> q;
-      if (r < a.rows && col_in) q.load(src + L::col(lane, 0)); else q.zero();
-      q.unpack(v[p]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < L::kValues; ++j)
-        v[p][j] = r < a.rows && col0 + L::col(lane, j) < a.cols ? load1(src + L::col(lane, j)) : 0.0f;
-    }
+  for (int p = 0; p < kPasses; ++p) {
+    if (col_in && row0 + 2 * p < a.rows) v[p].load(x + (row0 + 2 * p) * a.ld + col); else v[p].zero();
   }
-
-  auto store = [&](uint8_t* codes, int p, const float (&f)[L::kValues]) {
-    const int64_t r = row0 + L::row(lane, p);
-    if (r >= a.rows) return;
-    uint8_t* dst = codes + r * a.cols + col0;
-    if constexpr (kVec) {
-      if (col_in)
-        *reinterpret_cast<uint2*>(dst + L::col(lane, 0)) =
-            make_uint2(cvt_fp8x4<kFmt>(v[p][0] * f[0], v[p][1] * f[1], v[p][2] * f[2], v[p][3] * f[3]),
-                       cvt_fp8x4<kFmt>(v[p][4] * f[4], v[p][5] * f[5], v[p][6] * f[6], v[p][7] * f[7]));
-    } else {
+  auto store = [&](uint8_t* codes, int p, const float (&f)[8]) {
+    if (col_in && row0 + 2 * p < a.rows) *reinterpret_cast<uint2*>(codes + (row0 + 2 * p) * a.cols + col) = codes8<kFmt>(v[p], f);
+  };
+  auto same = [](float (&f)[8], float y) {
 #pragma unroll
-      for (int j = 0; j < L::kValues; ++j)
-        if (col0 + L::col(lane, j) < a.cols) dst[L::col(lane, j)] = static_cast<uint8_t>(cvt_fp8x2<kFmt>(v[p][j] * f[j], 0.0f) & 0xFFu);
-    }
+    for (int j = 0; j < 8; ++j) f[j] = y;
   };
 
+  ColMax<T> m;
+  if constexpr (kCol || kTile) {
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) m.see(v[p]);
+    m.across(16);
+  }
+  if constexpr (kCol) {
+    if (lane < 16) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s_max[warp][lane * 8 + j] = m.bits(j);
+    }
+  }
+  if constexpr (kTile) {
+    uint32_t all = m.bits(0);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) all = max(all, m.bits(j));
+    all = __reduce_max_sync(0xFFFFFFFFu, all);
+    if (lane == 0) s_max[warp][0] = all;
+  }
   if constexpr (kRow) {
-    const int64_t blocks = a.col_tiles;
 #pragma unroll
-    for (int p = 0; p < L::kPasses; ++p) {
-      uint32_t m = 0u;
+    for (int p = 0; p < kPasses; ++p) {
+      uint32_t r = v[p].max_abs();
 #pragma unroll
-      for (int j = 0; j < L::kValues; ++j) m = max(m, abs_bits(v[p][j]));
-#pragma unroll
-      for (int s = 1; s < (kVec ? 16 : 32); s <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
-      const uint32_t e = scale_byte<kFmt>(m);
-      float f[L::kValues];
-#pragma unroll
-      for (int j = 0; j < L::kValues; ++j) f[j] = mx8_encode_factor(e);
+      for (int s = 1; s < 16; s <<= 1) r = max(r, __shfl_xor_sync(0xFFFFFFFFu, r, s));
+      const uint32_t e = scale_byte<kFmt>(r);
+      float f[8];
+      same(f, mx8_encode_factor(e));
       store(a.row_codes, p, f);
-      const int64_t r = row0 + L::row(lane, p);
-      if ((lane & (kVec ? 15 : 31)) == 0 && r < a.rows) a.row_scales[r * blocks + tile_c] = static_cast<uint8_t>(e);
+      if ((lane & 15) == 0 && row0 + 2 * p < a.rows) a.row_scales[(row0 + 2 * p) * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
+    }
+  }
+  if constexpr (kTile) {
+    __syncthreads();
+    uint32_t all = 0u;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) all = max(all, s_max[w][0]);
+    const uint32_t e = scale_byte<kFmt>(all);
+    if (threadIdx.x == 0) a.row_scales[tile_r * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
+    float f[8];
+    same(f, mx8_encode_factor(e));
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) store(a.row_codes, p, f);
+  }
+  if constexpr (kCol) {
+    __syncthreads();
+    // a column's maximum is taken by one thread and handed to the 16 that need it
+    if (threadIdx.x < kB) {
+      uint32_t c = 0u;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) c = max(c, s_max[w][threadIdx.x]);
+      const uint32_t e = scale_byte<kFmt>(c);
+      s_max[0][threadIdx.x] = __float_as_uint(mx8_encode_factor(e));
+      if (tile_c * kB + threadIdx.x < a.cols) a.col_scales[tile_r * a.cols + tile_c * kB + threadIdx.x] = static_cast<uint8_t>(e);
+    }
+    __syncthreads();
+    float f[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 q = *reinterpret_cast<const float4*>(&s_max[0][(lane & 15) * 8 + 4 * h]);
+      f[4 * h] = q.x, f[4 * h + 1] = q.y, f[4 * h + 2] = q.z, f[4 * h + 3] = q.w;
+    }
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) store(a.col_codes, p, f);
+  }
+}
+
+// Any other width, pitch or alignment: 32 lanes to a row, values 32 apart, a row at a time, four values a lane.
+template <typename T, int kFmt, bool kRow, bool kCol, bool kTile>
+__global__ void __launch_bounds__(kThreads, 2)
+block_quant_ragged_kernel(const T* x, const QuantArgs a) {
+  constexpr int kPasses = 16, kValues = 4;
+  __shared__ __align__(16) uint32_t s_max[kWarps][kB];
+  pdl_trigger();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t tile_r = blockIdx.x / a.col_tiles, tile_c = blockIdx.x - tile_r * a.col_tiles;
+  const int64_t row0 = tile_r * kB + warp * 16, col0 = tile_c * kB + lane;
+  float v[kPasses][kValues];
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p)
+#pragma unroll
+    for (int j = 0; j < kValues; ++j)
+      v[p][j] = row0 + p < a.rows && col0 + 32 * j < a.cols ? load1(x + (row0 + p) * a.ld + col0 + 32 * j) : 0.0f;
+  auto store = [&](uint8_t* codes, int p, const float (&f)[kValues]) {
+    if (row0 + p >= a.rows) return;
+#pragma unroll
+    for (int j = 0; j < kValues; ++j)
+      if (col0 + 32 * j < a.cols) codes[(row0 + p) * a.cols + col0 + 32 * j] = static_cast<uint8_t>(cvt_fp8x2<kFmt>(v[p][j] * f[j], 0.0f) & 0xFFu);
+  };
+  if constexpr (kRow) {
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      uint32_t r = 0u;
+#pragma unroll
+      for (int j = 0; j < kValues; ++j) r = max(r, abs_bits(v[p][j]));
+      const uint32_t e = scale_byte<kFmt>(__reduce_max_sync(0xFFFFFFFFu, r));
+      const float y = mx8_encode_factor(e), f[kValues] = {y, y, y, y};
+      store(a.row_codes, p, f);
+      if (lane == 0 && row0 + p < a.rows) a.row_scales[(row0 + p) * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
     }
   }
   if constexpr (kCol || kTile) {
-    uint32_t m[L::kValues];
+    uint32_t m[kValues];
 #pragma unroll
-    for (int j = 0; j < L::kValues; ++j) {
+    for (int j = 0; j < kValues; ++j) {
       m[j] = 0u;
 #pragma unroll
-      for (int p = 0; p < L::kPasses; ++p) m[j] = max(m[j], abs_bits(v[p][j]));
-      if (kVec) m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
+      for (int p = 0; p < kPasses; ++p) m[j] = max(m[j], abs_bits(v[p][j]));
+      s_max[warp][32 * j + lane] = m[j];
+    }
+    __syncthreads();
+    float f[kValues];
+    uint32_t c[kValues];
+#pragma unroll
+    for (int j = 0; j < kValues; ++j) {
+      c[j] = 0u;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) c[j] = max(c[j], s_max[w][32 * j + lane]);
     }
     if constexpr (kTile) {
-      uint32_t all = m[0];
-#pragma unroll
-      for (int j = 1; j < L::kValues; ++j) all = max(all, m[j]);
-      all = __reduce_max_sync(0xFFFFFFFFu, all);
-      if (lane == 0) s_max[warp][0] = all;
-      __syncthreads();
-      all = 0u;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) all = max(all, s_max[w][0]);
-      const uint32_t e = scale_byte<kFmt>(all);
+      const uint32_t e = scale_byte<kFmt>(__reduce_max_sync(0xFFFFFFFFu, max(max(c[0], c[1]), max(c[2], c[3]))));
       if (threadIdx.x == 0) a.row_scales[tile_r * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
-      float f[L::kValues];
 #pragma unroll
-      for (int j = 0; j < L::kValues; ++j) f[j] = mx8_encode_factor(e);
-#pragma unroll
-      for (int p = 0; p < L::kPasses; ++p) store(a.row_codes, p, f);
+      for (int j = 0; j < kValues; ++j) f[j] = mx8_encode_factor(e);
     } else {
-      if (!kVec || lane < 16) {
 #pragma unroll
-        for (int j = 0; j < L::kValues; ++j) s_max[warp][L::col(lane, j)] = m[j];
-      }
-      __syncthreads();
-      float f[L::kValues];
-#pragma unroll
-      for (int j = 0; j < L::kValues; ++j) {
-        uint32_t c = 0u;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) c = max(c, s_max[w][L::col(lane, j)]);
-        const uint32_t e = scale_byte<kFmt>(c);
+      for (int j = 0; j < kValues; ++j) {
+        const uint32_t e = scale_byte<kFmt>(c[j]);
         f[j] = mx8_encode_factor(e);
-        if (warp == 0 && (!kVec || lane < 16) && col0 + L::col(lane, j) < a.cols)
-          a.col_scales[tile_r * a.cols + col0 + L::col(lane, j)] = static_cast<uint8_t>(e);
+        if (warp == 0 && col0 + 32 * j < a.cols) a.col_scales[tile_r * a.cols + col0 + 32 * j] = static_cast<uint8_t>(e);
       }
-#pragma unroll
-      for (int p = 0; p < L::kPasses; ++p) store(a.col_codes, p, f);
     }
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) store(kTile ? a.row_codes : a.col_codes, p, f);
   }
 }
 
@@ -183,17 +271,23 @@ bool sizes_ok(int64_t rows, int64_t cols) {
 bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int finish(cudaError_t e) { return e == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA; }
 
-template <typename T, int kFmt, bool kVec>
-cudaError_t launch_of(int what, const T* x, const QuantArgs& a, int64_t tiles, cudaStream_t st) {
+constexpr int kBoth = 3;
+
+template <typename T, int kFmt, bool kRow, bool kCol, bool kTile>
+cudaError_t launch_one(const T* x, const QuantArgs& a, int64_t tiles, bool vec, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>(tiles)), block(kThreads);
+  return vec ? launch_pdl(block_quant_kernel<T, kFmt, kRow, kCol, kTile>, grid, block, 0, st, 1, x, a)
+             : launch_pdl(block_quant_ragged_kernel<T, kFmt, kRow, kCol, kTile>, grid, block, 0, st, 1, x, a);
+}
+template <typename T, int kFmt>
+cudaError_t launch_of(int what, const T* x, const QuantArgs& a, int64_t tiles, bool vec, cudaStream_t st) {
   switch (what) {
-    case FALQON_ALONG_ROW: return launch_pdl(block_quant_kernel<T, kFmt, kVec, true, false, false>, grid, block, 0, st, 1, x, a);
-    case FALQON_ALONG_COL: return launch_pdl(block_quant_kernel<T, kFmt, kVec, false, true, false>, grid, block, 0, st, 1, x, a);
-    case FALQON_TILE: return launch_pdl(block_quant_kernel<T, kFmt, kVec, false, false, true>, grid, block, 0, st, 1, x, a);
-    default: return launch_pdl(block_quant_kernel<T, kFmt, kVec, true, true, false>, grid, block, 0, st, 1, x, a);
+    case FALQON_ALONG_ROW: return launch_one<T, kFmt, true, false, false>(x, a, tiles, vec, st);
+    case FALQON_ALONG_COL: return launch_one<T, kFmt, false, true, false>(x, a, tiles, vec, st);
+    case FALQON_TILE: return launch_one<T, kFmt, false, false, true>(x, a, tiles, vec, st);
+    default: return launch_one<T, kFmt, true, true, false>(x, a, tiles, vec, st);
   }
 }
-constexpr int kBoth = 3;
 
 template <typename T>
 int quantize(int what, const void* x, int64_t rows, int64_t cols, int64_t ld, int fmt, uint8_t* row_codes, uint8_t* row_scales,
@@ -202,8 +296,7 @@ int quantize(int what, const void* x, int64_t rows, int64_t cols, int64_t ld, in
   const QuantArgs a{rows, cols, ld, (cols + kB - 1) / kB, row_codes, row_scales, col_codes, col_scales};
   const bool vec = cols % 8 == 0 && (ld * sizeof(T)) % 16 == 0 && aligned_to(x, 16) && aligned_to(row_codes, 8) && aligned_to(col_codes, 8);
   const T* src = static_cast<const T*>(x);
-  if (fmt == FALQON_E4M3) return finish(vec ? launch_of<T, 0, true>(what, src, a, tiles, st) : launch_of<T, 0, false>(what, src, a, tiles, st));
-  return finish(vec ? launch_of<T, 1, true>(what, src, a, tiles, st) : launch_of<T, 1, false>(what, src, a, tiles, st));
+  return finish(fmt == FALQON_E4M3 ? launch_of<T, 0>(what, src, a, tiles, vec, st) : launch_of<T, 1>(what, src, a, tiles, vec, st));
 }
 
 int quantize_checked(int what, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int fmt, uint8_t* row_codes,
