@@ -584,6 +584,22 @@ bool make_tensor_map_u16(CUtensorMap* map, const void* base, int64_t rows, int64
   return r == CUDA_SUCCESS;
 }
 
+// 3-D tensor of 16-bit elements [batch][rows][cols] with a row pitch of ld and a matrix pitch of `stride` ELEMENTS; box = box_cols x
+// box_rows of one matrix (what lies outside of that matrix reads as zero), 128-byte swizzle.
+bool make_tensor_map_batch16(CUtensorMap* map, const void* base, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                             uint32_t box_cols, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(stride) * 2};
+  cuuint32_t box[3] = {box_cols, box_rows, 1};
+  cuuint32_t elem_strides[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, elem_strides,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 int sm_count() {   // of the current device
   static std::atomic<int> counts[64];
   int dev = 0, n = 0;

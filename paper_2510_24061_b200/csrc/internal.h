@@ -163,6 +163,9 @@ bool make_tensor_map_u16(CUtensorMap_st* map, const void* base, int64_t rows, in
 // 2-D uint8 tensor [rows][cols] with row pitch ld bytes; box = box_cols x box_rows, 128-byte swizzle.
 bool make_tensor_map(CUtensorMap_st* map, const uint8_t* base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
                      uint32_t box_rows);
+// 3-D tensor of 16-bit elements [batch][rows][cols], pitches in elements; box = box_cols x box_rows of one matrix, 128-byte swizzle.
+bool make_tensor_map_batch16(CUtensorMap_st* map, const void* base, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                             uint32_t box_cols, uint32_t box_rows);
 int sm_count();
 
 // ---- gemm_db.cu: S5b in one kernel -- dB = g~^T O~_A / (s_g s_OA) over token slabs, the slab sum taken in slab

@@ -267,6 +267,13 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_smem, const void* 
       ::"r"(dst_smem), "l"(tensor_map), "r"(bar_cluster), "r"(x), "r"(y)
       : "memory");
 }
+// The same for a tensor of three dimensions.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tensor_map, uint32_t bar_cluster, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst_smem), "l"(tensor_map), "r"(bar_cluster), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_result_addr, uint32_t ncols) {  // one warp in EACH CTA
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result_addr), "r"(ncols)
                : "memory");
@@ -288,7 +295,16 @@ __device__ __forceinline__ void umma_f8_pair(uint32_t d_tmem, uint64_t a_desc, u
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// The same with a power-of-two scale byte (E8M0) for each row of A and of B and each 32 values of K.  sfa, sfb: TMEM columns
+// 256 x N x 16 of 16-bit operands of one type (idesc says which).
+__device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// umma_f8_pair with a power-of-two scale byte (E8M0) for each row of A and of B and each 32 values of K.  sfa, sfb: TMEM columns
 // that hold them, row i at lane i % 32 of column i / 32 (the same in all four quadrants; each CTA its own 128 rows of A and
 // all N rows of B); idesc names the byte of the 32-bit word that this K step takes.
 __device__ __forceinline__ void umma_mx8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa,

@@ -21,6 +21,13 @@ from .training import _dtype, _need, _new, _on_device, _ptr
 lib = fq.lib
 _p, _f, _i, _i64, _sz = C.c_void_p, C.c_float, C.c_int, C.c_int64, C.c_size_t
 
+
+class falqon_ortho(C.Structure):
+    _fields_ = [("batch", _i64), ("rows", _i64), ("cols", _i64), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("steps", C.c_int32),
+                ("eps", _f), ("scale", _f), ("coefficients", C.POINTER(_f))]
+
+
+_ortho_p = C.POINTER(falqon_ortho)
 _SIGNATURES = {
     "falqon_block_quantize": (_i, [_p, _i, _i64, _i64, _i64, _i, _i, _p, _p, _p]),
     "falqon_block_quantize_both": (_i, [_p, _i, _i64, _i64, _i64, _i, _p, _p, _p, _p, _p]),
@@ -30,6 +37,8 @@ _SIGNATURES = {
     "falqon_block_weight_grad": (_i, [_p, _p, _i, _p, _p, _i, _i64, _i64, _i64, _p, _i, _p]),
     "falqon_block_linear_scratch_bytes": (_sz, [_i64, _i64, _i64]),
     "falqon_block_linear": (_i, [_p, _i, _p, _p, _i, _i64, _i64, _i64, _p, _i, _p, _sz, _p]),
+    "falqon_orthogonalize_scratch_bytes": (_sz, [_ortho_p]),
+    "falqon_orthogonalize": (_i, [_ortho_p, _p, _p, _p, _sz, _p]),
 }
 DENSE_EXPORTS = list(_SIGNATURES)
 for _name, (_res, _args) in _SIGNATURES.items():
@@ -37,6 +46,7 @@ for _name, (_res, _args) in _SIGNATURES.items():
     getattr(lib, _name).argtypes = _args
 
 BLOCK = 128
+ORTHO_MAX_STEPS = 32
 ALONG = {"row": 0, "col": 1, "tile": 2}
 FORMATS = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 _FMT_CODE = {torch.float8_e4m3fn: fq.E4M3, torch.float8_e5m2: fq.E5M2}
@@ -189,4 +199,37 @@ def block_weight_grad(dy: Blocks, x: Blocks, dtype: torch.dtype = torch.float32,
     fq._check("falqon_block_weight_grad",
               lib.falqon_block_weight_grad(dy.codes.data_ptr(), dy.scales.data_ptr(), _FMT_CODE[dy.codes.dtype], x.codes.data_ptr(), x.scales.data_ptr(),
                                            _FMT_CODE[x.codes.dtype], T, n, m, out.data_ptr(), _dtype(out), stream))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------------------- the optimizer's update
+def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients: Optional[Sequence[Sequence[float]]] = None, eps: float = 1e-7, scale: float = 1.0,
+                  dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """falqon_orthogonalize: scale * X after ``steps`` of X <- a X + (b G + c G G) X, G = X X^T, from X = g / (|g|_F + eps).
+    g: contiguous [rows, cols] or [batch, rows, cols] (each matrix for itself), bf16 or fp32; the result is of its type or ``dtype``: bf16
+    results are made of fp16 products, fp32 ones of three such products each.  coefficients: (a, b, c) of each step (steps is then their
+    number), None: the Muon optimizer's 3.4445, -4.7750, 2.0315.  scratch: falqon_orthogonalize_scratch_bytes, allocated if None.  out may be g."""
+    _need(g.dim() in (2, 3) and g.is_contiguous() and g.numel() > 0, "g must be a contiguous, non-empty [rows, cols] or [batch, rows, cols] tensor")
+    dtype = (out.dtype if out is not None else g.dtype) if dtype is None else dtype
+    if out is not None and (out.shape != g.shape or out.dtype != dtype or not out.is_contiguous()):
+        raise ValueError(f"out must be a contiguous {dtype} tensor of shape {tuple(g.shape)}")
+    table = None
+    if coefficients is not None:
+        _need(all(len(c) == 3 for c in coefficients), "coefficients are (a, b, c) of each step")
+        steps = len(coefficients)
+        table = (_f * (3 * steps))(*(v for c in coefficients for v in c))
+    _need(1 <= steps <= ORTHO_MAX_STEPS, f"steps must be 1 to {ORTHO_MAX_STEPS}")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}")
+    rows, cols = g.shape[-2:]
+    plan = falqon_ortho(g.shape[0] if g.dim() == 3 else 1, rows, cols, _dtype(g), fq.BF16 if dtype == torch.bfloat16 else fq.F32, steps, eps, scale, table)
+    stream = _on_device(g, out, scratch)
+    out = torch.empty(g.shape, dtype=dtype, device=g.device) if out is None else out
+    size = lib.falqon_orthogonalize_scratch_bytes(C.byref(plan))
+    if size == 0:
+        raise fq.FalqonError("falqon_orthogonalize_scratch_bytes", fq.ERR_INVALID_ARG)
+    if scratch is None:
+        scratch = _new(size, dtype=torch.uint8, device=g.device)
+    fq._check("falqon_orthogonalize",
+              lib.falqon_orthogonalize(C.byref(plan), g.data_ptr(), out.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), stream))
     return out
