@@ -14,12 +14,14 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/falqon_dense.h"
 #include "gemm_common.cuh"
 #include "internal.h"
 #include "mx8.cuh"
+#include "ortho_thin.h"
 #include "ptx.cuh"
 
 namespace falqon {
@@ -571,6 +573,12 @@ bool range_ok(const float* abc, int steps) {
   return true;
 }
 
+// The coefficients of all steps.
+void coefficients_of(const falqon_ortho* p, float* abc) {
+  for (int i = 0; i < p->steps; ++i)
+    for (int k = 0; k < 3; ++k) abc[3 * i + k] = p->coefficients != nullptr ? p->coefficients[3 * i + k] : kQuintic[k];
+}
+
 struct Layout {
   int64_t s, l, ld, ld_s;        // short and long side; pitches of X and of the square matrices
   bool tall, precise;
@@ -764,7 +772,12 @@ using namespace falqon;
 
 extern "C" {
 
-size_t falqon_orthogonalize_scratch_bytes(const falqon_ortho* p) { return plan_ok(p) ? layout_of(p).total : 0; }
+size_t falqon_orthogonalize_scratch_bytes(const falqon_ortho* p) {
+  if (!plan_ok(p)) return 0;
+  float abc[3 * FALQON_ORTHO_MAX_STEPS];
+  coefficients_of(p, abc);
+  return ortho_thin_takes(p->batch, p->rows, p->cols, abc, p->steps) ? ortho_thin_scratch_bytes(p->batch, p->rows, p->cols) : layout_of(p).total;
+}
 
 int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* scratch, size_t scratch_bytes, falqon_stream stream) {
   if (!plan_ok(p) || g == nullptr || out == nullptr || !(p->eps >= 0.0f) || !std::isfinite(p->eps) || !std::isfinite(p->scale) ||
@@ -773,6 +786,10 @@ int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* 
     return FALQON_ERR_INVALID_ARG;
   if (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0 || scratch_bytes < falqon_orthogonalize_scratch_bytes(p))
     return FALQON_ERR_WORKSPACE;
+  ThinPlan thin{p->batch, p->rows, p->cols, p->dtype == FALQON_BF16, p->out_dtype == FALQON_BF16, p->steps, p->eps, p->scale, {}};
+  coefficients_of(p, thin.abc);
+  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.abc, p->steps))
+    return launch_ortho_thin(thin, g, out, scratch, static_cast<cudaStream_t>(stream)) == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA;
   return run(p, g, out, static_cast<uint8_t*>(scratch), static_cast<cudaStream_t>(stream));
 }
 
