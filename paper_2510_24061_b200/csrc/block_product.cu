@@ -4,7 +4,7 @@
 // take the same byte four times) and a tile is accumulated in fp32 over all of K without leaving tensor memory; scales that are
 // not powers of two would have to be applied to every partial tile of 128 on its way through registers.
 //
-// Two CTAs of a cluster compute a tile of 256 x block_n (one tcgen05.mma cta_group::2), a persistent pair walking its tiles:
+// Two CTAs of a cluster compute a tile of 256 x block_n (one tcgen05.mma cta_group::2), a persistent pair walking its tiles (tile_walk.cuh):
 //   warp 0        TMA producer: 128 rows of A and block_n / 2 rows of B per CTA and stage of 128 values of K
 //   warp 1        (leader) issues the MMAs
 //   warps 2..9    epilogue: tensor memory -> registers -> shared memory -> full 128-byte lines
@@ -21,6 +21,7 @@
 #include "gemm_common.cuh"
 #include "internal.h"
 #include "ptx.cuh"
+#include "tile_walk.cuh"
 
 namespace falqon {
 namespace {
@@ -49,7 +50,8 @@ struct Scales {               // byte of row i and block kb: p[(i >> shift) * ro
 
 struct ProductArgs {
   int M, N, kblocks;
-  int m_tiles, n_tiles, block_n;
+  int m_tiles;
+  TileWalk walk;
   bool a_mn, b_mn;
   uint32_t idesc;             // without N and the scale bytes
   Scales sa, sb;
@@ -129,22 +131,26 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   pdl_wait();
 
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
-  const int tiles = p.m_tiles * p.n_tiles;
+  const int items = p.walk.items;
   bool aborted = false;
-  auto inst_n = [&](int n0) {        // columns of a tile: at the right edge rounded up to what a half may be
-    const int gran = p.b_mn ? 32 : 16;
-    return min(p.block_n, (p.N - n0 + gran - 1) / gran * gran);
+  struct Piece { int row0, n0, width; };           // of this CTA: rows, columns; no columns: a piece behind the right edge, of which there is nothing
+  auto piece = [&](int item) {
+    int first, width;
+    const int tile = walk_tile(p.walk, item, &first, &width), n_idx = tile / p.m_tiles, n0 = n_idx * p.walk.block_n + first;
+    return Piece{(tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM, n0, n0 < p.N ? min(width, p.N - n0) : 0};
   };
+  const int gran = p.b_mn ? 32 : 16;               // columns of the instruction: what half of them may be
+  auto inst_n = [&](const Piece& t) { return (t.width + gran - 1) / gran * gran; };
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     int stage = 0;
     uint32_t phase = 0;
-    const uint32_t bytes = kATileBytes + (p.b_mn ? kMnChunkBytes : static_cast<uint32_t>(p.block_n >> 1) * kBlockKBytes);
-    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
-      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
-      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM;
-      const int bn0 = n0 + static_cast<int>(rank) * (inst_n(n0) >> 1);
+    const uint32_t bytes = kATileBytes + (p.b_mn ? kMnChunkBytes : static_cast<uint32_t>(p.walk.block_n >> 1) * kBlockKBytes);
+    for (int item = pair; item < items && !aborted; item += pairs) {
+      const Piece t = piece(item);
+      if (t.width == 0) continue;
+      const int row0 = t.row0, bn0 = t.n0 + static_cast<int>(rank) * (inst_n(t) >> 1);
       for (int kb = 0; kb < p.kblocks; ++kb) {
         if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) { aborted = true; break; }
         if (elect_one()) {
@@ -173,9 +179,10 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       const uint64_t a_desc0 = p.a_mn ? make_smem_desc(base, kMnChunkBytes, 1024) : make_smem_desc(base, 16, 1024);
       const uint64_t b_desc0 = p.b_mn ? make_smem_desc(base + kATileBytes, kMnChunkBytes, 1024) : make_smem_desc(base + kATileBytes, 16, 1024);
       const uint32_t a_step = (p.a_mn ? kUmmaK * 128 : kUmmaK) >> 4, b_step = (p.b_mn ? kUmmaK * 128 : kUmmaK) >> 4;
-      for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
-        const int n0 = (tile / p.m_tiles) * p.block_n;
-        const uint32_t idesc_n = p.idesc | (static_cast<uint32_t>(inst_n(n0) >> 3) << 17);
+      for (int item = pair; item < items && !aborted; item += pairs) {
+        const Piece t = piece(item);
+        if (t.width == 0) continue;
+        const uint32_t idesc_n = p.idesc | (static_cast<uint32_t>(inst_n(t) >> 3) << 17);
         if (!first) {   // the tile before: its part of the overlap is in registers, everything older is stored
           if (!mbar_wait_warp(acc_empty_bar, acc_phase, p.status)) { aborted = true; break; }
           acc_phase ^= 1u;
@@ -219,28 +226,34 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     // each load: 4096 x 16384 x 4096 333 us).
     constexpr int kAhead = 3;
     struct Entry { Bytes a, b0, b1; };
-    int next_tile = pair, next_kb = 0;
+    int next_item = pair, next_kb = 0;
     const uint8_t *row_a = nullptr, *row_b0 = nullptr, *row_b1 = nullptr;
     auto fetch = [&](Entry& w) {
-      if (next_tile >= tiles) return;
+      if (next_item >= items) return;
       if (next_kb == 0) {
-        const int n_idx = next_tile / p.m_tiles, n0 = n_idx * p.block_n;
-        row_a = scale_row(p.sa, (next_tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM + 32 * q + lane);
-        row_b0 = scale_row(p.sb, n0 + 32 * q + lane);
-        row_b1 = p.block_n > 128 ? scale_row(p.sb, n0 + 128 + 32 * q + lane) : nullptr;
+        const Piece t = piece(next_item);
+        row_a = scale_row(p.sa, t.row0 + 32 * q + lane);
+        row_b0 = scale_row(p.sb, t.n0 + 32 * q + lane);
+        row_b1 = t.width > 128 ? scale_row(p.sb, t.n0 + 128 + 32 * q + lane) : nullptr;
       }
       scale_fetch(w.a, p.sa, row_a, next_kb, p.kblocks);
       scale_fetch(w.b0, p.sb, row_b0, next_kb, p.kblocks);
       scale_fetch(w.b1, p.sb, row_b1, next_kb, p.kblocks);
       next_kb += kGroupBlocks;
-      if (next_kb >= p.kblocks) next_kb = 0, next_tile += pairs;
+      if (next_kb >= p.kblocks) {
+        next_kb = 0;
+        do next_item += pairs; while (next_item < items && piece(next_item).width == 0);
+      }
     };
     int group = 0;
     uint32_t phase = 0;
+    while (next_item < items && piece(next_item).width == 0) next_item += pairs;
+    int steps = 0;
+    for (int item = pair; item < items; item += pairs) steps += piece(item).width != 0;
+    steps *= (p.kblocks + kGroupBlocks - 1) / kGroupBlocks;
     Entry ahead[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) fetch(ahead[j]);
-    const int steps = (tiles - pair + pairs - 1) / pairs * ((p.kblocks + kGroupBlocks - 1) / kGroupBlocks);
     for (int step0 = 0; step0 < steps && !aborted; step0 += kAhead) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -284,20 +297,20 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   } else {
     // ------------------------------------------------------------ epilogue
     const int quad = warp & 3, half = (warp - 2) >> 2;
-    const int chunks = (p.block_n + 63) / 64, low = (chunks + 1) / 2;       // chunks of 64 columns: half 0 takes [0, low) upwards,
-    const int count = half == 0 ? low : chunks - low;                       // half 1 [low, chunks) downwards: the overlap first
     uint8_t* stage_out = gen + kStagingOff + (warp - 2) * 32 * 128;
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
     int acc = 0;
     uint32_t full_phase = 0;
-    for (int tile = pair; tile < tiles && !aborted; tile += pairs) {
-      const int n_idx = tile / p.m_tiles, n0 = n_idx * p.block_n;
-      const int row0 = (tile - n_idx * p.m_tiles) * 256 + static_cast<int>(rank) * kBlockM + quad * 32;
+    for (int item = pair; item < items && !aborted; item += pairs) {
+      const Piece of = piece(item);
+      if (of.width == 0) continue;
+      const int chunks = (of.width + 63) / 64, low = (chunks + 1) / 2;        // chunks of 64 columns: half 0 takes [0, low) upwards,
+      const int count = half == 0 ? low : chunks - low;                       // half 1 [low, chunks) downwards: the overlap first
+      const int row0 = of.row0 + quad * 32, n0 = of.n0, end = of.width;
       if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
       full_phase ^= 1u;
       tc_fence_after_sync();
       const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
-      const int end = min(p.block_n, p.N - n0);
       if (count == 0) {
         tc_fence_before_sync();
         __syncwarp();
@@ -315,7 +328,6 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           __syncwarp();
           if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, 0));
         }
-        if (c0 >= end) continue;
         uint8_t* my = stage_out + lane * 128;
         const int sw = lane & 7;
         // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
@@ -393,14 +405,13 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
   g.m_tiles = static_cast<int>((M + 255) / 256);
   const int64_t pairs_all = sm_count() / 2;
-  // The tile's width: what makes (waves of tiles) x (time of a tile) least; a tile's time goes with the bytes that its
-  // operands bring through L2, 256 rows of A and w of B (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 less).
+  // The tile's width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 less)
   int64_t best = 0;
   for (int w = 256; w >= 64; w -= 32) {
-    const int64_t tiles = g.m_tiles * ((N + w - 1) / w), cost = ((tiles + pairs_all - 1) / pairs_all) * (w + 256);
-    if (best == 0 || cost < best) best = cost, g.block_n = w;
+    int64_t cost;
+    const TileWalk walk = plan_walk(g.m_tiles * ((N + w - 1) / w), pairs_all, w, 256, &cost);
+    if (best == 0 || cost < best) best = cost, g.walk = walk;
   }
-  g.n_tiles = static_cast<int>((N + g.block_n - 1) / g.block_n);
   g.a_mn = a.mn;
   g.b_mn = b.mn;
   // instruction descriptor of the block-scaled kinds: formats at 7 and 10, majors at 15 and 16, N / 8 at 17, E8M0 scales at 23,
@@ -415,8 +426,8 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   if (g.status == nullptr) return cudaErrorInvalidValue;
   CUtensorMap ma, mb;
   if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, 128)) return cudaErrorInvalidValue;
-  if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.block_n / 2))) return cudaErrorInvalidValue;
-  const int64_t tiles = static_cast<int64_t>(g.m_tiles) * g.n_tiles, pairs = tiles < pairs_all ? tiles : pairs_all;
+  if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
+  const int64_t pairs = g.walk.items < pairs_all ? g.walk.items : pairs_all;
   static DeviceMask configured{0};
   const cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
   if (e != cudaSuccess) return e;

@@ -371,9 +371,11 @@ cudaError_t launch_side(const ThinPlan& p, int64_t l, int s, const void* g, void
 
 }  // namespace
 
-bool ortho_thin_takes(int64_t batch, int64_t rows, int64_t cols, const float* abc, int steps) {
+bool ortho_thin_takes(int64_t batch, int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps) {
   const int64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-  if (s > kThinMost) return false;
+  // The other way takes 17 to 22 launches, whatever the size, but works at the fp16 rate, and at a third of it for fp32 results.  bf16,
+  // 7 of 4096 x 64: 86 us here, 153 there; 7 of 4096 x 128: 224 and 194; 16: 450 and 264.  fp32, 7 of 4096 x 128: 209 and 270; 16: 383 and 399.
+  if (s > (out_bf16 ? kThinMost / 2 : kThinMost)) return false;
   // how far an error of G may grow before the last step's polynomial is taken: 2^-50 to 2^-24
   double growth = 1.0;
   for (int i = 0; i + 1 < steps; ++i) growth *= std::max(1.0, static_cast<double>(abc[3 * i]) * abc[3 * i]);

@@ -23,6 +23,7 @@
 #include "mx8.cuh"
 #include "ortho_thin.h"
 #include "ptx.cuh"
+#include "tile_walk.cuh"
 
 namespace falqon {
 namespace {
@@ -49,7 +50,8 @@ struct ProductArgs {
   int M, N, batch;
   int kblocks;                 // blocks of K
   int splits, per_split;       // CTAs that share the blocks of a tile
-  int m_tiles, n_tiles, block_n, tiles;   // tiles of a matrix
+  int m_tiles, tiles;          // tiles of a matrix
+  TileWalk walk;               // over all tiles of all matrices and splits
   bool symmetric;              // only tiles that touch the upper triangle; the lower one is their mirror
   bool a_mn, b_mn;
   uint32_t idesc;              // without N
@@ -76,24 +78,26 @@ __device__ __forceinline__ void locate(const ProductArgs& p, int t, int& m_idx, 
   }
   n_idx = 0;
   for (;; ++n_idx) {
-    const int rows = min(p.m_tiles, ((n_idx + 1) * p.block_n + 255) / 256);
+    const int rows = min(p.m_tiles, ((n_idx + 1) * p.walk.block_n + 255) / 256);
     if (t < rows) break;
     t -= rows;
   }
   m_idx = t;
 }
 
-struct Item {       // a piece of work: a tile of a matrix, and the part of its contraction
-  int b, split, row0, n0, k_begin, k_end;
+struct Item {       // a piece of work: columns of a tile of a matrix (none: behind the right edge), and the part of its contraction
+  int b, split, row0, n0, width, k_begin, k_end;
   __device__ __forceinline__ Item(const ProductArgs& p, int item) {
-    const int per_matrix = p.tiles * p.splits;
-    b = item / per_matrix;
-    const int rest = item - b * per_matrix;
+    int first;
+    const int t = walk_tile(p.walk, item, &first, &width), per_matrix = p.tiles * p.splits;
+    b = t / per_matrix;
+    const int rest = t - b * per_matrix;
     split = rest / p.tiles;
     int m_idx, n_idx;
     locate(p, rest - split * p.tiles, m_idx, n_idx);
     row0 = m_idx * 256;
-    n0 = n_idx * p.block_n;
+    n0 = n_idx * p.walk.block_n + first;
+    width = n0 < p.N ? min(width, (p.N - n0 + 31) / 32 * 32) : 0;
     k_begin = split * p.per_split;
     k_end = min(p.kblocks, k_begin + p.per_split);
   }
@@ -245,19 +249,19 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
   pdl_wait();
 
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
-  const int items = p.tiles * p.splits * p.batch;
+  const int items = p.walk.items;
   bool aborted = false;
-  auto inst_n = [&](int n0) { return min(p.block_n, (p.N - n0 + 31) / 32 * 32); };
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     int stage = 0;
     uint32_t phase = 0;
-    const int b_chunks = (p.block_n / 2 + 63) / 64;
-    const uint32_t bytes = (kPrecise ? 2 : 1) * (kATileBytes + (p.b_mn ? b_chunks * kHalfChunk : static_cast<uint32_t>(p.block_n / 2) * 128u));
     for (int item = pair; item < items && !aborted; item += pairs) {
       const Item it(p, item);
-      const int row0 = it.row0 + static_cast<int>(rank) * kBlockM, bn0 = it.n0 + static_cast<int>(rank) * (inst_n(it.n0) >> 1);
+      if (it.width == 0) continue;
+      const int b_chunks = (it.width / 2 + 63) / 64;
+      const uint32_t bytes = (kPrecise ? 2 : 1) * (kATileBytes + (p.b_mn ? b_chunks * kHalfChunk : static_cast<uint32_t>(p.walk.block_n / 2) * 128u));
+      const int row0 = it.row0 + static_cast<int>(rank) * kBlockM, bn0 = it.n0 + static_cast<int>(rank) * (it.width >> 1);
       for (int kb = it.k_begin; kb < it.k_end; ++kb) {
         if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) { aborted = true; break; }
         if (elect_one()) {
@@ -305,7 +309,8 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
       const uint32_t a_step = (p.a_mn ? 16 * 128 : 32) >> 4, b_step = (p.b_mn ? 16 * 128 : 32) >> 4;    // 16 values of K
       for (int item = pair; item < items && !aborted; item += pairs) {
         const Item it(p, item);
-        const uint32_t idesc = p.idesc | (static_cast<uint32_t>(inst_n(it.n0) >> 3) << 17);
+        if (it.width == 0) continue;
+        const uint32_t idesc = p.idesc | (static_cast<uint32_t>(it.width >> 3) << 17);
         const int chunk = kPrecise ? kChunk : it.k_end - it.k_begin;
         for (int k0 = it.k_begin; k0 < it.k_end && !aborted; k0 += chunk) {
           if (!mbar_wait_warp(acc_empty_bar(acc), acc_phase ^ 1u, p.status)) { aborted = true; break; }
@@ -347,7 +352,6 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
     const int quad = warp & 3, half = (warp - 2) >> 2;
     float* stage_out = reinterpret_cast<float*>(gen + kStagingOff + (warp - 2) * kStageOutBytes);
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
-    const int chunks = p.block_n / 32, first = half == 0 ? 0 : (chunks + 1) / 2, count = half == 0 ? (chunks + 1) / 2 : chunks / 2;
     int acc = 0;
     uint32_t acc_phase = 0, parity = 0;
     auto next_acc = [&]() {       // this accumulator has been read
@@ -359,6 +363,8 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
     };
     for (int item = pair; item < items && !aborted; item += pairs) {
       const Item it(p, item);
+      if (it.width == 0) continue;
+      const int chunks = it.width / 32, first = half == 0 ? 0 : (chunks + 1) / 2, count = half == 0 ? (chunks + 1) / 2 : chunks / 2;
       const int row0 = it.row0 + static_cast<int>(rank) * kBlockM + quad * 32;
       if constexpr (kPrecise) {
         float sum[2][32];
@@ -588,20 +594,20 @@ struct Layout {
   size_t x[4], sq[4], parts, norm, total;    // offsets: X hi, lo of two turns; G hi, lo, B hi, lo
 };
 
-int pick_width(int64_t M, int64_t N, int64_t batch, bool symmetric, bool precise, int64_t* tiles_out) {
+// The tile's width that takes the least time; *tiles: tiles of a matrix.
+TileWalk pick_walk(int64_t M, int64_t N, int64_t batch, bool symmetric, bool precise, int64_t splits, int64_t* tiles_out) {
   const int64_t pairs = sm_count() / 2;
-  int64_t best = 0, best_tiles = 0;
-  int width = 0;
+  int64_t best = 0;
+  TileWalk walk{};
   for (int w = precise ? 128 : 256; w >= 64; w -= 32) {
-    int64_t tiles = 0;
+    int64_t tiles = 0, cost;
     const int64_t mt = (M + 255) / 256, nt = (N + w - 1) / w;
     if (!symmetric) tiles = mt * nt;
     else for (int64_t n = 0; n < nt; ++n) tiles += std::min(mt, ((n + 1) * w + 255) / 256);
-    const int64_t cost = (tiles * batch + pairs - 1) / pairs * (w + (precise ? 64 : 256));
-    if (best == 0 || cost < best) best = cost, width = w, best_tiles = tiles;
+    const TileWalk of = plan_walk(tiles * batch * splits, pairs, w, precise ? 64 : 256, &cost);
+    if (best == 0 || cost < best) best = cost, walk = of, *tiles_out = tiles;
   }
-  *tiles_out = best_tiles;
-  return width;
+  return walk;
 }
 
 bool plan_ok(const falqon_ortho* p) {
@@ -622,7 +628,7 @@ Layout layout_of(const falqon_ortho* p) {
   y.sq_bytes = static_cast<size_t>(p->batch * y.s * y.ld_s) * 2;
   // G's contraction is the long one: where its tiles leave pairs idle, several share a tile, each at least four blocks of K
   int64_t tiles;
-  pick_width(y.s, y.s, p->batch, true, y.precise, &tiles);
+  pick_walk(y.s, y.s, p->batch, true, y.precise, 1, &tiles);
   const int64_t pairs = sm_count() / 2, blocks = (y.l + kKBlock - 1) / kKBlock;
   int64_t splits = pairs / (tiles * p->batch);
   if (splits > blocks / 4) splits = blocks / 4;
@@ -652,12 +658,11 @@ cudaError_t launch_product(ProductArgs g, const Matrix& a, const Matrix& b, int6
                            cudaStream_t st) {
   g.M = static_cast<int>(M), g.N = static_cast<int>(N), g.batch = static_cast<int>(batch);
   g.kblocks = static_cast<int>((K + kKBlock - 1) / kKBlock);
+  if (g.splits < 1) g.splits = 1;
   int64_t tiles;
-  g.block_n = pick_width(M, N, batch, g.symmetric, precise, &tiles);
+  g.walk = pick_walk(M, N, batch, g.symmetric, precise, g.splits, &tiles);
   g.tiles = static_cast<int>(tiles);
   g.m_tiles = static_cast<int>((M + 255) / 256);
-  g.n_tiles = static_cast<int>((N + g.block_n - 1) / g.block_n);
-  if (g.splits < 1) g.splits = 1;
   g.per_split = (g.kblocks + g.splits - 1) / g.splits;
   g.a_mn = a.mn, g.b_mn = b.mn;
   // fp32 accumulate, fp16 operands (0), majors at 15 and 16, M / 16 at 24
@@ -668,11 +673,11 @@ cudaError_t launch_product(ProductArgs g, const Matrix& a, const Matrix& b, int6
   auto map = [&](CUtensorMap* m, const Matrix& x, const __half* p, uint32_t box_rows) {
     return make_tensor_map_batch16(m, p, batch, x.rows, x.cols, x.ld, x.rows * x.ld, 64, box_rows);
   };
-  const uint32_t a_box = a.mn ? 64 : 128, b_box = b.mn ? 64 : static_cast<uint32_t>(g.block_n / 2);
+  const uint32_t a_box = a.mn ? 64 : 128, b_box = b.mn ? 64 : static_cast<uint32_t>(g.walk.block_n / 2);
   if (!map(&maps.a_hi, a, a.hi, a_box) || !map(&maps.b_hi, b, b.hi, b_box) || !map(&maps.a_lo, a, precise ? a.lo : a.hi, a_box) ||
       !map(&maps.b_lo, b, precise ? b.lo : b.hi, b_box))
     return cudaErrorInvalidValue;
-  const int64_t items = tiles * g.splits * batch, all = sm_count() / 2, pairs = items < all ? items : all;
+  const int64_t all = sm_count() / 2, pairs = g.walk.items < all ? g.walk.items : all;
   const dim3 grid(static_cast<unsigned>(2 * pairs)), block(kGemmThreads);
   if (precise) {
     static DeviceMask done{0};
@@ -776,7 +781,7 @@ size_t falqon_orthogonalize_scratch_bytes(const falqon_ortho* p) {
   if (!plan_ok(p)) return 0;
   float abc[3 * FALQON_ORTHO_MAX_STEPS];
   coefficients_of(p, abc);
-  return ortho_thin_takes(p->batch, p->rows, p->cols, abc, p->steps) ? ortho_thin_scratch_bytes(p->batch, p->rows, p->cols) : layout_of(p).total;
+  return ortho_thin_takes(p->batch, p->rows, p->cols, p->out_dtype == FALQON_BF16, abc, p->steps) ? ortho_thin_scratch_bytes(p->batch, p->rows, p->cols) : layout_of(p).total;
 }
 
 int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* scratch, size_t scratch_bytes, falqon_stream stream) {
@@ -788,7 +793,7 @@ int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* 
     return FALQON_ERR_WORKSPACE;
   ThinPlan thin{p->batch, p->rows, p->cols, p->dtype == FALQON_BF16, p->out_dtype == FALQON_BF16, p->steps, p->eps, p->scale, {}};
   coefficients_of(p, thin.abc);
-  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.abc, p->steps))
+  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.out_bf16, thin.abc, p->steps))
     return launch_ortho_thin(thin, g, out, scratch, static_cast<cudaStream_t>(stream)) == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA;
   return run(p, g, out, static_cast<uint8_t*>(scratch), static_cast<cudaStream_t>(stream));
 }
