@@ -6,15 +6,13 @@
 
 namespace falqon {
 
-constexpr int64_t kMostFew = 32;        // tokens that the kernel for few rows takes
-constexpr int64_t kMostPlain = 4;       // tokens that it quantizes itself
+constexpr int64_t kMostFew = 4;
 
-// Whether T tokens of n values may come unquantized (their codes fit in shared memory).
-bool block_linear_plain(int64_t T, int64_t n);
-// T <= kMostFew; n, m multiples of 16.
+// Whether the kernel takes T tokens of n values: kMostFew at the most, whose codes fit in shared memory.
+bool block_linear_takes(int64_t T, int64_t n);
+// block_linear_takes(T, n); n, m multiples of 16; x as codes, or plain (quantized on the way).
 cudaError_t launch_block_linear_codes(const uint8_t* x, const uint8_t* xs, int x_fmt, const uint8_t* w, const uint8_t* ws, int w_fmt, int64_t T,
                                       int64_t n, int64_t m, void* y, bool bf16, cudaStream_t st);
-// block_linear_plain(T, n)
 cudaError_t launch_block_linear_plain(const void* x, bool x_bf16, const uint8_t* w, const uint8_t* ws, int w_fmt, int64_t T, int64_t n, int64_t m,
                                       void* y, bool bf16, cudaStream_t st);
 

@@ -28,18 +28,20 @@ namespace {
 
 constexpr int kEpiWarps = 8, kScaleWarps = 4;
 constexpr int kThreads = 32 * (2 + kEpiWarps + kScaleWarps);
-constexpr uint32_t kStageBytes = 32 * 1024;          // 16 KB of A, up to 16 KB of B
-constexpr int kStages = 6;
+// A stage is 128 values of K of this CTA's rows of A (of which only as many as there are: the MMA reads 128 whatever lies behind
+// them, and the results of rows that are not there are not stored) and its half of B's: 32 KB at the most, and as many stages as fit.
+constexpr uint32_t kRingBytes = 6 * 32 * 1024;
+constexpr int kMostStages = 16;
 constexpr uint32_t kAccStride = 192;                 // the second accumulator's first column
 constexpr uint32_t kScaleCol0 = 448;                 // ring of kGroups entries of 4 (A) + 8 (B) columns
 constexpr int kGroups = 5;
 constexpr uint32_t kGroupCols = 12;
 constexpr int kGroupBlocks = 4;                      // blocks of K per entry: the bytes of a word
-constexpr uint32_t kStagingOff = kStages * kStageBytes;
+constexpr uint32_t kStagingOff = kRingBytes;             // (the last stage's MMA may read into it)
 constexpr uint32_t kWordsOff = kStagingOff + kEpiWarps * 32 * 128;
 constexpr uint32_t kWordsBytes = 12 * 32 * 4;        // an entry's scale words, passed between the scale warps
 constexpr uint32_t kBarsOff = kWordsOff + kWordsBytes;
-constexpr uint32_t kSmem = kBarsOff + 256 + 1024;
+constexpr uint32_t kSmem = kBarsOff + 512 + 1024;
 
 struct Scales {               // byte of row i and block kb: p[(i >> shift) * row + kb * block]
   const uint8_t* p;
@@ -53,6 +55,8 @@ struct ProductArgs {
   int m_tiles;
   TileWalk walk;
   bool a_mn, b_mn;
+  int stages;
+  uint32_t a_bytes, b_off, stage_bytes;      // of A in a stage, where B starts, stride
   uint32_t idesc;             // without N and the scale bytes
   Scales sa, sb;
   void* out;
@@ -90,12 +94,14 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
+  const int n_stages = p.stages;
+  const uint32_t stage_bytes = p.stage_bytes;
   const uint32_t bars = base + kBarsOff;
   auto full_bar = [&](int s) { return bars + 8u * s; };
-  auto empty_bar = [&](int s) { return bars + 8u * (kStages + s); };
-  auto sf_full_bar = [&](int g) { return bars + 8u * (2 * kStages + g); };
-  auto sf_empty_bar = [&](int g) { return bars + 8u * (2 * kStages + kGroups + g); };
-  const uint32_t acc_full_bar = bars + 8u * (2 * kStages + 2 * kGroups), acc_empty_bar = acc_full_bar + 8u;
+  auto empty_bar = [&](int s) { return bars + 8u * (n_stages + s); };
+  auto sf_full_bar = [&](int g) { return bars + 8u * (2 * n_stages + g); };
+  auto sf_empty_bar = [&](int g) { return bars + 8u * (2 * n_stages + kGroups + g); };
+  const uint32_t acc_full_bar = bars + 8u * (2 * n_stages + 2 * kGroups), acc_empty_bar = acc_full_bar + 8u;
   const uint32_t slot = acc_empty_bar + 8u;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -105,7 +111,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   if (threadIdx.x == 0) {
     prefetch_tensor_map(&map_a);
     prefetch_tensor_map(&map_b);
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < n_stages; ++s) {
       mbar_init(full_bar(s), 1);                       // the leader's expect_tx; the bytes of both CTAs
       mbar_init(empty_bar(s), 1);                      // one commit to both CTAs
     }
@@ -146,7 +152,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     // ------------------------------------------------------------ TMA producer
     int stage = 0;
     uint32_t phase = 0;
-    const uint32_t bytes = kATileBytes + (p.b_mn ? kMnChunkBytes : static_cast<uint32_t>(p.walk.block_n >> 1) * kBlockKBytes);
+    const uint32_t bytes = p.a_bytes + (p.b_mn ? kMnChunkBytes : static_cast<uint32_t>(p.walk.block_n >> 1) * kBlockKBytes);
     for (int item = pair; item < items && !aborted; item += pairs) {
       const Piece t = piece(item);
       if (t.width == 0) continue;
@@ -156,19 +162,19 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         if (elect_one()) {
           if (leader) mbar_expect_tx(full_bar(stage), 2 * bytes);
           const uint32_t fb = map_to_cta(full_bar(stage), 0);
-          const uint32_t a_dst = base + static_cast<uint32_t>(stage) * kStageBytes, b_dst = a_dst + kATileBytes;
+          const uint32_t a_dst = base + static_cast<uint32_t>(stage) * stage_bytes, b_dst = a_dst + p.b_off;
           if (p.a_mn) tma_load_2d_pair(a_dst, &map_a, fb, row0, kb * kBlockKBytes);
           else        tma_load_2d_pair(a_dst, &map_a, fb, kb * kBlockKBytes, row0);
           if (p.b_mn) tma_load_2d_pair(b_dst, &map_b, fb, bn0, kb * kBlockKBytes);
           else        tma_load_2d_pair(b_dst, &map_b, fb, kb * kBlockKBytes, bn0);
         }
         __syncwarp();
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        if (++stage == n_stages) { stage = 0; phase ^= 1u; }
       }
     }
-    for (int i = 0; i < kStages && !aborted; ++i) {   // the MMAs have let go of every stage before this CTA may leave
+    for (int i = 0; i < n_stages && !aborted; ++i) {   // the MMAs have let go of every stage before this CTA may leave
       if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) aborted = true;
-      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      if (++stage == n_stages) { stage = 0; phase ^= 1u; }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
@@ -177,7 +183,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       uint32_t phase = 0, sf_phase = 0, acc_phase = 0;
       bool first = true;
       const uint64_t a_desc0 = p.a_mn ? make_smem_desc(base, kMnChunkBytes, 1024) : make_smem_desc(base, 16, 1024);
-      const uint64_t b_desc0 = p.b_mn ? make_smem_desc(base + kATileBytes, kMnChunkBytes, 1024) : make_smem_desc(base + kATileBytes, 16, 1024);
+      const uint64_t b_desc0 = p.b_mn ? make_smem_desc(base + p.b_off, kMnChunkBytes, 1024) : make_smem_desc(base + p.b_off, 16, 1024);
       const uint32_t a_step = (p.a_mn ? kUmmaK * 128 : kUmmaK) >> 4, b_step = (p.b_mn ? kUmmaK * 128 : kUmmaK) >> 4;
       for (int item = pair; item < items && !aborted; item += pairs) {
         const Piece t = piece(item);
@@ -195,7 +201,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           if (byte == 0 && !mbar_wait_warp(sf_full_bar(group), sf_phase, p.status)) { aborted = true; break; }
           if (!mbar_wait_warp(full_bar(stage), phase, p.status)) { aborted = true; break; }
           tc_fence_after_sync();
-          const uint32_t off = (static_cast<uint32_t>(stage) * kStageBytes) >> 4;
+          const uint32_t off = (static_cast<uint32_t>(stage) * stage_bytes) >> 4;
           const uint32_t sfa = tmem + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
           const uint32_t idesc = idesc_n | (static_cast<uint32_t>(byte) << 29) | (static_cast<uint32_t>(byte) << 4);
           const bool last = byte == kGroupBlocks - 1 || kb == p.kblocks - 1;
@@ -207,7 +213,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             if (last) umma_commit_pair(sf_empty_bar(group), 3);
           }
           __syncwarp();
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
           if (last && ++group == kGroups) { group = 0; sf_phase ^= 1u; }
         }
         if (aborted) break;
@@ -406,12 +412,18 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.m_tiles = static_cast<int>((M + 255) / 256);
   const int64_t pairs_all = sm_count() / 2;
   // The tile's width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 less)
+  const int64_t a_rows = a.mn || M >= 128 ? 128 : round_up(M, 8);
   int64_t best = 0;
   for (int w = 256; w >= 64; w -= 32) {
     int64_t cost;
-    const TileWalk walk = plan_walk(g.m_tiles * ((N + w - 1) / w), pairs_all, w, 256, &cost);
+    const TileWalk walk = plan_walk(g.m_tiles * ((N + w - 1) / w), pairs_all, w, static_cast<int>(2 * a_rows), &cost);
     if (best == 0 || cost < best) best = cost, g.walk = walk;
   }
+  g.a_bytes = static_cast<uint32_t>(a_rows) * kBlockKBytes;
+  g.b_off = static_cast<uint32_t>(round_up(g.a_bytes, 1024));
+  g.stage_bytes = g.b_off + (b.mn ? kMnChunkBytes : static_cast<uint32_t>(g.walk.block_n / 2) * kBlockKBytes);
+  g.stages = static_cast<int>(kRingBytes / g.stage_bytes);
+  if (g.stages > kMostStages) g.stages = kMostStages;
   g.a_mn = a.mn;
   g.b_mn = b.mn;
   // instruction descriptor of the block-scaled kinds: formats at 7 and 10, majors at 15 and 16, N / 8 at 17, E8M0 scales at 23,
@@ -425,7 +437,7 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.status = device_status_ptr();
   if (g.status == nullptr) return cudaErrorInvalidValue;
   CUtensorMap ma, mb;
-  if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, 128)) return cudaErrorInvalidValue;
+  if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, static_cast<uint32_t>(a_rows))) return cudaErrorInvalidValue;
   if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
   const int64_t pairs = g.walk.items < pairs_all ? g.walk.items : pairs_all;
   static DeviceMask configured{0};
@@ -469,7 +481,7 @@ int falqon_block_forward(const uint8_t* x_codes, const uint8_t* x_scales, falqon
   if (!ok16(x_codes) || !ok16(w_codes) || !ok16(y) || x_scales == nullptr || w_scales == nullptr || !fmt_ok(x_fmt) || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
-  if (T <= kMostFew)
+  if (block_linear_takes(T, n))
     return finish(launch_block_linear_codes(x_codes, x_scales, x_fmt, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
                                             static_cast<cudaStream_t>(stream)));
   const Operand a{x_codes, T, n, false, x_fmt, scales_of(x_scales, FALQON_ALONG_ROW, T, n, false)};
@@ -500,7 +512,7 @@ int falqon_block_weight_grad(const uint8_t* dy_codes, const uint8_t* dy_scales, 
 }
 
 size_t falqon_block_linear_scratch_bytes(int64_t T, int64_t n, int64_t m) {
-  if (!layer_ok(T, n, m) || !tiles_ok(T, m) || block_linear_plain(T, n)) return 0;
+  if (!layer_ok(T, n, m) || !tiles_ok(T, m) || block_linear_takes(T, n)) return 0;
   return static_cast<size_t>(T * n + round_up(T * ((n + 127) / 128), 16));
 }
 
@@ -509,7 +521,7 @@ int falqon_block_linear(const void* x, int x_dtype, const uint8_t* w_codes, cons
   if (!ok16(x) || (x_dtype != FALQON_BF16 && x_dtype != FALQON_F32) || !ok16(w_codes) || !ok16(y) || w_scales == nullptr || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
-  if (block_linear_plain(T, n))
+  if (block_linear_takes(T, n))
     return finish(launch_block_linear_plain(x, x_dtype == FALQON_BF16, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
                                             static_cast<cudaStream_t>(stream)));
   if (!ok16(scratch) || scratch_bytes < falqon_block_linear_scratch_bytes(T, n, m)) return FALQON_ERR_WORKSPACE;
