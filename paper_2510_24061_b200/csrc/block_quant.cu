@@ -67,38 +67,68 @@ struct ColMax<float> {
   __device__ __forceinline__ uint32_t bits(int j) const { return m[j]; }
 };
 
+// Codes of eight values times four pairs of factors (powers of two: exact).
 template <int kFmt, typename T>
-__device__ __forceinline__ uint2 codes8(const Vec8<T>& v, const float (&f)[8]) {
-  float x[8];
-  v.unpack(x);
-  return make_uint2(cvt_fp8x4<kFmt>(x[0] * f[0], x[1] * f[1], x[2] * f[2], x[3] * f[3]), cvt_fp8x4<kFmt>(x[4] * f[4], x[5] * f[5], x[6] * f[6], x[7] * f[7]));
+__device__ __forceinline__ uint2 codes8(const Vec8<T>& v, const f2 (&f)[4]) {
+  f2 x[4];
+  v.pairs(x);
+  float y[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) unpack_f32x2(mul2(x[k], f[k]), y[2 * k], y[2 * k + 1]);
+  return make_uint2(cvt_fp8x4<kFmt>(y[0], y[1], y[2], y[3]), cvt_fp8x4<kFmt>(y[4], y[5], y[6], y[7]));
+}
+
+// The largest |value| of two rows over the 16 lanes that hold them, as fp32 bit patterns: bf16 rows side by side in one register.
+__device__ __forceinline__ void row_maxima(const Vec8<bf16_t>& a, const Vec8<bf16_t>& b, uint32_t& ma, uint32_t& mb) {
+  auto of = [](const Vec8<bf16_t>& v) {
+    const uint32_t w[4] = {v.q.x, v.q.y, v.q.z, v.q.w};
+    uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) m = ColMax<bf16_t>::larger(m, w[k] & 0x7FFF7FFFu);
+    return m;
+  };
+  const uint32_t x = of(a), y = of(b);
+  uint32_t m = ColMax<bf16_t>::larger(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+#pragma unroll
+  for (int s = 1; s < 16; s <<= 1) m = ColMax<bf16_t>::larger(m, __shfl_xor_sync(0xFFFFFFFFu, m, s));
+  ma = m << 16, mb = m & 0xFFFF0000u;
+}
+__device__ __forceinline__ void row_maxima(const Vec8<float>& a, const Vec8<float>& b, uint32_t& ma, uint32_t& mb) {
+  ma = a.max_abs(), mb = b.max_abs();
+#pragma unroll
+  for (int s = 1; s < 16; s <<= 1) {
+    ma = max(ma, __shfl_xor_sync(0xFFFFFFFFu, ma, s));
+    mb = max(mb, __shfl_xor_sync(0xFFFFFFFFu, mb, s));
+  }
 }
 
 // Rows of whole 16-byte vectors.  A warp lies on 16 rows of the tile, two at a time, 16 lanes x 8 values to a row; values stay as they
 // came (bf16: half the registers).
 template <typename T, int kFmt, bool kRow, bool kCol, bool kTile>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? (kRow && kCol ? 3 : 4) : 2)
 block_quant_kernel(const T* x, const QuantArgs a) {
   constexpr int kPasses = 8;
   __shared__ __align__(16) uint32_t s_max[kWarps][kB];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t tile_r = blockIdx.x / a.col_tiles, tile_c = blockIdx.x - tile_r * a.col_tiles;
+  const int64_t tile_r = blockIdx.x / static_cast<uint32_t>(a.col_tiles), tile_c = blockIdx.x - tile_r * a.col_tiles;
   const int64_t row0 = tile_r * kB + warp * 16 + (lane >> 4), col = tile_c * kB + (lane & 15) * 8;
-  const bool col_in = col < a.cols;      // a vector is inside or outside as a whole
+  // passes with a row of this lane; none behind the right edge (a vector is inside or outside as a whole)
+  const int passes = col < a.cols && row0 < a.rows ? static_cast<int>(min(static_cast<int64_t>(kPasses), (a.rows - row0 + 1) / 2)) : 0;
 
   Vec8<T> v[kPasses];
+  {
+    const T* src = x + row0 * a.ld + col;
 #pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    if (col_in && row0 + 2 * p < a.rows) v[p].load(x + (row0 + 2 * p) * a.ld + col); else v[p].zero();
+    for (int p = 0; p < kPasses; ++p, src += 2 * a.ld) {
+      if (p < passes) v[p].load(src); else v[p].zero();
+    }
   }
-  auto store = [&](uint8_t* codes, int p, const float (&f)[8]) {
-    if (col_in && row0 + 2 * p < a.rows) *reinterpret_cast<uint2*>(codes + (row0 + 2 * p) * a.cols + col) = codes8<kFmt>(v[p], f);
-  };
-  auto same = [](float (&f)[8], float y) {
+  const int64_t first = row0 * a.cols + col, step = 2 * a.cols;
+  auto same = [](f2 (&f)[4], uint32_t e) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = y;
+    for (int j = 0; j < 4; ++j) f[j] = twice(mx8_encode_factor(e));
   };
 
   ColMax<T> m;
@@ -110,7 +140,8 @@ block_quant_kernel(const T* x, const QuantArgs a) {
   if constexpr (kCol) {
     if (lane < 16) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s_max[warp][lane * 8 + j] = m.bits(j);
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<uint4*>(&s_max[warp][lane * 8 + 4 * h]) = make_uint4(m.bits(4 * h), m.bits(4 * h + 1), m.bits(4 * h + 2), m.bits(4 * h + 3));
     }
   }
   if constexpr (kTile) {
@@ -121,16 +152,23 @@ block_quant_kernel(const T* x, const QuantArgs a) {
     if (lane == 0) s_max[warp][0] = all;
   }
   if constexpr (kRow) {
+    uint8_t* dst = a.row_codes + first;
+    uint8_t* scale = a.row_scales + row0 * a.col_tiles + tile_c;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      uint32_t r = v[p].max_abs();
+    for (int p = 0; p < kPasses; p += 2) {
+      uint32_t r[2];
+      row_maxima(v[p], v[p + 1], r[0], r[1]);
 #pragma unroll
-      for (int s = 1; s < 16; s <<= 1) r = max(r, __shfl_xor_sync(0xFFFFFFFFu, r, s));
-      const uint32_t e = scale_byte<kFmt>(r);
-      float f[8];
-      same(f, mx8_encode_factor(e));
-      store(a.row_codes, p, f);
-      if ((lane & 15) == 0 && row0 + 2 * p < a.rows) a.row_scales[(row0 + 2 * p) * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
+      for (int k = 0; k < 2; ++k, dst += step, scale += 2 * a.col_tiles) {
+        const uint32_t e = scale_byte<kFmt>(r[k]);
+        f2 f[4];
+        same(f, e);
+        const uint2 c = codes8<kFmt>(v[p + k], f);
+        if (p + k < passes) {
+          *reinterpret_cast<uint2*>(dst) = c;
+          if ((lane & 15) == 0) *scale = static_cast<uint8_t>(e);
+        }
+      }
     }
   }
   if constexpr (kTile) {
@@ -140,10 +178,12 @@ block_quant_kernel(const T* x, const QuantArgs a) {
     for (int w = 0; w < kWarps; ++w) all = max(all, s_max[w][0]);
     const uint32_t e = scale_byte<kFmt>(all);
     if (threadIdx.x == 0) a.row_scales[tile_r * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
-    float f[8];
-    same(f, mx8_encode_factor(e));
+    f2 f[4];
+    same(f, e);
+    uint8_t* dst = a.row_codes + first;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) store(a.row_codes, p, f);
+    for (int p = 0; p < kPasses; ++p, dst += step)
+      if (p < passes) *reinterpret_cast<uint2*>(dst) = codes8<kFmt>(v[p], f);
   }
   if constexpr (kCol) {
     __syncthreads();
@@ -157,14 +197,16 @@ block_quant_kernel(const T* x, const QuantArgs a) {
       if (tile_c * kB + threadIdx.x < a.cols) a.col_scales[tile_r * a.cols + tile_c * kB + threadIdx.x] = static_cast<uint8_t>(e);
     }
     __syncthreads();
-    float f[8];
+    f2 f[4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float4 q = *reinterpret_cast<const float4*>(&s_max[0][(lane & 15) * 8 + 4 * h]);
-      f[4 * h] = q.x, f[4 * h + 1] = q.y, f[4 * h + 2] = q.z, f[4 * h + 3] = q.w;
+      f[2 * h] = pack_f32x2(q.x, q.y), f[2 * h + 1] = pack_f32x2(q.z, q.w);
     }
+    uint8_t* dst = a.col_codes + first;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) store(a.col_codes, p, f);
+    for (int p = 0; p < kPasses; ++p, dst += step)
+      if (p < passes) *reinterpret_cast<uint2*>(dst) = codes8<kFmt>(v[p], f);
   }
 }
 
