@@ -221,28 +221,37 @@ block_quant_ragged_kernel(const T* x, const QuantArgs a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t tile_r = blockIdx.x / a.col_tiles, tile_c = blockIdx.x - tile_r * a.col_tiles;
   const int64_t row0 = tile_r * kB + warp * 16, col0 = tile_c * kB + lane;
+  const int rows = row0 < a.rows ? static_cast<int>(min(static_cast<int64_t>(kPasses), a.rows - row0)) : 0;
+  bool in[kValues];
+#pragma unroll
+  for (int j = 0; j < kValues; ++j) in[j] = col0 + 32 * j < a.cols;
   float v[kPasses][kValues];
+  {
+    const T* src = x + row0 * a.ld + col0;
 #pragma unroll
-  for (int p = 0; p < kPasses; ++p)
+    for (int p = 0; p < kPasses; ++p, src += a.ld)
+#pragma unroll
+      for (int j = 0; j < kValues; ++j) v[p][j] = p < rows && in[j] ? load1(src + 32 * j) : 0.0f;
+  }
+  const int64_t first = row0 * a.cols + col0;
+  auto store = [&](uint8_t* dst, int p, const float (&f)[kValues]) {
+    const uint32_t c = cvt_fp8x4<kFmt>(v[p][0] * f[0], v[p][1] * f[1], v[p][2] * f[2], v[p][3] * f[3]);
 #pragma unroll
     for (int j = 0; j < kValues; ++j)
-      v[p][j] = row0 + p < a.rows && col0 + 32 * j < a.cols ? load1(x + (row0 + p) * a.ld + col0 + 32 * j) : 0.0f;
-  auto store = [&](uint8_t* codes, int p, const float (&f)[kValues]) {
-    if (row0 + p >= a.rows) return;
-#pragma unroll
-    for (int j = 0; j < kValues; ++j)
-      if (col0 + 32 * j < a.cols) codes[(row0 + p) * a.cols + col0 + 32 * j] = static_cast<uint8_t>(cvt_fp8x2<kFmt>(v[p][j] * f[j], 0.0f) & 0xFFu);
+      if (p < rows && in[j]) dst[32 * j] = static_cast<uint8_t>(c >> (8 * j));
   };
   if constexpr (kRow) {
+    uint8_t* dst = a.row_codes + first;
+    uint8_t* scale = a.row_scales + row0 * a.col_tiles + tile_c;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
+    for (int p = 0; p < kPasses; ++p, dst += a.cols, scale += a.col_tiles) {
       uint32_t r = 0u;
 #pragma unroll
       for (int j = 0; j < kValues; ++j) r = max(r, abs_bits(v[p][j]));
       const uint32_t e = scale_byte<kFmt>(__reduce_max_sync(0xFFFFFFFFu, r));
       const float y = mx8_encode_factor(e), f[kValues] = {y, y, y, y};
-      store(a.row_codes, p, f);
-      if (lane == 0 && row0 + p < a.rows) a.row_scales[(row0 + p) * a.col_tiles + tile_c] = static_cast<uint8_t>(e);
+      store(dst, p, f);
+      if (lane == 0 && p < rows) *scale = static_cast<uint8_t>(e);
     }
   }
   if constexpr (kCol || kTile) {
@@ -273,11 +282,12 @@ block_quant_ragged_kernel(const T* x, const QuantArgs a) {
       for (int j = 0; j < kValues; ++j) {
         const uint32_t e = scale_byte<kFmt>(c[j]);
         f[j] = mx8_encode_factor(e);
-        if (warp == 0 && col0 + 32 * j < a.cols) a.col_scales[tile_r * a.cols + col0 + 32 * j] = static_cast<uint8_t>(e);
+        if (warp == 0 && in[j]) a.col_scales[tile_r * a.cols + col0 + 32 * j] = static_cast<uint8_t>(e);
       }
     }
+    uint8_t* dst = (kTile ? a.row_codes : a.col_codes) + first;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) store(kTile ? a.row_codes : a.col_codes, p, f);
+    for (int p = 0; p < kPasses; ++p, dst += a.cols) store(dst, p, f);
   }
 }
 
