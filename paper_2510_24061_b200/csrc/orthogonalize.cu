@@ -674,9 +674,9 @@ cudaError_t launch_product(ProductArgs g, const Matrix& a, const Matrix& b, int6
     return make_tensor_map_batch16(m, p, batch, x.rows, x.cols, x.ld, x.rows * x.ld, 64, box_rows);
   };
   const uint32_t a_box = a.mn ? 64 : 128, b_box = b.mn ? 64 : static_cast<uint32_t>(g.walk.block_n / 2);
-  if (!map(&maps.a_hi, a, a.hi, a_box) || !map(&maps.b_hi, b, b.hi, b_box) || !map(&maps.a_lo, a, precise ? a.lo : a.hi, a_box) ||
-      !map(&maps.b_lo, b, precise ? b.lo : b.hi, b_box))
-    return cudaErrorInvalidValue;
+  if (!map(&maps.a_hi, a, a.hi, a_box) || !map(&maps.b_hi, b, b.hi, b_box)) return cudaErrorInvalidValue;
+  if (!precise) maps.a_lo = maps.a_hi, maps.b_lo = maps.b_hi;
+  else if (!map(&maps.a_lo, a, a.lo, a_box) || !map(&maps.b_lo, b, b.lo, b_box)) return cudaErrorInvalidValue;
   const int64_t all = sm_count() / 2, pairs = g.walk.items < all ? g.walk.items : all;
   const dim3 grid(static_cast<unsigned>(2 * pairs)), block(kGemmThreads);
   if (precise) {

@@ -67,22 +67,32 @@ def _scale_shape(rows: int, cols: int, along: str) -> Tuple[int, int]:
 
 def _blocks(q: Blocks, along: Union[str, Tuple[str, ...]], name: str):
     codes, scales, of = q
-    if of not in along or codes.dtype not in _FMT_CODE or codes.dim() != 2 or codes.numel() == 0 or not codes.is_contiguous():
+    if of not in along or codes.dtype not in _FMT_CODE or codes.dim() != 2 or not codes.is_contiguous() or codes.numel() == 0:
         raise ValueError(f"{name} must be Blocks along {along} with contiguous, non-empty [rows, cols] codes")
-    if scales.dtype != torch.uint8 or scales.shape != _scale_shape(*codes.shape, of) or not scales.is_contiguous():
-        raise ValueError(f"{name}.scales must be a contiguous uint8 tensor of shape {_scale_shape(*codes.shape, of)}")
+    shape = _scale_shape(*codes.shape, of)
+    if scales.dtype != torch.uint8 or scales.shape != shape or not scales.is_contiguous():
+        raise ValueError(f"{name}.scales must be a contiguous uint8 tensor of shape {shape}")
 
 
 def _values(x: torch.Tensor, name: str):
-    """A matrix of consecutive values in a row; its row pitch in values."""
-    if x.dim() != 2 or x.numel() == 0 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
-        raise ValueError(f"{name} must be a non-empty [rows, cols] tensor of consecutive values")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    """(rows, cols, row pitch in values) of a matrix of consecutive values in a row."""
+    if x.dim() == 2:
+        (rows, cols), (pitch, step) = x.shape, x.stride()
+        if rows == 1:
+            pitch = cols
+        if rows > 0 and cols > 0 and (step == 1 or cols == 1) and pitch >= cols:
+            return rows, cols, pitch
+    raise ValueError(f"{name} must be a non-empty [rows, cols] tensor of consecutive values")
 
 
-def _new_blocks(x: torch.Tensor, along: str, fmt: str) -> Blocks:
-    rows, cols = x.shape
-    return Blocks(_new(rows, cols, dtype=FORMATS[fmt], device=x.device), _new(*_scale_shape(rows, cols, along), dtype=torch.uint8, device=x.device), along)
+def _format(fmt: str) -> torch.dtype:
+    if fmt not in FORMATS:
+        raise ValueError(f"fmt must be one of {sorted(FORMATS)}")
+    return FORMATS[fmt]
+
+
+def _new_blocks(rows: int, cols: int, along: str, codes: torch.dtype, device) -> Blocks:
+    return Blocks(_new(rows, cols, dtype=codes, device=device), _new(*_scale_shape(rows, cols, along), dtype=torch.uint8, device=device), along)
 
 
 def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, device, name: str) -> torch.Tensor:
@@ -97,15 +107,18 @@ def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtyp
 def block_quantize(x: torch.Tensor, along: str = "row", fmt: str = "e4m3", out: Optional[Blocks] = None) -> Blocks:
     """falqon_block_quantize: x [rows, cols] (a row pitch is allowed) in 8 bits, a scale for each block of 128 values ``along`` a
     "row", a "col"umn, or for each 128 x 128 "tile".  fmt "e4m3" or "e5m2"."""
-    _need(along in ALONG, f"along must be one of {sorted(ALONG)}")
-    _need(fmt in FORMATS, f"fmt must be one of {sorted(FORMATS)}")
-    ld = _values(x, "x")
-    if out is not None:
+    if along not in ALONG:
+        raise ValueError(f"along must be one of {sorted(ALONG)}")
+    codes = _format(fmt)
+    rows, cols, ld = _values(x, "x")
+    if out is None:
+        stream = _on_device(x)
+        out = _new_blocks(rows, cols, along, codes, x.device)
+    else:
         _blocks(out, (along,), "out")
-        _need(out.codes.shape == x.shape and out.codes.dtype == FORMATS[fmt], "out must hold codes like x in fmt")
-    stream = _on_device(x, *(out[:2] if out is not None else ()))
-    out = _new_blocks(x, along, fmt) if out is None else out
-    fq._check("falqon_block_quantize", lib.falqon_block_quantize(x.data_ptr(), _dtype(x), *x.shape, ld, _FMT_CODE[FORMATS[fmt]], ALONG[along],
+        _need(out.codes.shape == x.shape and out.codes.dtype == codes, "out must hold codes like x in fmt")
+        stream = _on_device(x, out.codes, out.scales)
+    fq._check("falqon_block_quantize", lib.falqon_block_quantize(x.data_ptr(), _dtype(x), rows, cols, ld, _FMT_CODE[codes], ALONG[along],
                                                                  out.codes.data_ptr(), out.scales.data_ptr(), stream))
     return out
 
@@ -113,13 +126,13 @@ def block_quantize(x: torch.Tensor, along: str = "row", fmt: str = "e4m3", out: 
 def block_quantize_both(x: torch.Tensor, fmt: str = "e4m3") -> Tuple[Blocks, Blocks]:
     """falqon_block_quantize_both: (along "row", along "col") from one read of x: what a training step needs of a layer's input and of
     its output's gradient."""
-    _need(fmt in FORMATS, f"fmt must be one of {sorted(FORMATS)}")
-    ld = _values(x, "x")
-    stream = _on_device(x)
-    row, col = _new_blocks(x, "row", fmt), _new_blocks(x, "col", fmt)
+    codes = _format(fmt)
+    rows, cols, ld = _values(x, "x")
+    stream, device = _on_device(x), x.device
+    row, col = _new_blocks(rows, cols, "row", codes, device), _new_blocks(rows, cols, "col", codes, device)
     fq._check("falqon_block_quantize_both",
-              lib.falqon_block_quantize_both(x.data_ptr(), _dtype(x), *x.shape, ld, _FMT_CODE[FORMATS[fmt]], row.codes.data_ptr(),
-                                             row.scales.data_ptr(), col.codes.data_ptr(), col.scales.data_ptr(), stream))
+              lib.falqon_block_quantize_both(x.data_ptr(), _dtype(x), rows, cols, ld, _FMT_CODE[codes], row.codes.data_ptr(), row.scales.data_ptr(),
+                                             col.codes.data_ptr(), col.scales.data_ptr(), stream))
     return row, col
 
 
@@ -218,7 +231,8 @@ def orthogonalize(g: torch.Tensor, steps: int = 5, coefficients: Optional[Sequen
         _need(all(len(c) == 3 for c in coefficients), "coefficients are (a, b, c) of each step")
         steps = len(coefficients)
         table = (_f * (3 * steps))(*(v for c in coefficients for v in c))
-    _need(1 <= steps <= ORTHO_MAX_STEPS, f"steps must be 1 to {ORTHO_MAX_STEPS}")
+    if not 1 <= steps <= ORTHO_MAX_STEPS:
+        raise ValueError(f"steps must be 1 to {ORTHO_MAX_STEPS}")
     if dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"unsupported dtype {dtype}")
     rows, cols = g.shape[-2:]
