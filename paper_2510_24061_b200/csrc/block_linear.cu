@@ -5,8 +5,9 @@
 // used.  A warp reads 512 codes of a row at a time (whole lines), a lane 16 of them, all of one block; codes are multiplied as fp16
 // (products exact) into fp32 sums, the scales stay outside of a lane's 16.  Some warps of a CTA share the contraction, each with its own part of x;
 // CTAs walk over the rows, two units of kRows x 512 codes on their way.  x is quantized by every warp for its own part, which is
-// read once per CTA.  (The same with mma.sync m16n8k16, whose rate is low here, 16 rows and all of x a CTA: 4096 -> 11008, one token 15.8
-// us, four 27.7; now 9.8 and XX.)  With more tokens the tensor cores' tiles are faster: eight 22.8 us.
+// read once per CTA.  4096 -> 11008, bf16: one token 11.4 us (4.0 TB/s; the loads alone 8.9), two 15.0, four 23.3 (bound by the
+// multiplications); the tensor cores' tiles with a quantizer before them 19 to 20 us from five tokens up to 130.  4096 -> 4096: 5.5, 7.4 and
+// 10.9 us, theirs 16.6.  (By mma.sync m16n8k16, whose rate is low here, with 16 rows and all of x to a CTA: one token 15.8, four 27.7.)
 #include <type_traits>
 
 #include "../../include/falqon_dense.h"

@@ -126,12 +126,13 @@ struct ChainArgs {
   int nparts, steps;
   double eps, scale;
   double* out;                   // [batch][side][side]: P times scale and f
+  int* status;
   float abc[3 * kThinMostSteps];
 };
 
 // The steps.  A cluster to a matrix: a CTA owns tile rows cta, cta + cluster, .. (their rows of G and P in its shared memory), a warp tile
-// columns w, w + 8, ..  The right operand of a product (G and Q in turn) lies whole in every CTA: a CTA writes its rows of it to
-// all of them, by two buffers in turn where two fit.  The matrices are symmetric and commute, so both operands are read by rows.
+// columns w, w + 8, ..  The right operand of a product (G and Q in turn) lies whole in every CTA: a CTA copies its rows of it
+// to all of them (bulk copies that count on the receiver's barrier), by two buffers in turn where two fit.  The matrices are symmetric and commute, so both operands are read by rows.
 template <int kTiles>
 __global__ void __launch_bounds__(kThreads)
 thin_chain_kernel(const __grid_constant__ ChainArgs p) {
@@ -140,6 +141,7 @@ thin_chain_kernel(const __grid_constant__ ChainArgs p) {
   constexpr int kBuffers = kTiles <= 8 ? 2 : 1, kFull = S::kSide * S::kPitch, kOwn = 8 * kOwnRows * S::kPitch;
   extern __shared__ __align__(16) double smem[];
   __shared__ double s_f;
+  __shared__ __align__(8) uint64_t s_bar[kBuffers];
   double *g_rows = smem + kBuffers * kFull, *p_rows = g_rows + kOwn;       // tile row cta + kC t at 8 t
   pdl_trigger();
   pdl_wait();
@@ -147,9 +149,12 @@ thin_chain_kernel(const __grid_constant__ ChainArgs p) {
   const int cta = static_cast<int>(cluster_ctarank()), b = blockIdx.x / kC;
   const int fi = lane >> 2, fj = 2 * (lane & 3);                 // this lane's two results in a tile
   int now = 0;                                                   // the buffer of the right operand
-  uint32_t peers[kC];
-#pragma unroll
-  for (int c = 0; c < kC; ++c) peers[c] = map_to_cta(smem_u32(smem), static_cast<uint32_t>(c));
+  uint32_t phase[kBuffers] = {};
+  bool lost = false;             // a copy that has not come in time: go on without waiting, the status says so
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kBuffers; ++i) mbar_init(smem_u32(&s_bar[i]), 1);
+    mbar_fence_init();
+  }
 
   double d1[kOwnRows][kOwnCols][2], d2[kOwnRows][kOwnCols][2];
   auto each = [&](auto f) {
@@ -181,13 +186,20 @@ thin_chain_kernel(const __grid_constant__ ChainArgs p) {
     }
     const int next = kBuffers == 1 ? 0 : now ^ 1;
     each([&](int t, int u, int r, int c) {
-      const uint32_t at = static_cast<uint32_t>(next * kFull + (8 * r + fi) * S::kPitch + 8 * c + fj) * 8u;
-#pragma unroll
-      for (int k = 0; k < kC; ++k)
-        asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(peers[k] + at), "d"(d[t][u][0]), "d"(d[t][u][1]) : "memory");
+      *reinterpret_cast<double2*>(smem + next * kFull + (8 * r + fi) * S::kPitch + 8 * c + fj) = make_double2(d[t][u][0], d[t][u][1]);
     });
-    cluster_arrive();
-    cluster_wait();
+    fence_proxy_async_smem();
+    __syncthreads();
+    constexpr uint32_t kRowBytes = 8 * S::kPitch * 8;
+    const uint32_t bar = smem_u32(&s_bar[next]);
+    if (threadIdx.x == 0) mbar_expect_tx(bar, (kC - 1) * kOwnRows * kRowBytes);
+    if (threadIdx.x < kC * kOwnRows) {          // a copy per thread
+      const int peer = threadIdx.x % kC, r = cta + kC * (threadIdx.x / kC);
+      const uint32_t rows = smem_u32(smem + next * kFull + 8 * r * S::kPitch);
+      if (peer != cta) bulk_copy_to_cta(map_to_cta(rows, static_cast<uint32_t>(peer)), rows, kRowBytes, map_to_cta(bar, static_cast<uint32_t>(peer)));
+    }
+    if (!lost) lost = !mbar_wait_warp(bar, phase[next], p.status);
+    phase[next] ^= 1u;
     now = next;
   };
 
@@ -208,7 +220,7 @@ thin_chain_kernel(const __grid_constant__ ChainArgs p) {
     d1[t][u][0] = x, d1[t][u][1] = y;
     keep(g_rows, t, c, d1[t][u]);
   });
-  cluster_arrive();               // the peers have started: their shared memory may be written
+  cluster_arrive();               // the peers have started: their barriers are there, their shared memory may be written
   cluster_wait();
   publish(d1);
   if (warp == 0) {
@@ -351,7 +363,8 @@ cudaError_t launch_of(const ThinPlan& p, int64_t l, int s, const void* g, void* 
   cudaError_t e = launch_pdl(thin_gram_kernel<T, kTall, kTiles>, dim3(static_cast<unsigned>(nparts), batch), dim3(kThreads), 0, st, 1, x, l, s, per, parts);
   if (e != cudaSuccess) return e;
   ChainArgs c{};
-  c.parts = parts, c.nparts = static_cast<int>(nparts), c.steps = p.steps, c.eps = p.eps, c.scale = p.scale, c.out = pm;
+  c.parts = parts, c.nparts = static_cast<int>(nparts), c.steps = p.steps, c.eps = p.eps, c.scale = p.scale, c.out = pm, c.status = device_status_ptr();
+  if (c.status == nullptr) return cudaErrorInvalidValue;
   for (int i = 0; i < 3 * p.steps; ++i) c.abc[i] = p.abc[i];
   constexpr int kChainBytes = ((kTiles <= 8 ? 2 : 1) * S::kSide + 2 * 8 * (kTiles / S::kCluster)) * S::kPitch * 8;
   static DeviceMask done{0};

@@ -120,7 +120,14 @@ __device__ __forceinline__ void bulk_load_1d(uint32_t dst_smem, const void* src,
                ::"r"(dst_smem), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// The same copy with an L2 eviction hint: the lines it brings in are the first to go, so that a tensor that is read once
+// Untiled bulk copy from this CTA's shared memory to that of a CTA of its cluster (`dst`, `bar`: shared::cluster addresses there), completing
+// on that CTA's mbarrier; addresses and `bytes` multiples of 16.
+__device__ __forceinline__ void bulk_copy_to_cta(uint32_t dst, uint32_t src_smem, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "r"(src_smem), "r"(bytes), "r"(bar) : "memory");
+}
+
+// bulk_load_1d with an L2 eviction hint: the lines it brings in are the first to go, so that a tensor that is read once
 // and then lives in shared memory does not push another kernel's dirty lines out of L2 while it streams in.
 __device__ __forceinline__ uint64_t l2_policy_evict_first() {
   uint64_t p;
