@@ -430,9 +430,11 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
 }
 
 // ---------------------------------------------------------------- the parts of G added up in order, mirrored
-// parts [batch][splits][s][ld], of which chunks of 32 x 32 on and above the diagonal are filled; a CTA takes one of these.
+// out = the parts' sum + beta C: parts [batch][splits][s][ld], of which chunks of 32 x 32 on and above the diagonal are filled; a CTA takes
+// one of these.  C (nullable): laid out like the result.
 __global__ void __launch_bounds__(256)
-ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, __half* hi, __half* lo, int64_t ld_o, int64_t stride_o) {
+ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float beta, const __half* c_hi, const __half* c_lo, __half* hi, __half* lo,
+                       int64_t ld_o, int64_t stride_o) {
   __shared__ float tile[32][33];
   pdl_trigger();
   pdl_wait();
@@ -446,6 +448,11 @@ ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, __half
     if (r < s && c < s) {
       const float* q = parts + (static_cast<int64_t>(b) * splits * s + r) * ld + c;
       for (int k = 0; k < splits; ++k) v += ld_stream(q + static_cast<int64_t>(k) * s * ld);
+      auto term = [&](const __half* m) {
+        return __half2float(__ushort_as_half(ld_stream(reinterpret_cast<const unsigned short*>(m) + b * stride_o + r * ld_o + c)));
+      };
+      if (c_lo != nullptr) v = fmaf(term(c_lo), beta, v);
+      if (c_hi != nullptr) v = fmaf(term(c_hi), beta, v);
     }
     tile[y + 8 * i][x] = v;
   }
@@ -585,30 +592,46 @@ void coefficients_of(const falqon_ortho* p, float* abc) {
     for (int k = 0; k < 3; ++k) abc[3 * i + k] = p->coefficients != nullptr ? p->coefficients[3 * i + k] : kQuintic[k];
 }
 
+// How a product is run: its tiles' width and walk, and over how many CTAs a tile's contraction is split.
+struct Way {
+  TileWalk walk;
+  int tiles, splits;
+};
+// The way that should take the least time.  A block of K takes an instruction of 256 rows about as long at 64 columns as at 128 (measured:
+// 0.22 us at 64 columns, 0.39 at 256; three products at once 0.73 and 0.78 at 64 and 128), so wide tiles whose contraction is split beat
+// narrow ones, where the adding up (a launch, 4 us, and its bytes) is worth it.
+Way pick_way(int64_t M, int64_t N, int64_t K, int64_t batch, bool symmetric, bool precise) {
+  const int64_t pairs = sm_count() / 2, blocks = (K + kKBlock - 1) / kKBlock;
+  const int constant = precise ? 850 : 178;
+  const double per_unit = precise ? 0.0008 : 0.0009;
+  double best = 0.0;
+  Way way{};
+  for (int w = precise ? 128 : 256; w >= 64; w -= 32) {
+    int64_t tiles = 0;
+    const int64_t mt = (M + 255) / 256, nt = (N + w - 1) / w;
+    if (!symmetric) tiles = mt * nt;
+    else for (int64_t n = 0; n < nt; ++n) tiles += std::min(mt, ((n + 1) * w + 255) / 256);
+    const int64_t most = symmetric ? std::max<int64_t>(1, std::min(pairs / (tiles * batch), blocks / 4)) : 1;
+    for (int64_t s = 1; s <= most; ++s) {
+      const int64_t per = (blocks + s - 1) / s, splits = (blocks + per - 1) / per;      // none without a block
+      int64_t cost;
+      const TileWalk walk = plan_walk(tiles * batch * splits, pairs, w, constant, &cost);
+      double us = static_cast<double>(cost) * per_unit * static_cast<double>(per);
+      if (splits > 1) us += 4.0 + static_cast<double>(batch * splits * M * N) * 4e-6;   // half of M N written, then read: 4 bytes at 2 TB/s
+      if (best == 0.0 || us < best) best = us, way = Way{walk, static_cast<int>(tiles), static_cast<int>(splits)};
+    }
+  }
+  return way;
+}
+
 struct Layout {
   int64_t s, l, ld, ld_s;        // short and long side; pitches of X and of the square matrices
   bool tall, precise;
-  int splits, gram_tiles;
+  Way gram, square;
   int norm_parts;
   size_t x_bytes, sq_bytes;
   size_t x[4], sq[4], parts, norm, total;    // offsets: X hi, lo of two turns; G hi, lo, B hi, lo
 };
-
-// The tile's width that takes the least time; *tiles: tiles of a matrix.
-TileWalk pick_walk(int64_t M, int64_t N, int64_t batch, bool symmetric, bool precise, int64_t splits, int64_t* tiles_out) {
-  const int64_t pairs = sm_count() / 2;
-  int64_t best = 0;
-  TileWalk walk{};
-  for (int w = precise ? 128 : 256; w >= 64; w -= 32) {
-    int64_t tiles = 0, cost;
-    const int64_t mt = (M + 255) / 256, nt = (N + w - 1) / w;
-    if (!symmetric) tiles = mt * nt;
-    else for (int64_t n = 0; n < nt; ++n) tiles += std::min(mt, ((n + 1) * w + 255) / 256);
-    const TileWalk of = plan_walk(tiles * batch * splits, pairs, w, precise ? 64 : 256, &cost);
-    if (best == 0 || cost < best) best = cost, walk = of, *tiles_out = tiles;
-  }
-  return walk;
-}
 
 bool plan_ok(const falqon_ortho* p) {
   return p != nullptr && p->batch >= 1 && p->batch <= 65535 && p->rows >= 1 && p->cols >= 1 && p->rows <= 32768 && p->cols <= 32768 &&
@@ -626,14 +649,9 @@ Layout layout_of(const falqon_ortho* p) {
   y.ld_s = round_up(y.s, 64);
   y.x_bytes = static_cast<size_t>(p->batch * p->rows * y.ld) * 2;
   y.sq_bytes = static_cast<size_t>(p->batch * y.s * y.ld_s) * 2;
-  // G's contraction is the long one: where its tiles leave pairs idle, several share a tile, each at least four blocks of K
-  int64_t tiles;
-  pick_walk(y.s, y.s, p->batch, true, y.precise, 1, &tiles);
-  const int64_t pairs = sm_count() / 2, blocks = (y.l + kKBlock - 1) / kKBlock;
-  int64_t splits = pairs / (tiles * p->batch);
-  if (splits > blocks / 4) splits = blocks / 4;
-  const int64_t per = splits > 1 ? (blocks + splits - 1) / splits : blocks;
-  y.splits = static_cast<int>((blocks + per - 1) / per);      // none without a block
+  y.gram = pick_way(y.s, y.s, y.l, p->batch, true, y.precise);
+  y.square = pick_way(y.s, y.s, y.s, p->batch, true, y.precise);
+  const int splits = std::max(y.gram.splits, y.square.splits);
   const int64_t count = p->rows * p->cols;
   int64_t np = (count + 16383) / 16384;
   const int64_t cap = std::max<int64_t>(1, 8 * static_cast<int64_t>(sm_count()) / p->batch);
@@ -642,7 +660,7 @@ Layout layout_of(const falqon_ortho* p) {
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 1023) / 1024 * 1024; return o; };
   for (int i = 0; i < 4; ++i) y.x[i] = take(y.x_bytes);
   for (int i = 0; i < 4; ++i) y.sq[i] = take((i & 1) == 0 || y.precise ? y.sq_bytes : 0);
-  y.parts = take(y.splits > 1 ? static_cast<size_t>(p->batch) * y.splits * y.s * y.ld_s * 4 : 0);
+  y.parts = take(splits > 1 ? static_cast<size_t>(p->batch) * splits * y.s * y.ld_s * 4 : 0);
   y.norm = take(static_cast<size_t>(p->batch) * y.norm_parts * 8);
   y.total = at;
   return y;
@@ -654,14 +672,11 @@ struct Matrix {          // [batch][rows][cols] as hi and lo; mn: contracted alo
   bool mn;
 };
 
-cudaError_t launch_product(ProductArgs g, const Matrix& a, const Matrix& b, int64_t batch, int64_t M, int64_t N, int64_t K, bool precise,
+cudaError_t launch_product(ProductArgs g, const Way& way, const Matrix& a, const Matrix& b, int64_t batch, int64_t M, int64_t N, int64_t K, bool precise,
                            cudaStream_t st) {
   g.M = static_cast<int>(M), g.N = static_cast<int>(N), g.batch = static_cast<int>(batch);
   g.kblocks = static_cast<int>((K + kKBlock - 1) / kKBlock);
-  if (g.splits < 1) g.splits = 1;
-  int64_t tiles;
-  g.walk = pick_walk(M, N, batch, g.symmetric, precise, g.splits, &tiles);
-  g.tiles = static_cast<int>(tiles);
+  g.walk = way.walk, g.tiles = way.tiles, g.splits = way.splits;
   g.m_tiles = static_cast<int>((M + 255) / 256);
   g.per_split = (g.kblocks + g.splits - 1) / g.splits;
   g.a_mn = a.mn, g.b_mn = b.mn;
@@ -717,38 +732,37 @@ int run(const falqon_ortho* p, const void* g, void* out, uint8_t* scratch, cudaS
   if (e != cudaSuccess) return FALQON_ERR_CUDA;
   __half *g_hi = halves(y.sq[0]), *g_lo = y.precise ? halves(y.sq[1]) : nullptr, *b_hi = halves(y.sq[2]), *b_lo = y.precise ? halves(y.sq[3]) : nullptr;
   const int64_t sq_stride = y.s * y.ld_s, x_stride = p->rows * y.ld;
+  const Way apply = pick_way(p->rows, p->cols, y.s, p->batch, false, y.precise);
+  // a symmetric product: to `hi`, `lo` at once, or in parts that are added up there
+  auto symmetric = [&](ProductArgs a, const Way& way, const Matrix& x, int64_t K, __half* hi, __half* lo) {
+    a.symmetric = true;
+    a.mode = way.splits > 1 ? kPart : kHiLo;
+    a.parts = reinterpret_cast<float*>(scratch + y.parts);
+    a.o_hi = hi, a.o_lo = lo, a.ld_o = y.ld_s, a.stride_o = sq_stride;
+    const __half *c_hi = a.c_hi, *c_lo = a.c_lo;
+    if (way.splits > 1) a.c_hi = a.c_lo = nullptr;
+    cudaError_t r = launch_product(a, way, x, x, p->batch, y.s, y.s, K, y.precise, st);
+    if (r != cudaSuccess || way.splits == 1) return r;
+    const unsigned n = static_cast<unsigned>((y.s + 31) / 32);
+    return launch_pdl(ortho_add_parts_kernel, dim3(n, n, static_cast<unsigned>(p->batch)), dim3(256), 0, st, 1, a.parts, way.splits, static_cast<int>(y.s),
+                      y.ld_s, a.beta, c_hi, c_lo, hi, lo, y.ld_s, sq_stride);
+  };
   for (int i = 0; i < p->steps; ++i) {
     const float* abc = p->coefficients != nullptr ? p->coefficients + 3 * i : kQuintic;
     const int now = 2 * (i & 1), then = 2 - now;
     __half *x_hi = halves(y.x[now]), *x_lo = halves(y.x[now + 1]);
     // G = X X^T (X^T X where tall)
     {
-      const Matrix x{x_hi, x_lo, p->rows, p->cols, y.ld, y.tall};
       ProductArgs a{};
-      a.symmetric = true;
       a.alpha = 1.0f / kScale;
-      a.splits = y.splits;
-      a.mode = y.splits > 1 ? kPart : kHiLo;
-      a.parts = reinterpret_cast<float*>(scratch + y.parts);
-      a.o_hi = g_hi, a.o_lo = g_lo, a.ld_o = y.ld_s, a.stride_o = sq_stride;
-      if ((e = launch_product(a, x, x, p->batch, y.s, y.s, y.l, y.precise, st)) != cudaSuccess) return FALQON_ERR_CUDA;
-      if (y.splits > 1) {
-        const unsigned n = static_cast<unsigned>((y.s + 31) / 32);
-        if ((e = launch_pdl(ortho_add_parts_kernel, dim3(n, n, static_cast<unsigned>(p->batch)), dim3(256), 0, st, 1, a.parts, y.splits,
-                            static_cast<int>(y.s), y.ld_s, g_hi, g_lo, y.ld_s, sq_stride)) != cudaSuccess)
-          return FALQON_ERR_CUDA;
-      }
+      if (symmetric(a, y.gram, Matrix{x_hi, x_lo, p->rows, p->cols, y.ld, y.tall}, y.l, g_hi, g_lo) != cudaSuccess) return FALQON_ERR_CUDA;
     }
     // B = b G + c G G
     {
-      const Matrix q{g_hi, g_lo, y.s, y.s, y.ld_s, false};
       ProductArgs a{};
-      a.symmetric = true;
       a.alpha = abc[2] / kScale, a.beta = abc[1];
       a.c_hi = g_hi, a.c_lo = g_lo, a.ld_c = y.ld_s, a.stride_c = sq_stride;
-      a.mode = kHiLo;
-      a.o_hi = b_hi, a.o_lo = b_lo, a.ld_o = y.ld_s, a.stride_o = sq_stride;
-      if ((e = launch_product(a, q, q, p->batch, y.s, y.s, y.s, y.precise, st)) != cudaSuccess) return FALQON_ERR_CUDA;
+      if (symmetric(a, y.square, Matrix{g_hi, g_lo, y.s, y.s, y.ld_s, false}, y.s, b_hi, b_lo) != cudaSuccess) return FALQON_ERR_CUDA;
     }
     // X <- a X + B X (a X + X B where tall)
     {
@@ -762,8 +776,8 @@ int run(const falqon_ortho* p, const void* g, void* out, uint8_t* scratch, cudaS
       a.o_hi = halves(y.x[then]), a.o_lo = halves(y.x[then + 1]), a.ld_o = y.ld, a.stride_o = x_stride;
       a.out = out, a.out_bf16 = p->out_dtype == FALQON_BF16;
       a.out_vec = p->cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (a.out_bf16 ? 7 : 15)) == 0;
-      e = y.tall ? launch_product(a, x, m, p->batch, p->rows, p->cols, y.s, y.precise, st)
-                 : launch_product(a, m, x, p->batch, p->rows, p->cols, y.s, y.precise, st);
+      e = y.tall ? launch_product(a, apply, x, m, p->batch, p->rows, p->cols, y.s, y.precise, st)
+                 : launch_product(a, apply, m, x, p->batch, p->rows, p->cols, y.s, y.precise, st);
       if (e != cudaSuccess) return FALQON_ERR_CUDA;
     }
   }
