@@ -5,7 +5,7 @@
 // not powers of two would have to be applied to every partial tile of 128 on its way through registers.
 //
 // Two CTAs of a cluster compute a tile of 256 x block_n (one tcgen05.mma cta_group::2), a persistent pair walking its tiles (tile_walk.cuh):
-//   warp 0        TMA producer: 128 rows of A and block_n / 2 rows of B per CTA and stage of 128 values of K
+//   warp 0        TMA producer: up to 128 rows of A and block_n / 2 rows of B per CTA and stage of 128 values of K
 //   warp 1        (leader) issues the MMAs
 //   warps 2..9    epilogue: tensor memory -> registers -> shared memory -> full 128-byte lines
 //   warps 10..13  scales: global memory -> tensor memory (tcgen05.st), four blocks of K at a time, the four bytes of a word
@@ -13,6 +13,9 @@
 // columns 192..255, and the epilogue reads those first: the next tile's MMAs start as soon as they are in registers, so that the
 // rest of the epilogue runs beside them.
 // The three products differ in how the codes lie (K-major or MN-major, no transposed copies) and in the strides of their scales.
+// Few tiles and a long contraction: a cluster of four or eight CTAs shares a tile, its pairs' parts added up in order through shared memory.
+// What bounds it: the tensor cores under the board's power cap -- 4096 x 4096 x 11008 forward 145 to 156 us (2.4 to 2.55 PFLOP/s), the same
+// kernel without block scales no faster; with few rows the MMAs, which take 0.22 us a block of K however narrow the tile is.
 // Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
 #include <cuda.h>
 
@@ -55,6 +58,7 @@ struct ProductArgs {
   int m_tiles;
   TileWalk walk;
   bool a_mn, b_mn;
+  int split, split_blocks;    // pairs of a cluster that share a tile's contraction, and how many of its blocks each takes (1: all)
   int stages;
   uint32_t a_bytes, b_off, stage_bytes;      // of A in a stage, where B starts, stride
   uint32_t idesc;             // without N and the scale bytes
@@ -89,6 +93,9 @@ __device__ __forceinline__ uint32_t scale_word(const Bytes& w, const Scales& s) 
   return s.words ? w.v[0] : w.v[0] | w.v[1] << 8 | w.v[2] << 16 | w.v[3] << 24;
 }
 
+constexpr int kPartPitch = 256 + 4;           // of a part's rows in fp32: 128 of them fit into the ring
+__device__ __forceinline__ float* part_of(uint8_t* gen) { return reinterpret_cast<float*>(gen); }
+
 __global__ void __launch_bounds__(kThreads, 1)
 block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
@@ -105,8 +112,10 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const uint32_t slot = acc_empty_bar + 8u;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
+  // rank: in the pair.  With split > 1 a cluster is that many pairs, and they have one tile.
+  const uint32_t cluster_rank = cluster_ctarank(), rank = cluster_rank & 1u, first_rank = cluster_rank & ~1u;
   const bool leader = rank == 0;
+  const uint16_t both = static_cast<uint16_t>(3u << first_rank);
 
   if (threadIdx.x == 0) {
     prefetch_tensor_map(&map_a);
@@ -136,7 +145,8 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(gen + (slot - base));
   pdl_wait();
 
-  const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  const int pairs = gridDim.x / (2 * p.split), pair = blockIdx.x / (2 * p.split);      // that have tiles of their own
+  const int kb_begin = static_cast<int>(cluster_rank >> 1) * p.split_blocks, kb_end = min(p.kblocks, kb_begin + p.split_blocks);
   const int items = p.walk.items;
   bool aborted = false;
   struct Piece { int row0, n0, width; };           // of this CTA: rows, columns; no columns: a piece behind the right edge, of which there is nothing
@@ -157,11 +167,11 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       const Piece t = piece(item);
       if (t.width == 0) continue;
       const int row0 = t.row0, bn0 = t.n0 + static_cast<int>(rank) * (inst_n(t) >> 1);
-      for (int kb = 0; kb < p.kblocks; ++kb) {
+      for (int kb = kb_begin; kb < kb_end; ++kb) {
         if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.status)) { aborted = true; break; }
         if (elect_one()) {
           if (leader) mbar_expect_tx(full_bar(stage), 2 * bytes);
-          const uint32_t fb = map_to_cta(full_bar(stage), 0);
+          const uint32_t fb = map_to_cta(full_bar(stage), first_rank);
           const uint32_t a_dst = base + static_cast<uint32_t>(stage) * stage_bytes, b_dst = a_dst + p.b_off;
           if (p.a_mn) tma_load_2d_pair(a_dst, &map_a, fb, row0, kb * kBlockKBytes);
           else        tma_load_2d_pair(a_dst, &map_a, fb, kb * kBlockKBytes, row0);
@@ -196,7 +206,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
         first = false;
         const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
-        for (int kb = 0; kb < p.kblocks; ++kb) {
+        for (int kb = kb_begin; kb < kb_end; ++kb) {
           const int byte = kb % kGroupBlocks;
           if (byte == 0 && !mbar_wait_warp(sf_full_bar(group), sf_phase, p.status)) { aborted = true; break; }
           if (!mbar_wait_warp(full_bar(stage), phase, p.status)) { aborted = true; break; }
@@ -204,20 +214,20 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           const uint32_t off = (static_cast<uint32_t>(stage) * stage_bytes) >> 4;
           const uint32_t sfa = tmem + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
           const uint32_t idesc = idesc_n | (static_cast<uint32_t>(byte) << 29) | (static_cast<uint32_t>(byte) << 4);
-          const bool last = byte == kGroupBlocks - 1 || kb == p.kblocks - 1;
+          const bool last = byte == kGroupBlocks - 1 || kb == kb_end - 1;
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < kBlockKBytes / kUmmaK; ++k)
-              umma_mx8_pair(d, a_desc0 + off + k * a_step, b_desc0 + off + k * b_step, idesc, sfa, sfa + 4, (kb > 0 || k > 0) ? 1u : 0u);
-            umma_commit_pair(empty_bar(stage), 3);
-            if (last) umma_commit_pair(sf_empty_bar(group), 3);
+              umma_mx8_pair(d, a_desc0 + off + k * a_step, b_desc0 + off + k * b_step, idesc, sfa, sfa + 4, (kb > kb_begin || k > 0) ? 1u : 0u);
+            umma_commit_pair(empty_bar(stage), both);
+            if (last) umma_commit_pair(sf_empty_bar(group), both);
           }
           __syncwarp();
           if (++stage == n_stages) { stage = 0; phase ^= 1u; }
           if (last && ++group == kGroups) { group = 0; sf_phase ^= 1u; }
         }
         if (aborted) break;
-        if (elect_one()) umma_commit_pair(acc_full_bar, 3);
+        if (elect_one()) umma_commit_pair(acc_full_bar, both);
         __syncwarp();
         acc ^= 1;
       }
@@ -232,11 +242,11 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     // each load: 4096 x 16384 x 4096 333 us).
     constexpr int kAhead = 3;
     struct Entry { Bytes a, b0, b1; };
-    int next_item = pair, next_kb = 0;
+    int next_item = pair, next_kb = kb_begin;
     const uint8_t *row_a = nullptr, *row_b0 = nullptr, *row_b1 = nullptr;
     auto fetch = [&](Entry& w) {
       if (next_item >= items) return;
-      if (next_kb == 0) {
+      if (next_kb == kb_begin) {
         const Piece t = piece(next_item);
         row_a = scale_row(p.sa, t.row0 + 32 * q + lane);
         row_b0 = scale_row(p.sb, t.n0 + 32 * q + lane);
@@ -246,8 +256,8 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       scale_fetch(w.b0, p.sb, row_b0, next_kb, p.kblocks);
       scale_fetch(w.b1, p.sb, row_b1, next_kb, p.kblocks);
       next_kb += kGroupBlocks;
-      if (next_kb >= p.kblocks) {
-        next_kb = 0;
+      if (next_kb >= kb_end) {
+        next_kb = kb_begin;
         do next_item += pairs; while (next_item < items && piece(next_item).width == 0);
       }
     };
@@ -256,7 +266,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     while (next_item < items && piece(next_item).width == 0) next_item += pairs;
     int steps = 0;
     for (int item = pair; item < items; item += pairs) steps += piece(item).width != 0;
-    steps *= (p.kblocks + kGroupBlocks - 1) / kGroupBlocks;
+    steps *= (kb_end - kb_begin + kGroupBlocks - 1) / kGroupBlocks;
     Entry ahead[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) fetch(ahead[j]);
@@ -284,7 +294,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           tc_fence_before_sync();
           __syncwarp();
           // (a release at cluster scope would wait for the loads ahead, too: 281 us instead of 253)
-          if (lane == 0) mbar_arrive_remote(map_to_cta(sf_full_bar(group), 0));
+          if (lane == 0) mbar_arrive_remote(map_to_cta(sf_full_bar(group), first_rank));
         }
         // the words have been read; and all four warps leave together, or the barriers would be waited for in vain
         uint32_t any;
@@ -320,7 +330,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       if (count == 0) {
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, 0));
+        if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
       }
       for (int i = 0; i < count; ++i) {
         const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
@@ -332,7 +342,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         if (i == 0) {
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, 0));
+          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
         }
         uint8_t* my = stage_out + lane * 128;
         const int sw = lane & 7;
@@ -351,6 +361,17 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
           }
           __syncwarp();
         };
+        if (p.split > 1) {      // to be added up: this CTA's rows of the tile as fp32, where the stages were (every copy has been multiplied)
+          if (row0 + lane < p.M) {
+            float* row = part_of(gen) + (row0 + lane - of.row0) * kPartPitch + c0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              reinterpret_cast<uint4*>(row)[j] = make_uint4(v0[4 * j], v0[4 * j + 1], v0[4 * j + 2], v0[4 * j + 3]);
+              reinterpret_cast<uint4*>(row + 32)[j] = make_uint4(v1[4 * j], v1[4 * j + 1], v1[4 * j + 2], v1[4 * j + 3]);
+            }
+          }
+          continue;
+        }
         if (p.bf16) {
           auto put = [&](const uint32_t (&v)[32], int first_piece) {
 #pragma unroll
@@ -378,6 +399,28 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
       }
       acc ^= 1;
+    }
+  }
+
+  if (p.split > 1) {
+    // ------------------------------------------------------------ the pairs' parts of the tile, added up in order, a strip of columns a pair
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    const Piece t = piece(pair);
+    const int rows = max(0, min(kBlockM, p.M - t.row0)), strip = t.width > 0 ? (t.width / 4 + p.split - 1) / p.split : 0;   // in groups of four columns
+    const int first = static_cast<int>(cluster_rank >> 1) * strip, count = max(0, min(strip, t.width / 4 - first));
+    for (int u = threadIdx.x; u < rows * count; u += kThreads) {
+      const int r = u / count, c = 4 * (first + u - r * count);
+      const uint32_t at = smem_u32(part_of(gen) + r * kPartPitch + c);
+      float4 v = ld_shared_cluster_f32x4(map_to_cta(at, rank));
+      for (int s = 1; s < p.split; ++s) {
+        const float4 w = ld_shared_cluster_f32x4(map_to_cta(at, rank + 2 * s));
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      }
+      const long long o = static_cast<long long>(t.row0 + r) * p.N + t.n0 + c;
+      if (p.bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + o) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+      else *reinterpret_cast<float4*>(static_cast<float*>(p.out) + o) = v;
     }
   }
 
@@ -411,13 +454,23 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
   g.m_tiles = static_cast<int>((M + 255) / 256);
   const int64_t pairs_all = sm_count() / 2;
-  // The tile's width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 less)
+  constexpr int kClustersOf4 = 32, kClustersOf8 = 14;      // that are resident together, one CTA to an SM, with SMs in groups of 16 to 20
   const int64_t a_rows = a.mn || M >= 128 ? 128 : round_up(M, 8);
-  int64_t best = 0;
+  // The tiles' width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 243);
+  // or so few tiles that two or four pairs can share each one's contraction (a cluster's parts are added up through its shared memory).
+  // A block of K takes 0.16 us and 0.9 ns a column, adding up about 2.5 us (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 x 11008
+  // x 4096 29 and 20.5; 512 x 4096 x 4096 15.7 and 17.1).
+  double best = 0.0;
   for (int w = 256; w >= 64; w -= 32) {
-    int64_t cost;
-    const TileWalk walk = plan_walk(g.m_tiles * ((N + w - 1) / w), pairs_all, w, static_cast<int>(2 * a_rows), &cost);
-    if (best == 0 || cost < best) best = cost, g.walk = walk;
+    const int64_t tiles = g.m_tiles * ((N + w - 1) / w);
+    for (int s = 1; s <= 4; s *= 2) {
+      const int64_t per = s == 1 ? g.kblocks : round_up((g.kblocks + s - 1) / s, kGroupBlocks);
+      if (s > 1 && (tiles > (s == 2 ? kClustersOf4 : kClustersOf8) || per * (s - 1) >= g.kblocks)) continue;
+      int64_t cost;
+      const TileWalk walk = plan_walk(tiles, s == 1 ? pairs_all : tiles, w, 178, &cost);
+      const double us = static_cast<double>(cost) * 0.0009 * static_cast<double>(per) + (s > 1 ? 2.5 : 0.0);
+      if (best == 0.0 || us < best) best = us, g.walk = walk, g.split = s, g.split_blocks = static_cast<int>(per);
+    }
   }
   g.a_bytes = static_cast<uint32_t>(a_rows) * kBlockKBytes;
   g.b_off = static_cast<uint32_t>(round_up(g.a_bytes, 1024));
@@ -439,11 +492,11 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   CUtensorMap ma, mb;
   if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, static_cast<uint32_t>(a_rows))) return cudaErrorInvalidValue;
   if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
-  const int64_t pairs = g.walk.items < pairs_all ? g.walk.items : pairs_all;
+  const int64_t pairs = (g.walk.items < pairs_all ? g.walk.items : pairs_all) * g.split;
   static DeviceMask configured{0};
   const cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
   if (e != cudaSuccess) return e;
-  return launch_pdl(block_product_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, 2, ma, mb, g);
+  return launch_pdl(block_product_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g);
 }
 
 Scales scales_of(const uint8_t* p, int along, int64_t rows, int64_t cols, bool over_rows) {
