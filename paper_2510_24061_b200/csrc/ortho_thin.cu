@@ -208,7 +208,7 @@ thin_chain_kernel(const __grid_constant__ ChainArgs p) {
     double x = 0.0, y = 0.0;
     const int i = 8 * r + fi, j = 8 * c + fj;
     const double* q = parts + (r <= c ? i * S::kSide + j : j * S::kSide + i);
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < p.nparts; ++k, q += S::kSize) {
       if (r <= c) {
         const double2 v = __ldcg(reinterpret_cast<const double2*>(q));

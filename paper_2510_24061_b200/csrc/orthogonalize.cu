@@ -199,9 +199,9 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
 // kPrecise: both operands as hi + lo, which a stage holds together: hi hi in one accumulator, hi lo + lo hi in a second, whose sums are
 // 2^11 times smaller.  The tensor core's additions cut off instead of rounding, which over a long sum of squares (G's diagonal) is a
 // bias; so the first is added up in registers every kChunk blocks of K (1000 x 1531: results 1.5e-5 off without, 7.9e-6 every 8
-// blocks, 3.9e-6 every 4; plain fp32 products 3.0e-6).  Columns 0..255 are two accumulators of hi hi, a chunk each in turn, 256..511 two of
+// blocks, 3.9e-6 every 4, 2.0e-6 every 2 in 3 % more time; plain fp32 products 3.0e-6).  Columns 0..255 are two accumulators of hi hi, a chunk each in turn, 256..511 two of
 // the others, a tile each in turn: by the time a tile's first chunk may be written, the tile before the last has been read.
-constexpr int kChunk = 4;
+constexpr int kChunk = 2;
 
 template <bool kPrecise>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -432,7 +432,7 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
 // ---------------------------------------------------------------- the parts of G added up in order, mirrored
 // out = the parts' sum + beta C: parts [batch][splits][s][ld], of which chunks of 32 x 32 on and above the diagonal are filled; a CTA takes
 // one of these.  C (nullable): laid out like the result.
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float beta, const __half* c_hi, const __half* c_lo, __half* hi, __half* lo,
                        int64_t ld_o, int64_t stride_o) {
   __shared__ float tile[32][33];
@@ -440,37 +440,36 @@ ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float 
   pdl_wait();
   const int b = blockIdx.z, r0 = blockIdx.y * 32, c0 = blockIdx.x * 32;
   if (c0 < r0) return;
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, r = r0 + y, c = c0 + x;
+  float v = 0.0f;
+  if (r < s && c < s) {
+    const float* q = parts + (static_cast<int64_t>(b) * splits * s + r) * ld + c;
+    // in order, the loads of eight parts on their way at once (a value a thread: 256 threads with four each took 10 us for 18 parts of 300 x 300)
+    for (int k = 0; k < splits; k += 8) {
+      float part[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = r0 + y + 8 * i, c = c0 + x;
-    float v = 0.0f;
-    if (r < s && c < s) {
-      const float* q = parts + (static_cast<int64_t>(b) * splits * s + r) * ld + c;
-      for (int k = 0; k < splits; ++k) v += ld_stream(q + static_cast<int64_t>(k) * s * ld);
-      auto term = [&](const __half* m) {
-        return __half2float(__ushort_as_half(ld_stream(reinterpret_cast<const unsigned short*>(m) + b * stride_o + r * ld_o + c)));
-      };
-      if (c_lo != nullptr) v = fmaf(term(c_lo), beta, v);
-      if (c_hi != nullptr) v = fmaf(term(c_hi), beta, v);
+      for (int i = 0; i < 8; ++i) part[i] = k + i < splits ? ld_stream(q + static_cast<int64_t>(k + i) * s * ld) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v += part[i];
     }
-    tile[y + 8 * i][x] = v;
+    auto term = [&](const __half* m) {
+      return __half2float(__ushort_as_half(ld_stream(reinterpret_cast<const unsigned short*>(m) + b * stride_o + r * ld_o + c)));
+    };
+    if (c_lo != nullptr) v = fmaf(term(c_lo), beta, v);
+    if (c_hi != nullptr) v = fmaf(term(c_hi), beta, v);
   }
+  tile[y][x] = v;
   __syncthreads();
-  auto put = [&](int r, int c, float v) {
-    if (r >= s || c >= s) return;
-    const int64_t at = b * stride_o + r * ld_o + c;
-    const __half h = __float2half_rn(v);
+  auto put = [&](int row, int col, float w) {
+    if (row >= s || col >= s) return;
+    const int64_t at = b * stride_o + row * ld_o + col;
+    const __half h = __float2half_rn(w);
     hi[at] = h;
-    if (lo != nullptr) lo[at] = __float2half_rn(v - __half2float(h));
+    if (lo != nullptr) lo[at] = __float2half_rn(w - __half2float(h));
   };
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int rr = y + 8 * i;
-    const bool diagonal = r0 == c0;
-    put(r0 + rr, c0 + x, diagonal ? tile[min(rr, x)][max(rr, x)] : tile[rr][x]);
-    if (!diagonal) put(c0 + rr, r0 + x, tile[x][rr]);
-  }
+  const bool diagonal = r0 == c0;
+  put(r, c, diagonal ? tile[min(y, x)][max(y, x)] : v);
+  if (!diagonal) put(c0 + y, r0 + x, tile[x][y]);
 }
 
 // ---------------------------------------------------------------- the norm, and X from g
@@ -744,7 +743,7 @@ int run(const falqon_ortho* p, const void* g, void* out, uint8_t* scratch, cudaS
     cudaError_t r = launch_product(a, way, x, x, p->batch, y.s, y.s, K, y.precise, st);
     if (r != cudaSuccess || way.splits == 1) return r;
     const unsigned n = static_cast<unsigned>((y.s + 31) / 32);
-    return launch_pdl(ortho_add_parts_kernel, dim3(n, n, static_cast<unsigned>(p->batch)), dim3(256), 0, st, 1, a.parts, way.splits, static_cast<int>(y.s),
+    return launch_pdl(ortho_add_parts_kernel, dim3(n, n, static_cast<unsigned>(p->batch)), dim3(1024), 0, st, 1, a.parts, way.splits, static_cast<int>(y.s),
                       y.ld_s, a.beta, c_hi, c_lo, hi, lo, y.ld_s, sq_stride);
   };
   for (int i = 0; i < p->steps; ++i) {
