@@ -447,6 +447,30 @@ struct Operand {
   Scales s;
 };
 
+// How many clusters of four or eight CTAs, one CTA to an SM, the current device holds at once: a matter of its groups of SMs, which are not
+// all whole.  Asked once per device; 0 where it cannot be told (no tile is split then).
+int resident_clusters(int size) {
+  static std::atomic<int> known[2][kMaxDevices];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  std::atomic<int>& at = known[size == 8][dev];
+  if ((n = at.load(std::memory_order_acquire)) != 0) return n < 0 ? 0 : n;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(sm_count() / size * size));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(size);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, block_product_kernel, &cfg) != cudaSuccess || n < 1) n = -1;
+  at.store(n, std::memory_order_release);
+  return n < 0 ? 0 : n;
+}
+
 cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
   ProductArgs g{};
   g.M = static_cast<int>(M);
@@ -454,21 +478,24 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
   g.m_tiles = static_cast<int>((M + 255) / 256);
   const int64_t pairs_all = sm_count() / 2;
-  constexpr int kClustersOf4 = 32, kClustersOf8 = 14;      // that are resident together, one CTA to an SM, with SMs in groups of 16 to 20
+  static DeviceMask configured{0};
+  cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
+  if (e != cudaSuccess) return e;
   const int64_t a_rows = a.mn || M >= 128 ? 128 : round_up(M, 8);
   // The tiles' width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 243);
   // or so few tiles that two or four pairs can share each one's contraction (a cluster's parts are added up through its shared memory).
-  // A block of K takes 0.16 us and 0.9 ns a column, adding up about 2.5 us (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 x 11008
-  // x 4096 29 and 20.5; 512 x 4096 x 4096 15.7 and 17.1).
+  // A block of K takes 0.16 us and 0.9 ns a column, adding up 1.5 to 3.5 us
+  // with the rows (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 rows 11008 -> 4096 30.6 and 20.5, 4096 -> 4096 15.1 and
+  // 12.3; 512 rows 4096 -> 4096 15.8 and 17.1, which stays unsplit).
   double best = 0.0;
   for (int w = 256; w >= 64; w -= 32) {
     const int64_t tiles = g.m_tiles * ((N + w - 1) / w);
     for (int s = 1; s <= 4; s *= 2) {
       const int64_t per = s == 1 ? g.kblocks : round_up((g.kblocks + s - 1) / s, kGroupBlocks);
-      if (s > 1 && (tiles > (s == 2 ? kClustersOf4 : kClustersOf8) || per * (s - 1) >= g.kblocks)) continue;
+      if (s > 1 && (tiles > resident_clusters(2 * s) || per * (s - 1) >= g.kblocks)) continue;
       int64_t cost;
       const TileWalk walk = plan_walk(tiles, s == 1 ? pairs_all : tiles, w, 178, &cost);
-      const double us = static_cast<double>(cost) * 0.0009 * static_cast<double>(per) + (s > 1 ? 2.5 : 0.0);
+      const double us = static_cast<double>(cost) * 0.0009 * static_cast<double>(per) + (s > 1 ? 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0 : 0.0);
       if (best == 0.0 || us < best) best = us, g.walk = walk, g.split = s, g.split_blocks = static_cast<int>(per);
     }
   }
@@ -493,9 +520,6 @@ cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_
   if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, static_cast<uint32_t>(a_rows))) return cudaErrorInvalidValue;
   if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
   const int64_t pairs = (g.walk.items < pairs_all ? g.walk.items : pairs_all) * g.split;
-  static DeviceMask configured{0};
-  const cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
-  if (e != cudaSuccess) return e;
   return launch_pdl(block_product_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g);
 }
 
