@@ -29,7 +29,7 @@ extern "C" {
 typedef enum { FALQON_ALONG_ROW = 0, FALQON_ALONG_COL = 1, FALQON_TILE = 2 } falqon_blocking;
 
 /* x has a row pitch of ld >= cols values and is aligned to its type only (16-byte aligned rows are faster).  Codes are dense
- * and need no alignment (8 bytes are faster).  rows, cols <= 2^30, rows * cols <= 2^42. */
+ * and need no alignment (8 bytes are faster).  rows, cols <= 2^30, rows * cols <= 2^42, rows * ld <= 2^44. */
 int falqon_block_quantize(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, falqon_fp8 fmt, falqon_blocking along,
                           uint8_t *codes, uint8_t *scales, falqon_stream stream);
 /* FALQON_ALONG_ROW and FALQON_ALONG_COL of the same tensor in one read: what a training step needs of a layer's input (forward,

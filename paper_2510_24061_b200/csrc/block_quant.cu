@@ -353,7 +353,7 @@ int quantize(int what, const void* x, int64_t rows, int64_t cols, int64_t ld, in
 
 int quantize_checked(int what, const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int fmt, uint8_t* row_codes,
                      uint8_t* row_scales, uint8_t* col_codes, uint8_t* col_scales, cudaStream_t st) {
-  if (x == nullptr || x == row_codes || x == col_codes || !sizes_ok(rows, cols) || ld < cols || ld > (int64_t{1} << 40) || (dtype != FALQON_BF16 && dtype != FALQON_F32) ||
+  if (x == nullptr || x == row_codes || x == col_codes || !sizes_ok(rows, cols) || ld < cols || ld > (int64_t{1} << 44) / rows || (dtype != FALQON_BF16 && dtype != FALQON_F32) ||
       (fmt != FALQON_E4M3 && fmt != FALQON_E5M2) || !aligned_to(x, dtype == FALQON_BF16 ? 2 : 4))
     return FALQON_ERR_INVALID_ARG;
   return dtype == FALQON_BF16 ? quantize<bf16_t>(what, x, rows, cols, ld, fmt, row_codes, row_scales, col_codes, col_scales, st)

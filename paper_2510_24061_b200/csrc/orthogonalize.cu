@@ -722,8 +722,7 @@ cudaError_t launch_start(const falqon_ortho* p, const Layout& y, const void* g, 
                                static_cast<double>(p->eps), hi, lo, y.ld, stride);
 }
 
-int run(const falqon_ortho* p, const void* g, void* out, uint8_t* scratch, cudaStream_t st) {
-  const Layout y = layout_of(p);
+int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_t* scratch, cudaStream_t st) {
   auto halves = [&](size_t off) { return reinterpret_cast<__half*>(scratch + off); };
   double* norm = reinterpret_cast<double*>(scratch + y.norm);
   cudaError_t e = p->dtype == FALQON_BF16 ? launch_start<bf16_t>(p, y, g, norm, halves(y.x[0]), halves(y.x[1]), st)
@@ -802,13 +801,16 @@ int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* 
       !range_ok(p->coefficients, p->steps) || (reinterpret_cast<uintptr_t>(g) & (p->dtype == FALQON_BF16 ? 1 : 3)) != 0 ||
       (reinterpret_cast<uintptr_t>(out) & (p->out_dtype == FALQON_BF16 ? 1 : 3)) != 0 || (g == out && p->dtype != p->out_dtype))
     return FALQON_ERR_INVALID_ARG;
-  if (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0 || scratch_bytes < falqon_orthogonalize_scratch_bytes(p))
-    return FALQON_ERR_WORKSPACE;
+  if (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) return FALQON_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
   ThinPlan thin{p->batch, p->rows, p->cols, p->dtype == FALQON_BF16, p->out_dtype == FALQON_BF16, p->steps, p->eps, p->scale, {}};
   coefficients_of(p, thin.abc);
-  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.out_bf16, thin.abc, p->steps))
-    return launch_ortho_thin(thin, g, out, scratch, static_cast<cudaStream_t>(stream)) == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA;
-  return run(p, g, out, static_cast<uint8_t*>(scratch), static_cast<cudaStream_t>(stream));
+  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.out_bf16, thin.abc, p->steps)) {
+    if (scratch_bytes < ortho_thin_scratch_bytes(p->batch, p->rows, p->cols)) return FALQON_ERR_WORKSPACE;
+    return launch_ortho_thin(thin, g, out, scratch, st) == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA;
+  }
+  const Layout y = layout_of(p);
+  return scratch_bytes < y.total ? FALQON_ERR_WORKSPACE : run(p, y, g, out, static_cast<uint8_t*>(scratch), st);
 }
 
 }  // extern "C"

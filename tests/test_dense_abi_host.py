@@ -71,7 +71,7 @@ def test_quantizer_refusals(dense, fq):
     assert refused(_0=None) and refused(_7=None) and refused(_8=None)
     assert refused(_1=2) and refused(_1=-1)                            # dtype
     assert refused(_2=0) and refused(_3=0) and refused(_2=-4)
-    assert refused(_4=7) and refused(_4=1 << 41)                       # row pitch
+    assert refused(_4=7) and refused(_4=(1 << 42) + 1)                 # row pitch
     assert refused(_5=2) and refused(_6=3) and refused(_6=-1)          # format, blocking
     assert refused(_2=(1 << 30) + 1) and refused(_2=1 << 30, _3=1 << 13, _4=1 << 13)       # sizes
     assert refused(_0=FAKE + 1) and refused(_0=FAKE + 2, _1=1)         # alignment to the type
