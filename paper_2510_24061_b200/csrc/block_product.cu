@@ -19,6 +19,9 @@
 // Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
 #include <cuda.h>
 
+#include <algorithm>
+#include <atomic>
+
 #include "../../include/falqon_dense.h"
 #include "block_linear.h"
 #include "gemm_common.cuh"
@@ -471,34 +474,67 @@ int resident_clusters(int size) {
   return n < 0 ? 0 : n;
 }
 
-cudaError_t launch_product(const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
-  ProductArgs g{};
-  g.M = static_cast<int>(M);
-  g.N = static_cast<int>(N);
-  g.kblocks = static_cast<int>((K + kBlockKBytes - 1) / kBlockKBytes);
-  g.m_tiles = static_cast<int>((M + 255) / 256);
-  const int64_t pairs_all = sm_count() / 2;
+// How a product is run, and how long that should take.
+struct Way {
+  TileWalk walk;
+  int split, split_blocks;
+  double us;
+};
+// The tiles' width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 243); or so few tiles that two
+// or four pairs can share each one's contraction (a cluster's parts are added up through its shared memory).  Measured: a block of K
+// takes 0.16 us and 0.9 ns a column, or its copies' time at 80 GB/s to an SM (128 columns of an MN-major B whatever the width); adding up
+// 1.5 to 3.5 us with the rows (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 rows 11008 -> 4096 30.6 and 20.5, 4096 ->
+// 4096 15.1 and 12.3; 512 rows 4096 -> 4096 15.8 and 17.1, which stays unsplit).
+Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn) {
+  const int64_t pairs = sm_count() / 2, m_tiles = (M + 255) / 256;
+  Way best{};
+  for (int w = 256; w >= 64; w -= 32) {
+    const int64_t tiles = m_tiles * ((N + w - 1) / w);
+    const double copies = static_cast<double>((std::min<int64_t>(M, a_rows) + (b_mn ? 128 : w / 2)) * kBlockKBytes) / 80e3;
+    auto block_us = [&](int width) { return std::max(0.16 + 0.0009 * width, copies); };
+    for (int s = 1; s <= 4; s *= 2) {
+      const int64_t per = s == 1 ? kblocks : round_up((kblocks + s - 1) / s, kGroupBlocks);
+      if (s > 1 && (tiles > resident_clusters(2 * s) || per * (s - 1) >= kblocks)) continue;
+      int64_t cost;
+      const TileWalk walk = plan_walk(tiles, s == 1 ? pairs : tiles, w, 178, &cost);
+      const double waves = s == 1 ? static_cast<double>(tiles / pairs) : 1.0;
+      double us = static_cast<double>(per) * (waves * block_us(w) + (walk.items > walk.full ? block_us(walk.part_n) : 0.0));
+      if (s > 1) us += 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0;
+      if (best.us == 0.0 || us < best.us) best = Way{walk, s, static_cast<int>(per), us};
+    }
+  }
+  return best;
+}
+int64_t rows_of_a(const Operand& a, int64_t M) { return a.mn || M >= 128 ? 128 : round_up(M, 8); }
+
+cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
   static DeviceMask configured{0};
   cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
   if (e != cudaSuccess) return e;
-  const int64_t a_rows = a.mn || M >= 128 ? 128 : round_up(M, 8);
-  // The tiles' width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 243);
-  // or so few tiles that two or four pairs can share each one's contraction (a cluster's parts are added up through its shared memory).
-  // A block of K takes 0.16 us and 0.9 ns a column, adding up 1.5 to 3.5 us
-  // with the rows (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 rows 11008 -> 4096 30.6 and 20.5, 4096 -> 4096 15.1 and
-  // 12.3; 512 rows 4096 -> 4096 15.8 and 17.1, which stays unsplit).
-  double best = 0.0;
-  for (int w = 256; w >= 64; w -= 32) {
-    const int64_t tiles = g.m_tiles * ((N + w - 1) / w);
-    for (int s = 1; s <= 4; s *= 2) {
-      const int64_t per = s == 1 ? g.kblocks : round_up((g.kblocks + s - 1) / s, kGroupBlocks);
-      if (s > 1 && (tiles > resident_clusters(2 * s) || per * (s - 1) >= g.kblocks)) continue;
-      int64_t cost;
-      const TileWalk walk = plan_walk(tiles, s == 1 ? pairs_all : tiles, w, 178, &cost);
-      const double us = static_cast<double>(cost) * 0.0009 * static_cast<double>(per) + (s > 1 ? 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0 : 0.0);
-      if (best == 0.0 || us < best) best = us, g.walk = walk, g.split = s, g.split_blocks = static_cast<int>(per);
+  const int64_t kblocks = (K + kBlockKBytes - 1) / kBlockKBytes;
+  Way way = pick_way(M, N, kblocks, rows_of_a(a, M), b.mn);
+  // Rows that do not fill a tile of 256 may cost a wave of their own: they go into a second launch (about 4 us) where that is less (777 rows,
+  // 13824 -> 5120: 80 tiles on 74 pairs 95 us, 60 tiles and then 9 rows 79).
+  const int64_t whole = M / 256 * 256;
+  if (!a.mn && whole > 0 && whole < M) {
+    const Way first = pick_way(whole, N, kblocks, 128, b.mn), rest = pick_way(M - whole, N, kblocks, rows_of_a(a, M - whole), b.mn);
+    if (first.us + rest.us + 4.0 < 0.95 * way.us) {
+      Operand tail = a;
+      tail.codes += whole * a.cols, tail.rows = M - whole;
+      tail.s.p += whole * a.s.row, tail.s.rows = static_cast<int>(M - whole);
+      e = launch_product(tail, b, M - whole, N, K, static_cast<uint8_t*>(out) + whole * N * (out_dt == FALQON_BF16 ? 2 : 4), out_dt, st);
+      if (e != cudaSuccess) return e;
+      M = whole, a.rows = whole, a.s.rows = static_cast<int>(whole);
+      way = first;
     }
   }
+  ProductArgs g{};
+  g.M = static_cast<int>(M);
+  g.N = static_cast<int>(N);
+  g.kblocks = static_cast<int>(kblocks);
+  g.m_tiles = static_cast<int>((M + 255) / 256);
+  g.walk = way.walk, g.split = way.split, g.split_blocks = way.split_blocks;
+  const int64_t pairs_all = sm_count() / 2, a_rows = rows_of_a(a, M);
   g.a_bytes = static_cast<uint32_t>(a_rows) * kBlockKBytes;
   g.b_off = static_cast<uint32_t>(round_up(g.a_bytes, 1024));
   g.stage_bytes = g.b_off + (b.mn ? kMnChunkBytes : static_cast<uint32_t>(g.walk.block_n / 2) * kBlockKBytes);

@@ -198,3 +198,15 @@ def test_which_kernels_run(dense):
     # more steps than fp64 digits allow from the Gram matrix
     assert "thin" not in names(lambda: dense.orthogonalize(torch.ones((64, 900), device="cuda"), steps=9))[-1]
     assert "thin" in names(lambda: dense.orthogonalize(torch.ones((64, 900), device="cuda"), steps=8))[-1]
+
+
+def test_rows_that_do_not_fill_a_tile_go_their_own_way(dense):
+    """777 rows over a long contraction: three tiles of 256, and a launch for the nine rows behind them; each within the products' bound."""
+    T, n, m = 777, 5120, 13824
+    g = torch.Generator(device="cuda").manual_seed(4)
+    w = dense.block_quantize(torch.randn((m, n), generator=g, device="cuda"), "tile")
+    dy = dense.block_quantize(torch.randn((T, m), generator=g, device="cuda") * torch.exp2(torch.arange(T, device="cuda") % 9 - 4.0)[:, None])
+    ran = names(lambda: dense.block_input_grad(dy, w))
+    assert len(ran) == 2 and all("block_product" in k for k in ran), ran
+    for dtype in (torch.bfloat16, torch.float32):
+        within(dense.block_input_grad(dy, w, dtype), orc.value(dy), orc.value(w))
