@@ -384,16 +384,16 @@ cudaError_t launch_side(const ThinPlan& p, int64_t l, int s, const void* g, void
 
 }  // namespace
 
-bool ortho_thin_takes(int64_t batch, int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps) {
-  const int64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-  // The other way takes 17 to 22 launches, whatever the size, but works at the fp16 rate, and at a third of it for fp32 results.  bf16,
-  // 7 of 4096 x 64: 86 us here, 153 there; 7 of 4096 x 128: 224 and 194; 16: 450 and 264.  fp32, 7 of 4096 x 128: 209 and 270; 16: 383 and 399.
+bool ortho_thin_takes(int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps) {
+  const int64_t s = rows < cols ? rows : cols;
+  // The other way takes 17 to 22 launches, whatever the size, but works at the fp16 rate, and at a third of it for fp32 results.  bf16, 7 of
+  // 4096 x 64: 65 us here, 153 there; 64 of 14336 x 64: 1040 and 1420; 7 of 4096 x 128: 224 and 194; 16: 450 and 264.  fp32, 7 of 4096 x
+  // 128: 180 and 270; 64: 1075 and 1090; 16 of 128 x 14336: 670 and 1550.
   if (s > (out_bf16 ? kThinMost / 2 : kThinMost)) return false;
   // how far an error of G may grow before the last step's polynomial is taken: 2^-50 to 2^-24
   double growth = 1.0;
   for (int i = 0; i + 1 < steps; ++i) growth *= std::max(1.0, static_cast<double>(abc[3 * i]) * abc[3 * i]);
-  if (!(growth <= 67108864.0)) return false;
-  return s * s * l <= (int64_t{1} << 31) / batch;
+  return growth <= 67108864.0;
 }
 
 size_t ortho_thin_scratch_bytes(int64_t batch, int64_t rows, int64_t cols) {

@@ -19,8 +19,8 @@ struct ThinPlan {
   float abc[3 * kThinMostSteps];
 };
 
-// (its results' type decides, too)
-bool ortho_thin_takes(int64_t batch, int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps);
+// Whether matrices of this shape, with results of this type and these steps, are taken.
+bool ortho_thin_takes(int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps);
 size_t ortho_thin_scratch_bytes(int64_t batch, int64_t rows, int64_t cols);
 cudaError_t launch_ortho_thin(const ThinPlan& p, const void* g, void* out, void* scratch, cudaStream_t st);
 

@@ -793,7 +793,7 @@ size_t falqon_orthogonalize_scratch_bytes(const falqon_ortho* p) {
   if (!plan_ok(p)) return 0;
   float abc[3 * FALQON_ORTHO_MAX_STEPS];
   coefficients_of(p, abc);
-  return ortho_thin_takes(p->batch, p->rows, p->cols, p->out_dtype == FALQON_BF16, abc, p->steps) ? ortho_thin_scratch_bytes(p->batch, p->rows, p->cols) : layout_of(p).total;
+  return ortho_thin_takes(p->rows, p->cols, p->out_dtype == FALQON_BF16, abc, p->steps) ? ortho_thin_scratch_bytes(p->batch, p->rows, p->cols) : layout_of(p).total;
 }
 
 int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* scratch, size_t scratch_bytes, falqon_stream stream) {
@@ -805,7 +805,7 @@ int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   ThinPlan thin{p->batch, p->rows, p->cols, p->dtype == FALQON_BF16, p->out_dtype == FALQON_BF16, p->steps, p->eps, p->scale, {}};
   coefficients_of(p, thin.abc);
-  if (ortho_thin_takes(p->batch, p->rows, p->cols, thin.out_bf16, thin.abc, p->steps)) {
+  if (ortho_thin_takes(p->rows, p->cols, thin.out_bf16, thin.abc, p->steps)) {
     if (scratch_bytes < ortho_thin_scratch_bytes(p->batch, p->rows, p->cols)) return FALQON_ERR_WORKSPACE;
     return launch_ortho_thin(thin, g, out, scratch, st) == cudaSuccess ? FALQON_OK : FALQON_ERR_CUDA;
   }
