@@ -594,7 +594,7 @@ int falqon_block_forward(const uint8_t* x_codes, const uint8_t* x_scales, falqon
   if (!ok16(x_codes) || !ok16(w_codes) || !ok16(y) || x_scales == nullptr || w_scales == nullptr || !fmt_ok(x_fmt) || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
-  if (block_linear_takes(T, n))
+  if (block_linear_takes(T, n, m))
     return finish(launch_block_linear_codes(x_codes, x_scales, x_fmt, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
                                             static_cast<cudaStream_t>(stream)));
   const Operand a{x_codes, T, n, false, x_fmt, scales_of(x_scales, FALQON_ALONG_ROW, T, n, false)};
@@ -625,7 +625,7 @@ int falqon_block_weight_grad(const uint8_t* dy_codes, const uint8_t* dy_scales, 
 }
 
 size_t falqon_block_linear_scratch_bytes(int64_t T, int64_t n, int64_t m) {
-  if (!layer_ok(T, n, m) || !tiles_ok(T, m) || block_linear_takes(T, n)) return 0;
+  if (!layer_ok(T, n, m) || !tiles_ok(T, m) || block_linear_takes(T, n, m)) return 0;
   return static_cast<size_t>(T * n + round_up(T * ((n + 127) / 128), 16));
 }
 
@@ -634,7 +634,7 @@ int falqon_block_linear(const void* x, int x_dtype, const uint8_t* w_codes, cons
   if (!ok16(x) || (x_dtype != FALQON_BF16 && x_dtype != FALQON_F32) || !ok16(w_codes) || !ok16(y) || w_scales == nullptr || !fmt_ok(w_fmt) ||
       (y_dtype != FALQON_BF16 && y_dtype != FALQON_F32) || !layer_ok(T, n, m) || !tiles_ok(T, m))
     return FALQON_ERR_INVALID_ARG;
-  if (block_linear_takes(T, n))
+  if (block_linear_takes(T, n, m))
     return finish(launch_block_linear_plain(x, x_dtype == FALQON_BF16, w_codes, w_scales, w_fmt, T, n, m, y, y_dtype == FALQON_BF16,
                                             static_cast<cudaStream_t>(stream)));
   if (!ok16(scratch) || scratch_bytes < falqon_block_linear_scratch_bytes(T, n, m)) return FALQON_ERR_WORKSPACE;

@@ -99,8 +99,8 @@ def test_product_refusals(dense, fq, call):
 
 def test_linear_refusals_and_scratch(dense, fq):
     lib = dense.lib
-    for T in (1, 2, 4):
-        assert lib.falqon_block_linear_scratch_bytes(T, 4096, 11008) == 0       # one launch, no scratch
+    for T, m in ((1, 11008), (2, 11008), (4, 4096)):
+        assert lib.falqon_block_linear_scratch_bytes(T, 4096, m) == 0           # one launch, no scratch
     assert lib.falqon_block_linear_scratch_bytes(5, 4096, 11008) == 5 * 4096 + 160
     assert lib.falqon_block_linear_scratch_bytes(100, 2064, 1040) == 100 * 2064 + 1712
     for bad in ((0, 128, 128), (1, 120, 128), (1, 128, 100), (-1, 128, 128), ((1 << 30) + 1, 128, 128)):

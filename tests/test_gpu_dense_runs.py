@@ -187,6 +187,8 @@ def test_which_kernels_run(dense):
     assert len(few) == 1 and "block_linear" in few[0]
     more = names(lambda: dense.block_forward(x[:5], w))
     assert len(more) == 2 and "block_quant_kernel" in more[0] and "block_product" in more[1]
+    large = dense.block_quantize(torch.zeros((32768 + 16, 1024), device="cuda"), "tile")          # just over 2^25 weights
+    assert len(names(lambda: dense.block_forward(x[:2], large))) == 1 and len(names(lambda: dense.block_forward(x[:3], large))) == 2
     q = dense.block_quantize(x[:4].contiguous())
     assert "block_linear" in names(lambda: dense.block_forward(q, w))[0]
     assert "block_product" in names(lambda: dense.block_forward(dense.block_quantize(x[:5].contiguous()), w))[-1]
