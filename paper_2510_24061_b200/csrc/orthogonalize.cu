@@ -103,16 +103,16 @@ struct Item {       // a piece of work: columns of a tile of a matrix (none: beh
   }
 };
 
-__device__ __forceinline__ void store_hi_lo(__half* hi, __half* lo, int64_t at, const float (&v)[4]) {
+__device__ __forceinline__ void store_hi_lo(__half* hi, __half* lo, const float (&v)[4]) {      // lo: nullable
   __half2 h0 = __floats2half2_rn(v[0], v[1]), h1 = __floats2half2_rn(v[2], v[3]);
   uint2 u;
   u.x = *reinterpret_cast<uint32_t*>(&h0), u.y = *reinterpret_cast<uint32_t*>(&h1);
-  *reinterpret_cast<uint2*>(hi + at) = u;
+  *reinterpret_cast<uint2*>(hi) = u;
   if (lo != nullptr) {
     const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
     h0 = __floats2half2_rn(v[0] - f0.x, v[1] - f0.y), h1 = __floats2half2_rn(v[2] - f1.x, v[3] - f1.y);
     u.x = *reinterpret_cast<uint32_t*>(&h0), u.y = *reinterpret_cast<uint32_t*>(&h1);
-    *reinterpret_cast<uint2*>(lo + at) = u;
+    *reinterpret_cast<uint2*>(lo) = u;
   }
 }
 __device__ __forceinline__ void add_halves(float (&v)[4], const uint2& u, float f) {
@@ -134,21 +134,24 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     *reinterpret_cast<float4*>(stage + staged(lane, 4 * j)) = make_float4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
+  // rows 4 i + sub that there are, of this lane's columns
+  const int rows = col0 + col < p.N ? min(32, p.M - row0) - sub : 0;
   uint2 ch[8], cl[8];
   const bool with_c = p.c_hi != nullptr, with_lo = p.c_lo != nullptr;
+  {
+    const int64_t at = it.b * p.stride_c + (row0 + sub) * p.ld_c + col0 + col, step = 4 * p.ld_c;
+    const __half *hi = p.c_hi + at, *lo = p.c_lo + at;
+    const int hi_rows = with_c ? rows : 0, lo_rows = with_lo ? rows : 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = row0 + 4 * i + sub;
-    const bool in = r < p.M && col0 + col < p.N;
-    const int64_t at = it.b * p.stride_c + r * p.ld_c + col0 + col;
-    ch[i] = with_c && in ? ld_stream(reinterpret_cast<const uint2*>(p.c_hi + at)) : make_uint2(0u, 0u);
-    cl[i] = with_lo && in ? ld_stream(reinterpret_cast<const uint2*>(p.c_lo + at)) : make_uint2(0u, 0u);
+    for (int i = 0; i < 8; ++i, hi += step, lo += step) {
+      ch[i] = 4 * i < hi_rows ? ld_stream(reinterpret_cast<const uint2*>(hi)) : make_uint2(0u, 0u);
+      cl[i] = 4 * i < lo_rows ? ld_stream(reinterpret_cast<const uint2*>(lo)) : make_uint2(0u, 0u);
+    }
   }
   __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int rl = 4 * i + sub, r = row0 + rl;
-    float v[4];
+  // alpha D + beta C of this lane's four columns of row 4 i + sub
+  auto value = [&](int i, float (&v)[4]) {
+    const int rl = 4 * i + sub;
     if (diagonal) {     // the upper triangle's value on both sides
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = stage[staged(min(rl, col + k), max(rl, col + k))];
@@ -160,37 +163,70 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
     for (int k = 0; k < 4; ++k) v[k] *= p.alpha;
     if (with_lo) add_halves(v, cl[i], p.beta);
     if (with_c) add_halves(v, ch[i], p.beta);
-    if (r < p.M && col0 + col < p.N) {
-      if (p.mode == kHiLo) {
-        store_hi_lo(p.o_hi, p.o_lo, it.b * p.stride_o + r * p.ld_o + col0 + col, v);
-      } else if (p.mode == kPart) {
-        *reinterpret_cast<float4*>(p.parts + ((static_cast<int64_t>(it.b) * p.splits + it.split) * p.M + r) * p.ld_o + col0 + col) = make_float4(v[0], v[1], v[2], v[3]);
-      } else {
-        const int64_t at = (static_cast<int64_t>(it.b) * p.M + r) * p.N + col0 + col;
-        if (p.out_vec) {
-          if (p.out_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-          else *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
+    if (mirror) *reinterpret_cast<float4*>(stage + staged(rl, col)) = make_float4(v[0], v[1], v[2], v[3]);
+  };
+  float v[4];
+  if (p.mode == kHiLo) {
+    const int64_t at = it.b * p.stride_o + (row0 + sub) * p.ld_o + col0 + col, step = 4 * p.ld_o;
+    __half *hi = p.o_hi + at, *lo = p.o_lo != nullptr ? p.o_lo + at : nullptr;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (col0 + col + k < p.N) {
-              if (p.out_bf16) store1(static_cast<bf16_t*>(p.out) + at + k, v[k]);
-              else static_cast<float*>(p.out)[at + k] = v[k];
-            }
-        }
+    for (int i = 0; i < 8; ++i, hi += step) {
+      value(i, v);
+      if (4 * i < rows) store_hi_lo(hi, lo, v);
+      if (lo != nullptr) lo += step;
+    }
+  } else if (p.mode == kPart) {
+    float* to = p.parts + ((static_cast<int64_t>(it.b) * p.splits + it.split) * p.M + row0 + sub) * p.ld_o + col0 + col;
+    const int64_t step = 4 * p.ld_o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i, to += step) {
+      value(i, v);
+      if (4 * i < rows) *reinterpret_cast<float4*>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  } else if (p.out_vec) {
+    const int64_t at = (static_cast<int64_t>(it.b) * p.M + row0 + sub) * p.N + col0 + col, step = 4 * static_cast<int64_t>(p.N);
+    uint16_t* half = static_cast<uint16_t*>(p.out) + at;
+    float* full = static_cast<float*>(p.out) + at;
+#pragma unroll
+    for (int i = 0; i < 8; ++i, half += step, full += step) {
+      value(i, v);
+      if (4 * i < rows) {
+        if (p.out_bf16) *reinterpret_cast<uint2*>(half) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        else *reinterpret_cast<float4*>(full) = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
-    if (mirror) *reinterpret_cast<float4*>(stage + staged(rl, col)) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll 1
+    for (int i = 0; 4 * i < rows; ++i) {
+      // (the arrays of C's values are indexed by constants elsewhere; here a select does it)
+      uint2 h = ch[0], l = cl[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j)
+        if (j == i) h = ch[j], l = cl[j];
+      const float4 q = *reinterpret_cast<const float4*>(stage + staged(4 * i + sub, col));
+      v[0] = q.x * p.alpha, v[1] = q.y * p.alpha, v[2] = q.z * p.alpha, v[3] = q.w * p.alpha;
+      if (with_lo) add_halves(v, l, p.beta);
+      if (with_c) add_halves(v, h, p.beta);
+      const int64_t at = (static_cast<int64_t>(it.b) * p.M + row0 + 4 * i + sub) * p.N + col0 + col;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (col0 + col + k < p.N) {
+          if (p.out_bf16) store1(static_cast<bf16_t*>(p.out) + at + k, v[k]);
+          else static_cast<float*>(p.out)[at + k] = v[k];
+        }
+    }
   }
   __syncwarp();
-  if (mirror) {
+  if (mirror) {       // a column of the chunk is a row of its mirror
+    const int64_t at = it.b * p.stride_o + (col0 + sub) * p.ld_o + row0 + col, step = 4 * p.ld_o;
+    __half *hi = p.o_hi + at, *lo = p.o_lo != nullptr ? p.o_lo + at : nullptr;
+    const int mirrored = row0 + col < p.M ? min(32, p.N - col0) - sub : 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = 4 * i + sub;                    // a column of the chunk is a row of its mirror
-      float v[4];
+    for (int i = 0; i < 8; ++i, hi += step) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = stage[staged(col + k, c)];
-      if (col0 + c < p.N && row0 + col < p.M) store_hi_lo(p.o_hi, p.o_lo, it.b * p.stride_o + (col0 + c) * p.ld_o + row0 + col, v);
+      for (int k = 0; k < 4; ++k) v[k] = stage[staged(col + k, 4 * i + sub)];
+      if (4 * i < mirrored) store_hi_lo(hi, lo, v);
+      if (lo != nullptr) lo += step;
     }
     __syncwarp();
   }
@@ -547,8 +583,8 @@ ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, 
     for (int k = 0; k < 8; ++k) v[k] = static_cast<float>(static_cast<double>(v[k]) * f);
     const int64_t at = b * stride_o + r * ld + c;
     const float v0[4] = {v[0], v[1], v[2], v[3]}, v1[4] = {v[4], v[5], v[6], v[7]};
-    store_hi_lo(hi, lo, at, v0);
-    store_hi_lo(hi, lo, at + 4, v1);
+    store_hi_lo(hi + at, lo + at, v0);
+    store_hi_lo(hi + at + 4, lo + at + 4, v1);
   }
 }
 
