@@ -16,6 +16,9 @@
 // Few tiles and a long contraction: a cluster of four or eight CTAs shares a tile, its pairs' parts added up in order through shared memory.
 // What bounds it: the tensor cores under the board's power cap -- 4096 x 4096 x 11008 forward 145 to 156 us (2.4 to 2.55 PFLOP/s), the same
 // kernel without block scales no faster; with few rows the MMAs, which take 0.22 us a block of K however narrow the tile is.
+// fp32 results: the tensor cores' additions cut off instead of rounding, which is 1.3e-6 of the result's norm over 4096 terms and 7e-6 over
+// 16384 if nothing is done; so every 8192 terms the threads add a part to what they have stored, by ordinary additions (16384 terms:
+// 3.3e-6, 4096 x 4096 results 253 -> 265 us; parts of 4096 terms 1.4e-6 and 310 us).  A contraction shared by a cluster is in parts already.
 // Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
 #include <cuda.h>
 
@@ -43,6 +46,7 @@ constexpr uint32_t kScaleCol0 = 448;                 // ring of kGroups entries 
 constexpr int kGroups = 5;
 constexpr uint32_t kGroupCols = 12;
 constexpr int kGroupBlocks = 4;                      // blocks of K per entry: the bytes of a word
+constexpr int kPassBlocks = 64;                      // fp32 results: 8192 terms
 constexpr uint32_t kStagingOff = kRingBytes;             // (the last stage's MMA may read into it)
 constexpr uint32_t kWordsOff = kStagingOff + kEpiWarps * 32 * 128;
 constexpr uint32_t kWordsBytes = 12 * 32 * 4;        // an entry's scale words, passed between the scale warps
@@ -62,6 +66,7 @@ struct ProductArgs {
   TileWalk walk;
   bool a_mn, b_mn;
   int split, split_blocks;    // pairs of a cluster that share a tile's contraction, and how many of its blocks each takes (1: all)
+  int pass_blocks;            // blocks of K summed in tensor memory, a multiple of kGroupBlocks
   int stages;
   uint32_t a_bytes, b_off, stage_bytes;      // of A in a stage, where B starts, stride
   uint32_t idesc;             // without N and the scale bytes
@@ -202,37 +207,40 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         const Piece t = piece(item);
         if (t.width == 0) continue;
         const uint32_t idesc_n = p.idesc | (static_cast<uint32_t>(inst_n(t) >> 3) << 17);
-        if (!first) {   // the tile before: its part of the overlap is in registers, everything older is stored
-          if (!mbar_wait_warp(acc_empty_bar, acc_phase, p.status)) { aborted = true; break; }
-          acc_phase ^= 1u;
-          tc_fence_after_sync();
-        }
-        first = false;
-        const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
-        for (int kb = kb_begin; kb < kb_end; ++kb) {
-          const int byte = kb % kGroupBlocks;
-          if (byte == 0 && !mbar_wait_warp(sf_full_bar(group), sf_phase, p.status)) { aborted = true; break; }
-          if (!mbar_wait_warp(full_bar(stage), phase, p.status)) { aborted = true; break; }
-          tc_fence_after_sync();
-          const uint32_t off = (static_cast<uint32_t>(stage) * stage_bytes) >> 4;
-          const uint32_t sfa = tmem + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
-          const uint32_t idesc = idesc_n | (static_cast<uint32_t>(byte) << 29) | (static_cast<uint32_t>(byte) << 4);
-          const bool last = byte == kGroupBlocks - 1 || kb == kb_end - 1;
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < kBlockKBytes / kUmmaK; ++k)
-              umma_mx8_pair(d, a_desc0 + off + k * a_step, b_desc0 + off + k * b_step, idesc, sfa, sfa + 4, (kb > kb_begin || k > 0) ? 1u : 0u);
-            umma_commit_pair(empty_bar(stage), both);
-            if (last) umma_commit_pair(sf_empty_bar(group), both);
+        for (int pass = kb_begin; pass < kb_end && !aborted; pass += p.pass_blocks) {
+          if (!first) {   // the pass or tile before: its part of the overlap is in registers, everything older is stored
+            if (!mbar_wait_warp(acc_empty_bar, acc_phase, p.status)) { aborted = true; break; }
+            acc_phase ^= 1u;
+            tc_fence_after_sync();
           }
+          first = false;
+          const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
+          const int end = min(kb_end, pass + p.pass_blocks);
+          for (int kb = pass; kb < end; ++kb) {
+            const int byte = kb % kGroupBlocks;
+            if (byte == 0 && !mbar_wait_warp(sf_full_bar(group), sf_phase, p.status)) { aborted = true; break; }
+            if (!mbar_wait_warp(full_bar(stage), phase, p.status)) { aborted = true; break; }
+            tc_fence_after_sync();
+            const uint32_t off = (static_cast<uint32_t>(stage) * stage_bytes) >> 4;
+            const uint32_t sfa = tmem + kScaleCol0 + static_cast<uint32_t>(group) * kGroupCols;
+            const uint32_t idesc = idesc_n | (static_cast<uint32_t>(byte) << 29) | (static_cast<uint32_t>(byte) << 4);
+            const bool last = byte == kGroupBlocks - 1 || kb == end - 1;
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kBlockKBytes / kUmmaK; ++k)
+                umma_mx8_pair(d, a_desc0 + off + k * a_step, b_desc0 + off + k * b_step, idesc, sfa, sfa + 4, (kb > pass || k > 0) ? 1u : 0u);
+              umma_commit_pair(empty_bar(stage), both);
+              if (last) umma_commit_pair(sf_empty_bar(group), both);
+            }
+            __syncwarp();
+            if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+            if (last && ++group == kGroups) { group = 0; sf_phase ^= 1u; }
+          }
+          if (aborted) break;
+          if (elect_one()) umma_commit_pair(acc_full_bar, both);
           __syncwarp();
-          if (++stage == n_stages) { stage = 0; phase ^= 1u; }
-          if (last && ++group == kGroups) { group = 0; sf_phase ^= 1u; }
+          acc ^= 1;
         }
-        if (aborted) break;
-        if (elect_one()) umma_commit_pair(acc_full_bar, both);
-        __syncwarp();
-        acc ^= 1;
       }
     }
   } else if (warp >= 2 + kEpiWarps) {
@@ -326,82 +334,92 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       const int chunks = (of.width + 63) / 64, low = (chunks + 1) / 2;        // chunks of 64 columns: half 0 takes [0, low) upwards,
       const int count = half == 0 ? low : chunks - low;                       // half 1 [low, chunks) downwards: the overlap first
       const int row0 = of.row0 + quad * 32, n0 = of.n0, end = of.width;
-      if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
-      full_phase ^= 1u;
-      tc_fence_after_sync();
-      const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
-      if (count == 0) {
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
-      }
-      for (int i = 0; i < count; ++i) {
-        const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
-        uint32_t v0[32], v1[32];
-        __syncwarp();
-        tmem_ld_32x32b_x32(t + c0, v0);
-        tmem_ld_32x32b_x32(t + c0 + 32, v1);
-        tmem_ld_wait();
-        if (i == 0) {
+      for (int pass = kb_begin; pass < kb_end; pass += p.pass_blocks) {
+        const bool more = pass > kb_begin;     // than the first: added to what this thread has stored
+        if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
+        full_phase ^= 1u;
+        tc_fence_after_sync();
+        const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
+        if (count == 0) {
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
         }
-        uint8_t* my = stage_out + lane * 128;
-        const int sw = lane & 7;
-        // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
-        // so a piece lies inside or outside as a whole
-        auto flush = [&](int col, int per_piece, int esize) {
+        for (int i = 0; i < count; ++i) {
+          const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
+          uint32_t v0[32], v1[32];
           __syncwarp();
-          const int piece = lane & 7;
-          const bool in = col + piece * per_piece < end;
-#pragma unroll
-          for (int r0 = 0; r0 < 32; r0 += 4) {
-            const int r = r0 + (lane >> 3);
-            const uint4 val = *reinterpret_cast<const uint4*>(stage_out + r * 128 + ((piece ^ (r & 7)) << 4));
-            if (in && row0 + r < p.M)
-              *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (static_cast<long long>(row0 + r) * p.N + n0 + col + piece * per_piece) * esize) = val;
+          tmem_ld_32x32b_x32(t + c0, v0);
+          tmem_ld_32x32b_x32(t + c0 + 32, v1);
+          tmem_ld_wait();
+          if (i == 0) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
           }
-          __syncwarp();
-        };
-        if (p.split > 1) {      // to be added up: this CTA's rows of the tile as fp32, where the stages were (every copy has been multiplied)
-          if (row0 + lane < p.M) {
-            float* row = part_of(gen) + (row0 + lane - of.row0) * kPartPitch + c0;
+          uint8_t* my = stage_out + lane * 128;
+          const int sw = lane & 7;
+          // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
+          // so a piece lies inside or outside as a whole
+          auto flush = [&](int col, int per_piece, int esize) {
+            __syncwarp();
+            const int piece = lane & 7;
+            const bool in = col + piece * per_piece < end;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              reinterpret_cast<uint4*>(row)[j] = make_uint4(v0[4 * j], v0[4 * j + 1], v0[4 * j + 2], v0[4 * j + 3]);
-              reinterpret_cast<uint4*>(row + 32)[j] = make_uint4(v1[4 * j], v1[4 * j + 1], v1[4 * j + 2], v1[4 * j + 3]);
+            for (int r0 = 0; r0 < 32; r0 += 4) {
+              const int r = r0 + (lane >> 3);
+              uint4 val = *reinterpret_cast<const uint4*>(stage_out + r * 128 + ((piece ^ (r & 7)) << 4));
+              if (in && row0 + r < p.M) {
+                uint4* to = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (static_cast<long long>(row0 + r) * p.N + n0 + col + piece * per_piece) * esize);
+                if (more) {                      // (fp32)
+                  const uint4 so_far = ld_stream(to);
+                  val.x = __float_as_uint(__uint_as_float(val.x) + __uint_as_float(so_far.x)), val.y = __float_as_uint(__uint_as_float(val.y) + __uint_as_float(so_far.y));
+                  val.z = __float_as_uint(__uint_as_float(val.z) + __uint_as_float(so_far.z)), val.w = __float_as_uint(__uint_as_float(val.w) + __uint_as_float(so_far.w));
+                }
+                *to = val;
+              }
             }
+            __syncwarp();
+          };
+          if (p.split > 1) {      // to be added up: this CTA's rows of the tile as fp32, where the stages were (every copy has been multiplied)
+            if (row0 + lane < p.M) {
+              float* row = part_of(gen) + (row0 + lane - of.row0) * kPartPitch + c0;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                reinterpret_cast<uint4*>(row)[j] = make_uint4(v0[4 * j], v0[4 * j + 1], v0[4 * j + 2], v0[4 * j + 3]);
+                reinterpret_cast<uint4*>(row + 32)[j] = make_uint4(v1[4 * j], v1[4 * j + 1], v1[4 * j + 2], v1[4 * j + 3]);
+              }
+            }
+            continue;
           }
-          continue;
-        }
-        if (p.bf16) {
-          auto put = [&](const uint32_t (&v)[32], int first_piece) {
+          if (p.bf16) {
+            auto put = [&](const uint32_t (&v)[32], int first_piece) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint4 o;
-              o.x = pack_bf16x2(__uint_as_float(v[8 * j]), __uint_as_float(v[8 * j + 1]));
-              o.y = pack_bf16x2(__uint_as_float(v[8 * j + 2]), __uint_as_float(v[8 * j + 3]));
-              o.z = pack_bf16x2(__uint_as_float(v[8 * j + 4]), __uint_as_float(v[8 * j + 5]));
-              o.w = pack_bf16x2(__uint_as_float(v[8 * j + 6]), __uint_as_float(v[8 * j + 7]));
-              *reinterpret_cast<uint4*>(my + (((first_piece + j) ^ sw) << 4)) = o;
-            }
-          };
-          put(v0, 0);
-          put(v1, 4);
-          flush(c0, 8, 2);
-        } else {
-          auto put = [&](const uint32_t (&v)[32]) {
+              for (int j = 0; j < 4; ++j) {
+                uint4 o;
+                o.x = pack_bf16x2(__uint_as_float(v[8 * j]), __uint_as_float(v[8 * j + 1]));
+                o.y = pack_bf16x2(__uint_as_float(v[8 * j + 2]), __uint_as_float(v[8 * j + 3]));
+                o.z = pack_bf16x2(__uint_as_float(v[8 * j + 4]), __uint_as_float(v[8 * j + 5]));
+                o.w = pack_bf16x2(__uint_as_float(v[8 * j + 6]), __uint_as_float(v[8 * j + 7]));
+                *reinterpret_cast<uint4*>(my + (((first_piece + j) ^ sw) << 4)) = o;
+              }
+            };
+            put(v0, 0);
+            put(v1, 4);
+            flush(c0, 8, 2);
+          } else {
+            auto put = [&](const uint32_t (&v)[32]) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(my + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          };
-          put(v0);
-          flush(c0, 4, 4);
-          put(v1);
-          flush(c0 + 32, 4, 4);
+              for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(my + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            };
+            put(v0);
+            flush(c0, 4, 4);
+            put(v1);
+            flush(c0 + 32, 4, 4);
+          }
         }
+        acc ^= 1;
       }
-      acc ^= 1;
     }
   }
 
@@ -534,6 +552,7 @@ cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, in
   g.kblocks = static_cast<int>(kblocks);
   g.m_tiles = static_cast<int>((M + 255) / 256);
   g.walk = way.walk, g.split = way.split, g.split_blocks = way.split_blocks;
+  g.pass_blocks = out_dt == FALQON_F32 && way.split == 1 ? kPassBlocks : g.split_blocks;
   const int64_t pairs_all = sm_count() / 2, a_rows = rows_of_a(a, M);
   g.a_bytes = static_cast<uint32_t>(a_rows) * kBlockKBytes;
   g.b_off = static_cast<uint32_t>(round_up(g.a_bytes, 1024));

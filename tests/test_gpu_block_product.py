@@ -59,6 +59,24 @@ def test_weight_grad(dense, T, n, m, dtype):
     close(dense.block_weight_grad(dy, x, dtype), orc.value(dy).T, orc.value(x))
 
 
+@pytest.mark.parametrize("way,T,n,m", [("dw", 16500, 2064, 2000), ("dw", 8193, 2064, 2000), ("fwd", 2100, 8320, 2064), ("dx", 2100, 2064, 16400)])
+def test_long_contraction_in_fp32(dense, way, T, n, m):
+    """Parts of 8192 terms, each off as above by at most 257 * 2^-22 of its own sum of sizes, and ordinary additions of up to three of them,
+    each off by at most half a step of what is then there: 3 * 2^-24 of the whole sum of sizes, with a tenth to spare."""
+    if way == "dw":
+        dy, x = dense.block_quantize(data(T, m, 41), "col", "e5m2"), dense.block_quantize(data(T, n, 42), "col")
+        got, a, b = dense.block_weight_grad(dy, x, torch.float32), orc.value(dy).T, orc.value(x)
+    elif way == "fwd":
+        x, w = dense.block_quantize(data(T, n, 43), "row"), dense.block_quantize(data(m, n, 44), "tile")
+        got, a, b = dense.block_forward(x, w, torch.float32), orc.value(x), orc.value(w).T
+    else:
+        dy, w = dense.block_quantize(data(T, m, 45), "row", "e5m2"), dense.block_quantize(data(m, n, 46), "tile")
+        got, a, b = dense.block_input_grad(dy, w, torch.float32), orc.value(dy), orc.value(w)
+    off, size = (got.double() - a @ b).abs(), a.abs() @ b.abs()
+    bound = (257 * 2.0 ** -22 + 3 * 2.0 ** -24 * 1.1) * size
+    assert not (off > bound).any(), (int((off > bound).sum()), float((off / bound.clamp(min=1e-300)).max()))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("x_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("T,n,m", SIZES + [(2, 4096, 4096), (5, 11008, 512), (16, 2064, 1040), (19, 2064, 1040), (33, 512, 512)])
