@@ -387,8 +387,8 @@ cudaError_t launch_side(const ThinPlan& p, int64_t l, int s, const void* g, void
 bool ortho_thin_takes(int64_t rows, int64_t cols, bool out_bf16, const float* abc, int steps) {
   const int64_t s = rows < cols ? rows : cols;
   // The other way takes 17 to 22 launches, whatever the size, but works at the fp16 rate, and at a third of it for fp32 results.  bf16, 7 of
-  // 4096 x 64: 65 us here, 153 there; 64 of 14336 x 64: 1040 and 1420; 7 of 4096 x 128: 224 and 194; 16: 450 and 264.  fp32, 7 of 4096 x
-  // 128: 180 and 270; 64: 1075 and 1090; 16 of 128 x 14336: 670 and 1550.
+  // 4096 x 64: 65 us here, 124 there; 64 of 14336 x 64: 1040 and 1270; 7 of 4096 x 128: 202 and 168; 16: 400 and 260.  fp32, 7 of 4096 x
+  // 128: 181 and 223; 16 of 128 x 14336: 674 and 1131; 64 of 4096 x 128: 1076 and 912, but by fp64 sums.
   if (s > (out_bf16 ? kThinMost / 2 : kThinMost)) return false;
   // how far an error of G may grow before the last step's polynomial is taken: 2^-50 to 2^-24
   double growth = 1.0;
