@@ -18,7 +18,8 @@
 // kernel without block scales no faster; with few rows the MMAs, which take 0.22 us a block of K however narrow the tile is.
 // fp32 results: the tensor cores' additions cut off instead of rounding, which is 1.3e-6 of the result's norm over 4096 terms and 7e-6 over
 // 16384 if nothing is done; so every 8192 terms the threads add a part to what they have stored, by ordinary additions (16384 terms:
-// 3.3e-6, 4096 x 4096 results 253 -> 265 us; parts of 4096 terms 1.4e-6 and 310 us).  A contraction shared by a cluster is in parts already.
+// 3.3e-6, 4096 x 4096 results 253 -> 265 us; parts of 4096 terms 1.4e-6 and 310 us).  Where a cluster shares the contraction and a pair's share
+// is longer than that, the sums of its passes stay in tensor memory (131072 terms of positive values, 256 x 1024 results: 2.4e-5 -> 3.9e-6, 93 -> 98 us).
 // Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
 #include <cuda.h>
 
@@ -42,11 +43,13 @@ constexpr int kThreads = 32 * (2 + kEpiWarps + kScaleWarps);
 constexpr uint32_t kRingBytes = 6 * 32 * 1024;
 constexpr int kMostStages = 16;
 constexpr uint32_t kAccStride = 192;                 // the second accumulator's first column
+constexpr int kSumCol0 = 256, kSumCols = 192;        // sums of passes, where one accumulator will do
 constexpr uint32_t kScaleCol0 = 448;                 // ring of kGroups entries of 4 (A) + 8 (B) columns
 constexpr int kGroups = 5;
 constexpr uint32_t kGroupCols = 12;
 constexpr int kGroupBlocks = 4;                      // blocks of K per entry: the bytes of a word
 constexpr int kPassBlocks = 64;                      // fp32 results: 8192 terms
+constexpr double kPassUs = 1.5;                      // what a pass more costs a cluster's pair, whose MMAs wait for the epilogue
 constexpr uint32_t kStagingOff = kRingBytes;             // (the last stage's MMA may read into it)
 constexpr uint32_t kWordsOff = kStagingOff + kEpiWarps * 32 * 128;
 constexpr uint32_t kWordsBytes = 12 * 32 * 4;        // an entry's scale words, passed between the scale warps
@@ -104,6 +107,52 @@ __device__ __forceinline__ uint32_t scale_word(const Bytes& w, const Scales& s) 
 constexpr int kPartPitch = 256 + 4;           // of a part's rows in fp32: 128 of them fit into the ring
 __device__ __forceinline__ float* part_of(uint8_t* gen) { return reinterpret_cast<float*>(gen); }
 
+// A pass of several of a tile that a cluster shares, columns [begin, end), 32 at a time: added to the passes before it, whose sums lie in tensor
+// memory behind the accumulator (columns 192 and up: in the staging buffers, which such a tile has no other use for); after the last
+// pass to this CTA's part of the tile, stored where the row is there.
+__device__ __forceinline__ void add_pass(uint8_t* gen, uint32_t t, int r, int begin, int end, bool more, bool last, bool there) {
+  const int sw = r & 7;
+  for (int c = begin; c < end; c += 32) {
+    uint32_t v[32], w[32];
+    float4* kept = reinterpret_cast<float4*>(gen + kStagingOff) + r * 16 + ((c & 32) >> 2);
+    const bool in_smem = c >= kSumCols;
+    __syncwarp();
+    tmem_ld_32x32b_x32(t + c, v);
+    if (more && !in_smem) tmem_ld_32x32b_x32(t + kSumCol0 + c, w);
+    tmem_ld_wait();
+    if (more && in_smem) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint4 q = reinterpret_cast<const uint4*>(kept)[j ^ sw];
+        w[4 * j] = q.x, w[4 * j + 1] = q.y, w[4 * j + 2] = q.z, w[4 * j + 3] = q.w;
+      }
+    }
+    if (more) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(v[j]));
+    }
+    if (!last && !in_smem) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) {
+        const uint32_t q[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+        tmem_st_32x32b_x8(t + kSumCol0 + c + j, q);
+      }
+      tmem_st_wait();
+    } else {
+      uint4* row = reinterpret_cast<uint4*>(part_of(gen) + r * kPartPitch + c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint4 q = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        if (!last) reinterpret_cast<uint4*>(kept)[j ^ sw] = q;
+        else if (there) row[j] = q;
+      }
+    }
+  }
+}
+
+// kInPasses: a cluster shares a tile and a pair's part of the contraction takes several passes: one accumulator, and behind it the sum of
+// the passes so far.  (A kernel of its own: as a branch in the other's epilogue it made that spill registers.)
+template <bool kInPasses>
 __global__ void __launch_bounds__(kThreads, 1)
 block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
@@ -156,6 +205,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const int pairs = gridDim.x / (2 * p.split), pair = blockIdx.x / (2 * p.split);      // that have tiles of their own
   const int kb_begin = static_cast<int>(cluster_rank >> 1) * p.split_blocks, kb_end = min(p.kblocks, kb_begin + p.split_blocks);
   const int items = p.walk.items;
+  constexpr uint32_t kStride = kInPasses ? 0 : kAccStride;
   bool aborted = false;
   struct Piece { int row0, n0, width; };           // of this CTA: rows, columns; no columns: a piece behind the right edge, of which there is nothing
   auto piece = [&](int item) {
@@ -214,7 +264,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             tc_fence_after_sync();
           }
           first = false;
-          const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
+          const uint32_t d = tmem + static_cast<uint32_t>(acc) * kStride;
           const int end = min(kb_end, pass + p.pass_blocks);
           for (int kb = pass; kb < end; ++kb) {
             const int byte = kb % kGroupBlocks;
@@ -339,7 +389,15 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
         full_phase ^= 1u;
         tc_fence_after_sync();
-        const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
+        const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kStride;
+        if constexpr (kInPasses) {
+          add_pass(gen, t, quad * 32 + lane, half == 0 ? 0 : 64 * low, 64 * (half == 0 ? low : chunks), more, pass + p.pass_blocks >= kb_end,
+                   row0 + lane < p.M);
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
+          continue;
+        }
         if (count == 0) {
           tc_fence_before_sync();
           __syncwarp();
@@ -487,7 +545,7 @@ int resident_clusters(int size) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, block_product_kernel, &cfg) != cudaSuccess || n < 1) n = -1;
+  if (cudaOccupancyMaxActiveClusters(&n, block_product_kernel<false>, &cfg) != cudaSuccess || n < 1) n = -1;
   at.store(n, std::memory_order_release);
   return n < 0 ? 0 : n;
 }
@@ -495,7 +553,7 @@ int resident_clusters(int size) {
 // How a product is run, and how long that should take.
 struct Way {
   TileWalk walk;
-  int split, split_blocks;
+  int split, split_blocks, pass_blocks;
   double us;
 };
 // The tiles' width: what takes the least time (4096 x 16384 x 4096: five waves of 192 columns 280 us, four of 256 243); or so few tiles that two
@@ -503,7 +561,7 @@ struct Way {
 // takes 0.16 us and 0.9 ns a column, or its copies' time at 80 GB/s to an SM (128 columns of an MN-major B whatever the width); adding up
 // 1.5 to 3.5 us with the rows (weight gradient of 16384 rows, 256 x 1024: 50 us unsplit, 19.6; 8 rows 11008 -> 4096 30.6 and 20.5, 4096 ->
 // 4096 15.1 and 12.3; 512 rows 4096 -> 4096 15.8 and 17.1, which stays unsplit).
-Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn) {
+Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn, bool f32) {
   const int64_t pairs = sm_count() / 2, m_tiles = (M + 255) / 256;
   Way best{};
   for (int w = 256; w >= 64; w -= 32) {
@@ -517,8 +575,9 @@ Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn) {
       const TileWalk walk = plan_walk(tiles, s == 1 ? pairs : tiles, w, 178, &cost);
       const double waves = s == 1 ? static_cast<double>(tiles / pairs) : 1.0;
       double us = static_cast<double>(per) * (waves * block_us(w) + (walk.items > walk.full ? block_us(walk.part_n) : 0.0));
-      if (s > 1) us += 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0;
-      if (best.us == 0.0 || us < best.us) best = Way{walk, s, static_cast<int>(per), us};
+      const int pass = static_cast<int>(f32 ? std::min<int64_t>(per, kPassBlocks) : per);
+      if (s > 1) us += 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0 + kPassUs * static_cast<double>((per - 1) / pass);
+      if (best.us == 0.0 || us < best.us) best = Way{walk, s, static_cast<int>(per), pass, us};
     }
   }
   return best;
@@ -526,16 +585,18 @@ Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn) {
 int64_t rows_of_a(const Operand& a, int64_t M) { return a.mn || M >= 128 ? 128 : round_up(M, 8); }
 
 cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
-  static DeviceMask configured{0};
-  cudaError_t e = set_max_dynamic_smem(block_product_kernel, static_cast<int>(kSmem), configured);
+  static DeviceMask configured{0}, configured_passes{0};
+  cudaError_t e = set_max_dynamic_smem(block_product_kernel<false>, static_cast<int>(kSmem), configured);
+  if (e == cudaSuccess) e = set_max_dynamic_smem(block_product_kernel<true>, static_cast<int>(kSmem), configured_passes);
   if (e != cudaSuccess) return e;
   const int64_t kblocks = (K + kBlockKBytes - 1) / kBlockKBytes;
-  Way way = pick_way(M, N, kblocks, rows_of_a(a, M), b.mn);
+  const bool f32 = out_dt == FALQON_F32;
+  Way way = pick_way(M, N, kblocks, rows_of_a(a, M), b.mn, f32);
   // Rows that do not fill a tile of 256 may cost a wave of their own: they go into a second launch (about 4 us) where that is less (777 rows,
   // 13824 -> 5120: 80 tiles on 74 pairs 95 us, 60 tiles and then 9 rows 79).
   const int64_t whole = M / 256 * 256;
   if (!a.mn && whole > 0 && whole < M) {
-    const Way first = pick_way(whole, N, kblocks, 128, b.mn), rest = pick_way(M - whole, N, kblocks, rows_of_a(a, M - whole), b.mn);
+    const Way first = pick_way(whole, N, kblocks, 128, b.mn, f32), rest = pick_way(M - whole, N, kblocks, rows_of_a(a, M - whole), b.mn, f32);
     if (first.us + rest.us + 4.0 < 0.95 * way.us) {
       Operand tail = a;
       tail.codes += whole * a.cols, tail.rows = M - whole;
@@ -551,8 +612,7 @@ cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, in
   g.N = static_cast<int>(N);
   g.kblocks = static_cast<int>(kblocks);
   g.m_tiles = static_cast<int>((M + 255) / 256);
-  g.walk = way.walk, g.split = way.split, g.split_blocks = way.split_blocks;
-  g.pass_blocks = out_dt == FALQON_F32 && way.split == 1 ? kPassBlocks : g.split_blocks;
+  g.walk = way.walk, g.split = way.split, g.split_blocks = way.split_blocks, g.pass_blocks = way.pass_blocks;
   const int64_t pairs_all = sm_count() / 2, a_rows = rows_of_a(a, M);
   g.a_bytes = static_cast<uint32_t>(a_rows) * kBlockKBytes;
   g.b_off = static_cast<uint32_t>(round_up(g.a_bytes, 1024));
@@ -575,7 +635,9 @@ cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, in
   if (!make_tensor_map(&ma, a.codes, a.rows, a.cols, a.cols, 128, static_cast<uint32_t>(a_rows))) return cudaErrorInvalidValue;
   if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
   const int64_t pairs = (g.walk.items < pairs_all ? g.walk.items : pairs_all) * g.split;
-  return launch_pdl(block_product_kernel, dim3(static_cast<unsigned>(2 * pairs)), dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g);
+  const dim3 grid(static_cast<unsigned>(2 * pairs));
+  return g.split > 1 && g.pass_blocks < g.split_blocks ? launch_pdl(block_product_kernel<true>, grid, dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g)
+                                                       : launch_pdl(block_product_kernel<false>, grid, dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g);
 }
 
 Scales scales_of(const uint8_t* p, int along, int64_t rows, int64_t cols, bool over_rows) {
