@@ -65,9 +65,10 @@ int falqon_block_linear(const void *x, int x_dtype, const uint8_t *w_codes, cons
  *   X = g / (|g|_F + eps);   steps times:  G = X X^T,  X <- a X + (b G + c G G) X;   out = scale * X
  * for each of `batch` matrices [rows][cols]; tall ones are taken from their short side, which gives the same.  The singular
  * values s of X become p(s) = a s + b s^3 + c s^5 at each step.
- * Arithmetic: sums are fp32 (the norm's fp64).  X and the term a X are held in 22 bits (two fp16 numbers, a power of two apart),
- * the products' operands in fp16 (11 bits) where the results are bf16; where they are fp32, each product is three: both
- * operands in 22 bits.  A matrix of zeros gives zeros; an infinity or a NaN makes NaN of its whole matrix. */
+ * Arithmetic: sums are fp32 (the norm's fp64).  X and the term a X are held in 22 bits (two fp16 numbers, a power of two apart; no
+ * finer than 2^-37 of X's norm, of which single values may be a small part), the products' operands in fp16 (11 bits) where the results
+ * are bf16; where they are fp32, each product is three: both operands in 22 bits.  Where |g| is far below eps, so that X is small
+ * altogether, its digits are kept by powers of two, a matrix's own.  A matrix of zeros gives zeros; an infinity or a NaN makes NaN of its whole matrix. */
 #define FALQON_ORTHO_MAX_STEPS 32
 
 typedef struct { /* host struct */

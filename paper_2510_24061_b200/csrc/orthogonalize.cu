@@ -6,7 +6,9 @@
 // bf16, results are 1 to 30 % off.  So X, and with it the term a X, is two fp16 numbers hi + lo (22 bits).  The products' operands are
 // the hi parts alone where results are bf16 (errors of 2^-12 of G and B; results 1.7e-3 to 2.5e-3 off, of which 1.66e-3 are their own
 // rounding), and three products hi hi + hi lo + lo hi where they are fp32.  All stored values are 2^13 times what they stand for: the host
-// has made sure that none passes 7.9, and small ones keep their digits above fp16's smallest.
+// has made sure that none passes 7.9, and small ones keep their digits above fp16's smallest.  Where |g| is below eps / 2, X is small
+// altogether and only grows by the first coefficient a step: X and B are then held 2^x and 2^b times as large, by exponents of each matrix and step
+// that ortho_scale_kernel derives from |g| / (|g| + eps) (1024 x 1024 at 1e-7 of eps: results 2 % off without them).
 //
 // One kernel does the three products: 256 x block_n tiles by CTA pairs (tcgen05.mma kind::f16, cta_group::2), operands K-major or MN-major
 // by TMA, so that tall matrices need no transposed copy; its epilogue is out = alpha D + beta C, written as hi and lo, as the result, or
@@ -45,6 +47,11 @@ constexpr uint32_t kBarsOff = kStagingOff + kStagingBytes;
 constexpr uint32_t kSmem = kBarsOff + 256 + 1024;
 
 enum Mode { kHiLo, kFinal, kPart };
+enum Product { kGram, kSquare, kApply };     // G = X X^T, B = b G + c G G, X <- a X + B X
+
+// Powers of two that a matrix's X before a step (x) and B of the step (b) are held with, beside kScale: [batch][steps].
+struct Exponents { int x, b; };
+constexpr int kMostX = 126, kMostB = 2 * kMostX;
 
 struct ProductArgs {
   int M, N, batch;
@@ -55,7 +62,10 @@ struct ProductArgs {
   bool symmetric;              // only tiles that touch the upper triangle; the lower one is their mirror
   bool a_mn, b_mn;
   uint32_t idesc;              // without N
-  float alpha, beta;
+  Product product;
+  float alpha, beta;           // before exponents
+  const Exponents* exps;       // of this step, matrices `steps` apart
+  int steps;
   const __half *c_hi, *c_lo;   // [batch][M][ld_c]; c_lo nullable, both null: no such term
   int64_t ld_c, stride_c;
   Mode mode;
@@ -103,6 +113,27 @@ struct Item {       // a piece of work: columns of a tile of a matrix (none: beh
   }
 };
 
+__device__ __forceinline__ Exponents exponents_at(const Exponents* p) {
+  const int2 v = ld_stream(reinterpret_cast<const int2*>(p));
+  return Exponents{v.x, v.y};
+}
+// What D, C and a final result of matrix b are multiplied by.
+struct Factors { float alpha, beta, post; };
+__device__ __forceinline__ Factors factors_of(const ProductArgs& p, int b) {
+  Factors f{p.alpha, p.beta, 1.0f};
+  if (p.product == kGram) return f;
+  const Exponents* at = p.exps + static_cast<int64_t>(b) * p.steps;
+  const Exponents e = exponents_at(at);
+  if (p.product == kSquare) {
+    if ((e.x | e.b) != 0) f.alpha = ldexpf(f.alpha, e.b - 4 * e.x), f.beta = ldexpf(f.beta, e.b - 2 * e.x);
+    return f;
+  }
+  const int up = p.mode == kFinal ? 0 : exponents_at(at + 1).x - e.x;
+  if ((up | e.b) != 0) f.alpha = ldexpf(f.alpha, up - e.b), f.beta = ldexpf(f.beta, up);
+  if (p.mode == kFinal) f.post = __uint_as_float(static_cast<uint32_t>(127 - e.x) << 23);
+  return f;
+}
+
 __device__ __forceinline__ void store_hi_lo(__half* hi, __half* lo, const float (&v)[4]) {      // lo: nullable
   __half2 h0 = __floats2half2_rn(v[0], v[1]), h1 = __floats2half2_rn(v[2], v[3]);
   uint2 u;
@@ -126,7 +157,7 @@ __device__ __forceinline__ int staged(int row, int col) { return row * 32 + ((((
 
 // 32 x 32 values of D at (row0, col0), one row a lane, through the staging buffer to where they belong: a lane then holds four columns of a
 // row, eight lanes a row, so that C is read and results are written in whole sectors.
-__device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& it, int row0, int col0, const float (&d)[32], float* stage) {
+__device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& it, const Factors& f, int row0, int col0, const float (&d)[32], float* stage) {
   if (row0 >= p.M || col0 >= p.N) return;
   if (p.symmetric && col0 < row0) return;           // the mirror of what another chunk writes
   const int lane = threadIdx.x & 31, sub = lane >> 3, col = (lane & 7) * 4;
@@ -160,9 +191,9 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
       v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] *= p.alpha;
-    if (with_lo) add_halves(v, cl[i], p.beta);
-    if (with_c) add_halves(v, ch[i], p.beta);
+    for (int k = 0; k < 4; ++k) v[k] *= f.alpha;
+    if (with_lo) add_halves(v, cl[i], f.beta);
+    if (with_c) add_halves(v, ch[i], f.beta);
     if (mirror) *reinterpret_cast<float4*>(stage + staged(rl, col)) = make_float4(v[0], v[1], v[2], v[3]);
   };
   float v[4];
@@ -191,6 +222,8 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
     for (int i = 0; i < 8; ++i, half += step, full += step) {
       value(i, v);
       if (4 * i < rows) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] *= f.post;
         if (p.out_bf16) *reinterpret_cast<uint2*>(half) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
         else *reinterpret_cast<float4*>(full) = make_float4(v[0], v[1], v[2], v[3]);
       }
@@ -204,15 +237,15 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
       for (int j = 1; j < 8; ++j)
         if (j == i) h = ch[j], l = cl[j];
       const float4 q = *reinterpret_cast<const float4*>(stage + staged(4 * i + sub, col));
-      v[0] = q.x * p.alpha, v[1] = q.y * p.alpha, v[2] = q.z * p.alpha, v[3] = q.w * p.alpha;
-      if (with_lo) add_halves(v, l, p.beta);
-      if (with_c) add_halves(v, h, p.beta);
+      v[0] = q.x * f.alpha, v[1] = q.y * f.alpha, v[2] = q.z * f.alpha, v[3] = q.w * f.alpha;
+      if (with_lo) add_halves(v, l, f.beta);
+      if (with_c) add_halves(v, h, f.beta);
       const int64_t at = (static_cast<int64_t>(it.b) * p.M + row0 + 4 * i + sub) * p.N + col0 + col;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         if (col0 + col + k < p.N) {
-          if (p.out_bf16) store1(static_cast<bf16_t*>(p.out) + at + k, v[k]);
-          else static_cast<float*>(p.out)[at + k] = v[k];
+          if (p.out_bf16) store1(static_cast<bf16_t*>(p.out) + at + k, v[k] * f.post);
+          else static_cast<float*>(p.out)[at + k] = v[k] * f.post;
         }
     }
   }
@@ -402,6 +435,7 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
       if (it.width == 0) continue;
       const int chunks = it.width / 32, first = half == 0 ? 0 : (chunks + 1) / 2, count = half == 0 ? (chunks + 1) / 2 : chunks / 2;
       const int row0 = it.row0 + static_cast<int>(rank) * kBlockM + quad * 32;
+      const Factors f = factors_of(p, it.b);
       if constexpr (kPrecise) {
         float sum[2][32];
         for (int k0 = it.k_begin; k0 < it.k_end; k0 += kChunk) {
@@ -429,7 +463,7 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
         if (aborted) break;
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-          if (c < count) finish_chunk(p, it, row0, it.n0 + 32 * (first + c), sum[c], stage_out);
+          if (c < count) finish_chunk(p, it, f, row0, it.n0 + 32 * (first + c), sum[c], stage_out);
         parity ^= 1u;
       } else {
         if (!mbar_wait_warp(acc_full_bar(acc), acc_phase, p.status)) { aborted = true; break; }
@@ -443,7 +477,7 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
           float d[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) d[j] = __uint_as_float(v[j]);
-          finish_chunk(p, it, row0, it.n0 + 32 * (first + c), d, stage_out);
+          finish_chunk(p, it, f, row0, it.n0 + 32 * (first + c), d, stage_out);
         }
         next_acc();
       }
@@ -467,10 +501,10 @@ ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
 
 // ---------------------------------------------------------------- the parts of G added up in order, mirrored
 // out = the parts' sum + beta C: parts [batch][splits][s][ld], of which chunks of 32 x 32 on and above the diagonal are filled; a CTA takes
-// one of these.  C (nullable): laid out like the result.
+// one of these.  C (nullable): laid out like the result; beta is then b of B = b G + c G G, exps this step's exponents, `steps` apart.
 __global__ void __launch_bounds__(1024)
-ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float beta, const __half* c_hi, const __half* c_lo, __half* hi, __half* lo,
-                       int64_t ld_o, int64_t stride_o) {
+ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float beta, const Exponents* exps, int steps, const __half* c_hi,
+                       const __half* c_lo, __half* hi, __half* lo, int64_t ld_o, int64_t stride_o) {
   __shared__ float tile[32][33];
   pdl_trigger();
   pdl_wait();
@@ -491,8 +525,12 @@ ortho_add_parts_kernel(const float* parts, int splits, int s, int64_t ld, float 
     auto term = [&](const __half* m) {
       return __half2float(__ushort_as_half(ld_stream(reinterpret_cast<const unsigned short*>(m) + b * stride_o + r * ld_o + c)));
     };
-    if (c_lo != nullptr) v = fmaf(term(c_lo), beta, v);
-    if (c_hi != nullptr) v = fmaf(term(c_hi), beta, v);
+    if (c_hi != nullptr) {
+      const Exponents e = exponents_at(exps + static_cast<int64_t>(b) * steps);
+      if ((e.x | e.b) != 0) beta = ldexpf(beta, e.b - 2 * e.x);
+      if (c_lo != nullptr) v = fmaf(term(c_lo), beta, v);
+      v = fmaf(term(c_hi), beta, v);
+    }
   }
   tile[y][x] = v;
   __syncthreads();
@@ -546,11 +584,37 @@ ortho_norm_kernel(const T* g, int64_t count, double* parts) {
   }
 }
 
-// X = g * 2^13 / (|g| + eps) as hi and lo; a lane takes eight columns of a row.
+// How often v can be doubled and stays below 1, at most `most` times.
+__device__ __forceinline__ int doublings(double v, int most) {
+  int e;
+  frexp(v, &e);          // v = m * 2^e with m < 1; zero: 0
+  return min(max(-e, 0), most);
+}
+
+struct Steps {
+  int count;
+  float abc[3 * FALQON_ORTHO_MAX_STEPS];
+  float bound[FALQON_ORTHO_MAX_STEPS];       // of the singular values of X before each step, where |g| is far above eps
+};
+
+// The exponents of a matrix whose X has the 2-norm `ratio`, from bounds of its singular values s before each step: s is at most the norm, then
+// at most |a| s + |b| s^3 + |c| s^5 and what it is for any matrix; b s^2 + c s^4 bounds B.  None for norms that are held well as they are.
+__device__ __forceinline__ void write_exponents(const Steps& p, double ratio, Exponents* e) {
+  const bool small = ratio <= 0.5;
+  double s = ratio;
+  for (int k = 0; k < p.count; ++k) {
+    s = fmin(1.001 * s, static_cast<double>(p.bound[k]));      // (what rounding may add)
+    const double a = fabs(p.abc[3 * k]), x = s * s, q = x * (fabs(p.abc[3 * k + 1]) + x * fabs(p.abc[3 * k + 2]));
+    e[k] = small ? Exponents{doublings(s, kMostX), doublings(1.001 * q, kMostB)} : Exponents{0, 0};
+    s *= a + q;
+  }
+}
+
+// X = g * 2^(13 + x) / (|g| + eps) as hi and lo; a lane takes eight columns of a row.  Its exponents, x of which is the first.
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kThreads)
-ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, int nparts, double eps, __half* hi, __half* lo, int64_t ld,
-                   int64_t stride_o) {
+ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, int nparts, double eps, const __grid_constant__ Steps steps,
+                   Exponents* exps, __half* hi, __half* lo, int64_t ld, int64_t stride_o) {
   __shared__ double s_sum[kThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -564,8 +628,11 @@ ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, 
   sum = 0.0;
   for (int w = 0; w < kThreads / 32; ++w) sum += s_sum[w];
   const double norm = sqrt(sum) + eps;
+  const double ratio = norm > 0.0 ? sqrt(sum) / norm : 0.0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) write_exponents(steps, ratio, exps + static_cast<int64_t>(b) * steps.count);
   // an infinity or a NaN anywhere: NaN everywhere; nothing but zeros: zeros
-  const double f = !(sum <= 1.7976931348623157e308) ? nan("") : norm > 0.0 ? static_cast<double>(kScale) / norm : 0.0;
+  double f = !(sum <= 1.7976931348623157e308) ? nan("") : norm > 0.0 ? static_cast<double>(kScale) / norm : 0.0;
+  if (ratio <= 0.5) f = ldexp(f, doublings(1.001 * ratio, kMostX));
   const int64_t groups = (cols + 7) / 8, total = rows * groups;
   const T* x = g + b * rows * cols;
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; u < total; u += static_cast<int64_t>(gridDim.x) * kThreads) {
@@ -592,13 +659,15 @@ ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, 
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 constexpr double kMostStored = 7.9;      // times 2^13 it stays below fp16's largest, 65504
 
-// Whether no value that is stored on the way can pass kMostStored: bounds of the singular values, step by step.
-bool range_ok(const float* abc, int steps) {
+// Whether no value that is stored on the way can pass kMostStored: bounds of the singular values, step by step, which are left in
+// `bounds` (nullable).
+bool range_ok(const float* abc, int steps, float* bounds) {
   double bound = 1.0;
   for (int i = 0; i < steps; ++i) {
     const double a = abc ? abc[3 * i] : kQuintic[0], b = abc ? abc[3 * i + 1] : kQuintic[1], c = abc ? abc[3 * i + 2] : kQuintic[2];
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
     bound *= 1.001;                       // what rounding may add
+    if (bounds != nullptr) bounds[i] = std::nextafter(static_cast<float>(bound), 1e30f);
     double p = 0.0, q = 0.0;
     auto at = [&](double x) {             // x = s^2
       const double v = std::fabs(b * x + c * x * x), s = std::sqrt(x), w = std::fabs(s * (a + b * x + c * x * x));
@@ -665,7 +734,7 @@ struct Layout {
   Way gram, square;
   int norm_parts;
   size_t x_bytes, sq_bytes;
-  size_t x[4], sq[4], parts, norm, total;    // offsets: X hi, lo of two turns; G hi, lo, B hi, lo
+  size_t x[4], sq[4], parts, norm, exps, total;    // offsets: X hi, lo of two turns; G hi, lo, B hi, lo
 };
 
 bool plan_ok(const falqon_ortho* p) {
@@ -697,6 +766,7 @@ Layout layout_of(const falqon_ortho* p) {
   for (int i = 0; i < 4; ++i) y.sq[i] = take((i & 1) == 0 || y.precise ? y.sq_bytes : 0);
   y.parts = take(splits > 1 ? static_cast<size_t>(p->batch) * splits * y.s * y.ld_s * 4 : 0);
   y.norm = take(static_cast<size_t>(p->batch) * y.norm_parts * 8);
+  y.exps = take(static_cast<size_t>(p->batch) * p->steps * sizeof(Exponents));
   y.total = at;
   return y;
 }
@@ -740,7 +810,7 @@ cudaError_t launch_product(ProductArgs g, const Way& way, const Matrix& a, const
 }
 
 template <typename T>
-cudaError_t launch_start(const falqon_ortho* p, const Layout& y, const void* g, double* norm, __half* hi, __half* lo, cudaStream_t st) {
+cudaError_t launch_start(const falqon_ortho* p, const Layout& y, const void* g, double* norm, Exponents* exps, __half* hi, __half* lo, cudaStream_t st) {
   const T* x = static_cast<const T*>(g);
   const int64_t count = p->rows * p->cols;
   const bool vec = count % 8 == 0 && (reinterpret_cast<uintptr_t>(g) & 15) == 0, rows_vec = vec && p->cols % 8 == 0;
@@ -752,17 +822,22 @@ cudaError_t launch_start(const falqon_ortho* p, const Layout& y, const void* g, 
   const int64_t cap = std::max<int64_t>(1, 8 * static_cast<int64_t>(sm_count()) / p->batch);
   const dim3 grid2(static_cast<unsigned>(want < cap ? want : cap), static_cast<unsigned>(p->batch));
   const int64_t stride = p->rows * y.ld;
+  Steps steps{};
+  steps.count = p->steps;
+  coefficients_of(p, steps.abc);
+  if (!range_ok(p->coefficients, p->steps, steps.bound)) return cudaErrorInvalidValue;
   return rows_vec ? launch_pdl(ortho_scale_kernel<T, true>, grid2, block, 0, st, 1, x, p->rows, p->cols, norm, y.norm_parts,
-                               static_cast<double>(p->eps), hi, lo, y.ld, stride)
+                               static_cast<double>(p->eps), steps, exps, hi, lo, y.ld, stride)
                   : launch_pdl(ortho_scale_kernel<T, false>, grid2, block, 0, st, 1, x, p->rows, p->cols, norm, y.norm_parts,
-                               static_cast<double>(p->eps), hi, lo, y.ld, stride);
+                               static_cast<double>(p->eps), steps, exps, hi, lo, y.ld, stride);
 }
 
 int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_t* scratch, cudaStream_t st) {
   auto halves = [&](size_t off) { return reinterpret_cast<__half*>(scratch + off); };
   double* norm = reinterpret_cast<double*>(scratch + y.norm);
-  cudaError_t e = p->dtype == FALQON_BF16 ? launch_start<bf16_t>(p, y, g, norm, halves(y.x[0]), halves(y.x[1]), st)
-                                          : launch_start<float>(p, y, g, norm, halves(y.x[0]), halves(y.x[1]), st);
+  Exponents* exps = reinterpret_cast<Exponents*>(scratch + y.exps);
+  cudaError_t e = p->dtype == FALQON_BF16 ? launch_start<bf16_t>(p, y, g, norm, exps, halves(y.x[0]), halves(y.x[1]), st)
+                                          : launch_start<float>(p, y, g, norm, exps, halves(y.x[0]), halves(y.x[1]), st);
   if (e != cudaSuccess) return FALQON_ERR_CUDA;
   __half *g_hi = halves(y.sq[0]), *g_lo = y.precise ? halves(y.sq[1]) : nullptr, *b_hi = halves(y.sq[2]), *b_lo = y.precise ? halves(y.sq[3]) : nullptr;
   const int64_t sq_stride = y.s * y.ld_s, x_stride = p->rows * y.ld;
@@ -779,21 +854,26 @@ int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_
     if (r != cudaSuccess || way.splits == 1) return r;
     const unsigned n = static_cast<unsigned>((y.s + 31) / 32);
     return launch_pdl(ortho_add_parts_kernel, dim3(n, n, static_cast<unsigned>(p->batch)), dim3(1024), 0, st, 1, a.parts, way.splits, static_cast<int>(y.s),
-                      y.ld_s, a.beta, c_hi, c_lo, hi, lo, y.ld_s, sq_stride);
+                      y.ld_s, a.beta, a.exps, a.steps, c_hi, c_lo, hi, lo, y.ld_s, sq_stride);
   };
   for (int i = 0; i < p->steps; ++i) {
     const float* abc = p->coefficients != nullptr ? p->coefficients + 3 * i : kQuintic;
     const int now = 2 * (i & 1), then = 2 - now;
     __half *x_hi = halves(y.x[now]), *x_lo = halves(y.x[now + 1]);
+    auto of_step = [&](Product product) {
+      ProductArgs a{};
+      a.product = product, a.exps = exps + i, a.steps = p->steps;
+      return a;
+    };
     // G = X X^T (X^T X where tall)
     {
-      ProductArgs a{};
+      ProductArgs a = of_step(kGram);
       a.alpha = 1.0f / kScale;
       if (symmetric(a, y.gram, Matrix{x_hi, x_lo, p->rows, p->cols, y.ld, y.tall}, y.l, g_hi, g_lo) != cudaSuccess) return FALQON_ERR_CUDA;
     }
     // B = b G + c G G
     {
-      ProductArgs a{};
+      ProductArgs a = of_step(kSquare);
       a.alpha = abc[2] / kScale, a.beta = abc[1];
       a.c_hi = g_hi, a.c_lo = g_lo, a.ld_c = y.ld_s, a.stride_c = sq_stride;
       if (symmetric(a, y.square, Matrix{g_hi, g_lo, y.s, y.s, y.ld_s, false}, y.s, b_hi, b_lo) != cudaSuccess) return FALQON_ERR_CUDA;
@@ -802,7 +882,7 @@ int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_
     {
       const bool last = i + 1 == p->steps;
       const Matrix m{b_hi, b_lo, y.s, y.s, y.ld_s, false}, x{x_hi, x_lo, p->rows, p->cols, y.ld, !y.tall};
-      ProductArgs a{};
+      ProductArgs a = of_step(kApply);
       const float f = last ? p->scale / kScale : 1.0f;
       a.alpha = f / kScale, a.beta = abc[0] * f;
       a.c_hi = x_hi, a.c_lo = x_lo, a.ld_c = y.ld, a.stride_c = x_stride;
@@ -834,7 +914,7 @@ size_t falqon_orthogonalize_scratch_bytes(const falqon_ortho* p) {
 
 int falqon_orthogonalize(const falqon_ortho* p, const void* g, void* out, void* scratch, size_t scratch_bytes, falqon_stream stream) {
   if (!plan_ok(p) || g == nullptr || out == nullptr || !(p->eps >= 0.0f) || !std::isfinite(p->eps) || !std::isfinite(p->scale) ||
-      !range_ok(p->coefficients, p->steps) || (reinterpret_cast<uintptr_t>(g) & (p->dtype == FALQON_BF16 ? 1 : 3)) != 0 ||
+      !range_ok(p->coefficients, p->steps, nullptr) || (reinterpret_cast<uintptr_t>(g) & (p->dtype == FALQON_BF16 ? 1 : 3)) != 0 ||
       (reinterpret_cast<uintptr_t>(out) & (p->out_dtype == FALQON_BF16 ? 1 : 3)) != 0 || (g == out && p->dtype != p->out_dtype))
     return FALQON_ERR_INVALID_ARG;
   if (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) return FALQON_ERR_WORKSPACE;
