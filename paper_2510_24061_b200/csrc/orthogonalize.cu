@@ -6,7 +6,7 @@
 // bf16, results are 1 to 30 % off.  So X, and with it the term a X, is two fp16 numbers hi + lo (22 bits).  The products' operands are
 // the hi parts alone where results are bf16 (errors of 2^-12 of G and B; results 1.7e-3 to 2.5e-3 off, of which 1.66e-3 are their own
 // rounding), and three products hi hi + hi lo + lo hi where they are fp32.  All stored values are 2^13 times what they stand for: the host
-// has made sure that none passes 7.9, and small ones keep their digits above fp16's smallest.  Where |g| is below eps / 2, X is small
+// has made sure that none passes 7.98, and small ones keep their digits above fp16's smallest.  Where |g| is below eps / 2, X is small
 // altogether and only grows by the first coefficient a step: X and B are then held 2^x and 2^b times as large, by exponents of each matrix and step
 // that ortho_scale_kernel derives from |g| / (|g| + eps) (1024 x 1024 at 1e-7 of eps: results 2 % off without them).
 //
@@ -658,8 +658,11 @@ ortho_scale_kernel(const T* g, int64_t rows, int64_t cols, const double* parts, 
 // ---------------------------------------------------------------- host side
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 constexpr double kMostStored = 7.9;      // times 2^13 it stays below fp16's largest, 65504
+// B may come nearer to it: its bound is that of b x + c x^2 at what G is held as, and what rounding adds is fp32's.  (Published schedules
+// for small singular values begin with polynomials that reach 7.97.)
+constexpr double kMostOfB = 7.98;
 
-// Whether no value that is stored on the way can pass kMostStored: bounds of the singular values, step by step, which are left in
+// Whether no value that is stored on the way can pass its limit: bounds of the singular values, step by step, which are left in
 // `bounds` (nullable).
 bool range_ok(const float* abc, int steps, float* bounds) {
   double bound = 1.0;
@@ -684,7 +687,7 @@ bool range_ok(const float* abc, int steps, float* bounds) {
     } else if (b != 0.0) {
       inside(-a / (3.0 * b));
     }
-    if (!(most <= kMostStored) || !(q <= kMostStored) || !(p <= kMostStored)) return false;
+    if (!(most <= kMostStored) || !(q <= kMostOfB) || !(p <= kMostStored)) return false;
     bound = p;
   }
   return true;
