@@ -592,12 +592,13 @@ cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, in
   const int64_t kblocks = (K + kBlockKBytes - 1) / kBlockKBytes;
   const bool f32 = out_dt == FALQON_F32;
   Way way = pick_way(M, N, kblocks, rows_of_a(a, M), b.mn, f32);
-  // Rows that do not fill a tile of 256 may cost a wave of their own: they go into a second launch (about 4 us) where that is less (777 rows,
-  // 13824 -> 5120: 80 tiles on 74 pairs 95 us, 60 tiles and then 9 rows 79).
+  // Rows that do not fill a tile of 256 may cost a wave of their own: they go into a second launch where that is less by what a launch costs
+  // more than its blocks (8.5 us measured) and a little.  Both sides, one launch and two: 777 rows forward 13824 -> 5120 79.9 and 73.7 us, input
+  // gradient of 5120 -> 13824 82 and 82 to 84; 1030 rows, input gradient of 4096 -> 11008 71.7 and 65.5 to 67.6, of 4096 -> 4096 37 and 39 (stays one).
   const int64_t whole = M / 256 * 256;
   if (!a.mn && whole > 0 && whole < M) {
     const Way first = pick_way(whole, N, kblocks, 128, b.mn, f32), rest = pick_way(M - whole, N, kblocks, rows_of_a(a, M - whole), b.mn, f32);
-    if (first.us + rest.us + 4.0 < 0.95 * way.us) {
+    if (first.us + rest.us + 8.5 < 0.98 * way.us) {
       Operand tail = a;
       tail.codes += whole * a.cols, tail.rows = M - whole;
       tail.s.p += whole * a.s.row, tail.s.rows = static_cast<int>(M - whole);
