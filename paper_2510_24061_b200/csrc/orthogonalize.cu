@@ -64,6 +64,7 @@ struct ProductArgs {
   uint32_t idesc;              // without N
   Product product;
   float alpha, beta;           // before exponents
+  int post;                    // kFinal: the scale's power of two, which is taken last, so that a small scale costs alpha no digits
   const Exponents* exps;       // of this step, matrices `steps` apart
   int steps;
   const __half *c_hi, *c_lo;   // [batch][M][ld_c]; c_lo nullable, both null: no such term
@@ -130,7 +131,7 @@ __device__ __forceinline__ Factors factors_of(const ProductArgs& p, int b) {
   }
   const int up = p.mode == kFinal ? 0 : exponents_at(at + 1).x - e.x;
   if ((up | e.b) != 0) f.alpha = ldexpf(f.alpha, up - e.b), f.beta = ldexpf(f.beta, up);
-  if (p.mode == kFinal) f.post = __uint_as_float(static_cast<uint32_t>(127 - e.x) << 23);
+  if (p.mode == kFinal) f.post = ldexpf(1.0f, p.post - e.x);
   return f;
 }
 
@@ -886,7 +887,9 @@ int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_
       const bool last = i + 1 == p->steps;
       const Matrix m{b_hi, b_lo, y.s, y.s, y.ld_s, false}, x{x_hi, x_lo, p->rows, p->cols, y.ld, !y.tall};
       ProductArgs a = of_step(kApply);
-      const float f = last ? p->scale / kScale : 1.0f;
+      int power = 0;
+      const float f = last ? 2.0f * std::frexp(p->scale, &power) / kScale : 1.0f;       // 1 <= |m| < 2, or 0
+      a.post = power - 1;
       a.alpha = f / kScale, a.beta = abc[0] * f;
       a.c_hi = x_hi, a.c_lo = x_lo, a.ld_c = y.ld, a.stride_c = x_stride;
       a.mode = last ? kFinal : kHiLo;
