@@ -1,13 +1,13 @@
-// Up to kMostFew tokens through a layer held in 8 bits by blocks of 128 (include/falqon_dense.h: falqon_block_linear, and
-// falqon_block_forward of so few rows):
+// One or two tokens, and up to kMostFew where w has at most 2^25 weights, through a layer held in 8 bits by blocks of 128
+// (include/falqon_dense.h: falqon_block_linear, and falqon_block_forward of so few rows):
 //   y[t][i] = sum over blocks kb of 2^(ex[t][kb] + ew[i / 128][kb] - 254) * sum over k in kb of x[t][k] w[i][k]
 // Bound by the bytes of w, which are read once, straight into registers: no stage in shared memory, no tile of 256 rows of which a few are
 // used.  A warp reads 512 codes of a row at a time (whole lines), a lane 16 of them, all of one block; codes are multiplied as fp16
 // (products exact) into fp32 sums, the scales stay outside of a lane's 16.  Some warps of a CTA share the contraction, each with its own part of x;
 // CTAs walk over the rows, two units of kRows x 512 codes on their way.  x is quantized by every warp for its own part, which is
-// read once per CTA.  4096 -> 11008, bf16: one token 11.4 us (4.0 TB/s; the loads alone 8.9), two 15.0, four 23.3 (bound by the
-// multiplications); the tensor cores' tiles with a quantizer before them 19 to 20 us from five tokens up to 130.  4096 -> 4096: 5.5, 7.4 and
-// 10.9 us, theirs 16.6.  (By mma.sync m16n8k16, whose rate is low here, with 16 rows and all of x to a CTA: one token 15.8, four 27.7.)
+// read once per CTA.  4096 -> 11008, bf16: one token 11.4 us (4.0 TB/s; the loads alone 8.9), two 15.0; the tensor cores' tiles with a
+// quantizer before them 18.6 to 20 us from three tokens up to 130.  4096 -> 4096: one token 5.5, two 7.4, four 10.9 us (bound by the
+// multiplications), theirs 13 to 15.  (By mma.sync m16n8k16, whose rate is low here, with 16 rows and all of x to a CTA: one token 15.8, four 27.7.)
 #include <type_traits>
 
 #include "../../include/falqon_dense.h"

@@ -14,8 +14,9 @@
 // rest of the epilogue runs beside them.
 // The three products differ in how the codes lie (K-major or MN-major, no transposed copies) and in the strides of their scales.
 // Few tiles and a long contraction: a cluster of four or eight CTAs shares a tile, its pairs' parts added up in order through shared memory.
-// What bounds it: the tensor cores under the board's power cap -- 4096 x 4096 x 11008 forward 145 to 156 us (2.4 to 2.55 PFLOP/s), the same
-// kernel without block scales no faster; with few rows the MMAs, which take 0.22 us a block of K however narrow the tile is.
+// What bounds it: 4096 x 4096 x 11008 forward, 145 to 163 us (2.3 to 2.55 PFLOP/s), has the MMAs running 73 % of the time at 1.54 GHz (135 us
+// under the profiler; 79 % while an SM has work), the rest being the last of 9.3 waves and the pipeline's ends; with few rows the MMAs, which
+// take 0.22 us a block of K however narrow the tile is.
 // fp32 results: the tensor cores' additions cut off instead of rounding, which is 1.3e-6 of the result's norm over 4096 terms and 7e-6 over
 // 16384 if nothing is done; so every 8192 terms the threads add a part to what they have stored, by ordinary additions (16384 terms:
 // 3.3e-6, 4096 x 4096 results 253 -> 265 us; parts of 4096 terms 1.4e-6 and 310 us).  Where a cluster shares the contraction and a pair's share

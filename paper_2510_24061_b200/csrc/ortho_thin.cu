@@ -388,7 +388,8 @@ bool ortho_thin_takes(int64_t rows, int64_t cols, bool out_bf16, const float* ab
   const int64_t s = rows < cols ? rows : cols;
   // The other way takes 17 to 22 launches, whatever the size, but works at the fp16 rate, and at a third of it for fp32 results.  bf16, 7 of
   // 4096 x 64: 65 us here, 124 there; 64 of 14336 x 64: 1040 and 1270; 7 of 4096 x 128: 202 and 168; 16: 400 and 260.  fp32, 7 of 4096 x
-  // 128: 181 and 223; 16 of 128 x 14336: 674 and 1131; 64 of 4096 x 128: 1076 and 912, but by fp64 sums.
+  // 128: 181 and 223; 16 of 128 x 14336: 674 and 1131; 64 of 4096 x 128: 1076 and 912 -- there the rule, which looks at the short side alone,
+  // costs a sixth of the time, and buys results that carry their own rounding only.
   if (s > (out_bf16 ? kThinMost / 2 : kThinMost)) return false;
   // how far an error of G may grow before the last step's polynomial is taken: 2^-50 to 2^-24
   double growth = 1.0;

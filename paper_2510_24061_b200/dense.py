@@ -5,7 +5,8 @@
   unquantized tokens, which is the form for serving;
 * ``orthogonalize``: an update orthogonalised by Newton-Schulz products, as the Muon optimizer takes it.
 
-Argument checks and marshalling only, like ``training``; the arithmetic runs in the library's kernels, on the current stream.
+Argument checks and marshalling only, like ``training``; the arithmetic runs in the library's kernels, on the current stream.  These are not
+autograd functions: results never require a gradient, and gradients are asked for by their own calls.
 Tensors are on the current device, bf16 or fp32; codes are torch.float8_e4m3fn or torch.float8_e5m2.
 """
 from __future__ import annotations
