@@ -48,3 +48,44 @@ def test_shared_contraction_in_parts(dense, way, T, n, m):
     got, a, b = product(dense, way, T, n, m, False)
     size, parts = a.abs() @ b.abs(), -(-a.shape[1] // 8192) + 4        # (a pair's last part may be short)
     assert not ((got.double() - a @ b).abs() > (257 * 2.0 ** -22 + parts * 2.0 ** -24 * 1.1) * size).any()
+
+
+@pytest.mark.parametrize("T,n,m", [(40000, 1040, 272), (70001, 528, 16), (50000, 1040, 656)])
+def test_passes_by_themselves_and_together(dense, T, n, m):
+    """The kernel of several passes between margins, the same bits twice, captured and replayed over new inputs, on two streams at once."""
+    from tests.test_gpu_train_guard_bands import fence, finish
+    make = lambda seed: (dense.block_quantize(data(T, m, seed, False), "col"), dense.block_quantize(data(T, n, seed + 1, False), "col"))  # noqa: E731
+    a, b = make(61), make(63)
+    p = lambda q: (q.codes.data_ptr(), q.scales.data_ptr(), 0)  # noqa: E731
+    out = fence(o=((m, n), torch.float32))
+    finish(dense.lib.falqon_block_weight_grad(*p(a[0]), *p(a[1]), T, n, m, out["o"].p, 1, None), out, T=T, n=n, m=m)
+    want = [dense.block_weight_grad(*a), dense.block_weight_grad(*b)]
+    assert torch.equal(out["o"].t, want[0]) and torch.equal(dense.block_weight_grad(*a), want[0])
+    held = [dense.Blocks(q.codes.clone(), q.scales.clone(), q.along) for q in a]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = dense.block_weight_grad(*held)
+    for source, w in ((a, want[0]), (b, want[1])):
+        for h, q in zip(held, source):
+            h.codes.copy_(q.codes)
+            h.scales.copy_(q.scales)
+        graph.replay()
+        assert torch.equal(got, w)
+    torch.cuda.synchronize()
+    streams, results = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(4):
+        for s, mine, q in zip(streams, results, (a, b)):
+            with torch.cuda.stream(s):
+                mine.append(dense.block_weight_grad(*q))
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, w) for mine, w in zip(results, want) for r in mine)
+
+
+def test_a_nan_block_in_a_later_pass(dense):
+    T, n, m = 60000, 528, 144
+    x, dy = data(T, n, 71, False), data(T, m, 72, False)
+    x[T - 5, 300], dy[T // 2, 17] = float("nan"), float("inf")
+    got = dense.block_weight_grad(dense.block_quantize(dy, "col"), dense.block_quantize(x, "col"))
+    bad = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+    bad[17], bad[:, 300] = True, True
+    assert torch.equal(torch.isnan(got), bad)

@@ -53,3 +53,22 @@ def test_a_large_eps(dense, rows, cols):
     g = of_norm(update((rows, cols), 13), 1.0)
     for eps in (1e20, 1e30):
         assert rel(dense.orthogonalize(g, eps=eps), orc.orthogonalize(g, [orc.QUINTIC] * 5, eps)) <= TOL[torch.float32]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(300, 700), (700, 130)])
+def test_captured_on_both_sides_of_eps(dense, rows, cols, dtype):
+    """A captured call finds each input's own exponents, in place too, and gives what an eager call gives."""
+    g = of_norm(update((3, rows, cols), 14), 1.0).to(dtype)
+    held = g.clone()
+    dense.orthogonalize(held)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dense.orthogonalize(held, out=held)
+    for sizes in ((1.0, 1e-9, 1e-12), (1e-14, 1.0, 1e-7), (1.0, 1.0, 1.0)):
+        x = (g.double() * torch.tensor(sizes, device="cuda", dtype=torch.float64)[:, None, None]).to(dtype)
+        held.copy_(x)
+        graph.replay()
+        assert torch.equal(held, dense.orthogonalize(x))
+        assert rel(held, orc.orthogonalize(x, [orc.QUINTIC] * 5, 1e-7)) <= TOL[dtype]
