@@ -42,8 +42,9 @@ int falqon_block_dequantize(const uint8_t *codes, const uint8_t *scales, falqon_
 
 /* ---- the products of a linear layer y = x w^T with w [m][n] held as FALQON_TILE E4M3 or E5M2 codes
  * n and m are multiples of 16, T >= 1; codes and results 16-byte aligned and dense.  Sums over the contraction are fp32 as the tensor
- * cores add: cut off instead of rounded, 1.3e-6 of the result's norm after 4096 terms (bf16's rounding is 1.7e-3); fp32 results are summed
- * in parts of at most 8192 terms, added up in fp32: 3.3e-6 after 16384, and no more after more.  Results are rounded once to their type.  A NaN block makes NaN of what it takes part in. */
+ * cores add: cut off instead of rounded, 2e-6 of the result's norm after 4096 terms (bf16's rounding is 1.7e-3).  fp32 results are summed
+ * so in parts of at most 2048 terms, which are added up by rounding additions: 1e-6, however long the contraction (a plain fp32 product:
+ * 8e-7 after 4096 terms, 1.6e-6 after 16384).  Results are rounded once to their type.  A NaN block makes NaN of what it takes part in. */
 /* y [T][m] = x w^T; x [T][n] as FALQON_ALONG_ROW codes */
 int falqon_block_forward(const uint8_t *x_codes, const uint8_t *x_scales, falqon_fp8 x_fmt, const uint8_t *w_codes, const uint8_t *w_scales,
                          falqon_fp8 w_fmt, int64_t T, int64_t n, int64_t m, void *y, int y_dtype, falqon_stream stream);

@@ -17,10 +17,10 @@
 // What bounds it: 4096 x 4096 x 11008 forward, 145 to 163 us (2.3 to 2.55 PFLOP/s), has the MMAs running 73 % of the time at 1.54 GHz (135 us
 // under the profiler; 79 % while an SM has work), the rest being the last of 9.3 waves and the pipeline's ends; with few rows the MMAs, which
 // take 0.22 us a block of K however narrow the tile is.
-// fp32 results: the tensor cores' additions cut off instead of rounding, which is 1.3e-6 of the result's norm over 4096 terms and 7e-6 over
-// 16384 if nothing is done; so every 8192 terms the threads add a part to what they have stored, by ordinary additions (16384 terms:
-// 3.3e-6, 4096 x 4096 results 253 -> 265 us; parts of 4096 terms 1.4e-6 and 310 us).  Where a cluster shares the contraction and a pair's share
-// is longer than that, the sums of its passes stay in tensor memory (131072 terms of positive values, 256 x 1024 results: 2.4e-5 -> 3.9e-6, 93 -> 98 us).
+// fp32 results: the tensor cores' additions cut off instead of rounding, so sums are taken out of tensor memory every 2048 terms and added up in
+// registers, 128 of them a thread (kSums), to which the other warps hand theirs.  Of the norm, with scales that differ from block to
+// block: 4096 terms 1.9e-6 in one sum, 9.7e-7 in two (a plain fp32 product 7.8e-7); 16384 terms 3.8e-6 in parts of 8192 and 9.8e-7 (1.6e-6).  A part more costs
+// 0.8 us, in which the MMAs wait: 4096^3 61 -> 65 us, in parts of 1024 terms 72.
 // Every wait is bounded; on a timeout the CTA records it, drains and frees its tensor memory.
 #include <cuda.h>
 
@@ -38,19 +38,26 @@ namespace falqon {
 namespace {
 
 constexpr int kEpiWarps = 8, kScaleWarps = 4;
-constexpr int kThreads = 32 * (2 + kEpiWarps + kScaleWarps);
+// Warps: TMA producer, MMA issuer, (kSums: two that fill up their group,) epilogue, scales.  kSums' epilogue holds 128 sums a thread: the groups of
+// four warps hand registers over (sum of the shares: what the CTA is launched with).
+template <bool kSums>
+struct Roles {
+  static constexpr int kEpi = kSums ? 4 : 2, kScale = kEpi + kEpiWarps, kThreads = 32 * (kScale + kScaleWarps);
+};
+constexpr int kRegsAtLaunch = 128, kRegsLight = 56, kRegsEpi = 176, kRegsScale = 96;
+static_assert(128 * kRegsLight + 32 * kEpiWarps * kRegsEpi + 32 * kScaleWarps * kRegsScale <= Roles<true>::kThreads * kRegsAtLaunch, "register pool of the CTA");
+static_assert(Roles<true>::kThreads * kRegsAtLaunch <= 65536, "registers of an SM");
 // A stage is 128 values of K of this CTA's rows of A (of which only as many as there are: the MMA reads 128 whatever lies behind
 // them, and the results of rows that are not there are not stored) and its half of B's: 32 KB at the most, and as many stages as fit.
 constexpr uint32_t kRingBytes = 6 * 32 * 1024;
 constexpr int kMostStages = 16;
 constexpr uint32_t kAccStride = 192;                 // the second accumulator's first column
-constexpr int kSumCol0 = 256, kSumCols = 192;        // sums of passes, where one accumulator will do
 constexpr uint32_t kScaleCol0 = 448;                 // ring of kGroups entries of 4 (A) + 8 (B) columns
 constexpr int kGroups = 5;
 constexpr uint32_t kGroupCols = 12;
 constexpr int kGroupBlocks = 4;                      // blocks of K per entry: the bytes of a word
-constexpr int kPassBlocks = 64;                      // fp32 results: 8192 terms
-constexpr double kPassUs = 1.5;                      // what a pass more costs a cluster's pair, whose MMAs wait for the epilogue
+constexpr int kPassBlocks = 16;                      // fp32 results: 2048 terms
+constexpr double kPassUs = 0.8;                      // what a pass more costs: the MMAs wait until the overlap has been read
 constexpr uint32_t kStagingOff = kRingBytes;             // (the last stage's MMA may read into it)
 constexpr uint32_t kWordsOff = kStagingOff + kEpiWarps * 32 * 128;
 constexpr uint32_t kWordsBytes = 12 * 32 * 4;        // an entry's scale words, passed between the scale warps
@@ -108,53 +115,9 @@ __device__ __forceinline__ uint32_t scale_word(const Bytes& w, const Scales& s) 
 constexpr int kPartPitch = 256 + 4;           // of a part's rows in fp32: 128 of them fit into the ring
 __device__ __forceinline__ float* part_of(uint8_t* gen) { return reinterpret_cast<float*>(gen); }
 
-// A pass of several of a tile that a cluster shares, columns [begin, end), 32 at a time: added to the passes before it, whose sums lie in tensor
-// memory behind the accumulator (columns 192 and up: in the staging buffers, which such a tile has no other use for); after the last
-// pass to this CTA's part of the tile, stored where the row is there.
-__device__ __forceinline__ void add_pass(uint8_t* gen, uint32_t t, int r, int begin, int end, bool more, bool last, bool there) {
-  const int sw = r & 7;
-  for (int c = begin; c < end; c += 32) {
-    uint32_t v[32], w[32];
-    float4* kept = reinterpret_cast<float4*>(gen + kStagingOff) + r * 16 + ((c & 32) >> 2);
-    const bool in_smem = c >= kSumCols;
-    __syncwarp();
-    tmem_ld_32x32b_x32(t + c, v);
-    if (more && !in_smem) tmem_ld_32x32b_x32(t + kSumCol0 + c, w);
-    tmem_ld_wait();
-    if (more && in_smem) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint4 q = reinterpret_cast<const uint4*>(kept)[j ^ sw];
-        w[4 * j] = q.x, w[4 * j + 1] = q.y, w[4 * j + 2] = q.z, w[4 * j + 3] = q.w;
-      }
-    }
-    if (more) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(v[j]));
-    }
-    if (!last && !in_smem) {
-#pragma unroll
-      for (int j = 0; j < 32; j += 8) {
-        const uint32_t q[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
-        tmem_st_32x32b_x8(t + kSumCol0 + c + j, q);
-      }
-      tmem_st_wait();
-    } else {
-      uint4* row = reinterpret_cast<uint4*>(part_of(gen) + r * kPartPitch + c);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint4 q = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        if (!last) reinterpret_cast<uint4*>(kept)[j ^ sw] = q;
-        else if (there) row[j] = q;
-      }
-    }
-  }
-}
-
-// kInPasses: a cluster shares a tile and a pair's part of the contraction takes several passes: one accumulator, and behind it the sum of
-// the passes so far.  (A kernel of its own: as a branch in the other's epilogue it made that spill registers.)
-template <bool kInPasses>
-__global__ void __launch_bounds__(kThreads, 1)
+// kSums: fp32 results of contractions longer than a pass, summed up in registers.
+template <bool kSums>
+__global__ void __launch_bounds__(Roles<kSums>::kThreads, 1)
 block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductArgs p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -206,7 +169,6 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const int pairs = gridDim.x / (2 * p.split), pair = blockIdx.x / (2 * p.split);      // that have tiles of their own
   const int kb_begin = static_cast<int>(cluster_rank >> 1) * p.split_blocks, kb_end = min(p.kblocks, kb_begin + p.split_blocks);
   const int items = p.walk.items;
-  constexpr uint32_t kStride = kInPasses ? 0 : kAccStride;
   bool aborted = false;
   struct Piece { int row0, n0, width; };           // of this CTA: rows, columns; no columns: a piece behind the right edge, of which there is nothing
   auto piece = [&](int item) {
@@ -217,6 +179,8 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
   const int gran = p.b_mn ? 32 : 16;               // columns of the instruction: what half of them may be
   auto inst_n = [&](const Piece& t) { return (t.width + gran - 1) / gran * gran; };
 
+  if (warp < Roles<kSums>::kEpi) {
+  if constexpr (kSums) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLight));
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     int stage = 0;
@@ -265,7 +229,7 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             tc_fence_after_sync();
           }
           first = false;
-          const uint32_t d = tmem + static_cast<uint32_t>(acc) * kStride;
+          const uint32_t d = tmem + static_cast<uint32_t>(acc) * kAccStride;
           const int end = min(kb_end, pass + p.pass_blocks);
           for (int kb = pass; kb < end; ++kb) {
             const int byte = kb % kGroupBlocks;
@@ -294,8 +258,10 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
       }
     }
-  } else if (warp >= 2 + kEpiWarps) {
+  }   // (warps 2 and 3 of kSums have no work)
+  } else if (warp >= Roles<kSums>::kScale) {
     // ------------------------------------------------------------ scales
+    if constexpr (kSums) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsScale));
     const int q = warp & 3;                                   // this warp's quadrant of tensor memory
     const uint32_t lane_base = static_cast<uint32_t>(q * 32) << 16;
     uint32_t* words = reinterpret_cast<uint32_t*>(gen + kWordsOff);
@@ -374,8 +340,11 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     }
   } else {
     // ------------------------------------------------------------ epilogue
-    const int quad = warp & 3, half = (warp - 2) >> 2;
-    uint8_t* stage_out = gen + kStagingOff + (warp - 2) * 32 * 128;
+    if constexpr (kSums) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpi));
+    const int quad = warp & 3, half = (warp - Roles<kSums>::kEpi) >> 2;
+    uint8_t* stage_out = gen + kStagingOff + (warp - Roles<kSums>::kEpi) * 32 * 128;
+    uint8_t* my = stage_out + lane * 128;
+    const int sw = lane & 7;
     const uint32_t lane_base = static_cast<uint32_t>(quad * 32) << 16;
     int acc = 0;
     uint32_t full_phase = 0;
@@ -384,74 +353,97 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
       if (of.width == 0) continue;
       const int chunks = (of.width + 63) / 64, low = (chunks + 1) / 2;        // chunks of 64 columns: half 0 takes [0, low) upwards,
       const int count = half == 0 ? low : chunks - low;                       // half 1 [low, chunks) downwards: the overlap first
+      auto column = [&](int i) { return 64 * (half == 0 ? i : chunks - 1 - i); };
       const int row0 = of.row0 + quad * 32, n0 = of.n0, end = of.width;
-      for (int pass = kb_begin; pass < kb_end; pass += p.pass_blocks) {
-        const bool more = pass > kb_begin;     // than the first: added to what this thread has stored
+      auto let_go = [&]() {     // what overlaps the other accumulator has been read (the rest will be before this one's next turn)
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
+      };
+      // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
+      // so a piece lies inside or outside as a whole
+      auto flush = [&](int col, int per_piece, int esize) {
+        __syncwarp();
+        const int piece = lane & 7;
+        const bool in = col + piece * per_piece < end;
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 4) {
+          const int r = r0 + (lane >> 3);
+          const uint4 val = *reinterpret_cast<const uint4*>(stage_out + r * 128 + ((piece ^ (r & 7)) << 4));
+          if (in && row0 + r < p.M)
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (static_cast<long long>(row0 + r) * p.N + n0 + col + piece * per_piece) * esize) = val;
+        }
+        __syncwarp();
+      };
+      auto store32 = [&](int col, const uint32_t* v) {       // 32 columns of fp32
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(my + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        flush(col, 4, 4);
+      };
+      auto share32 = [&](int col, const uint32_t* v) {       // to be added up: this CTA's rows of the tile as fp32, where the stages were
+        if (row0 + lane >= p.M) return;                      // (every copy has been multiplied)
+        uint4* row = reinterpret_cast<uint4*>(part_of(gen) + (row0 + lane - of.row0) * kPartPitch + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) row[j] = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      };
+      if constexpr (kSums) {
+        uint32_t sum[2][64];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 64; ++j) sum[i][j] = 0u;
+        for (int pass = kb_begin; pass < kb_end; pass += p.pass_blocks) {
+          if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
+          full_phase ^= 1u;
+          tc_fence_after_sync();
+          const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
+          if (count == 0) let_go();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (i < count) {
+#pragma unroll
+              for (int h = 0; h < 64; h += 32) {
+                uint32_t v[32];
+                __syncwarp();
+                tmem_ld_32x32b_x32(t + column(i) + h, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) sum[i][h + j] = __float_as_uint(__uint_as_float(sum[i][h + j]) + __uint_as_float(v[j]));
+              }
+              if (i == 0) let_go();
+            }
+          }
+          acc ^= 1;
+        }
+        if (aborted) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (i < count) {
+#pragma unroll
+            for (int h = 0; h < 64; h += 32) {
+              if (p.split > 1) share32(column(i) + h, sum[i] + h);
+              else store32(column(i) + h, sum[i] + h);
+            }
+          }
+        }
+      } else {
         if (!mbar_wait_warp(acc_full_bar, full_phase, p.status)) { aborted = true; break; }
         full_phase ^= 1u;
         tc_fence_after_sync();
-        const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kStride;
-        if constexpr (kInPasses) {
-          add_pass(gen, t, quad * 32 + lane, half == 0 ? 0 : 64 * low, 64 * (half == 0 ? low : chunks), more, pass + p.pass_blocks >= kb_end,
-                   row0 + lane < p.M);
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
-          continue;
-        }
-        if (count == 0) {
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
-        }
+        const uint32_t t = tmem + lane_base + static_cast<uint32_t>(acc) * kAccStride;
+        if (count == 0) let_go();
         for (int i = 0; i < count; ++i) {
-          const int c0 = 64 * (half == 0 ? i : chunks - 1 - i);
+          const int c0 = column(i);
           uint32_t v0[32], v1[32];
           __syncwarp();
           tmem_ld_32x32b_x32(t + c0, v0);
           tmem_ld_32x32b_x32(t + c0 + 32, v1);
           tmem_ld_wait();
-          if (i == 0) {
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty_bar, first_rank));
-          }
-          uint8_t* my = stage_out + lane * 128;
-          const int sw = lane & 7;
-          // 128 bytes of a row through shared memory: four rows, or eight pieces of 16 bytes, to an instruction; N is a multiple of 16,
-          // so a piece lies inside or outside as a whole
-          auto flush = [&](int col, int per_piece, int esize) {
-            __syncwarp();
-            const int piece = lane & 7;
-            const bool in = col + piece * per_piece < end;
-#pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += 4) {
-              const int r = r0 + (lane >> 3);
-              uint4 val = *reinterpret_cast<const uint4*>(stage_out + r * 128 + ((piece ^ (r & 7)) << 4));
-              if (in && row0 + r < p.M) {
-                uint4* to = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (static_cast<long long>(row0 + r) * p.N + n0 + col + piece * per_piece) * esize);
-                if (more) {                      // (fp32)
-                  const uint4 so_far = ld_stream(to);
-                  val.x = __float_as_uint(__uint_as_float(val.x) + __uint_as_float(so_far.x)), val.y = __float_as_uint(__uint_as_float(val.y) + __uint_as_float(so_far.y));
-                  val.z = __float_as_uint(__uint_as_float(val.z) + __uint_as_float(so_far.z)), val.w = __float_as_uint(__uint_as_float(val.w) + __uint_as_float(so_far.w));
-                }
-                *to = val;
-              }
-            }
-            __syncwarp();
-          };
-          if (p.split > 1) {      // to be added up: this CTA's rows of the tile as fp32, where the stages were (every copy has been multiplied)
-            if (row0 + lane < p.M) {
-              float* row = part_of(gen) + (row0 + lane - of.row0) * kPartPitch + c0;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                reinterpret_cast<uint4*>(row)[j] = make_uint4(v0[4 * j], v0[4 * j + 1], v0[4 * j + 2], v0[4 * j + 3]);
-                reinterpret_cast<uint4*>(row + 32)[j] = make_uint4(v1[4 * j], v1[4 * j + 1], v1[4 * j + 2], v1[4 * j + 3]);
-              }
-            }
-            continue;
-          }
-          if (p.bf16) {
+          if (i == 0) let_go();
+          if (p.split > 1) {
+            share32(c0, v0);
+            share32(c0 + 32, v1);
+          } else if (p.bf16) {
             auto put = [&](const uint32_t (&v)[32], int first_piece) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
@@ -467,14 +459,8 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             put(v1, 4);
             flush(c0, 8, 2);
           } else {
-            auto put = [&](const uint32_t (&v)[32]) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(my + ((j ^ sw) << 4)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            };
-            put(v0);
-            flush(c0, 4, 4);
-            put(v1);
-            flush(c0 + 32, 4, 4);
+            store32(c0, v0);
+            store32(c0 + 32, v1);
           }
         }
         acc ^= 1;
@@ -490,7 +476,9 @@ block_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     const Piece t = piece(pair);
     const int rows = max(0, min(kBlockM, p.M - t.row0)), strip = t.width > 0 ? (t.width / 4 + p.split - 1) / p.split : 0;   // in groups of four columns
     const int first = static_cast<int>(cluster_rank >> 1) * strip, count = max(0, min(strip, t.width / 4 - first));
-    for (int u = threadIdx.x; u < rows * count; u += kThreads) {
+    // (kSums: by the epilogue's threads, which have the registers)
+    constexpr int kFirst = kSums ? 32 * Roles<kSums>::kEpi : 0, kAdders = kSums ? 32 * kEpiWarps : Roles<kSums>::kThreads;
+    for (int u = static_cast<int>(threadIdx.x) - kFirst; u >= 0 && threadIdx.x < kFirst + kAdders && u < rows * count; u += kAdders) {
       const int r = u / count, c = 4 * (first + u - r * count);
       const uint32_t at = smem_u32(part_of(gen) + r * kPartPitch + c);
       float4 v = ld_shared_cluster_f32x4(map_to_cta(at, rank));
@@ -537,7 +525,7 @@ int resident_clusters(int size) {
   if ((n = at.load(std::memory_order_acquire)) != 0) return n < 0 ? 0 : n;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(sm_count() / size * size));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Roles<false>::kThreads);
   cfg.dynamicSmemBytes = kSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -577,7 +565,8 @@ Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn, b
       const double waves = s == 1 ? static_cast<double>(tiles / pairs) : 1.0;
       double us = static_cast<double>(per) * (waves * block_us(w) + (walk.items > walk.full ? block_us(walk.part_n) : 0.0));
       const int pass = static_cast<int>(f32 ? std::min<int64_t>(per, kPassBlocks) : per);
-      if (s > 1) us += 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0 + kPassUs * static_cast<double>((per - 1) / pass);
+      us += kPassUs * (waves + (walk.items > walk.full ? 1.0 : 0.0)) * static_cast<double>((per - 1) / pass);
+      if (s > 1) us += 1.5 + 2.0 * static_cast<double>(M < 256 ? M : 256) / 256.0;
       if (best.us == 0.0 || us < best.us) best = Way{walk, s, static_cast<int>(per), pass, us};
     }
   }
@@ -586,9 +575,9 @@ Way pick_way(int64_t M, int64_t N, int64_t kblocks, int64_t a_rows, bool b_mn, b
 int64_t rows_of_a(const Operand& a, int64_t M) { return a.mn || M >= 128 ? 128 : round_up(M, 8); }
 
 cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, int64_t K, void* out, int out_dt, cudaStream_t st) {
-  static DeviceMask configured{0}, configured_passes{0};
+  static DeviceMask configured{0}, configured_sums{0};
   cudaError_t e = set_max_dynamic_smem(block_product_kernel<false>, static_cast<int>(kSmem), configured);
-  if (e == cudaSuccess) e = set_max_dynamic_smem(block_product_kernel<true>, static_cast<int>(kSmem), configured_passes);
+  if (e == cudaSuccess) e = set_max_dynamic_smem(block_product_kernel<true>, static_cast<int>(kSmem), configured_sums);
   if (e != cudaSuccess) return e;
   const int64_t kblocks = (K + kBlockKBytes - 1) / kBlockKBytes;
   const bool f32 = out_dt == FALQON_F32;
@@ -638,8 +627,8 @@ cudaError_t launch_product(Operand a, const Operand& b, int64_t M, int64_t N, in
   if (!make_tensor_map(&mb, b.codes, b.rows, b.cols, b.cols, 128, b.mn ? 128 : static_cast<uint32_t>(g.walk.block_n / 2))) return cudaErrorInvalidValue;
   const int64_t pairs = (g.walk.items < pairs_all ? g.walk.items : pairs_all) * g.split;
   const dim3 grid(static_cast<unsigned>(2 * pairs));
-  return g.split > 1 && g.pass_blocks < g.split_blocks ? launch_pdl(block_product_kernel<true>, grid, dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g)
-                                                       : launch_pdl(block_product_kernel<false>, grid, dim3(kThreads), kSmem, st, 2 * g.split, ma, mb, g);
+  return g.pass_blocks < g.split_blocks ? launch_pdl(block_product_kernel<true>, grid, dim3(Roles<true>::kThreads), kSmem, st, 2 * g.split, ma, mb, g)
+                                        : launch_pdl(block_product_kernel<false>, grid, dim3(Roles<false>::kThreads), kSmem, st, 2 * g.split, ma, mb, g);
 }
 
 Scales scales_of(const uint8_t* p, int along, int64_t rows, int64_t cols, bool over_rows) {

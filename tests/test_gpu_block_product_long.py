@@ -1,13 +1,14 @@
-"""fp32 results of contractions so long that a cluster's CTA pairs have more than 8192 terms each: the tensor core's additions cut off, so
-what is summed in tensor memory is no longer than that, however a tile's contraction is shared.
+"""fp32 results of long contractions: the tensor core's additions cut off, so what is summed in tensor memory is no longer than 2048 terms,
+however a tile's contraction is shared.
 
-Tolerances.  Element by element, signs random: parts of 8192 terms, each off by at most 257 * 2^-22 of its own sum of sizes (the products' tests
-derive it), and an ordinary addition for each further part, off by at most half a step of what is then there.
+Tolerances.  Element by element, signs random: parts of 2048 terms, each off by at most 65 * 2^-22 of its own sum of sizes (the products' tests
+derive it), and an ordinary addition for each part, off by at most half a step of what is then there.
 Of the norm, all values positive, so that nothing that is cut off makes up for anything: an instruction adds 32 products to a sum and cuts off
-less than a step, 2^-23 of it.  Of equally many terms each, the sums before the end of a part are on average half of it, so 256 instructions lose at
-most 128.5 * 2^-23 = 1.53e-5 of a part and of the whole, and the ordinary additions up to 16 * 2^-25: 1.6e-5.  (The size of a step beside the
-sum varies between 2^-24 and 2^-23, and what is cut off between none and all of it: 3.9e-6 are measured for one part, 1e-5 for parts of 16384
-terms, 2.4e-5 for parts of 32768.)"""
+less than a step, 2^-23 of it.  Of equally many terms each, the sums before the end of a part are on average half of it, so 64 instructions lose at
+most 32.5 * 2^-23 = 3.9e-6 of a part and of the whole, and n ordinary additions of equal parts at most n / 2 * 2^-24.
+Of the norm, signs random, scales that differ from block to block: the sums before the end of a part are in size two thirds of it (the square root's
+average), a step is on average 0.72 * 2^-23 of a sum, and half a step is cut off on average, always towards zero: 64 * 2/3 * 0.72 / 2 * 2^-23 =
+1.8e-6 of a part, and no more of the whole.  (Parts of 8192 terms would leave four times as much.)"""
 import pytest
 import torch
 
@@ -44,10 +45,28 @@ def product(dense, way, T, n, m, positive):
 def test_shared_contraction_in_parts(dense, way, T, n, m):
     got, a, b = product(dense, way, T, n, m, True)
     want = a @ b
-    assert float((got.double() - want).norm() / want.norm()) <= 1.6e-5, float((got.double() - want).norm() / want.norm())
+    parts = -(-a.shape[1] // 2048) + 4        # (a pair's last part may be short)
+    off = float((got.double() - want).norm() / want.norm())
+    assert off <= 3.9e-6 + parts / 2 * 2.0 ** -24, off
     got, a, b = product(dense, way, T, n, m, False)
-    size, parts = a.abs() @ b.abs(), -(-a.shape[1] // 8192) + 4        # (a pair's last part may be short)
-    assert not ((got.double() - a @ b).abs() > (257 * 2.0 ** -22 + parts * 2.0 ** -24 * 1.1) * size).any()
+    size = a.abs() @ b.abs()
+    assert not ((got.double() - a @ b).abs() > (65 * 2.0 ** -22 + parts * 2.0 ** -24 * 1.1) * size).any()
+
+
+@pytest.mark.parametrize("way,T,n,m", [("dw", 8192, 1040, 2064), ("dw", 16384, 2048, 4096), ("fwd", 1000, 11008, 2064), ("fwd", 8, 11008, 4096), ("fwd", 300, 8192, 528),
+                                       ("dx", 1000, 2064, 11008), ("dx", 777, 5120, 13824), ("dw", 65536, 1024, 256)])
+def test_scales_that_differ(dense, way, T, n, m):
+    if way == "dw":
+        dy, x = dense.block_quantize(data(T, m, 57), "col"), dense.block_quantize(data(T, n, 58), "col")
+        got, a, b = dense.block_weight_grad(dy, x, torch.float32), orc.value(dy).T, orc.value(x)
+    elif way == "fwd":
+        x, w = dense.block_quantize(data(T, n, 57), "row"), dense.block_quantize(data(m, n, 58), "tile")
+        got, a, b = dense.block_forward(x, w, torch.float32), orc.value(x), orc.value(w).T
+    else:
+        dy, w = dense.block_quantize(data(T, m, 57), "row"), dense.block_quantize(data(m, n, 58), "tile")
+        got, a, b = dense.block_input_grad(dy, w, torch.float32), orc.value(dy), orc.value(w)
+    want = a @ b
+    assert float((got.double() - want).norm() / want.norm()) <= 1.8e-6, float((got.double() - want).norm() / want.norm())
 
 
 @pytest.mark.parametrize("T,n,m", [(40000, 1040, 272), (70001, 528, 16), (50000, 1040, 656)])

@@ -77,9 +77,11 @@ def test_clusters_that_share_a_tile(dense, way, T, n, m, size):
         within(call(dtype), a, b)
 
 
-@pytest.mark.parametrize("T,dtype,passes", [(32768, torch.float32, False), (32768 + 2048, torch.float32, True), (131072, torch.bfloat16, False)])
-def test_passes_of_a_shared_tile(dense, T, dtype, passes):
-    """A pair's share of more than 8192 terms is summed in passes for fp32 results, by the kernel made for it."""
-    call, _, _ = operands(dense, "dw", T, 1024, 256)
-    (size, name), = clusters(lambda: call(dtype))
-    assert size == 8 and ("Lb1E" in name) == passes, name
+@pytest.mark.parametrize("T,n,m,dtype,size,sums", [(8192, 1024, 256, torch.float32, 8, False), (8192 + 512, 1024, 256, torch.float32, 8, True),
+                                                   (131072, 1024, 256, torch.bfloat16, 8, False), (2048, 4096, 4096, torch.float32, 2, False),
+                                                   (2048 + 1, 4096, 4096, torch.float32, 2, True), (4096, 4096, 4096, torch.bfloat16, 2, False)])
+def test_sums_of_several_parts(dense, T, n, m, dtype, size, sums):
+    """fp32 results of more than 2048 terms a pair are summed in parts, by the kernel made for it."""
+    call, _, _ = operands(dense, "dw", T, n, m)
+    (got, name), = clusters(lambda: call(dtype))
+    assert got == size and ("Lb1E" in name) == sums, (got, name)
