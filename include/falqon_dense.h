@@ -68,7 +68,7 @@ int falqon_block_linear(const void *x, int x_dtype, const uint8_t *w_codes, cons
  * values s of X become p(s) = a s + b s^3 + c s^5 at each step.
  * Arithmetic: sums are fp32 (the norm's fp64).  X and the term a X are held in 22 bits (two fp16 numbers, a power of two apart; no
  * finer than 2^-37 of X's norm, of which single values may be a small part), the products' operands in fp16 (11 bits) where the results
- * are bf16; where they are fp32, each product is three: both operands in 22 bits.  Where |g| is far below eps, so that X is small
+ * are bf16 (of B X with a short side up to 96: 22 bits); where they are fp32, each product is three: both operands in 22 bits.  Where |g| is far below eps, so that X is small
  * altogether, its digits are kept by powers of two, a matrix's own.  A step whose polynomial cancels, a + q being small beside
  * q = b s^2 + c s^4, leaves up to 2^-11 |q| / |a + q| of that direction in bf16 results (0.2 % with Muon's coefficients, 2 % with the steepest
  * of published schedules, whose last steps take it away again).  A matrix of zeros gives zeros; an infinity or a NaN makes NaN of its whole matrix. */

@@ -4,8 +4,8 @@
 //
 // Numbers.  The singular values of X start as small as they like beside its norm and grow by a = 3.4 a step, noise in X with them: held in
 // bf16, results are 1 to 30 % off.  So X, and with it the term a X, is two fp16 numbers hi + lo (22 bits).  The products' operands are
-// the hi parts alone where results are bf16 (errors of 2^-12 of G and B; results 1.7e-3 to 2.5e-3 off, of which 1.66e-3 are their own
-// rounding), and three products hi hi + hi lo + lo hi where they are fp32.  All stored values are 2^13 times what they stand for: the host
+// the hi parts alone where results are bf16 (errors of 2^-12 of G and B; results 1.7e-3 to 2.4e-3 off, of which 1.66e-3 are their own
+// rounding; short sides up to 96 have the last of a step's products in full), and three products hi hi + hi lo + lo hi where they are fp32.  All stored values are 2^13 times what they stand for: the host
 // has made sure that none passes 7.98, and small ones keep their digits above fp16's smallest.  Where |g| is below eps / 2, X is small
 // altogether and only grows by the first coefficient a step: X and B are then held 2^x and 2^b times as large, by exponents of each matrix and step
 // that ortho_scale_kernel derives from |g| / (|g| + eps) (1024 x 1024 at 1e-7 of eps: results 2 % off without them).
@@ -732,9 +732,15 @@ Way pick_way(int64_t M, int64_t N, int64_t K, int64_t batch, bool symmetric, boo
   return way;
 }
 
+// bf16 results: up to this short side the product B X is three, too.  The roundings of B and X average out over the short side, and over few
+// values they leave as much as the results' own rounding: 69 x 759 2.56e-3 off, so 1.93e-3, where rounding the exact results leaves 1.66e-3 (96 x 14336
+// 2.2e-3 and 1.8e-3, 512 x 4096 2.15e-3 and 1.8e-3).  It costs a seventh to a quarter of the time (69 x 759 96 -> 109 us, 16 of 14336 x 80 516 -> 651, 512 x
+// 4096 159 -> 191), which longer sides are spared.
+constexpr int64_t kPreciseApply = 96;
+
 struct Layout {
   int64_t s, l, ld, ld_s;        // short and long side; pitches of X and of the square matrices
-  bool tall, precise;
+  bool tall, precise, apply_precise;      // precise: three products for one
   Way gram, square;
   int norm_parts;
   size_t x_bytes, sq_bytes;
@@ -753,6 +759,7 @@ Layout layout_of(const falqon_ortho* p) {
   y.s = y.tall ? p->cols : p->rows;
   y.l = y.tall ? p->rows : p->cols;
   y.precise = p->out_dtype == FALQON_F32;
+  y.apply_precise = y.precise || y.s <= kPreciseApply;
   y.ld = round_up(p->cols, 64);
   y.ld_s = round_up(y.s, 64);
   y.x_bytes = static_cast<size_t>(p->batch * p->rows * y.ld) * 2;
@@ -767,7 +774,7 @@ Layout layout_of(const falqon_ortho* p) {
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 1023) / 1024 * 1024; return o; };
   for (int i = 0; i < 4; ++i) y.x[i] = take(y.x_bytes);
-  for (int i = 0; i < 4; ++i) y.sq[i] = take((i & 1) == 0 || y.precise ? y.sq_bytes : 0);
+  for (int i = 0; i < 4; ++i) y.sq[i] = take((i & 1) == 0 || y.precise || (i == 3 && y.apply_precise) ? y.sq_bytes : 0);
   y.parts = take(splits > 1 ? static_cast<size_t>(p->batch) * splits * y.s * y.ld_s * 4 : 0);
   y.norm = take(static_cast<size_t>(p->batch) * y.norm_parts * 8);
   y.exps = take(static_cast<size_t>(p->batch) * p->steps * sizeof(Exponents));
@@ -843,9 +850,9 @@ int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_
   cudaError_t e = p->dtype == FALQON_BF16 ? launch_start<bf16_t>(p, y, g, norm, exps, halves(y.x[0]), halves(y.x[1]), st)
                                           : launch_start<float>(p, y, g, norm, exps, halves(y.x[0]), halves(y.x[1]), st);
   if (e != cudaSuccess) return FALQON_ERR_CUDA;
-  __half *g_hi = halves(y.sq[0]), *g_lo = y.precise ? halves(y.sq[1]) : nullptr, *b_hi = halves(y.sq[2]), *b_lo = y.precise ? halves(y.sq[3]) : nullptr;
+  __half *g_hi = halves(y.sq[0]), *g_lo = y.precise ? halves(y.sq[1]) : nullptr, *b_hi = halves(y.sq[2]), *b_lo = y.apply_precise ? halves(y.sq[3]) : nullptr;
   const int64_t sq_stride = y.s * y.ld_s, x_stride = p->rows * y.ld;
-  const Way apply = pick_way(p->rows, p->cols, y.s, p->batch, false, y.precise);
+  const Way apply = pick_way(p->rows, p->cols, y.s, p->batch, false, y.apply_precise);
   // a symmetric product: to `hi`, `lo` at once, or in parts that are added up there
   auto symmetric = [&](ProductArgs a, const Way& way, const Matrix& x, int64_t K, __half* hi, __half* lo) {
     a.symmetric = true;
@@ -896,8 +903,8 @@ int run(const falqon_ortho* p, const Layout& y, const void* g, void* out, uint8_
       a.o_hi = halves(y.x[then]), a.o_lo = halves(y.x[then + 1]), a.ld_o = y.ld, a.stride_o = x_stride;
       a.out = out, a.out_bf16 = p->out_dtype == FALQON_BF16;
       a.out_vec = p->cols % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (a.out_bf16 ? 7 : 15)) == 0;
-      e = y.tall ? launch_product(a, apply, x, m, p->batch, p->rows, p->cols, y.s, y.precise, st)
-                 : launch_product(a, apply, m, x, p->batch, p->rows, p->cols, y.s, y.precise, st);
+      e = y.tall ? launch_product(a, apply, x, m, p->batch, p->rows, p->cols, y.s, y.apply_precise, st)
+                 : launch_product(a, apply, m, x, p->batch, p->rows, p->cols, y.s, y.apply_precise, st);
       if (e != cudaSuccess) return FALQON_ERR_CUDA;
     }
   }
