@@ -268,14 +268,18 @@ __device__ __forceinline__ void finish_chunk(const ProductArgs& p, const Item& i
 
 // kPrecise: both operands as hi + lo, which a stage holds together: hi hi in one accumulator, hi lo + lo hi in a second, whose sums are
 // 2^11 times smaller.  The tensor core's additions cut off instead of rounding, which over a long sum of squares (G's diagonal) is a
-// bias; so the first is added up in registers every kChunk blocks of K (1000 x 1531: results 1.5e-5 off without, 7.9e-6 every 8
+// bias; so the first is added up in registers every block or two of K (1000 x 1531: results 1.5e-5 off without, 7.9e-6 every 8
 // blocks, 3.9e-6 every 4, 2.0e-6 every 2 in 3 % more time; plain fp32 products 3.0e-6).  Columns 0..255 are two accumulators of hi hi, a chunk each in turn, 256..511 two of
 // the others, a tile each in turn: by the time a tile's first chunk may be written, the tile before the last has been read.
-constexpr int kChunk = 2;
+// Short sides up to 512 every block: where all singular values are of a size the last steps multiply the bias tenfold (143 x 977 2.9e-6 -> 1.7e-6, plain
+// fp32 products 1.3e-6; 403 x 6139 3.1e-6, plain 2.2e-6), for 3 to 4 % of the time; 4096 x 4096 would take 13 % more and be no more exact than it needs to be.
+constexpr int64_t kShortChunks = 512;
 
-template <bool kPrecise>
+// kChunk: blocks of K between these additions; 0: not kPrecise.  (At run time it cost 4 %.)
+template <int kChunk>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 ortho_product_kernel(const __grid_constant__ Maps maps, const ProductArgs p) {
+  constexpr bool kPrecise = kChunk > 0;
   using St = Stage<kPrecise>;
   constexpr int kStages = St::kCount;
   constexpr uint32_t kStageBytes = St::kBytes;
@@ -810,14 +814,14 @@ cudaError_t launch_product(ProductArgs g, const Way& way, const Matrix& a, const
   else if (!map(&maps.a_lo, a, a.lo, a_box) || !map(&maps.b_lo, b, b.lo, b_box)) return cudaErrorInvalidValue;
   const int64_t all = sm_count() / 2, pairs = g.walk.items < all ? g.walk.items : all;
   const dim3 grid(static_cast<unsigned>(2 * pairs)), block(kGemmThreads);
-  if (precise) {
-    static DeviceMask done{0};
-    const cudaError_t e = set_max_dynamic_smem(ortho_product_kernel<true>, static_cast<int>(kSmem), done);
-    return e != cudaSuccess ? e : launch_pdl(ortho_product_kernel<true>, grid, block, kSmem, st, 2, maps, g);
-  }
-  static DeviceMask done{0};
-  const cudaError_t e = set_max_dynamic_smem(ortho_product_kernel<false>, static_cast<int>(kSmem), done);
-  return e != cudaSuccess ? e : launch_pdl(ortho_product_kernel<false>, grid, block, kSmem, st, 2, maps, g);
+  auto launch = [&](auto kernel, DeviceMask& done) {
+    const cudaError_t e = set_max_dynamic_smem(kernel, static_cast<int>(kSmem), done);
+    return e != cudaSuccess ? e : launch_pdl(kernel, grid, block, kSmem, st, 2, maps, g);
+  };
+  static DeviceMask done0{0}, done1{0}, done2{0};
+  if (!precise) return launch(ortho_product_kernel<0>, done0);
+  return std::min(a.rows, a.cols) <= kShortChunks && std::min(b.rows, b.cols) <= kShortChunks ? launch(ortho_product_kernel<1>, done1)
+                                                                                           : launch(ortho_product_kernel<2>, done2);
 }
 
 template <typename T>

@@ -59,3 +59,23 @@ def test_bf16_results_beside_their_own_rounding(dense, rows, cols):
     want = orc.orthogonalize(x, [orc.QUINTIC] * 5, 1e-7)
     least = rel(want.bfloat16(), want)
     assert rel(dense.orthogonalize(x), want) <= 1.5 * least, rel(dense.orthogonalize(x), want) / least
+
+
+@pytest.mark.parametrize("rows,cols", [(129, 977), (143, 977), (9953, 146), (530, 147), (403, 6139), (133, 232), (300, 700), (1106, 388)])
+def test_fp32_results_beside_plain_products(dense, rows, cols):
+    """As exact as plain fp32 products of the same steps, but for half as much again (sums that are cut off instead of rounded): the same inputs, whose
+    singular values come together after four steps, where the fifth multiplies what is systematic in them."""
+    assert not torch.backends.cuda.matmul.allow_tf32
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    k = min(rows, cols, 32)
+    g = (torch.randn((rows, k), generator=g, device="cuda") / torch.arange(1, k + 1, device="cuda") @ torch.randn((k, cols), generator=g, device="cuda")
+         + 0.5 * torch.randn((rows, cols), generator=g, device="cuda")) * 1e-3
+    want = orc.orthogonalize(g, [orc.QUINTIC] * 5, 1e-7)
+    x = g.mT if rows > cols else g
+    x = x / (x.double().norm() + 1e-7).float()
+    a, b, c = orc.QUINTIC
+    for _ in range(5):
+        m = x @ x.mT
+        x = a * x + (b * m + c * (m @ m)) @ x
+    plain, got = rel(x.mT if rows > cols else x, want), rel(dense.orthogonalize(g), want)
+    assert got <= 1.5 * plain, (got, plain)
