@@ -7,8 +7,8 @@
 // Two CTAs of a cluster compute a tile of 256 x block_n (one tcgen05.mma cta_group::2), a persistent pair walking its tiles (tile_walk.cuh):
 //   warp 0        TMA producer: up to 128 rows of A and block_n / 2 rows of B per CTA and stage of 128 values of K
 //   warp 1        (leader) issues the MMAs
-//   warps 2..9    epilogue: tensor memory -> registers -> shared memory -> full 128-byte lines
-//   warps 10..13  scales: global memory -> tensor memory (tcgen05.st), four blocks of K at a time, the four bytes of a word
+//   warps 2..9    epilogue: tensor memory -> registers -> shared memory -> full 128-byte lines     (4..11 where sums are held in registers)
+//   warps 10..13  (12..15) scales: global memory -> tensor memory (tcgen05.st), four blocks of K at a time, the four bytes of a word
 // Tensor memory: the scales' ring takes 64 of the 512 columns, which leaves 448 for two accumulators of up to 256.  They overlap in
 // columns 192..255, and the epilogue reads those first: the next tile's MMAs start as soon as they are in registers, so that the
 // rest of the epilogue runs beside them.

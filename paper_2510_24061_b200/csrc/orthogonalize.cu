@@ -5,8 +5,9 @@
 // Numbers.  The singular values of X start as small as they like beside its norm and grow by a = 3.4 a step, noise in X with them: held in
 // bf16, results are 1 to 30 % off.  So X, and with it the term a X, is two fp16 numbers hi + lo (22 bits).  The products' operands are
 // the hi parts alone where results are bf16 (errors of 2^-12 of G and B; results 1.7e-3 to 2.4e-3 off, of which 1.66e-3 are their own
-// rounding; short sides up to 96 have the last of a step's products in full), and three products hi hi + hi lo + lo hi where they are fp32.  All stored values are 2^13 times what they stand for: the host
-// has made sure that none passes 7.98, and small ones keep their digits above fp16's smallest.  Where |g| is below eps / 2, X is small
+// rounding; short sides up to 96 have the last of a step's products in full), and three products hi hi + hi lo + lo hi where they are
+// fp32.  All stored values are 2^13 times what they stand for: the host has made sure that none passes 7.98, and small ones keep their
+// digits above fp16's smallest.  Where |g| is below eps / 2, X is small
 // altogether and only grows by the first coefficient a step: X and B are then held 2^x and 2^b times as large, by exponents of each matrix and step
 // that ortho_scale_kernel derives from |g| / (|g| + eps) (1024 x 1024 at 1e-7 of eps: results 2 % off without them).
 //
